@@ -409,6 +409,128 @@ OSDP_API osdp_status osdp_cost_model(const osdp_operator_cost *ops, int32_t n, c
 OSDP_API osdp_status osdp_plan_search(const osdp_operator_cost *ops, int32_t n, const osdp_device_info *dev,
                                       uint8_t *modes, osdp_search_result *result);
 
+/* ---- AdamW over the shards --------------------------------------------------
+ * What the gradients in dw_shards are for: one step of Adam with decoupled weight decay over many tensors at once, in place.
+ * With M_i^(model) of Section 3.1 in mind (parameters and optimizer states are what ZDP shards) the moments may be held in
+ * 8 bits.  In fp32, with c = 1 or (clipping) max_norm / norm, t the step, counted from 1:
+ *     g = c * grad        m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+ *     p = p - lr * weight_decay * p - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * Parameters: OSDP_F32 (p is `param`); OSDP_BF16 with `master` (p is the fp32 master, and param = p rounded to bf16,
+ * nearest even); OSDP_BF16 without (p is `param` widened, rounded back stochastically: with nearest rounding a step below
+ * 2^-9 of a weight would always be lost).
+ *
+ * Moments, state_bits = 32: fp32 arrays.  state_bits = 8: one byte each, and for every block of 128 consecutive elements of a
+ * tensor (the last block may be short) two bytes in `exps`, m's and v's: b, the power of two the block shares.
+ *     m : sign, 4 exponent bits E, 3 fraction bits f        v : 5 exponent bits E, 3 fraction bits f, no sign
+ *     with B the largest E (15, 31) the value is 2^(b - 127 - B + E) * (1 + f / 8), and 2^(b - 126 - B) * f / 8 where E = 0
+ * b is the biased exponent of the block's largest magnitude rounded up to 3 fraction bits, at least 32 (m) or 48 (v);
+ * b = 0: all of the block is zero, so that zeroed arrays are the initial state; b = 255: the block held a NaN or an infinity, and all of it
+ * reads as NaN.  Magnitudes are rounded to one of the two neighbouring values, the upper one with the probability that
+ * keeps the mean (nearest rounding would freeze v: a step changes it by 1 - beta2 of itself, less than half of a
+ * fraction's step); a positive v is never rounded to 0, which would make the next step of its element a division by eps.
+ * The update itself uses m and v before their rounding.
+ *
+ * Random numbers: with mix(x) = { x *= 0x9E3779B1; x ^= x >> 15; x *= 0x2C1B3C6D; x ^= x >> 13 } on 32 bits, element i of the
+ * tensor at place j of the array has h = mix(lo(i) + mix(mix(mix(mix(mix(lo(seed)) ^ hi(seed)) ^ lo(t)) ^ j) ^ hi(i))),
+ * lo / hi = lower / upper 32 bits: m adds the lower 16 bits of h (below its last fraction bit, as a fraction of it) before it
+ * is cut, v the upper 16, a bf16 parameter the upper 16 of h * 0x297A2D39.  Results are a function of the inputs alone.
+ *
+ * Tensors: any lengths (0 too) and, element by element, any alignment; exps must be 2-byte aligned.  The widest accesses are
+ * used for those whose arrays are all 16-byte aligned (moments in 8 bits: 8-byte).  No two arrays of a call may overlap. */
+
+typedef enum { OSDP_BF16 = 0, OSDP_F32 = 1 } osdp_dtype;
+
+typedef struct {
+  int64_t n;          /* elements, 0 <= n < 2^40                                                     */
+  const void *grad;   /* device, of grad_type                                                        */
+  void *param;        /* device, of param_type                                                       */
+  float *master;      /* device fp32 copies of bf16 parameters, or NULL                              */
+  void *m, *v;        /* device: fp32 [n], or one byte each [n]                                      */
+  uint8_t *exps;      /* device, 8 bits: [2 * ceil(n / 128)], m's and v's of a block side by side    */
+  double weight_decay;
+} osdp_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps; /* lr >= 0; 0 <= beta < 1; eps >= 1e-12                              */
+  int64_t step;                 /* t >= 1                                                            */
+  uint64_t seed;                /* of the stochastic roundings                                       */
+  double max_norm;              /* > 0: gradients are scaled down to this norm (needs grad_sumsq); 0: they are not */
+  const double *grad_sumsq;     /* device, or NULL: the squared norm of all gradients (over all ranks: add up the ranks'
+                                   sums).  Where it is infinite or NaN the call leaves everything as it is */
+  const int64_t *step_device;   /* device, or NULL: t, in place of `step`, read when the kernels run: a captured graph
+                                   that is replayed takes the step (and seeds its roundings by it) from here */
+  const float *lr_device;       /* device, or NULL: lr, in place of `lr`                             */
+  int32_t grad_type;            /* an osdp_dtype                                                     */
+  int32_t param_type;           /* an osdp_dtype                                                     */
+  int32_t state_bits;           /* 32 or 8                                                           */
+  int32_t reserved;             /* 0                                                                 */
+} osdp_adamw_options;
+
+/* One step over `count` tensors (host array, 0 allowed; all with masters or all without).  A few launches however many
+ * tensors there are (56 to a launch); no workspace. */
+OSDP_API osdp_status osdp_adamw_step(const osdp_adamw_tensor *tensors, int32_t count, const osdp_adamw_options *options,
+                                     void *stream);
+
+/* *sumsq (device) = the sum over all tensors of the squares of their gradients, in double from the first product on;
+ * accumulate != 0: is added to it (gradients of two types, or of several calls).  Only n and grad of the tensors are
+ * looked at.  The order of the sum depends on the lengths alone: the same gradients give the same bits.
+ *   workspace: device, 8-byte aligned, >= osdp_adamw_grad_sumsq_workspace_bytes of the same tensors */
+OSDP_API osdp_status osdp_adamw_grad_sumsq(const osdp_adamw_tensor *tensors, int32_t count, int32_t grad_type,
+                                           int32_t accumulate, double *sumsq, void *workspace, size_t workspace_bytes,
+                                           void *stream);
+OSDP_API osdp_status osdp_adamw_grad_sumsq_workspace_bytes(const osdp_adamw_tensor *tensors, int32_t count, size_t *bytes);
+
+/* The values that moments in 8 bits stand for, for checkpoints and for looking at: m_out[i] and v_out[i] (host arrays of
+ * device pointers, bf16 [n]) of every tensor.  They have at most 4 significant bits, so bf16 holds them exactly. */
+OSDP_API osdp_status osdp_adamw_state_values(const osdp_adamw_tensor *tensors, int32_t count, void *const *m_out,
+                                             void *const *v_out, void *stream);
+
+/* ---- the operator in 8-bit integers ------------------------------------------
+ * Y = X . W with the weight held, sharded and gathered as 8-bit integers: half of the bytes S_i that the cost model of
+ * Section 3.1 counts for a gather, and the matrix cores' faster rate.  One scale for each output channel o and one for
+ * each token t:
+ *     amax_o = max_i |W[i, o]|    s_o = amax_o / 127    Wq[o, i] = round(W[i, o] * 127 / amax_o)
+ *     amax_t = max_i |X[t, i]|    s_t = amax_t / 127    Xq[t, i] = round(X[t, i] * 127 / amax_t)
+ *     Y[t, o] = bf16( (sum_i Xq[t, i] Wq[o, i]) * s_t * s_o )
+ * round: to the nearest whole number, halves away from zero, exactly (the quotient of two bf16 numbers is never so close to
+ * a half that fp32 could not tell).  The sum is one of whole numbers, so exact: Y does not depend on the shards, on k or on
+ * the kernel.  A token of zeros gives 0; a token or channel that holds a NaN or an infinity gives NaN in all of its outputs.
+ *
+ * Layout: Wq lies [O x I], input features contiguous, in N flat shards as elsewhere: f = o*I + i in shard f / L at f % L,
+ * L = ceil(I*O/N), the last shard's tail neither read nor written by the product (the quantization leaves it as it is).
+ * When N divides O, shard s is a block of O/N output channels.
+ *
+ * There is no backward pass through the roundings.  To train with this forward pass they count as the identity: dX and dW
+ * are those of osdp_split_linear_bwd on the bf16 shards, osdp_adamw_step updates these, and the 8-bit shards are
+ * made from them again.
+ *
+ * Shapes (else OSDP_ERR_UNSUPPORTED): I a multiple of 16 and at most 131072 (the sums fit 32 bits), O a multiple of 8, L a
+ * multiple of 16, leading dimensions multiples of 8; pointers 16-byte aligned; N <= 64; T, O < 2^31. */
+
+/* 8-bit shards and the channels' scales from bf16 shards (the layout of osdp_split_linear_fwd).
+ *   w_shards : host array of N device pointers, bf16, L elements each
+ *   q_shards : host array of N device pointers, one byte each, L elements each
+ *   w_scale  : device fp32 [O], 16-byte aligned
+ *   workspace: device, 256-byte aligned, >= osdp_split_linear_i8_quantize_workspace_bytes
+ * Of `shape`, I, O and N are looked at. */
+OSDP_API osdp_status osdp_split_linear_i8_quantize(const osdp_shape *shape, const void *const *w_shards, void *const *q_shards,
+                                                   float *w_scale, void *workspace, size_t workspace_bytes, void *stream);
+OSDP_API osdp_status osdp_split_linear_i8_quantize_workspace_bytes(const osdp_shape *shape, size_t *bytes);
+
+/* The forward pass.  Shards that are blocks of whole channels (N divides O) are read where they lie, and so are all shards
+ * for few tokens (at most 64); otherwise the k slices of output channels, c0_j = floor(j*O/k), are gathered one after
+ * another into one staging slot of a slice (size/k at one byte an element).
+ *   X : device [T x I] bf16, ldx >= I     Y : device [T x O] bf16, ldy >= O (every element written)
+ *   workspace: device, 256-byte aligned, >= osdp_split_linear_i8_workspace_bytes: [Xq and s_t][staging slot]
+ * T = 0 does nothing. */
+OSDP_API osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int64_t ldx,
+                                              const void *const *q_shards, const float *w_scale, void *Y, int64_t ldy,
+                                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace, and how many of them hold gathered weights.  Either pointer may be NULL.  Host only. */
+OSDP_API osdp_status osdp_split_linear_i8_workspace_bytes(const osdp_shape *shape, size_t *total, size_t *peak_weight_staging);
+
 /* ---- test and debug switches ------------------------------------------------
  * Process-wide switches for tests and for hunting stream races.  Result bits change with
  * "split_k", and for T <= 128 with "gemm_generic" = 1 and "tile" >= 0, which turn the sum of four parts

@@ -31,6 +31,10 @@ OSDP_SPLIT_PER_PASS = 3
 
 OSDP_NOALLOC_SCRATCH_BYTES = 64 << 20
 
+OSDP_BF16 = 0
+OSDP_F32 = 1
+OSDP_ADAMW_BLOCK = 128  # elements that share a power of two in moments of 8 bits
+
 OSDP_KERNEL_GATHER = 0
 OSDP_KERNEL_GEMM_FWD = 1
 OSDP_KERNEL_GEMM_DW = 2
@@ -47,6 +51,9 @@ EXPORTS = (
     "osdp_granularity_candidates", "osdp_granularity_measure",
     "osdp_granularity_select", "osdp_cost_model", "osdp_plan_search", "osdp_profile_begin", "osdp_profile_end", "osdp_profile_overlap",
     "osdp_debug_option", "osdp_strerror", "osdp_last_error", "osdp_version",
+    "osdp_adamw_step", "osdp_adamw_grad_sumsq", "osdp_adamw_grad_sumsq_workspace_bytes", "osdp_adamw_state_values",
+    "osdp_split_linear_i8_quantize", "osdp_split_linear_i8_quantize_workspace_bytes", "osdp_split_linear_i8_fwd",
+    "osdp_split_linear_i8_workspace_bytes",
 )
 
 
@@ -89,6 +96,19 @@ class osdp_kernel_stats(ctypes.Structure):
                 ("bytes", ctypes.c_double)]
 
 
+class osdp_adamw_tensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("grad", ctypes.c_void_p), ("param", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("exps", ctypes.c_void_p), ("weight_decay", ctypes.c_double)]
+
+
+class osdp_adamw_options(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_int64), ("seed", ctypes.c_uint64), ("max_norm", ctypes.c_double),
+                ("grad_sumsq", ctypes.c_void_p), ("step_device", ctypes.c_void_p), ("lr_device", ctypes.c_void_p),
+                ("grad_type", ctypes.c_int32), ("param_type", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 class OsdpError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"libosdp status {status}: {message}")
@@ -128,6 +148,15 @@ def _load() -> ctypes.CDLL:
     lib.osdp_cost_model.argtypes = [opc, i32, dvi, ctypes.POINTER(ctypes.c_uint8), i32,
                                     ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
     lib.osdp_plan_search.argtypes = [opc, i32, dvi, ctypes.POINTER(ctypes.c_uint8), ctypes.POINTER(osdp_search_result)]
+    adt, ado = ctypes.POINTER(osdp_adamw_tensor), ctypes.POINTER(osdp_adamw_options)
+    lib.osdp_adamw_step.argtypes = [adt, i32, ado, vp]
+    lib.osdp_adamw_grad_sumsq.argtypes = [adt, i32, i32, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.osdp_adamw_grad_sumsq_workspace_bytes.argtypes = [adt, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.osdp_adamw_state_values.argtypes = [adt, i32, vp, vp, vp]
+    lib.osdp_split_linear_i8_quantize.argtypes = [shp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.osdp_split_linear_i8_quantize_workspace_bytes.argtypes = [shp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.osdp_split_linear_i8_fwd.argtypes = [shp, vp, i64, vp, vp, vp, i64, vp, ctypes.c_size_t, vp]
+    lib.osdp_split_linear_i8_workspace_bytes.argtypes = [shp, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]
     lib.osdp_debug_option.argtypes = [ctypes.c_char_p, i32]
     lib.osdp_debug_option.restype = ctypes.c_int
     lib.osdp_profile_begin.argtypes = [i32]
@@ -139,7 +168,10 @@ def _load() -> ctypes.CDLL:
                  "osdp_split_linear_fwd", "osdp_split_linear_bwd", "osdp_split_linear_fwd_mixed",
                  "osdp_split_linear_bwd_mixed", "osdp_granularity_candidates",
                  "osdp_granularity_measure", "osdp_granularity_select", "osdp_cost_model", "osdp_plan_search",
-                 "osdp_profile_begin", "osdp_profile_end"):
+                 "osdp_profile_begin", "osdp_profile_end", "osdp_adamw_step", "osdp_adamw_grad_sumsq",
+                 "osdp_adamw_grad_sumsq_workspace_bytes", "osdp_adamw_state_values", "osdp_split_linear_i8_quantize",
+                 "osdp_split_linear_i8_quantize_workspace_bytes", "osdp_split_linear_i8_fwd",
+                 "osdp_split_linear_i8_workspace_bytes"):
         getattr(lib, name).restype = ctypes.c_int
     lib.osdp_strerror.argtypes = [ctypes.c_int]
     lib.osdp_strerror.restype = ctypes.c_char_p
@@ -373,6 +405,155 @@ def osdp_plan_search(ops, N, alpha, beta, m_limit, b_max=0):
         return None
     return dict(modes=list(modes), b=res.b, time_per_sample=res.time_per_sample, memory=res.memory,
                 batch_sizes_tried=res.batch_sizes_tried, plans_visited=res.plans_visited, exact=bool(res.exact))
+
+
+def _refuse(message: str):
+    raise OsdpError(OSDP_ERR_INVALID_ARG, message)
+
+
+class AdamWTable:
+    """The tensors of an AdamW step, as the library takes them: checked and put together once, used for every step.
+
+    ``grads``: bf16 or fp32 tensors of any shape; ``params``: bf16 or fp32; ``masters``: fp32 copies of bf16 parameters, or
+    None; ``m`` and ``v``: fp32, or uint8 together with ``exps`` (uint8, 2 * ceil(n / 128) of each tensor), all zeros at the
+    start.  ``weight_decay``: one number, or one for each tensor.  The table keeps the tensors alive.  One that is only
+    summed up (``osdp_adamw_grad_sumsq``) needs ``grads`` alone, one that is only looked at (``osdp_adamw_state_values``)
+    ``m``, ``v`` and ``exps``."""
+
+    def __init__(self, params=None, grads=None, masters=None, m=None, v=None, exps=None, weight_decay=0.0):
+        lists = dict(params=params, grads=grads, masters=masters, m=m, v=v, exps=exps)
+        lists = {name: list(ts) for name, ts in lists.items() if ts is not None}
+        first = next((lists[name] for name in ("grads", "params", "m") if name in lists), None)
+        if first is None:
+            _refuse("a table needs tensors")
+        count, lengths = len(first), [t.numel() for t in first]
+        types = {}
+        for name, ts in lists.items():
+            if len(ts) != count:
+                _refuse(f"{len(ts)} {name} for {count} tensors")
+            for i, t in enumerate(ts):
+                want = 2 * -(-lengths[i] // OSDP_ADAMW_BLOCK) if name == "exps" else lengths[i]
+                if not t.is_contiguous() or not t.is_cuda or (t.numel() < want if name == "exps" else t.numel() != want):
+                    _refuse(f"{name}[{i}] must be a contiguous GPU tensor of {want} elements")
+                if types.setdefault(name, t.dtype) != t.dtype:
+                    _refuse(f"{name} are of different types")
+        for name, allowed in (("params", ("torch.bfloat16", "torch.float32")), ("grads", ("torch.bfloat16", "torch.float32")),
+                              ("masters", ("torch.float32",)), ("m", ("torch.float32", "torch.uint8")),
+                              ("v", (str(types.get("m")),)), ("exps", ("torch.uint8",))):
+            if name in types and str(types[name]) not in allowed:
+                _refuse(f"{name} are {types[name]}, not {' or '.join(allowed)}")
+        self.state_bits = 8 if str(types.get("m")) == "torch.uint8" else 32
+        if self.state_bits == 8 and "exps" not in lists:
+            _refuse("moments in 8 bits need exps")
+        self.grad_type = OSDP_F32 if str(types.get("grads")) == "torch.float32" else OSDP_BF16
+        self.param_type = OSDP_F32 if str(types.get("params")) == "torch.float32" else OSDP_BF16
+        self.count, self.lengths = count, lengths
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
+        if len(decay) != count:
+            _refuse(f"{len(decay)} weight decays for {count} tensors")
+        self._keep = lists
+        self.tensors = (osdp_adamw_tensor * max(count, 1))()
+        for i in range(count):
+            c = self.tensors[i]
+            c.n, c.weight_decay = lengths[i], float(decay[i])
+            for name, field in (("params", "param"), ("grads", "grad"), ("masters", "master"), ("m", "m"), ("v", "v"), ("exps", "exps")):
+                setattr(c, field, lists[name][i].data_ptr() if name in lists and lengths[i] else None)
+
+    def set_grads(self, grads) -> None:
+        """New gradients, of the same lengths and type, in place of the table's."""
+        grads = list(grads)
+        if len(grads) != self.count:
+            _refuse(f"{len(grads)} gradients for {self.count} tensors")
+        want = "torch.float32" if self.grad_type == OSDP_F32 else "torch.bfloat16"
+        for i, g in enumerate(grads):
+            if g.numel() != self.lengths[i] or str(g.dtype) != want or not g.is_contiguous() or not g.is_cuda:
+                _refuse(f"grads[{i}] must be a contiguous GPU tensor of {self.lengths[i]} elements, {want}")
+        for i, g in enumerate(grads):
+            self.tensors[i].grad = g.data_ptr() if self.lengths[i] else None
+        self._keep["grads"] = grads
+
+
+def _bytes(workspace) -> int:
+    return workspace.numel() * workspace.element_size()
+
+
+def osdp_adamw_grad_sumsq_workspace_bytes(table: AdamWTable) -> int:
+    need = ctypes.c_size_t()
+    _check(lib.osdp_adamw_grad_sumsq_workspace_bytes(table.tensors, table.count, ctypes.byref(need)))
+    return need.value
+
+
+def osdp_adamw_grad_sumsq(table: AdamWTable, sumsq, workspace, *, accumulate: bool = False, stream=None) -> None:
+    """``sumsq`` (one float64 on the GPU) = sum of the squares of all of the table's gradients; accumulate: is added to it."""
+    if str(sumsq.dtype) != "torch.float64" or sumsq.numel() != 1:
+        _refuse("sumsq must be one float64")
+    _check(lib.osdp_adamw_grad_sumsq(table.tensors, table.count, table.grad_type, int(bool(accumulate)), sumsq.data_ptr(),
+                                     workspace.data_ptr(), _bytes(workspace), _stream(stream)))
+
+
+def osdp_adamw_step(table: AdamWTable, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1,
+                    grad_sumsq=None, max_norm: float = 0.0, seed: int = 0, step_device=None, lr_device=None, stream=None) -> None:
+    """One AdamW step, in place.  ``grad_sumsq`` (one float64), ``step_device`` (one int64) and ``lr_device`` (one float32)
+    are read on the GPU when the kernels run."""
+    for name, t, want in (("grad_sumsq", grad_sumsq, "torch.float64"), ("step_device", step_device, "torch.int64"),
+                          ("lr_device", lr_device, "torch.float32")):
+        if t is not None and (str(t.dtype) != want or t.numel() != 1):
+            _refuse(f"{name} must be one {want}")
+    o = osdp_adamw_options(lr, beta1, beta2, eps, int(step), int(seed) & 0xFFFFFFFFFFFFFFFF, max_norm,
+                           None if grad_sumsq is None else grad_sumsq.data_ptr(),
+                           None if step_device is None else step_device.data_ptr(),
+                           None if lr_device is None else lr_device.data_ptr(),
+                           table.grad_type, table.param_type, table.state_bits, 0)
+    _check(lib.osdp_adamw_step(table.tensors, table.count, ctypes.byref(o), _stream(stream)))
+
+
+def osdp_adamw_state_values(table: AdamWTable, m_out, v_out, *, stream=None) -> None:
+    """The bf16 values of moments in 8 bits: ``m_out`` and ``v_out`` hold one bf16 tensor for each of the table's."""
+    if table.state_bits != 8:
+        _refuse("the table's moments are not in 8 bits")
+    for name, outs in (("m_out", m_out), ("v_out", v_out)):
+        if len(outs) != table.count:
+            _refuse(f"{len(outs)} {name} for {table.count} tensors")
+        for i, t in enumerate(outs):
+            if t.numel() != table.lengths[i] or str(t.dtype) != "torch.bfloat16" or not t.is_contiguous():
+                _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values")
+    _check(lib.osdp_adamw_state_values(table.tensors, table.count, _ptrs(m_out), _ptrs(v_out), _stream(stream)))
+
+
+def osdp_split_linear_i8_quantize_workspace_bytes(I, O, N) -> int:
+    shape, need = _shape(0, I, O, N, 0), ctypes.c_size_t()
+    _check(lib.osdp_split_linear_i8_quantize_workspace_bytes(ctypes.byref(shape), ctypes.byref(need)))
+    return need.value
+
+
+def osdp_split_linear_i8_quantize(I, O, w_shards, q_shards, w_scale, workspace, *, stream=None) -> None:
+    """bf16 shards of W[I x O] -> int8 shards of Wq[O x I] and the channels' scales (fp32 [O])."""
+    shape = _shape(0, I, O, len(w_shards), 0)
+    L = -(-int(I) * int(O) // max(len(w_shards), 1))
+    if len(q_shards) != len(w_shards) or any(q.numel() < L for q in q_shards) or any(w.numel() < L for w in w_shards):
+        _refuse(f"w_shards and q_shards must be as many shards of {L} elements")
+    if w_scale.numel() < O or str(w_scale.dtype) != "torch.float32":
+        _refuse(f"w_scale must hold {O} float32")
+    _check(lib.osdp_split_linear_i8_quantize(ctypes.byref(shape), _ptrs(w_shards), _ptrs(q_shards), w_scale.data_ptr(),
+                                             workspace.data_ptr(), _bytes(workspace), _stream(stream)))
+
+
+def osdp_split_linear_i8_workspace_bytes(T, I, O, N, k):
+    """Returns (total workspace bytes, peak gathered-weight staging bytes)."""
+    shape, total, peak = _shape(T, I, O, N, k), ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib.osdp_split_linear_i8_workspace_bytes(ctypes.byref(shape), ctypes.byref(total), ctypes.byref(peak)))
+    return total.value, peak.value
+
+
+def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=None) -> None:
+    """Y[T x O] = X[T x I] . W with W as int8 shards of Wq[O x I]; X, Y 2-D bf16 tensors (row stride = ld)."""
+    T, I = X.shape
+    O = Y.shape[1]
+    if w_scale.numel() < O or w_scale.element_size() != 4:
+        _refuse(f"w_scale must hold {O} float32")
+    shape = _shape(T, I, O, len(q_shards), k)
+    _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), X.stride(0), _ptrs(q_shards), w_scale.data_ptr(),
+                                        Y.data_ptr(), Y.stride(0), workspace.data_ptr(), _bytes(workspace), _stream(stream)))
 
 
 def osdp_debug_option(name: str, value: int) -> None:

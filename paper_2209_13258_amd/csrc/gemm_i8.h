@@ -1,0 +1,179 @@
+// Products of 8-bit integers: Y[T x O] = bf16( (Xq . Wq^T) * s_t * s_o ), Xq [T x I] and Wq [O x I], both with the reduction contiguous.
+#pragma once
+#include "osdp_internal.h"
+
+namespace osdp {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Largest magnitude, as fp32 bits, of eight bf16 values (a NaN's is larger than any number's).
+__device__ __forceinline__ uint32_t i8_largest(uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m = max(m, max((w[j] << 16) & 0x7fff0000u, w[j] & 0x7fff0000u));
+  return m;
+}
+
+// From the bits of a row's or column's largest magnitude: its scale and the rounding of its values to 8 bits.
+struct I8Scale {
+  float scale, up, r;
+  __device__ __forceinline__ explicit I8Scale(uint32_t most) {
+    const float amax = __uint_as_float(most);
+    const bool number = most < 0x7f800000u;
+    scale = number ? amax / 127.f : __uint_as_float(0x7fc00000u);
+    up = amax < 0x1p-100f ? 0x1p100f : 1.f;  // (127 / amax would be no number; a power of two changes no quotient)
+    r = number && most != 0u ? 127.f / (amax * up) * (1.f + 0x1p-21f) : 0.f;
+  }
+  __device__ __forceinline__ uint32_t round(float x) const {  // lower 8 bits
+    const float t = fminf(fmaf(fabsf(x * up), r, 0.5f), 127.f);
+    const int q = static_cast<int>(r == 0.f ? 0.f : t);
+    return static_cast<uint32_t>(__float_as_uint(x) >> 31 ? -q : q);
+  }
+  __device__ __forceinline__ uint2 round8(uint4 v) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t out[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t q = round(__uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16));
+      out[j >> 2] |= (q & 255u) << (8 * (j & 3));
+    }
+    return uint2{out[0], out[1]};
+  }
+};
+
+// Bytes from one row of Xq to the next: whole pieces of 128, which end in zeros.
+constexpr int64_t i8_row_bytes(int64_t I) { return (I + 127) / 128 * 128; }
+
+struct I8Problem {
+  int32_t T, I, O, ldq;
+  const uint8_t *xq;
+  const float *x_scale;
+  ShardTable shards;      // of Wq
+  int64_t L;              // bytes of a shard
+  int32_t rows_each;      // > 0: rows of Wq (output channels) to a shard; 0: rows may go on in the next shard
+  const float *w_scale;
+  uint16_t *y;
+  int64_t ldy;
+};
+
+// Up to this many tokens the product reads the weight where it lies, however it is cut.
+constexpr int64_t kI8FewTokens = 64;
+
+// ---- few tokens -----------------------------------------------------------------------------------------------------
+// A workgroup owns 16 * NB output channels and 16 * MB tokens; its kWaves waves share the reduction, 64 * kUnroll bytes of
+// every row at a time, and add their sums up in LDS (integers: in any order).  Weights go from memory to registers, each lane 16
+// bytes of a row, the four lanes of a row 64 in sequence; nothing of them is used twice, so nothing is staged.
+template <int MB, int NB, int kWaves, int kUnroll, bool kFlat>
+__global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
+  constexpr int BM = 16 * MB, BN = 16 * NB, kStep = 64 * kUnroll;
+  __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
+  __shared__ int sums[BM * BN];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
+  if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
+  for (int i = tid; i < BM * BN; i += kWaves * 64) sums[i] = 0;
+  __syncthreads();
+  const int n0 = blockIdx.x * BN, m0 = blockIdx.y * BM;
+  // where this lane's rows of the weight begin (rows beyond the last repeat it; they are not stored)
+  const uint8_t *row[NB];
+  int64_t off[NB];
+  int shard[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int o = min(n0 + 16 * b + l16, p.O - 1);
+    if (!kFlat) {
+      const int s = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.rows_each));
+      row[b] = tab[s] + static_cast<int64_t>(o - s * p.rows_each) * p.I;
+    } else {
+      const uint64_t f = static_cast<uint64_t>(o) * p.I;
+      shard[b] = static_cast<int>(f / static_cast<uint64_t>(p.L));
+      off[b] = static_cast<int64_t>(f - static_cast<uint64_t>(shard[b]) * p.L);
+    }
+  }
+  const uint8_t *token[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) token[b] = p.xq + static_cast<int64_t>(min(m0 + 16 * b + l16, p.T - 1)) * p.ldq;
+  i32x4 acc[MB][NB];
+#pragma unroll
+  for (int bm = 0; bm < MB; ++bm)
+#pragma unroll
+    for (int bn = 0; bn < NB; ++bn) acc[bm][bn] = i32x4{0, 0, 0, 0};
+  for (int k0 = wave * kStep; k0 < p.I; k0 += kWaves * kStep) {
+    uint4 w[kUnroll][NB], x[kUnroll][MB];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int k = k0 + 64 * u + 16 * q4;
+      const int kw = k < p.I ? k : 0;       // beyond the row's end: any weights, the tokens are zeros there
+      const int kx = k < p.ldq ? k : p.ldq - 16;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const uint8_t *at;
+        if (!kFlat) {
+          at = row[b] + kw;
+        } else {
+          int64_t f = off[b] + kw;
+          int s = shard[b];
+          while (f >= p.L) {
+            f -= p.L;
+            ++s;
+          }
+          at = tab[s] + f;
+        }
+        w[u][b] = load_global16(at);
+      }
+#pragma unroll
+      for (int b = 0; b < MB; ++b) x[u][b] = load_global16(token[b] + kx);
+      if (k >= p.ldq) {
+#pragma unroll
+        for (int b = 0; b < MB; ++b) x[u][b] = uint4{0u, 0u, 0u, 0u};
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int bm = 0; bm < MB; ++bm)
+#pragma unroll
+        for (int bn = 0; bn < NB; ++bn)
+          acc[bm][bn] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u][bn]), __builtin_bit_cast(i32x4, x[u][bm]),
+                                                              acc[bm][bn], 0, 0, 0);
+  }
+#pragma unroll
+  for (int bm = 0; bm < MB; ++bm)
+#pragma unroll
+    for (int bn = 0; bn < NB; ++bn)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) atomicAdd(&sums[(16 * bm + l16) * BN + 16 * bn + 4 * q4 + i], acc[bm][bn][i]);
+  __syncthreads();
+  for (int i = tid; i < BM * BN / 8; i += kWaves * 64) {
+    const int r = i / (BN / 8), c = i % (BN / 8) * 8, m = m0 + r, n = n0 + c;
+    if (m >= p.T || n >= p.O) continue;
+    const float st = p.x_scale[m];
+    uint32_t out[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float y[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) y[e] = static_cast<float>(sums[r * BN + c + 2 * j + e]) * st * p.w_scale[n + 2 * j + e];
+      out[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(y[0]))) |
+               static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(y[1]))) << 16;
+    }
+    store_global16(p.y + static_cast<int64_t>(m) * p.ldy + n, uint4{out[0], out[1], out[2], out[3]});
+  }
+}
+
+template <int MB, int NB, int kWaves, int kUnroll>
+hipError_t launch_few(const I8Problem &p, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((p.O + 16 * NB - 1) / (16 * NB)), static_cast<unsigned>((p.T + 16 * MB - 1) / (16 * MB)));
+  if (p.rows_each > 0) hipLaunchKernelGGL((i8_few_kernel<MB, NB, kWaves, kUnroll, false>), grid, dim3(kWaves * 64), 0, stream, p);
+  else hipLaunchKernelGGL((i8_few_kernel<MB, NB, kWaves, kUnroll, true>), grid, dim3(kWaves * 64), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_i8(const I8Problem &p, hipStream_t stream) {
+  if (p.T <= 16) return launch_few<1, 1, 8, 4>(p, stream);
+  return launch_few<4, 4, 8, 1>(p, stream);
+}
+
+}  // namespace
+}  // namespace osdp

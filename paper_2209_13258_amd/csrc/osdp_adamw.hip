@@ -1,0 +1,684 @@
+// AdamW over many tensors at once, the sum of squares of their gradients, and the values of moments in 8 bits.
+//
+// Everything here is one pass over memory with some arithmetic on the way.  Per element a step moves 28 bytes (bf16
+// gradient, parameter written, fp32 master and moments), 16 with moments in 8 bits, 10 when there is no master copy either.
+//
+// A launch covers up to kBatch tensors, whose pointers travel by value in the kernel's arguments (nothing to allocate or
+// upload, and a captured graph keeps them).  Tensors are cut into tiles of 2048 elements, one to a workgroup of 256 at a time: 8
+// elements to a lane, so that a row of 16 lanes is one block of 128 that moments in 8 bits share a power of two over, and
+// its largest magnitude is found without leaving the row (four DPP steps, no LDS, no barrier).
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <limits>
+
+#include "osdp_internal.h"
+
+namespace osdp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPerLane = 8;
+constexpr int kTile = kThreads * kPerLane;
+constexpr int kBlock = 128;      // elements that share a power of two: kPerLane * 16 lanes
+constexpr int kBatch = 56;       // tensors to a launch: 4 KB of kernel arguments
+constexpr int64_t kMaxElements = int64_t{1} << 40;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct Tensor {
+  const void *grad;
+  void *param;
+  float *master;
+  void *m, *v;
+  uint8_t *exps;
+  int64_t n;
+  float decay;          // weight_decay
+  uint32_t end_tile;    // tiles of this and all earlier tensors of the batch
+};
+
+struct Batch {
+  Tensor t[kBatch];
+  uint64_t wide;        // bit i: tensor i is aligned for 16-byte accesses
+  int32_t count;
+  uint32_t first;       // place of t[0] in the caller's array
+  uint32_t tiles;
+};
+
+struct Step {
+  double lr, beta1, beta2;
+  int64_t step;
+  const double *sumsq;
+  const int64_t *step_device;
+  const float *lr_device;
+  double max_norm;
+  uint32_t seed_lo, seed_hi;
+  float b1, c1, b2, c2, eps;  // c: 1 - beta, taken in double
+  float rate, root;           // lr / (1 - beta1^t) and 1 / sqrt(1 - beta2^t), where t and lr come from the host
+};
+
+enum Form { kMaster = 0, kBf16 = 1, kF32 = 2 };
+
+// 32 bits stirred: multiplications by odd numbers and shifted sums without carry, each of them one to one.
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x *= 0x9E3779B1u;
+  x ^= x >> 15;
+  x *= 0x2C1B3C6Du;
+  return x ^ (x >> 13);
+}
+
+// base^n by squaring: the same in a kernel and on the host.
+__host__ __device__ inline double power(double base, int64_t n) {
+  double r = 1.0;
+  for (; n > 0; n >>= 1) {
+    if (n & 1) r *= base;
+    base *= base;
+  }
+  return r;
+}
+
+// Tensor and element of a tile: tensors are found by halving, on the scalar unit (the tile is common to the workgroup).
+__device__ __forceinline__ int tensor_of(const Batch &b, uint32_t tile) {
+  int lo = 0, hi = b.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (tile < b.t[mid].end_tile) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// Element j of the lane's eight: side by side where a tile is read 16 bytes at a time; otherwise the lanes of a row of 16
+// take neighbouring elements, so that accesses of single elements still cover whole segments.  Either way a row is a block.
+template <bool kWide>
+__device__ __forceinline__ uint32_t element(int j) {
+  const uint32_t row = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  return row * kBlock + (kWide ? lane * kPerLane + j : j * 16u + lane);
+}
+
+template <bool kWide>
+__device__ __forceinline__ void load8(const float *p, int64_t at, uint32_t left, float (&x)[8]) {
+  if constexpr (kWide) {
+    const f32x4 *q = reinterpret_cast<const f32x4 *>(p + at + element<true>(0));
+    const f32x4 a = q[0], b = q[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = element<false>(j) < left ? p[at + element<false>(j)] : 0.f;
+  }
+}
+
+template <bool kWide>
+__device__ __forceinline__ void load8(const uint16_t *p, int64_t at, uint32_t left, float (&x)[8]) {
+  if constexpr (kWide) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(p + at + element<true>(0));
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(w[j] << 16);
+      x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      x[j] = element<false>(j) < left ? __uint_as_float(static_cast<uint32_t>(p[at + element<false>(j)]) << 16) : 0.f;
+  }
+}
+
+template <bool kWide>
+__device__ __forceinline__ void load8(const uint8_t *p, int64_t at, uint32_t left, uint32_t (&x)[8]) {
+  if constexpr (kWide) {
+    const uint2 a = *reinterpret_cast<const uint2 *>(p + at + element<true>(0));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = (a.x >> (8 * j)) & 255u;
+      x[4 + j] = (a.y >> (8 * j)) & 255u;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = element<false>(j) < left ? p[at + element<false>(j)] : 0u;
+  }
+}
+
+template <bool kWide>
+__device__ __forceinline__ void store8(float *p, int64_t at, uint32_t left, const float (&x)[8]) {
+  if constexpr (kWide) {
+    f32x4 *q = reinterpret_cast<f32x4 *>(p + at + element<true>(0));
+    q[0] = f32x4{x[0], x[1], x[2], x[3]};
+    q[1] = f32x4{x[4], x[5], x[6], x[7]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (element<false>(j) < left) p[at + element<false>(j)] = x[j];
+  }
+}
+
+// bf16 bit patterns in the upper halves of x
+template <bool kWide>
+__device__ __forceinline__ void store8(uint16_t *p, int64_t at, uint32_t left, const uint32_t (&x)[8]) {
+  if constexpr (kWide) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (x[2 * j] >> 16) | (x[2 * j + 1] & 0xffff0000u);
+    *reinterpret_cast<uint4 *>(p + at + element<true>(0)) = uint4{w[0], w[1], w[2], w[3]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (element<false>(j) < left) p[at + element<false>(j)] = static_cast<uint16_t>(x[j] >> 16);
+  }
+}
+
+template <bool kWide>
+__device__ __forceinline__ void store8(uint8_t *p, int64_t at, uint32_t left, const uint32_t (&x)[8]) {
+  if constexpr (kWide) {
+    uint2 w = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w.x |= x[j] << (8 * j);
+      w.y |= x[4 + j] << (8 * j);
+    }
+    *reinterpret_cast<uint2 *>(p + at + element<true>(0)) = w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (element<false>(j) < left) p[at + element<false>(j)] = static_cast<uint8_t>(x[j]);
+  }
+}
+
+// Largest of a value over the 16 lanes of a row, in all of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+  auto turned = [](uint32_t v, auto ctrl) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x = max(x, turned(x, std::integral_constant<int, 0x128>{}));  // row_ror:8, :4, :2, :1
+  x = max(x, turned(x, std::integral_constant<int, 0x124>{}));
+  x = max(x, turned(x, std::integral_constant<int, 0x122>{}));
+  return max(x, turned(x, std::integral_constant<int, 0x121>{}));
+}
+
+// ---- moments in 8 bits: kTop is the largest exponent field (15: m, 31: v), kLow the least b -------------------------
+// With its exponent field and fraction put where fp32 has them, a code is the value times a power of two; where the field
+// is 0 fp32 reads them as it reads its own smallest numbers, which is what the format wants.
+template <int kTop>
+__device__ __forceinline__ float decode(uint32_t code, uint32_t b) {
+  const uint32_t magnitude = kTop == 15 ? code & 127u : code;
+  const uint32_t nan = b == 255u ? 0x7fc00000u : 0u;
+  const float x = __builtin_amdgcn_ldexpf(__uint_as_float((magnitude << 20) | nan), static_cast<int>(b) - kTop);
+  return kTop == 15 ? __uint_as_float(__float_as_uint(x) ^ ((code & 128u) << 24)) : x;
+}
+
+// The power of two of a block whose largest magnitude has these bits: rounding up to 3 fraction bits may carry into the
+// next binade, or (FLT_MAX) out of the numbers, like a NaN or an infinity.
+template <int kLow>
+__device__ __forceinline__ uint32_t block_exponent(uint32_t most) {
+  const uint32_t b = (most + 0xfffffu) >> 23;
+  return most == 0u ? 0u : max(b, static_cast<uint32_t>(kLow));
+}
+
+// In units of its binade's step a magnitude is x in [0, 16) (below 8 in the smallest binade only); x plus a fraction from
+// 16 random bits, cut, is 16 at most by the carry into the next binade, and never beyond the block's own largest code.
+template <int kTop>
+__device__ __forceinline__ uint32_t encode(float x, uint32_t b, uint32_t random16) {
+  const uint32_t bits = __float_as_uint(x), size = bits & 0x7fffffffu;
+  const uint32_t least = b - (kTop - 1);
+  const uint32_t e = max(size >> 23, least);
+  const float units = __builtin_amdgcn_ldexpf(__uint_as_float(size), 130 - static_cast<int>(e));
+  const uint32_t q = static_cast<uint32_t>(fmaf(static_cast<float>(random16), 0x1p-16f, units));
+  uint32_t code = (e - least) * 8u + q;
+  if (kTop == 31) code = size != 0u && code == 0u ? 1u : code;  // (a positive v stays positive)
+  if (b == 0u || b == 255u) return 0u;
+  return kTop == 15 ? code | ((bits >> 24) & 128u) : code;
+}
+
+struct Scalars {
+  float coef, rate, root, lr;
+  uint32_t key;
+};
+
+// m and v as the formulas have them, every operation rounded by itself.
+__device__ __forceinline__ void moments(const Step &s, float coef, float grad, float &m, float &v) {
+#pragma clang fp contract(off)
+  const float g = grad * coef;
+  const float mb = m * s.b1, gc = g * s.c1, vb = v * s.b2, gg = (g * g) * s.c2;
+  m = mb + gc;
+  v = vb + gg;
+}
+
+template <class Grad, int kForm, bool kState8, bool kWide>
+__device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const Scalars &k, int64_t at) {
+  const int64_t rest = t.n - at;
+  const uint32_t left = rest < kTile ? static_cast<uint32_t>(rest) : kTile;
+  using Param = std::conditional_t<kForm == kF32, float, uint16_t>;
+  float g[8], p[8], m[8], v[8];
+  uint32_t cm[8], cv[8];
+  uint16_t *exps = nullptr;
+  uint32_t shared = 0;
+  load8<kWide>(static_cast<const Grad *>(t.grad), at, left, g);
+  if constexpr (kForm == kMaster) load8<kWide>(static_cast<const float *>(t.master), at, left, p);
+  else load8<kWide>(static_cast<const Param *>(t.param), at, left, p);
+  if constexpr (kState8) {
+    exps = reinterpret_cast<uint16_t *>(t.exps) + at / kBlock + (threadIdx.x >> 4);
+    if ((threadIdx.x >> 4) * kBlock < left) shared = *exps;
+    load8<kWide>(static_cast<const uint8_t *>(t.m), at, left, cm);
+    load8<kWide>(static_cast<const uint8_t *>(t.v), at, left, cv);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = decode<15>(cm[j], shared & 255u);
+      v[j] = decode<31>(cv[j], shared >> 8);
+    }
+  } else {
+    load8<kWide>(static_cast<const float *>(t.m), at, left, m);
+    load8<kWide>(static_cast<const float *>(t.v), at, left, v);
+  }
+  const float decay = k.lr * t.decay;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    moments(s, k.coef, g[j], m[j], v[j]);
+    // (both approximations are within an ulp; the root of a number below fp32's normal range, 1e-19, is nothing beside eps)
+    const float size = fmaf(__builtin_amdgcn_sqrtf(v[j]), k.root, s.eps);
+    p[j] -= fmaf(m[j] * k.rate, __builtin_amdgcn_rcpf(size), decay * p[j]);
+  }
+  uint32_t h[8];
+  if constexpr (kState8 || kForm == kBf16) {
+    const uint32_t base = mix(k.key ^ static_cast<uint32_t>(at >> 32)) + static_cast<uint32_t>(at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = mix(base + element<kWide>(j));
+  }
+  if constexpr (kState8) {
+    uint32_t most_m = 0, most_v = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (!kWide && element<kWide>(j) >= left) m[j] = v[j] = 0.f;  // (0 * beta is NaN where the block was)
+      most_m = max(most_m, __float_as_uint(m[j]) & 0x7fffffffu);
+      most_v = max(most_v, __float_as_uint(v[j]) & 0x7fffffffu);
+    }
+    const uint32_t bm = block_exponent<32>(row_max(most_m)), bv = block_exponent<48>(row_max(most_v));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      cm[j] = encode<15>(m[j], bm, h[j] & 0xffffu);
+      cv[j] = encode<31>(v[j], bv, h[j] >> 16);
+    }
+    if ((threadIdx.x & 15) == 0 && (threadIdx.x >> 4) * kBlock < left) *exps = static_cast<uint16_t>(bm | (bv << 8));
+    store8<kWide>(static_cast<uint8_t *>(t.m), at, left, cm);
+    store8<kWide>(static_cast<uint8_t *>(t.v), at, left, cv);
+  } else {
+    store8<kWide>(static_cast<float *>(t.m), at, left, m);
+    store8<kWide>(static_cast<float *>(t.v), at, left, v);
+  }
+  if constexpr (kForm == kMaster) store8<kWide>(t.master, at, left, p);
+  if constexpr (kForm == kF32) {
+    store8<kWide>(static_cast<float *>(t.param), at, left, p);
+  } else {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t bits = __float_as_uint(p[j]);
+      if constexpr (kForm == kMaster) {
+        w[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(p[j]))) << 16;
+      } else {
+        // to one of its neighbours, the one above with the probability that keeps the mean; NaN and infinities as they are
+        const bool number = (bits & 0x7f800000u) != 0x7f800000u;
+        w[j] = number ? bits + ((h[j] * 0x297A2D39u) >> 16) : bits | ((bits & 0x7fffffu) ? 0x400000u : 0u);
+      }
+    }
+    store8<kWide>(static_cast<uint16_t *>(t.param), at, left, w);
+  }
+}
+
+// Scalars of a call: one for all lanes.
+__device__ __forceinline__ bool scalars_of(const Step &s, Scalars *k) {
+  k->coef = 1.f;
+  if (s.sumsq) {
+    const double sum = *s.sumsq;
+    if (!(sum < std::numeric_limits<double>::infinity())) return false;  // (NaN too)
+    if (s.max_norm > 0.0) {
+      const double norm = sqrt(sum);
+      if (norm > s.max_norm) k->coef = static_cast<float>(s.max_norm / norm);
+    }
+  }
+  k->rate = s.rate;
+  k->root = s.root;
+  k->lr = static_cast<float>(s.lr);
+  int64_t step = s.step;
+  if (s.step_device || s.lr_device) {
+    const double lr = s.lr_device ? static_cast<double>(*s.lr_device) : s.lr;
+    if (s.step_device) step = *s.step_device;
+    if (step < 1) step = 1;
+    k->lr = static_cast<float>(lr);
+    k->rate = static_cast<float>(lr / (1.0 - power(s.beta1, step)));
+    k->root = static_cast<float>(1.0 / sqrt(1.0 - power(s.beta2, step)));
+  }
+  k->key = mix(mix(mix(s.seed_lo) ^ s.seed_hi) ^ static_cast<uint32_t>(step));
+  return true;
+}
+
+template <class Grad, int kForm, bool kState8>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Batch b, Step s) {
+  Scalars k;
+  if (!scalars_of(s, &k)) return;
+  const uint32_t stirred = k.key;
+  for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
+    const int i = tensor_of(b, tile);
+    const Tensor &t = b.t[i];
+    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
+    k.key = mix(stirred ^ (b.first + static_cast<uint32_t>(i)));
+    if (((b.wide >> i) & 1u) && t.n - at >= kTile) adamw_tile<Grad, kForm, kState8, true>(t, s, k, at);
+    else adamw_tile<Grad, kForm, kState8, false>(t, s, k, at);
+  }
+}
+
+template <bool kWide>
+__device__ __forceinline__ void values_tile(const Tensor &t, int64_t at) {
+  const int64_t rest = t.n - at;
+  const uint32_t left = rest < kTile ? static_cast<uint32_t>(rest) : kTile;
+  uint32_t shared = 0, cm[8], cv[8], wm[8], wv[8];
+  if ((threadIdx.x >> 4) * kBlock < left) shared = reinterpret_cast<const uint16_t *>(t.exps)[at / kBlock + (threadIdx.x >> 4)];
+  load8<kWide>(static_cast<const uint8_t *>(t.m), at, left, cm);
+  load8<kWide>(static_cast<const uint8_t *>(t.v), at, left, cv);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    wm[j] = __float_as_uint(decode<15>(cm[j], shared & 255u));
+    wv[j] = __float_as_uint(decode<31>(cv[j], shared >> 8));
+  }
+  store8<kWide>(static_cast<uint16_t *>(t.param), at, left, wm);                          // (m's values)
+  store8<kWide>(reinterpret_cast<uint16_t *>(t.master), at, left, wv);                    // (v's values)
+}
+
+__global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
+  for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
+    const int i = tensor_of(b, tile);
+    const Tensor &t = b.t[i];
+    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
+    if (((b.wide >> i) & 1u) && t.n - at >= kTile) values_tile<true>(t, at);
+    else values_tile<false>(t, at);
+  }
+}
+
+// ---- sum of squares -------------------------------------------------------------------------------------------
+// Squares and sums are in double from the first product on (a bf16 gradient of 1e20 is one, its square in fp32 is not): the
+// vector unit multiplies and adds them as fast as fp32, and the pass stays bound by memory.
+constexpr int kSumBlocks = 1024;  // workgroups, and so partial sums, of a launch at most
+
+__device__ __forceinline__ double block_sum(double x) {
+  __shared__ double part[kThreads / 64];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  double sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) sum += part[w];
+  return sum;
+}
+
+template <class Grad>
+__global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, double *__restrict__ out) {
+  double sum = 0.0;
+  for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
+    const int i = tensor_of(b, tile);
+    const Tensor &t = b.t[i];
+    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
+    const int64_t rest = t.n - at;
+    float g[8];
+    if (((b.wide >> i) & 1u) && rest >= kTile) load8<true>(static_cast<const Grad *>(t.grad), at, kTile, g);
+    else load8<false>(static_cast<const Grad *>(t.grad), at, rest < kTile ? static_cast<uint32_t>(rest) : kTile, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fma(static_cast<double>(g[j]), static_cast<double>(g[j]), sum);
+  }
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) out[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(kThreads) void sumsq_finish_kernel(const double *__restrict__ part, int32_t count, int32_t accumulate,
+                                                                double *__restrict__ out) {
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < count; i += kThreads) sum += part[i];
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) *out = accumulate ? *out + sum : sum;
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------
+osdp_status fail(osdp_status st, const char *fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return report_error(st, buf);
+}
+
+osdp_status hip_status(hipError_t e, const char *what) {
+  if (e == hipSuccess) return OSDP_OK;
+  return fail(OSDP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+osdp_status device_ok() {
+  const hipError_t e = check_device();
+  if (e == hipErrorInvalidDevice)
+    return fail(OSDP_ERR_UNSUPPORTED, "the current device is not an MI355X (256 compute units in 8 XCDs), which the kernels are written for");
+  return hip_status(e, "querying the device");
+}
+
+bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+osdp_status check_count(const osdp_adamw_tensor *tensors, int32_t count) {
+  if (count < 0) return fail(OSDP_ERR_INVALID_ARG, "count must be >= 0 (got %d)", count);
+  if (count > 0 && !tensors) return fail(OSDP_ERR_INVALID_ARG, "tensors is NULL");
+  for (int32_t i = 0; i < count; ++i)
+    if (tensors[i].n < 0 || tensors[i].n >= kMaxElements)
+      return fail(OSDP_ERR_INVALID_ARG, "tensors[%d] has %lld elements: 0 to 2^40 - 1 are possible", i, (long long)tensors[i].n);
+  return OSDP_OK;
+}
+
+osdp_status check_array(const void *p, size_t align, int32_t i, const char *name) {
+  if (!p) return fail(OSDP_ERR_INVALID_ARG, "tensors[%d].%s is NULL", i, name);
+  if (!aligned(p, align)) return fail(OSDP_ERR_UNSUPPORTED, "tensors[%d].%s is not %zu-byte aligned", i, name, align);
+  return OSDP_OK;
+}
+
+size_t size_of(int32_t type) { return type == OSDP_BF16 ? 2 : 4; }
+
+// Calls launch(batch) for the tensors that have elements, up to kBatch at a time and at most `most` tiles where more would not
+// do; fill(i, &tensor) sets what the kernel reads and says whether it may use 16-byte accesses.
+template <class Fill, class Launch>
+osdp_status for_batches(const osdp_adamw_tensor *tensors, int32_t count, Fill &&fill, Launch &&launch) {
+  Batch b;
+  b.count = 0; b.tiles = 0; b.wide = 0;
+  int32_t last = -1;  // place of the batch's last tensor: places within a batch are consecutive
+  auto flush = [&]() -> osdp_status {
+    if (b.count == 0) return OSDP_OK;
+    const osdp_status st = launch(b);
+    b.count = 0; b.tiles = 0; b.wide = 0;
+    return st;
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    if (tensors[i].n == 0) continue;
+    const uint64_t tiles = (static_cast<uint64_t>(tensors[i].n) + kTile - 1) / kTile;  // < 2^29
+    if (b.count == kBatch || b.tiles + tiles >= (1ull << 31) || (b.count > 0 && i != last + 1)) {
+      const osdp_status st = flush();
+      if (st != OSDP_OK) return st;
+    }
+    if (b.count == 0) b.first = static_cast<uint32_t>(i);
+    Tensor &t = b.t[b.count];
+    t = Tensor{};
+    t.n = tensors[i].n;
+    if (fill(i, &t)) b.wide |= 1ull << b.count;
+    b.tiles += static_cast<uint32_t>(tiles);
+    t.end_tile = b.tiles;
+    ++b.count;
+    last = i;
+  }
+  return flush();
+}
+
+unsigned grid_of(const Batch &b, unsigned most) { return std::min<unsigned>(b.tiles, most); }
+constexpr unsigned kMostBlocks = 1u << 20;
+
+template <class Grad, int kForm, bool kState8>
+hipError_t launch_adamw(const Batch &b, const Step &s, hipStream_t stream) {
+  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(b, kMostBlocks)), dim3(kThreads), 0, stream, b, s);
+  return hipGetLastError();
+}
+
+template <class Grad>
+hipError_t launch_adamw(int form, bool state8, const Batch &b, const Step &s, hipStream_t stream) {
+  if (form == kMaster) return state8 ? launch_adamw<Grad, kMaster, true>(b, s, stream) : launch_adamw<Grad, kMaster, false>(b, s, stream);
+  if (form == kBf16) return state8 ? launch_adamw<Grad, kBf16, true>(b, s, stream) : launch_adamw<Grad, kBf16, false>(b, s, stream);
+  return state8 ? launch_adamw<Grad, kF32, true>(b, s, stream) : launch_adamw<Grad, kF32, false>(b, s, stream);
+}
+
+// Workgroups, and so partial sums, of the launch over a batch.
+unsigned sum_blocks(const Batch &b) { return grid_of(b, kSumBlocks); }
+
+osdp_status sumsq_parts(const osdp_adamw_tensor *tensors, int32_t count, int64_t *parts) {
+  *parts = 0;
+  return for_batches(tensors, count, [](int32_t, Tensor *) { return false; },
+                     [&](const Batch &b) { *parts += sum_blocks(b); return OSDP_OK; });
+}
+
+}  // namespace
+}  // namespace osdp
+
+using namespace osdp;
+
+extern "C" {
+
+osdp_status osdp_adamw_step(const osdp_adamw_tensor *tensors, int32_t count, const osdp_adamw_options *o, void *stream) {
+  osdp_status st = check_count(tensors, count);
+  if (st != OSDP_OK) return st;
+  if (!o) return fail(OSDP_ERR_INVALID_ARG, "options is NULL");
+  if (o->grad_type != OSDP_BF16 && o->grad_type != OSDP_F32) return fail(OSDP_ERR_INVALID_ARG, "unknown grad_type %d", o->grad_type);
+  if (o->param_type != OSDP_BF16 && o->param_type != OSDP_F32) return fail(OSDP_ERR_INVALID_ARG, "unknown param_type %d", o->param_type);
+  if (o->state_bits != 32 && o->state_bits != 8) return fail(OSDP_ERR_INVALID_ARG, "state_bits must be 32 or 8 (got %d)", o->state_bits);
+  if (!(o->lr >= 0.0) || !std::isfinite(o->lr)) return fail(OSDP_ERR_INVALID_ARG, "lr must be a number >= 0");
+  if (!(o->beta1 >= 0.0 && o->beta1 < 1.0) || !(o->beta2 >= 0.0 && o->beta2 < 1.0))
+    return fail(OSDP_ERR_INVALID_ARG, "beta1 and beta2 must lie in [0, 1)");
+  if (!(o->eps >= 1e-12) || !(o->eps <= 1e30)) return fail(OSDP_ERR_INVALID_ARG, "eps must be at least 1e-12");
+  if (!o->step_device && o->step < 1) return fail(OSDP_ERR_INVALID_ARG, "step must be >= 1 (got %lld)", (long long)o->step);
+  if (!(o->max_norm >= 0.0)) return fail(OSDP_ERR_INVALID_ARG, "max_norm must be >= 0");
+  if (o->max_norm > 0.0 && !o->grad_sumsq) return fail(OSDP_ERR_INVALID_ARG, "max_norm needs grad_sumsq");
+  if (!aligned(o->grad_sumsq, 8) || !aligned(o->step_device, 8) || !aligned(o->lr_device, 4))
+    return fail(OSDP_ERR_UNSUPPORTED, "grad_sumsq, step_device or lr_device is not aligned to its type");
+  const bool state8 = o->state_bits == 8;
+  int form = -1;
+  for (int32_t i = 0; i < count; ++i) {
+    const osdp_adamw_tensor &t = tensors[i];
+    if (t.n == 0) continue;
+    if ((st = check_array(t.grad, size_of(o->grad_type), i, "grad")) != OSDP_OK) return st;
+    if ((st = check_array(t.param, size_of(o->param_type), i, "param")) != OSDP_OK) return st;
+    if ((st = check_array(t.m, state8 ? 1 : 4, i, "m")) != OSDP_OK) return st;
+    if ((st = check_array(t.v, state8 ? 1 : 4, i, "v")) != OSDP_OK) return st;
+    if (state8 && (st = check_array(t.exps, 2, i, "exps")) != OSDP_OK) return st;
+    if (t.master && (st = check_array(t.master, 4, i, "master")) != OSDP_OK) return st;
+    if (!(t.weight_decay >= 0.0) || !std::isfinite(t.weight_decay)) return fail(OSDP_ERR_INVALID_ARG, "tensors[%d].weight_decay must be a number >= 0", i);
+    const int f = o->param_type == OSDP_F32 ? kF32 : (t.master ? kMaster : kBf16);
+    if (f == kF32 && t.master) return fail(OSDP_ERR_INVALID_ARG, "tensors[%d] has a master copy of fp32 parameters", i);
+    if (form >= 0 && f != form) return fail(OSDP_ERR_INVALID_ARG, "some of the tensors have masters and some have none");
+    form = f;
+  }
+  if ((st = device_ok()) != OSDP_OK) return st;
+  Step s{};
+  s.lr = o->lr; s.beta1 = o->beta1; s.beta2 = o->beta2;
+  s.step = o->step_device ? 1 : o->step;
+  s.sumsq = o->grad_sumsq; s.step_device = o->step_device; s.lr_device = o->lr_device;
+  s.max_norm = o->max_norm;
+  s.seed_lo = static_cast<uint32_t>(o->seed); s.seed_hi = static_cast<uint32_t>(o->seed >> 32);
+  s.b1 = static_cast<float>(o->beta1); s.c1 = static_cast<float>(1.0 - o->beta1);
+  s.b2 = static_cast<float>(o->beta2); s.c2 = static_cast<float>(1.0 - o->beta2);
+  s.eps = static_cast<float>(o->eps);
+  s.rate = static_cast<float>(o->lr / (1.0 - power(o->beta1, s.step)));
+  s.root = static_cast<float>(1.0 / std::sqrt(1.0 - power(o->beta2, s.step)));
+  return for_batches(
+      tensors, count,
+      [&](int32_t i, Tensor *t) {
+        const osdp_adamw_tensor &u = tensors[i];
+        t->grad = u.grad; t->param = u.param; t->master = u.master; t->m = u.m; t->v = u.v; t->exps = u.exps;
+        t->decay = static_cast<float>(u.weight_decay);
+        const size_t state = state8 ? 8 : 16;
+        return aligned(u.grad, 16) && aligned(u.param, 16) && aligned(u.master, 16) && aligned(u.m, state) && aligned(u.v, state);
+      },
+      [&](const Batch &b) {
+        const hipStream_t q = static_cast<hipStream_t>(stream);
+        return hip_status(o->grad_type == OSDP_BF16 ? launch_adamw<uint16_t>(form, state8, b, s, q) : launch_adamw<float>(form, state8, b, s, q),
+                          "launching the step");
+      });
+}
+
+osdp_status osdp_adamw_grad_sumsq_workspace_bytes(const osdp_adamw_tensor *tensors, int32_t count, size_t *bytes) {
+  osdp_status st = check_count(tensors, count);
+  if (st != OSDP_OK) return st;
+  if (!bytes) return fail(OSDP_ERR_INVALID_ARG, "bytes is NULL");
+  int64_t parts = 0;
+  if ((st = sumsq_parts(tensors, count, &parts)) != OSDP_OK) return st;
+  *bytes = static_cast<size_t>(parts) * sizeof(double);
+  return OSDP_OK;
+}
+
+osdp_status osdp_adamw_grad_sumsq(const osdp_adamw_tensor *tensors, int32_t count, int32_t grad_type, int32_t accumulate,
+                                  double *sumsq, void *workspace, size_t workspace_bytes, void *stream) {
+  osdp_status st = check_count(tensors, count);
+  if (st != OSDP_OK) return st;
+  if (grad_type != OSDP_BF16 && grad_type != OSDP_F32) return fail(OSDP_ERR_INVALID_ARG, "unknown grad_type %d", grad_type);
+  if (!sumsq) return fail(OSDP_ERR_INVALID_ARG, "sumsq is NULL");
+  if (!aligned(sumsq, 8)) return fail(OSDP_ERR_UNSUPPORTED, "sumsq is not 8-byte aligned");
+  for (int32_t i = 0; i < count; ++i)
+    if (tensors[i].n > 0 && (st = check_array(tensors[i].grad, size_of(grad_type), i, "grad")) != OSDP_OK) return st;
+  int64_t parts = 0;
+  if ((st = sumsq_parts(tensors, count, &parts)) != OSDP_OK) return st;
+  if (parts > 0 && !workspace) return fail(OSDP_ERR_INVALID_ARG, "workspace is NULL");
+  if (!aligned(workspace, 8)) return fail(OSDP_ERR_UNSUPPORTED, "workspace is not 8-byte aligned");
+  if (workspace_bytes < static_cast<size_t>(parts) * sizeof(double))
+    return fail(OSDP_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace_bytes, static_cast<size_t>(parts) * sizeof(double));
+  if ((st = device_ok()) != OSDP_OK) return st;
+  const hipStream_t q = static_cast<hipStream_t>(stream);
+  double *part = static_cast<double *>(workspace);
+  st = for_batches(
+      tensors, count,
+      [&](int32_t i, Tensor *t) {
+        t->grad = tensors[i].grad;
+        return aligned(t->grad, 16);
+      },
+      [&](const Batch &b) {
+        const unsigned blocks = sum_blocks(b);
+        if (grad_type == OSDP_BF16) hipLaunchKernelGGL(sumsq_kernel<uint16_t>, dim3(blocks), dim3(kThreads), 0, q, b, part);
+        else hipLaunchKernelGGL(sumsq_kernel<float>, dim3(blocks), dim3(kThreads), 0, q, b, part);
+        part += blocks;
+        return hip_status(hipGetLastError(), "launching the sum of squares");
+      });
+  if (st != OSDP_OK) return st;
+  hipLaunchKernelGGL(sumsq_finish_kernel, dim3(1), dim3(kThreads), 0, q, static_cast<const double *>(workspace),
+                     static_cast<int32_t>(parts), accumulate, sumsq);
+  return hip_status(hipGetLastError(), "launching the end of the sum of squares");
+}
+
+osdp_status osdp_adamw_state_values(const osdp_adamw_tensor *tensors, int32_t count, void *const *m_out, void *const *v_out,
+                                    void *stream) {
+  osdp_status st = check_count(tensors, count);
+  if (st != OSDP_OK) return st;
+  if (count > 0 && (!m_out || !v_out)) return fail(OSDP_ERR_INVALID_ARG, "m_out or v_out is NULL");
+  for (int32_t i = 0; i < count; ++i) {
+    if (tensors[i].n == 0) continue;
+    if ((st = check_array(tensors[i].m, 1, i, "m")) != OSDP_OK) return st;
+    if ((st = check_array(tensors[i].v, 1, i, "v")) != OSDP_OK) return st;
+    if ((st = check_array(tensors[i].exps, 2, i, "exps")) != OSDP_OK) return st;
+    if (!m_out[i] || !v_out[i]) return fail(OSDP_ERR_INVALID_ARG, "m_out[%d] or v_out[%d] is NULL", i, i);
+    if (!aligned(m_out[i], 2) || !aligned(v_out[i], 2)) return fail(OSDP_ERR_UNSUPPORTED, "m_out[%d] or v_out[%d] is not 2-byte aligned", i, i);
+  }
+  if ((st = device_ok()) != OSDP_OK) return st;
+  return for_batches(
+      tensors, count,
+      [&](int32_t i, Tensor *t) {
+        t->m = tensors[i].m; t->v = tensors[i].v; t->exps = tensors[i].exps;
+        t->param = m_out[i];
+        t->master = static_cast<float *>(v_out[i]);
+        return aligned(t->m, 8) && aligned(t->v, 8) && aligned(m_out[i], 16) && aligned(v_out[i], 16);
+      },
+      [&](const Batch &b) {
+        hipLaunchKernelGGL(values_kernel, dim3(grid_of(b, kMostBlocks)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), b);
+        return hip_status(hipGetLastError(), "launching the values of the moments");
+      });
+}
+
+}  // extern "C"

@@ -1,0 +1,402 @@
+// The operator in 8-bit integers: weight shards to 8 bits, tokens to 8 bits, and the product of the two.
+//
+// Rounding.  q = round(x * 127 / amax), halves away from zero, for bf16 x and amax.  With r = 127 / amax (1 + 2^-21), rounded,
+// trunc(|x| r + 1/2) is that number exactly: |x| r lies above |x| 127 / amax, by 2^-20 of it at most, so a half is never
+// missed; and a quotient of two numbers of 8 significant bits that is not a half but below one by less than 127 2^-j
+// stays away from it by 2^-8-j at least, which 2^7-j 2^-20 does not reach.  One multiplication and one addition a value
+// then do what a division would.
+//
+// Sums of products of 8-bit integers are exact in 32 bits (I <= 131072), whatever their order, so every kernel, every split of the
+// reduction and every cut of the weight gives the same bits.
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+
+#include "gemm_i8.h"
+
+namespace osdp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int64_t kMaxFeatures = 131072;
+constexpr size_t kAlign = 256;
+
+// ---- tokens to 8 bits -------------------------------------------------------------------------------------------
+// One workgroup a token: the row is read once, kept in registers (what lies beyond kHold * 2048 features is read again), its largest
+// magnitude found, and written as bytes.  Rows of Xq are a multiple of 128 bytes long and end in zeros.
+constexpr int kHold = 8;
+
+__global__ __launch_bounds__(kThreads) void quantize_tokens_kernel(const uint16_t *__restrict__ x, int64_t ldx, int32_t features,
+                                                                   int32_t ldq, int32_t tokens, uint8_t *__restrict__ q,
+                                                                   float *__restrict__ scale) {
+  __shared__ uint32_t part[kThreads / 64];
+  for (int32_t t = blockIdx.x; t < tokens; t += gridDim.x) {
+    const uint16_t *row = x + t * ldx;
+    uint4 held[kHold];
+    uint32_t most = 0;
+#pragma unroll
+    for (int c = 0; c < kHold; ++c) {
+      const int i = c * kThreads * 8 + threadIdx.x * 8;
+      held[c] = i < features ? *reinterpret_cast<const uint4 *>(row + i) : uint4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int c = 0; c < kHold; ++c) most = max(most, i8_largest(held[c]));
+    for (int i = kHold * kThreads * 8 + threadIdx.x * 8; i < features; i += kThreads * 8)
+      most = max(most, i8_largest(*reinterpret_cast<const uint4 *>(row + i)));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), d)));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) most = max(most, part[w]);
+    __syncthreads();
+    const I8Scale s(most);
+    if (threadIdx.x == 0) scale[t] = s.scale;
+    uint8_t *out = q + static_cast<int64_t>(t) * ldq;
+#pragma unroll
+    for (int c = 0; c < kHold; ++c) {
+      const int i = c * kThreads * 8 + threadIdx.x * 8;
+      if (i < ldq) *reinterpret_cast<uint2 *>(out + i) = s.round8(held[c]);
+    }
+    for (int i = kHold * kThreads * 8 + threadIdx.x * 8; i < ldq; i += kThreads * 8)
+      *reinterpret_cast<uint2 *>(out + i) = i < features ? s.round8(*reinterpret_cast<const uint4 *>(row + i)) : uint2{0u, 0u};
+  }
+}
+
+// ---- weight shards to 8 bits --------------------------------------------------------------------------------------
+// Two passes: the largest magnitude of every column over a range of rows, one range a workgroup (into the workspace); then,
+// over tiles of 128 x 128, their largest, the rounding, and the transposition through LDS.
+struct WeightShards {
+  ShardTable w, q;
+  ShardLayout w_lay;        // bf16 [I x O]
+  int64_t L;
+  int32_t I, O, q_rows;     // q_rows: output channels to a shard, 0: a flat cut
+};
+
+constexpr int kColumns = 256;  // of a workgroup of the first pass: 8 to a lane, 32 lanes side by side, 8 rows at a time
+constexpr int kStrip = 128;    // rows and columns of a tile of the second pass
+
+__device__ __forceinline__ const uint16_t *weight_at(const WeightShards &p, const uint16_t *const *tab, int r, int c) {
+  if (p.w_lay.rows_per_shard > 0) {
+    const int s = static_cast<int>(static_cast<uint32_t>(r) / static_cast<uint32_t>(p.w_lay.rows_per_shard));
+    return tab[s] + static_cast<int64_t>(r - s * p.w_lay.rows_per_shard) * p.O + c;
+  }
+  const uint64_t f = static_cast<uint64_t>(r) * p.O + c, s = f / static_cast<uint64_t>(p.L);
+  return tab[s] + (f - s * p.L);
+}
+
+__global__ __launch_bounds__(kThreads) void column_amax_kernel(WeightShards p, int32_t rows_each, uint32_t *__restrict__ part) {
+  __shared__ const uint16_t *tab[OSDP_MAX_SHARDS];
+  __shared__ uint32_t most[8][kColumns];
+  if (threadIdx.x < OSDP_MAX_SHARDS) tab[threadIdx.x] = static_cast<const uint16_t *>(p.w.p[threadIdx.x]);
+  __syncthreads();
+  const int lane = threadIdx.x & 31, line = threadIdx.x >> 5;
+  const int c = blockIdx.x * kColumns + lane * 8;
+  const int r0 = blockIdx.y * rows_each, r1 = min(r0 + rows_each, p.I);
+  uint32_t m[8] = {};
+  if (c < p.O) {
+#pragma unroll 4
+    for (int r = r0 + line; r < r1; r += 8) {
+      const uint4 v = load_global16(weight_at(p, tab, r, c));
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        m[2 * j] = max(m[2 * j], w[j] << 16 & 0x7fff0000u);
+        m[2 * j + 1] = max(m[2 * j + 1], w[j] & 0x7fff0000u);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) most[line][lane * 8 + j] = m[j];
+  __syncthreads();
+  const int col = blockIdx.x * kColumns + threadIdx.x;
+  uint32_t all = 0;
+#pragma unroll
+  for (int l = 0; l < 8; ++l) all = max(all, most[l][threadIdx.x]);
+  if (col < p.O) part[static_cast<int64_t>(blockIdx.y) * p.O + col] = all;
+}
+
+__global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards p, int32_t parts, const uint32_t *__restrict__ part,
+                                                                   float *__restrict__ scale) {
+  __shared__ const uint16_t *tab[OSDP_MAX_SHARDS];
+  __shared__ uint8_t *q_tab[OSDP_MAX_SHARDS];
+  __shared__ uint32_t most[kStrip];
+  __shared__ uint32_t tile[kStrip][kStrip / 4 + 1];  // [o][i / 4]
+  if (threadIdx.x < OSDP_MAX_SHARDS) {
+    tab[threadIdx.x] = static_cast<const uint16_t *>(p.w.p[threadIdx.x]);
+    q_tab[threadIdx.x] = static_cast<uint8_t *>(p.q.p[threadIdx.x]);
+  }
+  const int o0 = blockIdx.x * kStrip, i0 = blockIdx.y * kStrip;
+  if (threadIdx.x < kStrip) {
+    uint32_t m = 0;
+    const int o = o0 + threadIdx.x;
+    if (o < p.O) {
+      for (int y = 0; y < parts; ++y) m = max(m, part[static_cast<int64_t>(y) * p.O + o]);
+      if (blockIdx.y == 0) scale[o] = I8Scale(m).scale;
+    }
+    most[threadIdx.x] = m;
+  }
+  __syncthreads();
+  const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;  // 8 columns, 4 rows to a lane
+  const int c = o0 + cg * 8;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int r = i0 + half * 64 + rg * 4;
+    uint4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      v[j] = c < p.O && r + j < p.I ? load_global16(weight_at(p, tab, r + j, c)) : uint4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const I8Scale s(most[cg * 8 + j]);
+      uint32_t word = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t pair = (&v[e].x)[j >> 1];
+        word |= (s.round(__uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16)) & 255u) << (8 * e);
+      }
+      tile[cg * 8 + j][half * 16 + rg] = word;
+    }
+  }
+  __syncthreads();
+  const int piece = threadIdx.x & 7;
+#pragma unroll
+  for (int pass = 0; pass < 4; ++pass) {
+    const int row = pass * 32 + (threadIdx.x >> 3), o = o0 + row, i = i0 + piece * 16;
+    if (o < p.O && i < p.I) {
+      const uint4 v = {tile[row][piece * 4], tile[row][piece * 4 + 1], tile[row][piece * 4 + 2], tile[row][piece * 4 + 3]};
+      uint8_t *dst;
+      if (p.q_rows > 0) {
+        const int s = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.q_rows));
+        dst = q_tab[s] + static_cast<int64_t>(o - s * p.q_rows) * p.I + i;
+      } else {
+        const uint64_t f = static_cast<uint64_t>(o) * p.I + i, s = f / static_cast<uint64_t>(p.L);
+        dst = q_tab[s] + (f - s * p.L);
+      }
+      store_global16(dst, v);
+    }
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------
+osdp_status fail(osdp_status st, const char *fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return report_error(st, buf);
+}
+
+osdp_status hip_status(hipError_t e, const char *what) {
+  if (e == hipSuccess) return OSDP_OK;
+  return fail(OSDP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+osdp_status device_ok() {
+  const hipError_t e = check_device();
+  if (e == hipErrorInvalidDevice)
+    return fail(OSDP_ERR_UNSUPPORTED, "the current device is not an MI355X (256 compute units in 8 XCDs), which the kernels are written for");
+  return hip_status(e, "querying the device");
+}
+
+bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+struct Weight {
+  int64_t T, I, O, L;
+  int32_t N, k;
+  int64_t rows_each;  // output channels to a shard where N divides O, else 0
+};
+
+osdp_status check_weight(const osdp_shape *s, Weight *w) {
+  if (!s) return fail(OSDP_ERR_INVALID_ARG, "shape is NULL");
+  if (s->T < 0 || s->I <= 0 || s->O <= 0)
+    return fail(OSDP_ERR_INVALID_ARG, "I, O must be positive and T non-negative (got T %lld, I %lld, O %lld)", (long long)s->T, (long long)s->I, (long long)s->O);
+  if (s->N < 1) return fail(OSDP_ERR_INVALID_ARG, "N must be >= 1 (got %d)", s->N);
+  if (s->N > OSDP_MAX_SHARDS) return fail(OSDP_ERR_UNSUPPORTED, "N = %d exceeds %d shards", s->N, OSDP_MAX_SHARDS);
+  if (s->T >= (1ll << 31) || s->O >= (1ll << 31)) return fail(OSDP_ERR_UNSUPPORTED, "T and O must be below 2^31");
+  if (s->I % 16 || s->I > kMaxFeatures)
+    return fail(OSDP_ERR_UNSUPPORTED, "I must be a multiple of 16 and at most %lld (got %lld)", (long long)kMaxFeatures, (long long)s->I);
+  if (s->O % 8) return fail(OSDP_ERR_UNSUPPORTED, "O must be a multiple of 8 (got %lld)", (long long)s->O);
+  w->T = s->T; w->I = s->I; w->O = s->O; w->N = s->N;
+  w->L = (s->I * s->O + s->N - 1) / s->N;
+  if (w->L % 16) return fail(OSDP_ERR_UNSUPPORTED, "shard length %lld is not a multiple of 16", (long long)w->L);
+  w->rows_each = s->O % s->N == 0 ? s->O / s->N : 0;
+  return OSDP_OK;
+}
+
+osdp_status fill_table(const void *const *ptrs, int32_t N, const char *name, ShardTable *t) {
+  if (!ptrs) return fail(OSDP_ERR_INVALID_ARG, "%s is NULL", name);
+  std::memset(t, 0, sizeof *t);
+  for (int32_t s = 0; s < N; ++s) {
+    if (!ptrs[s]) return fail(OSDP_ERR_INVALID_ARG, "%s[%d] is NULL", name, s);
+    if (!aligned(ptrs[s], 16)) return fail(OSDP_ERR_UNSUPPORTED, "%s[%d] is not 16-byte aligned", name, s);
+    t->p[s] = const_cast<void *>(ptrs[s]);
+  }
+  return OSDP_OK;
+}
+
+osdp_status check_scale(const float *p) {
+  if (!p) return fail(OSDP_ERR_INVALID_ARG, "w_scale is NULL");
+  if (!aligned(p, 16)) return fail(OSDP_ERR_UNSUPPORTED, "w_scale is not 16-byte aligned");
+  return OSDP_OK;
+}
+
+osdp_status check_matrix(const void *p, int64_t ld, int64_t cols, const char *name) {
+  if (!p) return fail(OSDP_ERR_INVALID_ARG, "%s is NULL", name);
+  if (ld < cols) return fail(OSDP_ERR_INVALID_ARG, "leading dimension of %s (%lld) is below its row length %lld", name, (long long)ld, (long long)cols);
+  if (ld % 8) return fail(OSDP_ERR_UNSUPPORTED, "leading dimension of %s (%lld) is not a multiple of 8", name, (long long)ld);
+  if (!aligned(p, 16)) return fail(OSDP_ERR_UNSUPPORTED, "%s is not 16-byte aligned", name);
+  return OSDP_OK;
+}
+
+osdp_status check_workspace(const void *ws, size_t bytes, size_t need) {
+  if (!ws) return fail(OSDP_ERR_INVALID_ARG, "workspace is NULL");
+  if (!aligned(ws, kAlign)) return fail(OSDP_ERR_UNSUPPORTED, "workspace is not 256-byte aligned");
+  if (bytes < need) return fail(OSDP_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", bytes, need);
+  return OSDP_OK;
+}
+
+// Ranges of rows that the first pass over a weight is cut into: enough workgroups for the card, at least 64 rows each.
+int32_t amax_rows(const Weight &w) {
+  const int64_t strips = (w.O + kColumns - 1) / kColumns;
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((w.I + 63) / 64, 2048 / std::max<int64_t>(1, std::min<int64_t>(strips, 2048))));
+  return static_cast<int32_t>(((w.I + parts - 1) / parts + 7) / 8 * 8);
+}
+int32_t amax_parts(const Weight &w) {
+  const int32_t each = amax_rows(w);
+  return static_cast<int32_t>((w.I + each - 1) / each);
+}
+
+size_t token_bytes(const Weight &w) {
+  return round_up(static_cast<size_t>(w.T) * i8_row_bytes(w.I), kAlign) + round_up(static_cast<size_t>(w.T) * 4, kAlign);
+}
+
+// Whether the product reads the shards where they lie.
+bool in_place(const Weight &w) { return w.rows_each > 0 || w.T <= kI8FewTokens; }
+
+osdp_status check_slices(const osdp_shape *s, Weight *w, int64_t *widest) {
+  const int64_t k = s->k == 0 ? 1 : s->k;
+  if (s->k < 0) return fail(OSDP_ERR_INVALID_ARG, "k must be >= 0 (got %d)", s->k);
+  if (k > w->O) return fail(OSDP_ERR_INVALID_ARG, "k = %lld exceeds O = %lld", (long long)k, (long long)w->O);
+  w->k = static_cast<int32_t>(k);
+  *widest = 0;
+  for (int64_t j = 0; j < k; ++j) {
+    const int64_t c0 = j * w->O / k, c1 = (j + 1) * w->O / k;
+    if (c0 % 8 || c1 % 8) return fail(OSDP_ERR_UNSUPPORTED, "slice %lld = [%lld, %lld) is not aligned to 8 columns", (long long)j, (long long)c0, (long long)c1);
+    *widest = std::max(*widest, c1 - c0);
+  }
+  if (in_place(*w)) *widest = 0;
+  return OSDP_OK;
+}
+
+}  // namespace
+}  // namespace osdp
+
+using namespace osdp;
+
+extern "C" {
+
+osdp_status osdp_split_linear_i8_quantize_workspace_bytes(const osdp_shape *shape, size_t *bytes) {
+  Weight w;
+  const osdp_status st = check_weight(shape, &w);
+  if (st != OSDP_OK) return st;
+  if (!bytes) return fail(OSDP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = static_cast<size_t>(amax_parts(w)) * w.O * 4;
+  return OSDP_OK;
+}
+
+osdp_status osdp_split_linear_i8_quantize(const osdp_shape *shape, const void *const *w_shards, void *const *q_shards,
+                                          float *w_scale, void *workspace, size_t workspace_bytes, void *stream) {
+  Weight w;
+  osdp_status st = check_weight(shape, &w);
+  if (st != OSDP_OK) return st;
+  WeightShards p;
+  if ((st = fill_table(w_shards, w.N, "w_shards", &p.w)) != OSDP_OK) return st;
+  if ((st = fill_table(const_cast<const void *const *>(q_shards), w.N, "q_shards", &p.q)) != OSDP_OK) return st;
+  if ((st = check_scale(w_scale)) != OSDP_OK) return st;
+  const int32_t parts = amax_parts(w);
+  if ((st = check_workspace(workspace, workspace_bytes, static_cast<size_t>(parts) * w.O * 4)) != OSDP_OK) return st;
+  const int64_t tiles_i = (w.I + kStrip - 1) / kStrip, tiles_o = (w.O + kStrip - 1) / kStrip;
+  if (tiles_o >= (1ll << 24)) return fail(OSDP_ERR_UNSUPPORTED, "O = %lld is too large", (long long)w.O);
+  if ((st = device_ok()) != OSDP_OK) return st;
+  p.w_lay.O = w.O; p.w_lay.L = w.L; p.w_lay.N = w.N;
+  p.w_lay.rows_per_shard = w.I % w.N == 0 ? static_cast<int32_t>(w.I / w.N) : 0;
+  p.L = w.L;
+  p.I = static_cast<int32_t>(w.I); p.O = static_cast<int32_t>(w.O); p.q_rows = static_cast<int32_t>(w.rows_each);
+  const hipStream_t q = static_cast<hipStream_t>(stream);
+  uint32_t *part = static_cast<uint32_t *>(workspace);
+  hipLaunchKernelGGL(column_amax_kernel, dim3(static_cast<unsigned>((w.O + kColumns - 1) / kColumns), static_cast<unsigned>(parts)),
+                     dim3(kThreads), 0, q, p, amax_rows(w), part);
+  if ((st = hip_status(hipGetLastError(), "launching the columns' largest")) != OSDP_OK) return st;
+  hipLaunchKernelGGL(quantize_weight_kernel, dim3(static_cast<unsigned>(tiles_o), static_cast<unsigned>(tiles_i)), dim3(kThreads), 0, q,
+                     p, parts, part, w_scale);
+  return hip_status(hipGetLastError(), "launching the quantization");
+}
+
+osdp_status osdp_split_linear_i8_workspace_bytes(const osdp_shape *shape, size_t *total, size_t *peak_weight_staging) {
+  Weight w;
+  osdp_status st = check_weight(shape, &w);
+  if (st != OSDP_OK) return st;
+  int64_t widest = 0;
+  if ((st = check_slices(shape, &w, &widest)) != OSDP_OK) return st;
+  const size_t slot = static_cast<size_t>(widest) * w.I;
+  if (total) *total = token_bytes(w) + round_up(slot, kAlign);
+  if (peak_weight_staging) *peak_weight_staging = slot;
+  return OSDP_OK;
+}
+
+osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int64_t ldx, const void *const *q_shards,
+                                     const float *w_scale, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes,
+                                     void *stream) {
+  Weight w;
+  osdp_status st = check_weight(shape, &w);
+  if (st != OSDP_OK) return st;
+  int64_t widest = 0;
+  if ((st = check_slices(shape, &w, &widest)) != OSDP_OK) return st;
+  const bool no_tokens = w.T == 0;  // X and Y have no rows and may be NULL
+  if (!no_tokens && (st = check_matrix(X, ldx, w.I, "X")) != OSDP_OK) return st;
+  if (!no_tokens && (st = check_matrix(Y, ldy, w.O, "Y")) != OSDP_OK) return st;
+  ShardTable tab;
+  if ((st = fill_table(q_shards, w.N, "q_shards", &tab)) != OSDP_OK) return st;
+  if ((st = check_scale(w_scale)) != OSDP_OK) return st;
+  if (!no_tokens && (st = check_workspace(workspace, workspace_bytes, token_bytes(w) + round_up(static_cast<size_t>(widest) * w.I, kAlign))) != OSDP_OK) return st;
+  if ((st = device_ok()) != OSDP_OK) return st;
+  if (no_tokens) return OSDP_OK;
+  const hipStream_t q = static_cast<hipStream_t>(stream);
+  char *ws = static_cast<char *>(workspace);
+  I8Problem p{};
+  p.T = static_cast<int32_t>(w.T); p.I = static_cast<int32_t>(w.I);
+  p.ldq = static_cast<int32_t>(i8_row_bytes(w.I));
+  p.xq = reinterpret_cast<uint8_t *>(ws);
+  p.x_scale = reinterpret_cast<float *>(ws + round_up(static_cast<size_t>(w.T) * p.ldq, kAlign));
+  char *slot = ws + token_bytes(w);
+  hipLaunchKernelGGL(quantize_tokens_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(w.T, 1 << 20))), dim3(kThreads), 0, q,
+                     static_cast<const uint16_t *>(X), ldx, p.I, p.ldq, p.T, const_cast<uint8_t *>(p.xq), const_cast<float *>(p.x_scale));
+  if ((st = hip_status(hipGetLastError(), "launching the tokens' quantization")) != OSDP_OK) return st;
+  p.ldy = ldy;
+  p.L = w.L;
+  if (in_place(w)) {
+    p.O = static_cast<int32_t>(w.O);
+    p.shards = tab;
+    p.rows_each = static_cast<int32_t>(w.rows_each);
+    p.w_scale = w_scale; p.y = static_cast<uint16_t *>(Y);
+    return hip_status(launch_i8(p, q), "launching the product");
+  }
+  ShardLayout lay{};  // (two bytes an element, as the gather counts)
+  lay.O = w.I / 2; lay.L = w.L / 2; lay.N = w.N; lay.rows_per_shard = 0;
+  for (int64_t j = 0; j < w.k; ++j) {
+    const int64_t c0 = j * w.O / w.k, c1 = (j + 1) * w.O / w.k;
+    if ((st = hip_status(launch_gather(tab, lay, c0, c1 - c0, 0, w.I / 2, slot, q), "gathering a slice")) != OSDP_OK) return st;
+    p.O = static_cast<int32_t>(c1 - c0);
+    p.shards.p[0] = slot;
+    p.rows_each = p.O;
+    p.w_scale = w_scale + c0; p.y = static_cast<uint16_t *>(Y) + c0;
+    if ((st = hip_status(launch_i8(p, q), "launching the product")) != OSDP_OK) return st;
+  }
+  return OSDP_OK;
+}
+
+}  // extern "C"

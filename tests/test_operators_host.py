@@ -1,0 +1,149 @@
+"""AdamW over shards and the operator in 8-bit integers: sizes, layouts and refusals, which need no GPU."""
+import ctypes
+
+import pytest
+
+import paper_2209_13258_amd as osdp
+from paper_2209_13258_amd import binding as B
+
+P = 1 << 20  # an address that is aligned and that nothing here follows
+
+
+def tensor(n=1000, **more):
+    t = B.osdp_adamw_tensor(n, P, P, P, P, P, P, 0.1)
+    for k, v in more.items():
+        setattr(t, k, v)
+    return t
+
+
+def options(**more):
+    o = B.osdp_adamw_options(1e-3, 0.9, 0.999, 1e-8, 1, 0, 0.0, None, None, None, B.OSDP_BF16, B.OSDP_BF16, 32, 0)
+    for k, v in more.items():
+        setattr(o, k, v)
+    return o
+
+
+def step(tensors, o):
+    arr = (B.osdp_adamw_tensor * max(len(tensors), 1))(*tensors)
+    return osdp.lib.osdp_adamw_step(arr, len(tensors), ctypes.byref(o) if o is not None else None, None)
+
+
+def test_struct_layouts_match_the_header():
+    assert ctypes.sizeof(B.osdp_adamw_tensor) == 64
+    assert ctypes.sizeof(B.osdp_adamw_options) == 96
+
+
+@pytest.mark.parametrize("more", [
+    dict(lr=-1.0), dict(lr=float("nan")), dict(lr=float("inf")), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.5),
+    dict(beta2=float("nan")), dict(eps=0.0), dict(eps=1e-13), dict(eps=float("nan")), dict(eps=float("inf")), dict(step=0),
+    dict(step=-3), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(max_norm=1.0), dict(grad_type=2), dict(param_type=7),
+    dict(param_type=B.OSDP_F32), dict(state_bits=16), dict(state_bits=0)])
+def test_step_refuses_options(more):
+    assert step([tensor()], options(**more)) == B.OSDP_ERR_INVALID_ARG
+    assert osdp.lib.osdp_last_error()
+
+
+@pytest.mark.parametrize("more,bits,status", [
+    (dict(n=-1), 32, B.OSDP_ERR_INVALID_ARG), (dict(n=1 << 40), 32, B.OSDP_ERR_INVALID_ARG),
+    (dict(grad=None), 32, B.OSDP_ERR_INVALID_ARG), (dict(param=None), 32, B.OSDP_ERR_INVALID_ARG),
+    (dict(m=None), 32, B.OSDP_ERR_INVALID_ARG), (dict(v=None), 32, B.OSDP_ERR_INVALID_ARG),
+    (dict(exps=None), 8, B.OSDP_ERR_INVALID_ARG), (dict(weight_decay=-0.5), 32, B.OSDP_ERR_INVALID_ARG),
+    (dict(weight_decay=float("nan")), 32, B.OSDP_ERR_INVALID_ARG), (dict(grad=P + 1), 32, B.OSDP_ERR_UNSUPPORTED),
+    (dict(param=P + 1), 32, B.OSDP_ERR_UNSUPPORTED), (dict(master=P + 2), 32, B.OSDP_ERR_UNSUPPORTED),
+    (dict(m=P + 2), 32, B.OSDP_ERR_UNSUPPORTED), (dict(v=P + 1), 32, B.OSDP_ERR_UNSUPPORTED), (dict(exps=P + 1), 8, B.OSDP_ERR_UNSUPPORTED)])
+def test_step_refuses_tensors(more, bits, status):
+    assert step([tensor(), tensor(**more)], options(state_bits=bits)) == status
+
+
+def test_step_refuses_some_masters_and_misplaced_scalars():
+    assert step([tensor(), tensor(master=None)], options()) == B.OSDP_ERR_INVALID_ARG
+    assert step([tensor()], None) == B.OSDP_ERR_INVALID_ARG
+    assert step([tensor()], options(grad_sumsq=P + 4)) == B.OSDP_ERR_UNSUPPORTED
+    assert step([tensor()], options(step_device=P + 4)) == B.OSDP_ERR_UNSUPPORTED
+    assert step([tensor()], options(lr_device=P + 2)) == B.OSDP_ERR_UNSUPPORTED
+    assert osdp.lib.osdp_adamw_step(None, 1, ctypes.byref(options()), None) == B.OSDP_ERR_INVALID_ARG
+    assert osdp.lib.osdp_adamw_step(None, -1, ctypes.byref(options()), None) == B.OSDP_ERR_INVALID_ARG
+
+
+def test_sumsq_sizes_and_refusals():
+    def need(lengths):
+        arr = (B.osdp_adamw_tensor * len(lengths))(*[tensor(n=n) for n in lengths])
+        out = ctypes.c_size_t()
+        assert osdp.lib.osdp_adamw_grad_sumsq_workspace_bytes(arr, len(lengths), ctypes.byref(out)) == 0
+        return out.value
+    assert need([0]) == 0 and need([0, 0, 0]) == 0
+    assert 8 <= need([1]) <= need([1 << 20]) <= need([1 << 34])
+    assert need([1] * 200) >= 8 * 4 and need([1 << 39] * 3) < 1 << 20
+    arr = (B.osdp_adamw_tensor * 1)(tensor())
+    call = lambda **k: osdp.lib.osdp_adamw_grad_sumsq(arr, 1, k.get("type", 0), 0, k.get("out", P), k.get("ws", P), k.get("bytes", 1 << 20), None)  # noqa: E731
+    assert call(type=5) == B.OSDP_ERR_INVALID_ARG and call(out=None) == B.OSDP_ERR_INVALID_ARG
+    assert call(out=P + 4) == B.OSDP_ERR_UNSUPPORTED and call(ws=P + 4) == B.OSDP_ERR_UNSUPPORTED
+    assert call(ws=None) == B.OSDP_ERR_INVALID_ARG and call(bytes=0) == B.OSDP_ERR_WORKSPACE
+    assert osdp.lib.osdp_adamw_grad_sumsq_workspace_bytes(arr, 1, None) == B.OSDP_ERR_INVALID_ARG
+
+
+def test_state_values_refusals():
+    arr = (B.osdp_adamw_tensor * 1)(tensor())
+    one = lambda p: (ctypes.c_void_p * 1)(p)  # noqa: E731
+    assert osdp.lib.osdp_adamw_state_values(arr, 1, None, one(P), None) == B.OSDP_ERR_INVALID_ARG
+    assert osdp.lib.osdp_adamw_state_values(arr, 1, one(None), one(P), None) == B.OSDP_ERR_INVALID_ARG
+    assert osdp.lib.osdp_adamw_state_values(arr, 1, one(P), one(P + 1), None) == B.OSDP_ERR_UNSUPPORTED
+    bad = (B.osdp_adamw_tensor * 1)(tensor(exps=None))
+    assert osdp.lib.osdp_adamw_state_values(bad, 1, one(P), one(P), None) == B.OSDP_ERR_INVALID_ARG
+
+
+def i8_fwd(T=4, I=64, O=32, N=2, k=1, X=P, ldx=None, shards=None, scale=P, Y=P, ldy=None, ws=P, ws_bytes=1 << 30):
+    shape = B.osdp_shape(T, I, O, N, k)
+    tab = (ctypes.c_void_p * max(N, 1))(*(shards or [P] * max(N, 1)))
+    return osdp.lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X, I if ldx is None else ldx, tab, scale, Y,
+                                             O if ldy is None else ldy, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("more,status", [
+    (dict(I=24), B.OSDP_ERR_UNSUPPORTED), (dict(I=131088, O=8, N=1), B.OSDP_ERR_UNSUPPORTED), (dict(I=0), B.OSDP_ERR_INVALID_ARG),
+    (dict(O=12), B.OSDP_ERR_UNSUPPORTED), (dict(O=-8), B.OSDP_ERR_INVALID_ARG), (dict(T=-1), B.OSDP_ERR_INVALID_ARG),
+    (dict(T=1 << 31), B.OSDP_ERR_UNSUPPORTED), (dict(N=0), B.OSDP_ERR_INVALID_ARG), (dict(N=65), B.OSDP_ERR_UNSUPPORTED),
+    (dict(I=16, O=8, N=16), B.OSDP_ERR_UNSUPPORTED), (dict(k=-1), B.OSDP_ERR_INVALID_ARG), (dict(k=33), B.OSDP_ERR_INVALID_ARG),
+    (dict(k=3), B.OSDP_ERR_UNSUPPORTED), (dict(X=None), B.OSDP_ERR_INVALID_ARG), (dict(X=P + 8), B.OSDP_ERR_UNSUPPORTED),
+    (dict(ldx=56), B.OSDP_ERR_INVALID_ARG), (dict(ldx=68), B.OSDP_ERR_UNSUPPORTED), (dict(Y=None), B.OSDP_ERR_INVALID_ARG),
+    (dict(ldy=24), B.OSDP_ERR_INVALID_ARG), (dict(ldy=36), B.OSDP_ERR_UNSUPPORTED), (dict(shards=[P, None]), B.OSDP_ERR_INVALID_ARG),
+    (dict(shards=[P, P + 8]), B.OSDP_ERR_UNSUPPORTED), (dict(scale=None), B.OSDP_ERR_INVALID_ARG), (dict(scale=P + 4), B.OSDP_ERR_UNSUPPORTED),
+    (dict(ws=None), B.OSDP_ERR_INVALID_ARG), (dict(ws=P + 16), B.OSDP_ERR_UNSUPPORTED), (dict(ws_bytes=100), B.OSDP_ERR_WORKSPACE)])
+def test_i8_forward_refuses(more, status):
+    assert i8_fwd(**more) == status
+    assert osdp.lib.osdp_last_error()
+
+
+@pytest.mark.parametrize("T,I,O,N,k", [(1, 16, 8, 1, 0), (500, 2560, 10240, 8, 4), (500, 2560, 10248, 16, 3), (64, 4096, 24, 64, 1),
+                                       (65, 4096, 24, 16, 3), (0, 64, 32, 2, 1)])
+def test_i8_workspace_follows_the_law(T, I, O, N, k):
+    """One byte an element and 1/k of the weight, where slices are gathered; nothing where the shards are read in place."""
+    total, peak = osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, k)
+    gathers = T > 64 and O % N != 0
+    assert peak == (I * max((j + 1) * O // max(k, 1) - j * O // max(k, 1) for j in range(max(k, 1))) if gathers else 0)
+    rows = T * (-(-I // 128) * 128)
+    assert total >= rows + 4 * T + peak and total <= rows + 4 * T + peak + 3 * 256
+
+
+def test_i8_quantize_refuses():
+    def call(I=64, O=32, N=2, w=P, q=P, scale=P, ws=P, ws_bytes=1 << 30):
+        shape = B.osdp_shape(0, I, O, N, 0)
+        return osdp.lib.osdp_split_linear_i8_quantize(ctypes.byref(shape), (ctypes.c_void_p * 2)(P, w), (ctypes.c_void_p * 2)(P, q),
+                                                      scale, ws, ws_bytes, None)
+    assert call(w=None) == B.OSDP_ERR_INVALID_ARG and call(q=None) == B.OSDP_ERR_INVALID_ARG
+    assert call(w=P + 2) == B.OSDP_ERR_UNSUPPORTED and call(q=P + 8) == B.OSDP_ERR_UNSUPPORTED
+    assert call(scale=None) == B.OSDP_ERR_INVALID_ARG and call(scale=P + 4) == B.OSDP_ERR_UNSUPPORTED
+    assert call(ws=None) == B.OSDP_ERR_INVALID_ARG and call(ws=P + 64) == B.OSDP_ERR_UNSUPPORTED
+    assert call(ws_bytes=0) == B.OSDP_ERR_WORKSPACE and call(I=8) == B.OSDP_ERR_UNSUPPORTED and call(O=4) == B.OSDP_ERR_UNSUPPORTED
+    assert osdp.osdp_split_linear_i8_quantize_workspace_bytes(4096, 16384, 8) >= 4 * 16384
+    assert osdp.lib.osdp_split_linear_i8_quantize(None, None, None, None, None, 0, None) == B.OSDP_ERR_INVALID_ARG
+
+
+def test_the_binding_refuses_before_it_calls():
+    import torch
+    with pytest.raises(osdp.OsdpError):
+        osdp.AdamWTable()
+    with pytest.raises(osdp.OsdpError):   # not on a GPU
+        osdp.AdamWTable(grads=[torch.zeros(4)])
+    with pytest.raises(osdp.OsdpError):
+        osdp.AdamWTable(grads=[torch.zeros(4)], params=[])
