@@ -56,10 +56,30 @@ struct I8Problem {
   const float *w_scale;
   uint16_t *y;
   int64_t ldy;
+  void *sums;             // where parts of a reduction meet, and their counters, which are 0; NULL: nowhere
+  uint32_t *arrived;
 };
 
-// Up to this many tokens the product reads the weight where it lies, however it is cut.
-constexpr int64_t kI8FewTokens = 64;
+// Launches whose tiles do not fill the card share the reduction of a tile among workgroups (gemm_i8_w4.h), which meet in
+// kI8SumBytes of memory with a counter for each of kI8MostTiles.
+constexpr int64_t kI8MostTiles = 256;
+constexpr size_t kI8SumBytes = 16 << 20;
+
+// Up to this many tokens the product reads the weight where it lies, however it is cut; from there on if every shard is
+// a block of at least kI8ShardRows channels (tiles end with a shard).
+constexpr int64_t kI8FewTokens = 64, kI8ShardRows = 32;
+
+// Eight sums as Y: both scales, then the rounding to bf16.
+__device__ __forceinline__ void i8_store8(uint16_t *y, const int *sums, float st, const float *so) {
+  uint32_t out[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float lo = static_cast<float>(sums[2 * j]) * st * so[2 * j], hi = static_cast<float>(sums[2 * j + 1]) * st * so[2 * j + 1];
+    out[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(lo))) |
+             static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(hi))) << 16;
+  }
+  store_global16(y, uint4{out[0], out[1], out[2], out[3]});
+}
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------
 // A workgroup owns 16 * NB output channels and 16 * MB tokens; its kWaves waves share the reduction, 64 * kUnroll bytes of
@@ -148,18 +168,120 @@ __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
   for (int i = tid; i < BM * BN / 8; i += kWaves * 64) {
     const int r = i / (BN / 8), c = i % (BN / 8) * 8, m = m0 + r, n = n0 + c;
     if (m >= p.T || n >= p.O) continue;
-    const float st = p.x_scale[m];
-    uint32_t out[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float y[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) y[e] = static_cast<float>(sums[r * BN + c + 2 * j + e]) * st * p.w_scale[n + 2 * j + e];
-      out[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(y[0]))) |
-               static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(y[1]))) << 16;
-    }
-    store_global16(p.y + static_cast<int64_t>(m) * p.ldy + n, uint4{out[0], out[1], out[2], out[3]});
+    i8_store8(p.y + static_cast<int64_t>(m) * p.ldy + n, &sums[r * BN + c], p.x_scale[m], p.w_scale + n);
   }
+}
+
+// The same with the tokens' rounding in the launch, for at most 16 tokens of so few features that their bytes fit in LDS and
+// that every workgroup may well round all of them for itself: one launch instead of two, the first weights on their way meanwhile.
+template <int NB, int kWaves, int kUnroll, bool kFlat>
+__global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, const uint16_t *__restrict__ x, int64_t ldx) {
+  constexpr int BN = 16 * NB, kStep = 64 * kUnroll;
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows[];  // [T][ldq + 16]: 16 rows fall into 16 different bank groups
+  __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
+  __shared__ int sums[16 * BN];
+  __shared__ uint32_t most[16][kWaves];
+  __shared__ float scale[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
+  const int n0 = blockIdx.x * BN, pitch = p.ldq + 16;
+  if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
+  for (int i = tid; i < 16 * BN; i += kWaves * 64) sums[i] = 0;
+  __syncthreads();
+  const uint8_t *row[NB];
+  int64_t off[NB];
+  int shard[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int o = min(n0 + 16 * b + l16, p.O - 1);
+    if (!kFlat) {
+      const int s = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.rows_each));
+      row[b] = tab[s] + static_cast<int64_t>(o - s * p.rows_each) * p.I;
+    } else {
+      const uint64_t f = static_cast<uint64_t>(o) * p.I;
+      shard[b] = static_cast<int>(f / static_cast<uint64_t>(p.L));
+      off[b] = static_cast<int64_t>(f - static_cast<uint64_t>(shard[b]) * p.L);
+    }
+  }
+  auto load = [&](int k0, uint4 (&w)[kUnroll][NB]) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int k = k0 + 64 * u + 16 * q4, kw = k < p.I ? k : 0;  // beyond the row's end: any weights, the tokens are zeros there
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const uint8_t *at;
+        if (!kFlat) {
+          at = row[b] + kw;
+        } else {
+          int64_t f = off[b] + kw;
+          int s = shard[b];
+          while (f >= p.L) {
+            f -= p.L;
+            ++s;
+          }
+          at = tab[s] + f;
+        }
+        w[u][b] = load_global16(at);
+      }
+    }
+  };
+  uint4 w[kUnroll][NB];
+  load(wave * kStep, w);
+  // tokens to 8 bits: a row to a wave, or (fewer tokens than waves) to as many waves as there are for it
+  const int share = p.T >= kWaves ? 1 : kWaves / p.T, part = wave % share;
+  for (int t = wave / share; t < p.T; t += kWaves / share) {
+    uint32_t m = 0;
+    for (int i = (part * 64 + lane) * 8; i < p.I; i += share * 512) m = max(m, i8_largest(load_global16(x + t * ldx + i)));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d)));
+    if (lane == 0) most[t][part] = m;
+  }
+  __syncthreads();
+  for (int t = wave / share; t < p.T; t += kWaves / share) {
+    uint32_t m = 0;
+    for (int i = 0; i < share; ++i) m = max(m, most[t][i]);
+    const I8Scale s(m);
+    if (part == 0 && lane == 0) scale[t] = s.scale;
+    for (int i = (part * 64 + lane) * 8; i < p.ldq; i += share * 512)
+      *reinterpret_cast<uint2 *>(rows + t * pitch + i) = i < p.I ? s.round8(load_global16(x + t * ldx + i)) : uint2{0u, 0u};
+  }
+  __syncthreads();
+  const uint8_t *token = rows + min(l16, p.T - 1) * pitch + 16 * q4;
+  i32x4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = i32x4{0, 0, 0, 0};
+  for (int k0 = wave * kStep; k0 < p.I; k0 += kWaves * kStep) {
+    uint4 next[kUnroll][NB];
+    if (k0 + kWaves * kStep < p.I) load(k0 + kWaves * kStep, next);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (k0 + 64 * u >= p.I) break;
+      const i32x4 a = *reinterpret_cast<const i32x4 *>(token + k0 + 64 * u);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u][b]), a, acc[b], 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) w[u][b] = next[u][b];
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) atomicAdd(&sums[l16 * BN + 16 * b + 4 * q4 + i], acc[b][i]);
+  __syncthreads();
+  for (int i = tid; i < 2 * BN; i += kWaves * 64) {
+    const int m = i / (BN / 8), c = i % (BN / 8) * 8, n = n0 + c;
+    if (m < p.T && n < p.O) i8_store8(p.y + static_cast<int64_t>(m) * p.ldy + n, &sums[m * BN + c], scale[m], p.w_scale + n);
+  }
+}
+
+template <int NB, int kWaves, int kUnroll>
+hipError_t launch_fused(const I8Problem &p, const uint16_t *x, int64_t ldx, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((p.O + 16 * NB - 1) / (16 * NB)));
+  const unsigned lds = static_cast<unsigned>(p.T * (p.ldq + 16));
+  if (p.rows_each > 0) hipLaunchKernelGGL((i8_fused_kernel<NB, kWaves, kUnroll, false>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
+  else hipLaunchKernelGGL((i8_fused_kernel<NB, kWaves, kUnroll, true>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
+  return hipGetLastError();
 }
 
 template <int MB, int NB, int kWaves, int kUnroll>
@@ -168,11 +290,6 @@ hipError_t launch_few(const I8Problem &p, hipStream_t stream) {
   if (p.rows_each > 0) hipLaunchKernelGGL((i8_few_kernel<MB, NB, kWaves, kUnroll, false>), grid, dim3(kWaves * 64), 0, stream, p);
   else hipLaunchKernelGGL((i8_few_kernel<MB, NB, kWaves, kUnroll, true>), grid, dim3(kWaves * 64), 0, stream, p);
   return hipGetLastError();
-}
-
-hipError_t launch_i8(const I8Problem &p, hipStream_t stream) {
-  if (p.T <= 16) return launch_few<1, 1, 8, 4>(p, stream);
-  return launch_few<4, 4, 8, 1>(p, stream);
 }
 
 }  // namespace

@@ -13,7 +13,7 @@
 #include <cstdio>
 #include <cstring>
 
-#include "gemm_i8.h"
+#include "gemm_i8_w4.h"
 
 namespace osdp {
 namespace {
@@ -29,9 +29,10 @@ constexpr int kHold = 8;
 
 __global__ __launch_bounds__(kThreads) void quantize_tokens_kernel(const uint16_t *__restrict__ x, int64_t ldx, int32_t features,
                                                                    int32_t ldq, int32_t tokens, uint8_t *__restrict__ q,
-                                                                   float *__restrict__ scale) {
+                                                                   float *__restrict__ scale, uint32_t *__restrict__ counters) {
   __shared__ uint32_t part[kThreads / 64];
-  for (int32_t t = blockIdx.x; t < tokens; t += gridDim.x) {
+  if (counters && blockIdx.x == 0 && threadIdx.x < kI8MostTiles) counters[threadIdx.x] = 0;  // (of the product that follows)
+  for (int64_t t = blockIdx.x; t < tokens; t += gridDim.x) {
     const uint16_t *row = x + t * ldx;
     uint4 held[kHold];
     uint32_t most = 0;
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(kThreads) void quantize_tokens_kernel(const uint16_
     __syncthreads();
     const I8Scale s(most);
     if (threadIdx.x == 0) scale[t] = s.scale;
-    uint8_t *out = q + static_cast<int64_t>(t) * ldq;
+    uint8_t *out = q + t * ldq;
 #pragma unroll
     for (int c = 0; c < kHold; ++c) {
       const int i = c * kThreads * 8 + threadIdx.x * 8;
@@ -270,12 +271,93 @@ int32_t amax_parts(const Weight &w) {
   return static_cast<int32_t>((w.I + each - 1) / each);
 }
 
-size_t token_bytes(const Weight &w) {
-  return round_up(static_cast<size_t>(w.T) * i8_row_bytes(w.I), kAlign) + round_up(static_cast<size_t>(w.T) * 4, kAlign);
+// ---- which kernel ---------------------------------------------------------------------------------------------------
+enum class Kernel { kFew, k64, k128, k128Walk, k256Walk };
+struct Choice {
+  Kernel kernel;
+  int parts;
+};
+
+// The kernel, and the parts of a tile's reduction, that are estimated fastest for T tokens and `shards` blocks of `rows`
+// channels.  A launch takes `fixed` us, and for each round of workgroups over the card `start` and `block` for every 128 input
+// features; a tile's parts cost `each` apiece, and `meet` for every 256 workgroups' worth of sums.  The constants were fitted to 121 random sizes
+// (8 to 8192 tokens, 256 to 16384 input and output features), all of them timed with every kernel below and 1 to 8 parts: the choice is 1.4 % slower than
+// the best of them in the geometric mean and 28 % at most.  us for 16 / 64 x 64 / 128 x 128 / walking 128 x 128 / walking 256 x 256:
+//     30 tokens   400 -> 3456       6.1 /  7.4 /   9.5 /   9.6 /  15.5
+//    162         1152 -> 1344      10.2 /  8.9 /  11.7 /  12.9 /  22.0
+//    161        14448 ->  960      37.5 / 35.1 (four parts 21.2) / 55.4 (30.0) / 85.8 / 135
+//   1000         4096 -> 4096       230 / 36.9 /  27.9 /  32.6 /  51.6
+//    500         2560 -> 10240      186 / 31.9 /  31.9 /  27.4 /  38.0
+//   3000         4096 -> 16384     2630 /  349 /   242 /   202 /   167
+Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share) {
+  struct Prices {
+    Kernel kernel;
+    int side, room;  // tiles of side x side; workgroups that the card holds
+    double fixed, block, start, each, meet;
+  };
+  constexpr Prices kPrices[] = {{Kernel::kFew, 16, 1024, 5.05, 0.364, 0.81, 0, 0},
+                                {Kernel::k64, 64, 512, 4.84, 0.429, 3.07, 0.83, 0.83},
+                                {Kernel::k128, 128, 256, 2.63, 0.447, 6.37, 0.89, 4.43},
+                                {Kernel::k128Walk, 128, 512, 5.44, 1.048, 5.73, 0, 0},
+                                {Kernel::k256Walk, 256, 256, 0.95, 1.156, 12.8, 0, 0}};
+  const int64_t blocks = (I + 127) / 128;
+  Choice best = {Kernel::k256Walk, 1};
+  double least = -1.0;
+  for (const Prices &v : kPrices) {
+    const bool few = v.kernel == Kernel::kFew;
+    const int64_t across = few ? (rows * shards + 15) / 16 : shards * i8_shard_tiles(rows, v.side);
+    const int64_t tiles = across * ((T + v.side - 1) / v.side);
+    if (few && T > 4096) continue;
+    if ((v.kernel == Kernel::k64 || v.kernel == Kernel::k128) && tiles > (1 << 20)) continue;
+    for (int asked : {1, 2, 3, 4, 6, 8}) {
+      const int64_t each = (blocks + asked - 1) / asked, parts = (blocks + each - 1) / each, groups = tiles * parts;
+      if (asked > 1 && (v.each == 0 || !may_share || each < 2 || tiles > kI8MostTiles ||
+                        static_cast<size_t>(groups) * v.side * v.side * 4 > kI8SumBytes))
+        break;
+      double rounds = static_cast<double>((groups + v.room - 1) / v.room);
+      if (few) rounds = std::max(static_cast<double>(groups) / v.room, groups <= 256 ? 0.35 : 0.5);
+      else if (v.room == 512 && groups % 512 != 0 && groups % 512 <= 256) rounds -= 0.4;  // (one workgroup to a CU is faster than two)
+      double us = v.fixed + rounds * (static_cast<double>(each) * v.block + v.start);
+      if (parts > 1) us += v.each * static_cast<double>(parts) + v.meet * static_cast<double>(groups) / 256.0;
+      if (least < 0.0 || us < least) {
+        least = us;
+        best = {v.kernel, static_cast<int>(parts)};
+      }
+    }
+  }
+  return best;
+}
+
+hipError_t launch_product(const I8Problem &p, hipStream_t stream) {
+  if (p.rows_each == 0) return launch_few<1, 1, 8, 4>(p, stream);
+  const Choice c = choose(p.T, p.I, p.rows_each, p.O / p.rows_each, p.sums != nullptr);
+  switch (c.kernel) {
+    case Kernel::kFew: return launch_few<1, 1, 8, 4>(p, stream);
+    case Kernel::k64: return launch_i8_tiles<2, 2, 4>(p, c.parts, stream);
+    case Kernel::k128: return launch_i8_tiles<4, 4, 4>(p, c.parts, stream);
+    case Kernel::k128Walk: return launch_i8_tiles<4, 4, 2>(p, 1, stream);
+    case Kernel::k256Walk: return launch_i8_tiles<8, 8, 2>(p, 1, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+// Whether tokens are rounded inside the product's launch: every 16 channels do it again, which 2^14 values are quick enough
+// for, and in all 2^27 / 16 of them (one token: any number; it is read by every workgroup anyway).  us in one launch / two: 1 token 512 -> 512
+// 4.1 / 5.5, 4096 -> 16384 14.9 / 16.8; 8 of 2048 -> 512 6.5 / 6.9; beyond the line, 3 of 4096 -> 16384 18.2 / 15.6.
+bool rounds_inside(const Weight &w) {
+  const int64_t values = w.T * w.I;
+  return w.T <= 16 && values <= (1 << 14) && (w.T == 1 || values * w.O <= (1ll << 27));
 }
 
 // Whether the product reads the shards where they lie.
-bool in_place(const Weight &w) { return w.rows_each > 0 || w.T <= kI8FewTokens; }
+bool in_place(const Weight &w) { return w.T <= kI8FewTokens || w.rows_each >= kI8ShardRows; }
+
+// The workspace up to the staging slot: [Xq][s_t][counters][sums of tiles whose reduction is shared].  The last two do not depend on
+// T, so that what does for many tokens does for fewer.
+bool may_share(const Weight &w) { return w.I > 3 * 128 && w.O <= 16384; }
+size_t scale_offset(const Weight &w) { return round_up(static_cast<size_t>(w.T) * i8_row_bytes(w.I), kAlign); }
+size_t counter_offset(const Weight &w) { return scale_offset(w) + round_up(static_cast<size_t>(w.T) * 4, kAlign); }
+size_t token_bytes(const Weight &w) { return counter_offset(w) + (may_share(w) ? kI8MostTiles * 4 + kI8SumBytes : 0); }
 
 osdp_status check_slices(const osdp_shape *s, Weight *w, int64_t *widest) {
   const int64_t k = s->k == 0 ? 1 : s->k;
@@ -368,22 +450,25 @@ osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int
   const hipStream_t q = static_cast<hipStream_t>(stream);
   char *ws = static_cast<char *>(workspace);
   I8Problem p{};
-  p.T = static_cast<int32_t>(w.T); p.I = static_cast<int32_t>(w.I);
+  p.T = static_cast<int32_t>(w.T); p.I = static_cast<int32_t>(w.I); p.O = static_cast<int32_t>(w.O);
   p.ldq = static_cast<int32_t>(i8_row_bytes(w.I));
-  p.xq = reinterpret_cast<uint8_t *>(ws);
-  p.x_scale = reinterpret_cast<float *>(ws + round_up(static_cast<size_t>(w.T) * p.ldq, kAlign));
+  p.shards = tab; p.L = w.L; p.rows_each = static_cast<int32_t>(w.rows_each);
+  p.w_scale = w_scale; p.y = static_cast<uint16_t *>(Y); p.ldy = ldy;
+  const uint16_t *x = static_cast<const uint16_t *>(X);
+  if (rounds_inside(w)) return hip_status(launch_fused<1, 8, 2>(p, x, ldx, q), "launching the product");
+  uint8_t *xq = reinterpret_cast<uint8_t *>(ws);
+  float *x_scale = reinterpret_cast<float *>(ws + scale_offset(w));
+  p.xq = xq; p.x_scale = x_scale;
+  if (may_share(w)) {
+    p.arrived = reinterpret_cast<uint32_t *>(ws + counter_offset(w));
+    p.sums = p.arrived + kI8MostTiles;
+  }
   char *slot = ws + token_bytes(w);
-  hipLaunchKernelGGL(quantize_tokens_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(w.T, 1 << 20))), dim3(kThreads), 0, q,
-                     static_cast<const uint16_t *>(X), ldx, p.I, p.ldq, p.T, const_cast<uint8_t *>(p.xq), const_cast<float *>(p.x_scale));
+  hipLaunchKernelGGL(quantize_tokens_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(w.T, 1 << 20))), dim3(kThreads), 0, q, x, ldx, p.I,
+                     p.ldq, p.T, xq, x_scale, p.arrived);
   if ((st = hip_status(hipGetLastError(), "launching the tokens' quantization")) != OSDP_OK) return st;
-  p.ldy = ldy;
-  p.L = w.L;
   if (in_place(w)) {
-    p.O = static_cast<int32_t>(w.O);
-    p.shards = tab;
-    p.rows_each = static_cast<int32_t>(w.rows_each);
-    p.w_scale = w_scale; p.y = static_cast<uint16_t *>(Y);
-    return hip_status(launch_i8(p, q), "launching the product");
+    return hip_status(launch_product(p, q), "launching the product");
   }
   ShardLayout lay{};  // (two bytes an element, as the gather counts)
   lay.O = w.I / 2; lay.L = w.L / 2; lay.N = w.N; lay.rows_per_shard = 0;
@@ -394,7 +479,7 @@ osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int
     p.shards.p[0] = slot;
     p.rows_each = p.O;
     p.w_scale = w_scale + c0; p.y = static_cast<uint16_t *>(Y) + c0;
-    if ((st = hip_status(launch_i8(p, q), "launching the product")) != OSDP_OK) return st;
+    if ((st = hip_status(launch_product(p, q), "launching the product")) != OSDP_OK) return st;
   }
   return OSDP_OK;
 }

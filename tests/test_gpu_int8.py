@@ -102,12 +102,41 @@ def test_product_over_token_counts(T, I, O, N):
 @pytest.mark.parametrize("T", [1, 9, 40, 70, 140, 300])
 @pytest.mark.parametrize("I,O,N,k", [(16, 8, 1, 1), (16, 1024, 64, 2), (48, 24, 4, 3), (112, 40, 5, 5), (128, 136, 1, 0), (144, 80, 16, 2),
                                      (2064, 264, 3, 3), (8208, 48, 9, 1), (32, 2056, 16, 1), (336, 1000, 3, 5), (16384, 72, 8, 1),
-                                     (4096, 24, 64, 1)])
+                                     (4096, 24, 64, 1), (640, 2600, 8, 1), (512, 264, 8, 1), (272, 3000, 24, 1)])
 def test_product_over_weight_shapes_and_cuts(T, I, O, N, k):
     """Row blocks of channels, flat cuts inside a channel's row, shards shorter than a row, narrow and long ones."""
     print("int8 product", T, I, O, N, k, flush=True)
     w, x = Weight(I, O, N), tokens(T, I)
     same(forward(w, x, k), expected(x, w.q, w.scale))
+
+
+# one that each of the kernels is chosen for, with the parts that its tiles' reductions are cut into
+CHOICES = [((5, 512, 512, 8), "i8_fused_kernel", 1), ((30, 400, 3456, 8), "i8_few_kernel", 1), ((300, 1152, 2048, 8), "i8_w4_kernelILi2ELi2ELi4", 1),
+           ((161, 14448, 960, 8), "i8_w4_kernelILi2ELi2ELi4", 4), ((1000, 4096, 4096, 4), "i8_w4_kernelILi4ELi4ELi4", 1),
+           ((300, 16384, 2048, 4), "i8_w4_kernelILi4ELi4ELi4", 4), ((500, 2560, 10240, 8), "i8_w4_kernelILi4ELi4ELi2", 1),
+           ((1500, 1024, 16424, 8), "i8_w4_kernelILi8ELi8ELi2", 1)]
+
+
+@pytest.mark.parametrize("sizes,kernel,parts", CHOICES)
+def test_every_kernel_gives_the_same_whole_numbers(sizes, kernel, parts):
+    import gpu_harness as H
+    T, I, O, N = sizes
+    print("int8 product", *sizes, kernel, flush=True)
+    w, x = Weight(I, O, N), tokens(T, I)
+    want = expected(x, w.q, w.scale)
+    same(forward(w, x), want)
+    X, Y = bf16(x).cuda(), torch.zeros(T, O, dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, 1)[0], dtype=torch.uint8, device="cuda")
+    ran = H.kernels(lambda s: osdp.osdp_split_linear_i8_fwd(X, w.shards, w.dev_scale, Y, 1, ws, stream=s))
+    assert len(ran) == (1 if kernel == "i8_fused_kernel" else 2) and kernel in ran[-1][0], ran
+    if parts > 1:  # more workgroups than tiles, and the same numbers every time, whichever part arrives last
+        side = 64 if "ILi2ELi2" in ran[-1][0] else 128
+        assert ran[-1][1] >= 2 * -(-T // side) * N * -(-(O // N) // side)
+        for _ in range(20):
+            Y.zero_()
+            osdp.osdp_split_linear_i8_fwd(X, w.shards, w.dev_scale, Y, 1, ws)
+            torch.cuda.synchronize()
+            same(Y.float().cpu().numpy(), want)
 
 
 @pytest.mark.parametrize("T,I,O,N", [(1, 32768, 1024, 8), (33, 131072, 128, 2), (1030, 1024, 2048, 8), (700, 8192, 776, 1), (2100, 384, 3080, 8),

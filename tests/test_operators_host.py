@@ -115,14 +115,17 @@ def test_i8_forward_refuses(more, status):
 
 
 @pytest.mark.parametrize("T,I,O,N,k", [(1, 16, 8, 1, 0), (500, 2560, 10240, 8, 4), (500, 2560, 10248, 16, 3), (64, 4096, 24, 64, 1),
-                                       (65, 4096, 24, 16, 3), (0, 64, 32, 2, 1)])
+                                       (65, 4096, 24, 16, 3), (0, 64, 32, 2, 1), (300, 4096, 256, 16, 1), (300, 4096, 1000, 8, 1)])
 def test_i8_workspace_follows_the_law(T, I, O, N, k):
-    """One byte an element and 1/k of the weight, where slices are gathered; nothing where the shards are read in place."""
+    """One byte an element and 1/k of the weight, where slices are gathered; nothing where the shards are read in place.
+    What is for the tokens grows with them, and what their number does not decide is a constant."""
     total, peak = osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, k)
-    gathers = T > 64 and O % N != 0
+    gathers = T > 64 and (O % N != 0 or O // N < 32)
     assert peak == (I * max((j + 1) * O // max(k, 1) - j * O // max(k, 1) for j in range(max(k, 1))) if gathers else 0)
-    rows = T * (-(-I // 128) * 128)
-    assert total >= rows + 4 * T + peak and total <= rows + 4 * T + peak + 3 * 256
+    tokens = T * (-(-I // 128) * 128) + 4 * T
+    assert tokens + peak <= total <= tokens + peak + (16 << 20) + 1024 + 3 * 256
+    fewer = [osdp.osdp_split_linear_i8_workspace_bytes(t, I, O, N, k)[0] for t in range(0, T + 1, max(1, T // 50))]
+    assert fewer == sorted(fewer) and max(fewer) <= total, "what does for T tokens has to do for fewer"
 
 
 def test_i8_quantize_refuses():
