@@ -61,12 +61,13 @@ struct Step {
 enum Form { kMaster = 0, kBf16 = 1, kF32 = 2 };
 
 // 32 bits stirred: multiplications by odd numbers and shifted sums without carry, each of them one to one.
-__host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
-  x *= 0x9E3779B1u;
+constexpr uint32_t kStir = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t stir(uint32_t x) {  // mix() behind its first product
   x ^= x >> 15;
   x *= 0x2C1B3C6Du;
   return x ^ (x >> 13);
 }
+__device__ __forceinline__ uint32_t mix(uint32_t x) { return stir(x * kStir); }
 
 // base^n by squaring: the same in a kernel and on the host.
 __host__ __device__ inline double power(double base, int64_t n) {
@@ -97,50 +98,77 @@ __device__ __forceinline__ uint32_t element(int j) {
   return row * kBlock + (kWide ? lane * kPerLane + j : j * 16u + lane);
 }
 
-template <bool kWide>
-__device__ __forceinline__ void load8(const float *p, int64_t at, uint32_t left, float (&x)[8]) {
-  if constexpr (kWide) {
-    const f32x4 *q = reinterpret_cast<const f32x4 *>(p + at + element<true>(0));
-    const f32x4 a = q[0], b = q[1];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = element<false>(j) < left ? p[at + element<false>(j)] : 0.f;
-  }
-}
+// A lane's eight elements as they lie in memory, asked for (load) apart from where they are taken to pieces (get), so that all of a
+// tile's loads are on their way before the first of them is waited for.
+template <class T, bool kWide>
+struct Eight;
 
-template <bool kWide>
-__device__ __forceinline__ void load8(const uint16_t *p, int64_t at, uint32_t left, float (&x)[8]) {
-  if constexpr (kWide) {
-    const uint4 a = *reinterpret_cast<const uint4 *>(p + at + element<true>(0));
+template <class T>
+struct Eight<T, false> {
+  T x[8];
+  __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t left) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = static_cast<const T *>(p)[at + min(element<false>(j), left - 1)];  // (no branches: all at once)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = element<false>(j) < left ? x[j] : T{0};
+  }
+  __device__ __forceinline__ void get(float (&out)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (sizeof(T) == 4) out[j] = x[j];
+      else out[j] = __uint_as_float(static_cast<uint32_t>(x[j]) << 16);
+    }
+  }
+  __device__ __forceinline__ void get(uint32_t (&out)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) out[j] = static_cast<uint32_t>(x[j]);
+  }
+};
+
+template <>
+struct Eight<float, true> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t) {
+    const f32x4 *q = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + at + element<true>(0));
+    a = q[0];
+    b = q[1];
+  }
+  __device__ __forceinline__ void get(float (&out)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = a[j], out[4 + j] = b[j];
+  }
+};
+
+template <>
+struct Eight<uint16_t, true> {
+  uint4 a;
+  __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t) {
+    a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + at + element<true>(0));
+  }
+  __device__ __forceinline__ void get(float (&out)[8]) const {  // bf16
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __uint_as_float(w[j] << 16);
-      x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      out[2 * j] = __uint_as_float(w[j] << 16);
+      out[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      x[j] = element<false>(j) < left ? __uint_as_float(static_cast<uint32_t>(p[at + element<false>(j)]) << 16) : 0.f;
   }
-}
+};
 
-template <bool kWide>
-__device__ __forceinline__ void load8(const uint8_t *p, int64_t at, uint32_t left, uint32_t (&x)[8]) {
-  if constexpr (kWide) {
-    const uint2 a = *reinterpret_cast<const uint2 *>(p + at + element<true>(0));
+template <>
+struct Eight<uint8_t, true> {
+  uint2 a;
+  __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t) {
+    a = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(p) + at + element<true>(0));
+  }
+  __device__ __forceinline__ void get(uint32_t (&out)[8]) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      x[j] = (a.x >> (8 * j)) & 255u;
-      x[4 + j] = (a.y >> (8 * j)) & 255u;
+      out[j] = (a.x >> (8 * j)) & 255u;
+      out[4 + j] = (a.y >> (8 * j)) & 255u;
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = element<false>(j) < left ? p[at + element<false>(j)] : 0u;
   }
-}
+};
 
 template <bool kWide>
 __device__ __forceinline__ void store8(float *p, int64_t at, uint32_t left, const float (&x)[8]) {
@@ -200,36 +228,44 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
 
 // ---- moments in 8 bits: kTop is the largest exponent field (15: m, 31: v), kLow the least b -------------------------
 // With its exponent field and fraction put where fp32 has them, a code is the value times a power of two; where the field
-// is 0 fp32 reads them as it reads its own smallest numbers, which is what the format wants.
+// is 0 fp32 reads them as it reads its own smallest numbers, which is what the format wants.  nan: a quiet NaN's bits for a block that is none, else 0.
 template <int kTop>
-__device__ __forceinline__ float decode(uint32_t code, uint32_t b) {
+__device__ __forceinline__ float decode(uint32_t code, uint32_t b, uint32_t nan) {
   const uint32_t magnitude = kTop == 15 ? code & 127u : code;
-  const uint32_t nan = b == 255u ? 0x7fc00000u : 0u;
   const float x = __builtin_amdgcn_ldexpf(__uint_as_float((magnitude << 20) | nan), static_cast<int>(b) - kTop);
-  return kTop == 15 ? __uint_as_float(__float_as_uint(x) ^ ((code & 128u) << 24)) : x;
+  return kTop == 15 ? __uint_as_float(__float_as_uint(x) | ((code & 128u) << 24)) : x;
 }
+__device__ __forceinline__ uint32_t nan_bits(uint32_t b) { return b == 255u ? 0x7fc00000u : 0u; }
 
 // The power of two of a block whose largest magnitude has these bits: rounding up to 3 fraction bits may carry into the
 // next binade, or (FLT_MAX) out of the numbers, like a NaN or an infinity.
 template <int kLow>
-__device__ __forceinline__ uint32_t block_exponent(uint32_t most) {
-  const uint32_t b = (most + 0xfffffu) >> 23;
-  return most == 0u ? 0u : max(b, static_cast<uint32_t>(kLow));
-}
+__device__ __forceinline__ uint32_t block_exponent(uint32_t most) { return max((most + 0xfffffu) >> 23, static_cast<uint32_t>(kLow)); }
 
-// In units of its binade's step a magnitude is x in [0, 16) (below 8 in the smallest binade only); x plus a fraction from
-// 16 random bits, cut, is 16 at most by the carry into the next binade, and never beyond the block's own largest code.
-template <int kTop>
-__device__ __forceinline__ uint32_t encode(float x, uint32_t b, uint32_t random16) {
-  const uint32_t bits = __float_as_uint(x), size = bits & 0x7fffffffu;
+// Codes of eight values (magnitudes' bits) of a block, rounded with 16 random bits each, from bit kShift of h on.  Above the smallest
+// binade the random bits are added below the last fraction bit and the sum is cut: a carry runs into the exponent as it should,
+// and never beyond the block's own largest code.  A lane that has a value in the smallest binade (one in 10^4 of a bell curve's; zeros) takes
+// the general way, which is three times as long: in units of its binade's step a magnitude is x in [0, 16), and x plus the fraction is cut.
+template <int kTop, int kShift>
+__device__ __forceinline__ void encode8(const uint32_t (&size)[8], uint32_t b, const uint32_t (&h)[8], uint32_t (&code)[8]) {
   const uint32_t least = b - (kTop - 1);
-  const uint32_t e = max(size >> 23, least);
-  const float units = __builtin_amdgcn_ldexpf(__uint_as_float(size), 130 - static_cast<int>(e));
-  const uint32_t q = static_cast<uint32_t>(fmaf(static_cast<float>(random16), 0x1p-16f, units));
-  uint32_t code = (e - least) * 8u + q;
-  if (kTop == 31) code = size != 0u && code == 0u ? 1u : code;  // (a positive v stays positive)
-  if (b == 0u || b == 255u) return 0u;
-  return kTop == 15 ? code | ((bits >> 24) & 128u) : code;
+  uint32_t smallest = size[0];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    smallest = min(smallest, size[j]);
+    const uint32_t r = kShift ? (h[j] >> 12) & 0xffff0u : (h[j] & 0xffffu) << 4;
+    code[j] = ((size[j] + r) >> 20) - (least - 1) * 8u;
+  }
+  if (smallest < least << 23) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t e = max(size[j] >> 23, least);
+      const float units = __builtin_amdgcn_ldexpf(__uint_as_float(size[j]), 130 - static_cast<int>(e));
+      const uint32_t q = static_cast<uint32_t>(fmaf(static_cast<float>((h[j] >> kShift) & 0xffffu), 0x1p-16f, units));
+      code[j] = (e - least) * 8u + q;
+      if (kTop == 31) code[j] = max(code[j], min(size[j], 1u));  // (a positive v stays positive)
+    }
+  }
 }
 
 struct Scalars {
@@ -250,28 +286,37 @@ template <class Grad, int kForm, bool kState8, bool kWide>
 __device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const Scalars &k, int64_t at) {
   const int64_t rest = t.n - at;
   const uint32_t left = rest < kTile ? static_cast<uint32_t>(rest) : kTile;
-  using Param = std::conditional_t<kForm == kF32, float, uint16_t>;
+  using State = std::conditional_t<kState8, uint8_t, float>;
+  using Source = std::conditional_t<kForm == kBf16, uint16_t, float>;
+  Eight<Grad, kWide> grad;
+  Eight<Source, kWide> source;
+  Eight<State, kWide> old_m, old_v;
+  // the block's two powers; of a short last tile only those of blocks that there are
+  uint16_t *const exps = reinterpret_cast<uint16_t *>(t.exps) + at / kBlock + (threadIdx.x >> 4);
+  const bool block = kWide || (threadIdx.x >> 4) * kBlock < left;
+  uint32_t shared = 0;
+  old_m.load(t.m, at, left);
+  old_v.load(t.v, at, left);
+  if (kState8 && block) shared = *exps;
+  grad.load(t.grad, at, left);
+  source.load(kForm == kMaster ? static_cast<const void *>(t.master) : t.param, at, left);
   float g[8], p[8], m[8], v[8];
   uint32_t cm[8], cv[8];
-  uint16_t *exps = nullptr;
-  uint32_t shared = 0;
-  load8<kWide>(static_cast<const Grad *>(t.grad), at, left, g);
-  if constexpr (kForm == kMaster) load8<kWide>(static_cast<const float *>(t.master), at, left, p);
-  else load8<kWide>(static_cast<const Param *>(t.param), at, left, p);
   if constexpr (kState8) {
-    exps = reinterpret_cast<uint16_t *>(t.exps) + at / kBlock + (threadIdx.x >> 4);
-    if ((threadIdx.x >> 4) * kBlock < left) shared = *exps;
-    load8<kWide>(static_cast<const uint8_t *>(t.m), at, left, cm);
-    load8<kWide>(static_cast<const uint8_t *>(t.v), at, left, cv);
+    old_m.get(cm);
+    old_v.get(cv);
+    const uint32_t bm = shared & 255u, bv = shared >> 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      m[j] = decode<15>(cm[j], shared & 255u);
-      v[j] = decode<31>(cv[j], shared >> 8);
+      m[j] = decode<15>(cm[j], bm, nan_bits(bm));
+      v[j] = decode<31>(cv[j], bv, nan_bits(bv));
     }
   } else {
-    load8<kWide>(static_cast<const float *>(t.m), at, left, m);
-    load8<kWide>(static_cast<const float *>(t.v), at, left, v);
+    old_m.get(m);
+    old_v.get(v);
   }
+  grad.get(g);
+  source.get(p);
   const float decay = k.lr * t.decay;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -282,25 +327,31 @@ __device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const
   }
   uint32_t h[8];
   if constexpr (kState8 || kForm == kBf16) {
-    const uint32_t base = mix(k.key ^ static_cast<uint32_t>(at >> 32)) + static_cast<uint32_t>(at);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = mix(base + element<kWide>(j));
+    for (int j = 0; j < 8; ++j) h[j] = stir((k.key + static_cast<uint32_t>(at) + element<kWide>(0)) * kStir + static_cast<uint32_t>(kWide ? j : 16 * j) * kStir);
   }
   if constexpr (kState8) {
-    uint32_t most_m = 0, most_v = 0;
+    uint32_t sm[8], sv[8], most_m = 0, most_v = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (!kWide && element<kWide>(j) >= left) m[j] = v[j] = 0.f;  // (0 * beta is NaN where the block was)
-      most_m = max(most_m, __float_as_uint(m[j]) & 0x7fffffffu);
-      most_v = max(most_v, __float_as_uint(v[j]) & 0x7fffffffu);
+      sm[j] = __float_as_uint(m[j]) & 0x7fffffffu;
+      sv[j] = __float_as_uint(v[j]) & 0x7fffffffu;
+      most_m = max(most_m, sm[j]);
+      most_v = max(most_v, sv[j]);
     }
-    const uint32_t bm = block_exponent<32>(row_max(most_m)), bv = block_exponent<48>(row_max(most_v));
+    most_m = row_max(most_m);
+    most_v = row_max(most_v);
+    const uint32_t bm = block_exponent<32>(most_m), bv = block_exponent<48>(most_v);
+    encode8<15, 0>(sm, bm, h, cm);
+    encode8<31, 16>(sv, bv, h, cv);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      cm[j] = encode<15>(m[j], bm, h[j] & 0xffffu);
-      cv[j] = encode<31>(v[j], bv, h[j] >> 16);
+      cm[j] = bm == 255u ? 0u : cm[j] | ((__float_as_uint(m[j]) >> 24) & 128u);
+      cv[j] = bv == 255u ? 0u : cv[j];
     }
-    if ((threadIdx.x & 15) == 0 && (threadIdx.x >> 4) * kBlock < left) *exps = static_cast<uint16_t>(bm | (bv << 8));
+    if ((threadIdx.x & 15) == 0 && block)
+      *exps = static_cast<uint16_t>((most_m ? bm : 0u) | (most_v ? bv << 8 : 0u));
     store8<kWide>(static_cast<uint8_t *>(t.m), at, left, cm);
     store8<kWide>(static_cast<uint8_t *>(t.v), at, left, cv);
   } else {
@@ -314,14 +365,10 @@ __device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const
     uint32_t w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t bits = __float_as_uint(p[j]);
-      if constexpr (kForm == kMaster) {
-        w[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(p[j]))) << 16;
-      } else {
-        // to one of its neighbours, the one above with the probability that keeps the mean; NaN and infinities as they are
-        const bool number = (bits & 0x7f800000u) != 0x7f800000u;
-        w[j] = number ? bits + ((h[j] * 0x297A2D39u) >> 16) : bits | ((bits & 0x7fffffu) ? 0x400000u : 0u);
-      }
+      // without a master copy to one of its neighbours, the one above with the probability that keeps the mean (an infinity
+      // keeps its upper half whatever is added, a NaN might not)
+      if constexpr (kForm == kMaster) w[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(p[j]))) << 16;
+      else w[j] = __float_as_uint(p[j]) + (p[j] == p[j] ? (h[j] * 0x297A2D39u) >> 16 : 0u);
     }
     store8<kWide>(static_cast<uint16_t *>(t.param), at, left, w);
   }
@@ -361,9 +408,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Batch b, Step s) {
   const uint32_t stirred = k.key;
   for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
     const int i = tensor_of(b, tile);
-    const Tensor &t = b.t[i];
+    const Tensor t = b.t[i];
     const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
-    k.key = mix(stirred ^ (b.first + static_cast<uint32_t>(i)));
+    k.key = mix(mix(stirred ^ (b.first + static_cast<uint32_t>(i))) ^ static_cast<uint32_t>(at >> 32));
     if (((b.wide >> i) & 1u) && t.n - at >= kTile) adamw_tile<Grad, kForm, kState8, true>(t, s, k, at);
     else adamw_tile<Grad, kForm, kState8, false>(t, s, k, at);
   }
@@ -374,13 +421,16 @@ __device__ __forceinline__ void values_tile(const Tensor &t, int64_t at) {
   const int64_t rest = t.n - at;
   const uint32_t left = rest < kTile ? static_cast<uint32_t>(rest) : kTile;
   uint32_t shared = 0, cm[8], cv[8], wm[8], wv[8];
-  if ((threadIdx.x >> 4) * kBlock < left) shared = reinterpret_cast<const uint16_t *>(t.exps)[at / kBlock + (threadIdx.x >> 4)];
-  load8<kWide>(static_cast<const uint8_t *>(t.m), at, left, cm);
-  load8<kWide>(static_cast<const uint8_t *>(t.v), at, left, cv);
+  Eight<uint8_t, kWide> m, v;
+  m.load(t.m, at, left);
+  v.load(t.v, at, left);
+  if (kWide || (threadIdx.x >> 4) * kBlock < left) shared = reinterpret_cast<const uint16_t *>(t.exps)[at / kBlock + (threadIdx.x >> 4)];
+  m.get(cm);
+  v.get(cv);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    wm[j] = __float_as_uint(decode<15>(cm[j], shared & 255u));
-    wv[j] = __float_as_uint(decode<31>(cv[j], shared >> 8));
+    wm[j] = __float_as_uint(decode<15>(cm[j], shared & 255u, nan_bits(shared & 255u)));
+    wv[j] = __float_as_uint(decode<31>(cv[j], shared >> 8, nan_bits(shared >> 8)));
   }
   store8<kWide>(static_cast<uint16_t *>(t.param), at, left, wm);                          // (m's values)
   store8<kWide>(reinterpret_cast<uint16_t *>(t.master), at, left, wv);                    // (v's values)
@@ -389,7 +439,7 @@ __device__ __forceinline__ void values_tile(const Tensor &t, int64_t at) {
 __global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
   for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
     const int i = tensor_of(b, tile);
-    const Tensor &t = b.t[i];
+    const Tensor t = b.t[i];
     const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
     if (((b.wide >> i) & 1u) && t.n - at >= kTile) values_tile<true>(t, at);
     else values_tile<false>(t, at);
@@ -400,6 +450,8 @@ __global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
 // Squares and sums are in double from the first product on (a bf16 gradient of 1e20 is one, its square in fp32 is not): the
 // vector unit multiplies and adds them as fast as fp32, and the pass stays bound by memory.
 constexpr int kSumBlocks = 1024;  // workgroups, and so partial sums, of a launch at most
+constexpr int kSumTiles = 4;      // tiles that a workgroup has on their way at a time, where there are enough for all: 806 MB in 136 us
+                                  // (5.9 TB/s), with one tile at a time in 214
 
 __device__ __forceinline__ double block_sum(double x) {
   __shared__ double part[kThreads / 64];
@@ -413,19 +465,45 @@ __device__ __forceinline__ double block_sum(double x) {
   return sum;
 }
 
+// Tiles in runs of kSumTiles, or alone, one run after another to the workgroups.
 template <class Grad>
-__global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, double *__restrict__ out) {
+__global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, double *__restrict__ out) {
   double sum = 0.0;
-  for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
-    const int i = tensor_of(b, tile);
-    const Tensor &t = b.t[i];
-    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
-    const int64_t rest = t.n - at;
-    float g[8];
-    if (((b.wide >> i) & 1u) && rest >= kTile) load8<true>(static_cast<const Grad *>(t.grad), at, kTile, g);
-    else load8<false>(static_cast<const Grad *>(t.grad), at, rest < kTile ? static_cast<uint32_t>(rest) : kTile, g);
+  auto add = [&](const float (&g)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum = fma(static_cast<double>(g[j]), static_cast<double>(g[j]), sum);
+  };
+  for (uint32_t first = blockIdx.x * run; first < b.tiles; first += gridDim.x * run) {
+    const uint32_t end = min(first + run, b.tiles);
+    int i = tensor_of(b, first);
+    const int64_t start = i > 0 ? b.t[i - 1].end_tile : 0;
+    const int64_t at = (first - start) * kTile;
+    float g[8];
+    if (run == kSumTiles && first + kSumTiles <= b.tiles && ((b.wide >> i) & 1u) && b.t[i].n - at >= kSumTiles * kTile) {
+      Eight<Grad, true> x[kSumTiles];
+#pragma unroll
+      for (int u = 0; u < kSumTiles; ++u) x[u].load(b.t[i].grad, at + u * kTile, kTile);
+#pragma unroll
+      for (int u = 0; u < kSumTiles; ++u) {
+        x[u].get(g);
+        add(g);
+      }
+      continue;
+    }
+    for (uint32_t tile = first; tile < end; ++tile) {
+      i = tensor_of(b, tile);
+      const int64_t from = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile, rest = b.t[i].n - from;
+      if (((b.wide >> i) & 1u) && rest >= kTile) {
+        Eight<Grad, true> x;
+        x.load(b.t[i].grad, from, kTile);
+        x.get(g);
+      } else {
+        Eight<Grad, false> x;
+        x.load(b.t[i].grad, from, rest < kTile ? static_cast<uint32_t>(rest) : kTile);
+        x.get(g);
+      }
+      add(g);
+    }
   }
   sum = block_sum(sum);
   if (threadIdx.x == 0) out[blockIdx.x] = sum;
@@ -434,7 +512,13 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, double *__rest
 __global__ __launch_bounds__(kThreads) void sumsq_finish_kernel(const double *__restrict__ part, int32_t count, int32_t accumulate,
                                                                 double *__restrict__ out) {
   double sum = 0.0;
-  for (int i = threadIdx.x; i < count; i += kThreads) sum += part[i];
+  for (int i = threadIdx.x; i < count; i += 4 * kThreads) {
+    double x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = part[min(i + j * kThreads, count - 1)];  // (all four on their way at once)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += i + j * kThreads < count ? x[j] : 0.0;
+  }
   sum = block_sum(sum);
   if (threadIdx.x == 0) *out = accumulate ? *out + sum : sum;
 }
@@ -530,7 +614,8 @@ hipError_t launch_adamw(int form, bool state8, const Batch &b, const Step &s, hi
 }
 
 // Workgroups, and so partial sums, of the launch over a batch.
-unsigned sum_blocks(const Batch &b) { return grid_of(b, kSumBlocks); }
+uint32_t sum_run(const Batch &b) { return b.tiles >= kSumTiles * kSumBlocks ? kSumTiles : 1; }
+unsigned sum_blocks(const Batch &b) { return std::min<unsigned>(b.tiles, kSumBlocks); }
 
 osdp_status sumsq_parts(const osdp_adamw_tensor *tensors, int32_t count, int64_t *parts) {
   *parts = 0;
@@ -642,8 +727,8 @@ osdp_status osdp_adamw_grad_sumsq(const osdp_adamw_tensor *tensors, int32_t coun
       },
       [&](const Batch &b) {
         const unsigned blocks = sum_blocks(b);
-        if (grad_type == OSDP_BF16) hipLaunchKernelGGL(sumsq_kernel<uint16_t>, dim3(blocks), dim3(kThreads), 0, q, b, part);
-        else hipLaunchKernelGGL(sumsq_kernel<float>, dim3(blocks), dim3(kThreads), 0, q, b, part);
+        if (grad_type == OSDP_BF16) hipLaunchKernelGGL(sumsq_kernel<uint16_t>, dim3(blocks), dim3(kThreads), 0, q, b, sum_run(b), part);
+        else hipLaunchKernelGGL(sumsq_kernel<float>, dim3(blocks), dim3(kThreads), 0, q, b, sum_run(b), part);
         part += blocks;
         return hip_status(hipGetLastError(), "launching the sum of squares");
       });
