@@ -219,8 +219,15 @@ def _plan_ref(plan: Optional[Plan]):
     return ctypes.byref(p), (p, keep)
 
 
+_pointers = {}  # array types by length (making one anew costs half a microsecond)
+
+
 def _ptrs(tensors):
-    return (ctypes.c_void_p * len(tensors))(*[int(t.data_ptr()) for t in tensors])
+    n = len(tensors)
+    kind = _pointers.get(n)
+    if kind is None:
+        kind = _pointers[n] = ctypes.c_void_p * n
+    return kind(*[t.data_ptr() for t in tensors])
 
 
 def _stream(s) -> Optional[int]:
@@ -474,7 +481,7 @@ class AdamWTable:
 
 
 def _bytes(workspace) -> int:
-    return workspace.numel() * workspace.element_size()
+    return workspace.nbytes
 
 
 def osdp_adamw_grad_sumsq_workspace_bytes(table: AdamWTable) -> int:
@@ -551,7 +558,7 @@ def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=No
     O = Y.shape[1]
     if w_scale.numel() < O or w_scale.element_size() != 4:
         _refuse(f"w_scale must hold {O} float32")
-    shape = _shape(T, I, O, len(q_shards), k)
+    shape = osdp_shape(T, I, O, len(q_shards), k)
     _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), X.stride(0), _ptrs(q_shards), w_scale.data_ptr(),
                                         Y.data_ptr(), Y.stride(0), workspace.data_ptr(), _bytes(workspace), _stream(stream)))
 

@@ -16,6 +16,11 @@ __device__ __forceinline__ uint32_t i8_largest(uint4 v) {
   return m;
 }
 
+// Four lower bytes side by side.
+__device__ __forceinline__ uint32_t i8_pack(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
 // From the bits of a row's or column's largest magnitude: its scale and the rounding of its values to 8 bits.
 struct I8Scale {
   float scale, up, r;
@@ -26,20 +31,21 @@ struct I8Scale {
     up = amax < 0x1p-100f ? 0x1p100f : 1.f;  // (127 / amax would be no number; a power of two changes no quotient)
     r = number && most != 0u ? 127.f / (amax * up) * (1.f + 0x1p-21f) : 0.f;
   }
-  __device__ __forceinline__ uint32_t round(float x) const {  // lower 8 bits
-    const float t = fminf(fmaf(fabsf(x * up), r, 0.5f), 127.f);
-    const int q = static_cast<int>(r == 0.f ? 0.f : t);
-    return static_cast<uint32_t>(__float_as_uint(x) >> 31 ? -q : q);
+  __device__ __forceinline__ I8Scale(float ratio, float shift) : scale(0.f), up(shift), r(ratio) {}
+  // Lower 8 bits.  A half with the number's sign is added and the fraction dropped; what is no number gives 0.
+  __device__ __forceinline__ uint32_t round(float x) const {
+    const float half = __uint_as_float((__float_as_uint(x) & 0x80000000u) | 0x3f000000u);
+    const float t = fmaf(x * up, r, half);
+    uint32_t q;  // (the instruction itself, which makes 0 of a NaN; to a cast in C++ that would be undefined)
+    asm("v_cvt_i32_f32 %0, %1" : "=v"(q) : "v"(t));
+    return q;
   }
   __device__ __forceinline__ uint2 round8(uint4 v) const {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t out[2] = {0u, 0u};
+    uint32_t q[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t q = round(__uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16));
-      out[j >> 2] |= (q & 255u) << (8 * (j & 3));
-    }
-    return uint2{out[0], out[1]};
+    for (int j = 0; j < 8; ++j) q[j] = round(__uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16));
+    return uint2{i8_pack(q[0], q[1], q[2], q[3]), i8_pack(q[4], q[5], q[6], q[7])};
   }
 };
 

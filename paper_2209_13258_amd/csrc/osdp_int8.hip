@@ -23,69 +23,89 @@ constexpr int64_t kMaxFeatures = 131072;
 constexpr size_t kAlign = 256;
 
 // ---- tokens to 8 bits -------------------------------------------------------------------------------------------
-// One workgroup a token: the row is read once, kept in registers (what lies beyond kHold * 2048 features is read again), its largest
-// magnitude found, and written as bytes.  Rows of Xq are a multiple of 128 bytes long and end in zeros.
+// kWaves waves a token: the row is read once, kept in registers (what lies beyond kHold vectors a lane is read again), its largest
+// magnitude found, and written as bytes.  Rows of Xq are a multiple of 128 bytes long and end in zeros.  Rows of up to 4096 features
+// take one wave, and no barrier.
 constexpr int kHold = 8;
 
+template <int kWaves>
 __global__ __launch_bounds__(kThreads) void quantize_tokens_kernel(const uint16_t *__restrict__ x, int64_t ldx, int32_t features,
                                                                    int32_t ldq, int32_t tokens, uint8_t *__restrict__ q,
                                                                    float *__restrict__ scale, uint32_t *__restrict__ counters) {
   __shared__ uint32_t part[kThreads / 64];
+  constexpr int kRows = kThreads / 64 / kWaves, kStep = kWaves * 64 * 8;
   if (counters && blockIdx.x == 0 && threadIdx.x < kI8MostTiles) counters[threadIdx.x] = 0;  // (of the product that follows)
-  for (int64_t t = blockIdx.x; t < tokens; t += gridDim.x) {
+  const int own = threadIdx.x % (kWaves * 64) * 8;
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / (kWaves * 64); t < tokens; t += static_cast<int64_t>(gridDim.x) * kRows) {
     const uint16_t *row = x + t * ldx;
     uint4 held[kHold];
     uint32_t most = 0;
 #pragma unroll
     for (int c = 0; c < kHold; ++c) {
-      const int i = c * kThreads * 8 + threadIdx.x * 8;
-      held[c] = i < features ? *reinterpret_cast<const uint4 *>(row + i) : uint4{0u, 0u, 0u, 0u};
+      const int i = c * kStep + own;
+      held[c] = i < features ? load_global16(row + i) : uint4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
     for (int c = 0; c < kHold; ++c) most = max(most, i8_largest(held[c]));
-    for (int i = kHold * kThreads * 8 + threadIdx.x * 8; i < features; i += kThreads * 8)
-      most = max(most, i8_largest(*reinterpret_cast<const uint4 *>(row + i)));
+    for (int i = kHold * kStep + own; i < features; i += kStep) most = max(most, i8_largest(load_global16(row + i)));
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), d)));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-    __syncthreads();
+    if constexpr (kWaves > 1) {
+      if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) most = max(most, part[w]);
-    __syncthreads();
+      for (int w = 0; w < kThreads / 64; ++w) most = max(most, part[w]);
+      __syncthreads();
+    }
     const I8Scale s(most);
-    if (threadIdx.x == 0) scale[t] = s.scale;
+    if (own == 0) scale[t] = s.scale;
     uint8_t *out = q + t * ldq;
 #pragma unroll
     for (int c = 0; c < kHold; ++c) {
-      const int i = c * kThreads * 8 + threadIdx.x * 8;
+      const int i = c * kStep + own;
       if (i < ldq) *reinterpret_cast<uint2 *>(out + i) = s.round8(held[c]);
     }
-    for (int i = kHold * kThreads * 8 + threadIdx.x * 8; i < ldq; i += kThreads * 8)
-      *reinterpret_cast<uint2 *>(out + i) = i < features ? s.round8(*reinterpret_cast<const uint4 *>(row + i)) : uint2{0u, 0u};
+    for (int i = kHold * kStep + own; i < ldq; i += kStep)
+      *reinterpret_cast<uint2 *>(out + i) = i < features ? s.round8(load_global16(row + i)) : uint2{0u, 0u};
   }
+}
+
+hipError_t launch_quantize_tokens(const uint16_t *x, int64_t ldx, const I8Problem &p, uint8_t *xq, float *x_scale, hipStream_t stream) {
+  const bool one = p.I <= kHold * 64 * 8;
+  const int64_t rows = one ? kThreads / 64 : 1, groups = std::min<int64_t>((p.T + rows - 1) / rows, 1 << 20);
+  if (one) hipLaunchKernelGGL(quantize_tokens_kernel<1>, dim3(static_cast<unsigned>(groups)), dim3(kThreads), 0, stream, x, ldx, p.I, p.ldq, p.T, xq, x_scale, p.arrived);
+  else hipLaunchKernelGGL(quantize_tokens_kernel<4>, dim3(static_cast<unsigned>(groups)), dim3(kThreads), 0, stream, x, ldx, p.I, p.ldq, p.T, xq, x_scale, p.arrived);
+  return hipGetLastError();
 }
 
 // ---- weight shards to 8 bits --------------------------------------------------------------------------------------
 // Two passes: the largest magnitude of every column over a range of rows, one range a workgroup (into the workspace); then,
-// over tiles of 128 x 128, their largest, the rounding, and the transposition through LDS.
+// over tiles of 128 x 128, their largest, the rounding, and the transposition through LDS.  Both run at the rate of a copy (8192 -> 32768,
+// 537 MB: 117 us at 4.6 TB/s, then 163 us at 4.9 read and written).  Taking the columns in strips small enough for the second pass to find
+// them in the last-level cache did not pay: 298 us in strips of 128 MB, 307 of 96, 367 of 64, against 287 all at once.
 struct WeightShards {
-  ShardTable w, q;
-  ShardLayout w_lay;        // bf16 [I x O]
+  ShardTable w, q;          // bf16 [I x O], 8 bits [O x I]: flat, cut after every L elements
   int64_t L;
-  int32_t I, O, q_rows;     // q_rows: output channels to a shard, 0: a flat cut
+  int32_t I, O;
 };
 
 constexpr int kColumns = 256;  // of a workgroup of the first pass: 8 to a lane, 32 lanes side by side, 8 rows at a time
 constexpr int kStrip = 128;    // rows and columns of a tile of the second pass
 
-__device__ __forceinline__ const uint16_t *weight_at(const WeightShards &p, const uint16_t *const *tab, int r, int c) {
-  if (p.w_lay.rows_per_shard > 0) {
-    const int s = static_cast<int>(static_cast<uint32_t>(r) / static_cast<uint32_t>(p.w_lay.rows_per_shard));
-    return tab[s] + static_cast<int64_t>(r - s * p.w_lay.rows_per_shard) * p.O + c;
+// A place in a flat matrix that is cut into shards.  One division finds a workgroup's first place; from there on places move
+// ahead and shards are counted as they end.
+struct Place {
+  int32_t shard;
+  int64_t off;
+  __device__ __forceinline__ Place(int64_t flat, int64_t L) : shard(static_cast<int32_t>(flat / L)), off(flat - shard * L) {}
+  __device__ __forceinline__ void ahead(int64_t by, int64_t L) {
+    off += by;
+    while (off >= L) {
+      off -= L;
+      ++shard;
+    }
   }
-  const uint64_t f = static_cast<uint64_t>(r) * p.O + c, s = f / static_cast<uint64_t>(p.L);
-  return tab[s] + (f - s * p.L);
-}
+};
 
 __global__ __launch_bounds__(kThreads) void column_amax_kernel(WeightShards p, int32_t rows_each, uint32_t *__restrict__ part) {
   __shared__ const uint16_t *tab[OSDP_MAX_SHARDS];
@@ -97,14 +117,24 @@ __global__ __launch_bounds__(kThreads) void column_amax_kernel(WeightShards p, i
   const int r0 = blockIdx.y * rows_each, r1 = min(r0 + rows_each, p.I);
   uint32_t m[8] = {};
   if (c < p.O) {
-#pragma unroll 4
-    for (int r = r0 + line; r < r1; r += 8) {
-      const uint4 v = load_global16(weight_at(p, tab, r, c));
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    Place at(static_cast<int64_t>(r0) * p.O, p.L);
+    at.ahead(static_cast<int64_t>(line) * p.O + c, p.L);
+    // (rows beyond the last repeat it, so that the loads of four steps go out together)
+    for (int r = r0 + line; r < r1; r += 32) {
+      uint4 v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[2 * j] = max(m[2 * j], w[j] << 16 & 0x7fff0000u);
-        m[2 * j + 1] = max(m[2 * j + 1], w[j] & 0x7fff0000u);
+      for (int u = 0; u < 4; ++u) {
+        v[u] = load_global16(tab[at.shard] + at.off);
+        if (r + 8 * (u + 1) < r1) at.ahead(static_cast<int64_t>(8) * p.O, p.L);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          m[2 * j] = max(m[2 * j], w[j] << 16 & 0x7fff0000u);
+          m[2 * j + 1] = max(m[2 * j + 1], w[j] & 0x7fff0000u);
+        }
       }
     }
   }
@@ -122,60 +152,71 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
                                                                    float *__restrict__ scale) {
   __shared__ const uint16_t *tab[OSDP_MAX_SHARDS];
   __shared__ uint8_t *q_tab[OSDP_MAX_SHARDS];
-  __shared__ uint32_t most[kStrip];
+  __shared__ uint32_t most[2][kStrip];
+  __shared__ float ratio[kStrip], up[kStrip];
   __shared__ uint32_t tile[kStrip][kStrip / 4 + 1];  // [o][i / 4]
   if (threadIdx.x < OSDP_MAX_SHARDS) {
     tab[threadIdx.x] = static_cast<const uint16_t *>(p.w.p[threadIdx.x]);
     q_tab[threadIdx.x] = static_cast<uint8_t *>(p.q.p[threadIdx.x]);
   }
+  __syncthreads();
   const int o0 = blockIdx.x * kStrip, i0 = blockIdx.y * kStrip;
-  if (threadIdx.x < kStrip) {
+  const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;  // 8 columns, 4 rows to a lane, twice
+  uint4 v[2][4];  // (on their way while the columns' largest are looked up; beyond the edges anything, it is not stored)
+  {
+    const Place first(static_cast<int64_t>(i0) * p.O + o0, p.L);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        Place at = first;
+        at.ahead(static_cast<int64_t>(min(half * 64 + rg * 4 + j, p.I - 1 - i0)) * p.O + min(cg * 8, p.O - 8 - o0), p.L);
+        v[half][j] = load_global16(tab[at.shard] + at.off);
+      }
+  }
+  {
+    const int o = o0 + (threadIdx.x & (kStrip - 1)), first = threadIdx.x / kStrip;
     uint32_t m = 0;
-    const int o = o0 + threadIdx.x;
     if (o < p.O) {
-      for (int y = 0; y < parts; ++y) m = max(m, part[static_cast<int64_t>(y) * p.O + o]);
-      if (blockIdx.y == 0) scale[o] = I8Scale(m).scale;
+#pragma unroll 4
+      for (int y = first; y < parts; y += 2) m = max(m, part[static_cast<int64_t>(y) * p.O + o]);
     }
-    most[threadIdx.x] = m;
+    most[first][threadIdx.x & (kStrip - 1)] = m;
   }
   __syncthreads();
-  const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;  // 8 columns, 4 rows to a lane
-  const int c = o0 + cg * 8;
+  if (threadIdx.x < kStrip) {
+    const I8Scale s(max(most[0][threadIdx.x], most[1][threadIdx.x]));
+    ratio[threadIdx.x] = s.r;
+    up[threadIdx.x] = s.up;
+    if (blockIdx.y == 0 && o0 + static_cast<int>(threadIdx.x) < p.O) scale[o0 + threadIdx.x] = s.scale;
+  }
+  __syncthreads();
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int r = i0 + half * 64 + rg * 4;
-    uint4 v[4];
+  for (int j = 0; j < 8; ++j) {
+    const I8Scale s(ratio[cg * 8 + j], up[cg * 8 + j]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      v[j] = c < p.O && r + j < p.I ? load_global16(weight_at(p, tab, r + j, c)) : uint4{0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const I8Scale s(most[cg * 8 + j]);
-      uint32_t word = 0;
+    for (int half = 0; half < 2; ++half) {
+      uint32_t q[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t pair = (&v[e].x)[j >> 1];
-        word |= (s.round(__uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16)) & 255u) << (8 * e);
+        const uint32_t pair = (&v[half][e].x)[j >> 1];
+        q[e] = s.round(__uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16));
       }
+      const uint32_t word = i8_pack(q[0], q[1], q[2], q[3]);
       tile[cg * 8 + j][half * 16 + rg] = word;
     }
   }
   __syncthreads();
   const int piece = threadIdx.x & 7;
+  const Place out(static_cast<int64_t>(o0) * p.I + i0, p.L);
 #pragma unroll
   for (int pass = 0; pass < 4; ++pass) {
     const int row = pass * 32 + (threadIdx.x >> 3), o = o0 + row, i = i0 + piece * 16;
     if (o < p.O && i < p.I) {
       const uint4 v = {tile[row][piece * 4], tile[row][piece * 4 + 1], tile[row][piece * 4 + 2], tile[row][piece * 4 + 3]};
-      uint8_t *dst;
-      if (p.q_rows > 0) {
-        const int s = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.q_rows));
-        dst = q_tab[s] + static_cast<int64_t>(o - s * p.q_rows) * p.I + i;
-      } else {
-        const uint64_t f = static_cast<uint64_t>(o) * p.I + i, s = f / static_cast<uint64_t>(p.L);
-        dst = q_tab[s] + (f - s * p.L);
-      }
-      store_global16(dst, v);
+      Place at = out;
+      at.ahead(static_cast<int64_t>(row) * p.I + piece * 16, p.L);
+      store_global16(q_tab[at.shard] + at.off, v);
     }
   }
 }
@@ -260,10 +301,10 @@ osdp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   return OSDP_OK;
 }
 
-// Ranges of rows that the first pass over a weight is cut into: enough workgroups for the card, at least 64 rows each.
+// Ranges of rows that the first pass is cut into: enough workgroups for the card, at least 32 rows each.
 int32_t amax_rows(const Weight &w) {
   const int64_t strips = (w.O + kColumns - 1) / kColumns;
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((w.I + 63) / 64, 2048 / std::max<int64_t>(1, std::min<int64_t>(strips, 2048))));
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((w.I + 31) / 32, 1024 / std::min<int64_t>(strips, 1024)));
   return static_cast<int32_t>(((w.I + parts - 1) / parts + 7) / 8 * 8);
 }
 int32_t amax_parts(const Weight &w) {
@@ -404,10 +445,8 @@ osdp_status osdp_split_linear_i8_quantize(const osdp_shape *shape, const void *c
   const int64_t tiles_i = (w.I + kStrip - 1) / kStrip, tiles_o = (w.O + kStrip - 1) / kStrip;
   if (tiles_o >= (1ll << 24)) return fail(OSDP_ERR_UNSUPPORTED, "O = %lld is too large", (long long)w.O);
   if ((st = device_ok()) != OSDP_OK) return st;
-  p.w_lay.O = w.O; p.w_lay.L = w.L; p.w_lay.N = w.N;
-  p.w_lay.rows_per_shard = w.I % w.N == 0 ? static_cast<int32_t>(w.I / w.N) : 0;
   p.L = w.L;
-  p.I = static_cast<int32_t>(w.I); p.O = static_cast<int32_t>(w.O); p.q_rows = static_cast<int32_t>(w.rows_each);
+  p.I = static_cast<int32_t>(w.I); p.O = static_cast<int32_t>(w.O);
   const hipStream_t q = static_cast<hipStream_t>(stream);
   uint32_t *part = static_cast<uint32_t *>(workspace);
   hipLaunchKernelGGL(column_amax_kernel, dim3(static_cast<unsigned>((w.O + kColumns - 1) / kColumns), static_cast<unsigned>(parts)),
@@ -464,9 +503,7 @@ osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int
     p.sums = p.arrived + kI8MostTiles;
   }
   char *slot = ws + token_bytes(w);
-  hipLaunchKernelGGL(quantize_tokens_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(w.T, 1 << 20))), dim3(kThreads), 0, q, x, ldx, p.I,
-                     p.ldq, p.T, xq, x_scale, p.arrived);
-  if ((st = hip_status(hipGetLastError(), "launching the tokens' quantization")) != OSDP_OK) return st;
+  if ((st = hip_status(launch_quantize_tokens(x, ldx, p, xq, x_scale, q), "launching the tokens' quantization")) != OSDP_OK) return st;
   if (in_place(w)) {
     return hip_status(launch_product(p, q), "launching the product");
   }
