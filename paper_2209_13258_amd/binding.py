@@ -492,7 +492,7 @@ def osdp_adamw_grad_sumsq_workspace_bytes(table: AdamWTable) -> int:
 
 def osdp_adamw_grad_sumsq(table: AdamWTable, sumsq, workspace, *, accumulate: bool = False, stream=None) -> None:
     """``sumsq`` (one float64 on the GPU) = sum of the squares of all of the table's gradients; accumulate: is added to it."""
-    if str(sumsq.dtype) != "torch.float64" or sumsq.numel() != 1:
+    if sumsq.nbytes != 8 or sumsq.numel() != 1 or not sumsq.is_floating_point():
         _refuse("sumsq must be one float64")
     _check(lib.osdp_adamw_grad_sumsq(table.tensors, table.count, table.grad_type, int(bool(accumulate)), sumsq.data_ptr(),
                                      workspace.data_ptr(), _bytes(workspace), _stream(stream)))
@@ -502,10 +502,12 @@ def osdp_adamw_step(table: AdamWTable, *, lr: float, beta1: float = 0.9, beta2: 
                     grad_sumsq=None, max_norm: float = 0.0, seed: int = 0, step_device=None, lr_device=None, stream=None) -> None:
     """One AdamW step, in place.  ``grad_sumsq`` (one float64), ``step_device`` (one int64) and ``lr_device`` (one float32)
     are read on the GPU when the kernels run."""
-    for name, t, want in (("grad_sumsq", grad_sumsq, "torch.float64"), ("step_device", step_device, "torch.int64"),
-                          ("lr_device", lr_device, "torch.float32")):
-        if t is not None and (str(t.dtype) != want or t.numel() != 1):
-            _refuse(f"{name} must be one {want}")
+    if grad_sumsq is not None and (grad_sumsq.nbytes != 8 or grad_sumsq.numel() != 1 or not grad_sumsq.is_floating_point()):
+        _refuse("grad_sumsq must be one float64")
+    if step_device is not None and (step_device.nbytes != 8 or step_device.numel() != 1 or step_device.is_floating_point()):
+        _refuse("step_device must be one int64")
+    if lr_device is not None and (lr_device.nbytes != 4 or lr_device.numel() != 1 or not lr_device.is_floating_point()):
+        _refuse("lr_device must be one float32")
     o = osdp_adamw_options(lr, beta1, beta2, eps, int(step), int(seed) & 0xFFFFFFFFFFFFFFFF, max_norm,
                            None if grad_sumsq is None else grad_sumsq.data_ptr(),
                            None if step_device is None else step_device.data_ptr(),
@@ -535,11 +537,11 @@ def osdp_split_linear_i8_quantize_workspace_bytes(I, O, N) -> int:
 
 def osdp_split_linear_i8_quantize(I, O, w_shards, q_shards, w_scale, workspace, *, stream=None) -> None:
     """bf16 shards of W[I x O] -> int8 shards of Wq[O x I] and the channels' scales (fp32 [O])."""
-    shape = _shape(0, I, O, len(w_shards), 0)
-    L = -(-int(I) * int(O) // max(len(w_shards), 1))
-    if len(q_shards) != len(w_shards) or any(q.numel() < L for q in q_shards) or any(w.numel() < L for w in w_shards):
-        _refuse(f"w_shards and q_shards must be as many shards of {L} elements")
-    if w_scale.numel() < O or str(w_scale.dtype) != "torch.float32":
+    N = len(w_shards)
+    shape = osdp_shape(0, I, O, N, 0)
+    if len(q_shards) != N:
+        _refuse(f"{len(q_shards)} q_shards for {N} w_shards")
+    if w_scale.nbytes < 4 * O:
         _refuse(f"w_scale must hold {O} float32")
     _check(lib.osdp_split_linear_i8_quantize(ctypes.byref(shape), _ptrs(w_shards), _ptrs(q_shards), w_scale.data_ptr(),
                                              workspace.data_ptr(), _bytes(workspace), _stream(stream)))
@@ -556,7 +558,7 @@ def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=No
     """Y[T x O] = X[T x I] . W with W as int8 shards of Wq[O x I]; X, Y 2-D bf16 tensors (row stride = ld)."""
     T, I = X.shape
     O = Y.shape[1]
-    if w_scale.numel() < O or w_scale.element_size() != 4:
+    if w_scale.nbytes < 4 * O:
         _refuse(f"w_scale must hold {O} float32")
     shape = osdp_shape(T, I, O, len(q_shards), k)
     _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), X.stride(0), _ptrs(q_shards), w_scale.data_ptr(),

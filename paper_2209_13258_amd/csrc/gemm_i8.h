@@ -1,5 +1,7 @@
 // Products of 8-bit integers: Y[T x O] = bf16( (Xq . Wq^T) * s_t * s_o ), Xq [T x I] and Wq [O x I], both with the reduction contiguous.
 #pragma once
+#include <algorithm>
+
 #include "osdp_internal.h"
 
 namespace osdp {
@@ -178,8 +180,8 @@ __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
   }
 }
 
-// The same with the tokens' rounding in the launch, for at most 16 tokens of so few features that their bytes fit in LDS and
-// that every workgroup may well round all of them for itself: one launch instead of two, the first weights on their way meanwhile.
+// The same with the tokens' rounding in the launch, for tokens of so few features that the bytes of 16 of them fit in LDS and
+// that every workgroup may well round its 16 for itself: one launch instead of two, the first weights on their way meanwhile.
 template <int NB, int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, const uint16_t *__restrict__ x, int64_t ldx) {
   constexpr int BN = 16 * NB, kStep = 64 * kUnroll;
@@ -189,7 +191,8 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
   __shared__ uint32_t most[16][kWaves];
   __shared__ float scale[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
-  const int n0 = blockIdx.x * BN, pitch = p.ldq + 16;
+  const int n0 = blockIdx.x * BN, m0 = blockIdx.y * 16, pitch = p.ldq + 16, tokens = min(p.T - m0, 16);
+  x += static_cast<int64_t>(m0) * ldx;
   if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
   for (int i = tid; i < 16 * BN; i += kWaves * 64) sums[i] = 0;
   __syncthreads();
@@ -233,8 +236,8 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
   uint4 w[kUnroll][NB];
   load(wave * kStep, w);
   // tokens to 8 bits: a row to a wave, or (fewer tokens than waves) to as many waves as there are for it
-  const int share = p.T >= kWaves ? 1 : kWaves / p.T, part = wave % share;
-  for (int t = wave / share; t < p.T; t += kWaves / share) {
+  const int share = tokens >= kWaves ? 1 : kWaves / tokens, part = wave % share;
+  for (int t = wave / share; t < tokens; t += kWaves / share) {
     uint32_t m = 0;
     for (int i = (part * 64 + lane) * 8; i < p.I; i += share * 512) m = max(m, i8_largest(load_global16(x + t * ldx + i)));
 #pragma unroll
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
     if (lane == 0) most[t][part] = m;
   }
   __syncthreads();
-  for (int t = wave / share; t < p.T; t += kWaves / share) {
+  for (int t = wave / share; t < tokens; t += kWaves / share) {
     uint32_t m = 0;
     for (int i = 0; i < share; ++i) m = max(m, most[t][i]);
     const I8Scale s(m);
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
       *reinterpret_cast<uint2 *>(rows + t * pitch + i) = i < p.I ? s.round8(load_global16(x + t * ldx + i)) : uint2{0u, 0u};
   }
   __syncthreads();
-  const uint8_t *token = rows + min(l16, p.T - 1) * pitch + 16 * q4;
+  const uint8_t *token = rows + min(l16, tokens - 1) * pitch + 16 * q4;
   i32x4 acc[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = i32x4{0, 0, 0, 0};
@@ -277,14 +280,14 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
   __syncthreads();
   for (int i = tid; i < 2 * BN; i += kWaves * 64) {
     const int m = i / (BN / 8), c = i % (BN / 8) * 8, n = n0 + c;
-    if (m < p.T && n < p.O) i8_store8(p.y + static_cast<int64_t>(m) * p.ldy + n, &sums[m * BN + c], scale[m], p.w_scale + n);
+    if (m < tokens && n < p.O) i8_store8(p.y + static_cast<int64_t>(m0 + m) * p.ldy + n, &sums[m * BN + c], scale[m], p.w_scale + n);
   }
 }
 
 template <int NB, int kWaves, int kUnroll>
 hipError_t launch_fused(const I8Problem &p, const uint16_t *x, int64_t ldx, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>((p.O + 16 * NB - 1) / (16 * NB)));
-  const unsigned lds = static_cast<unsigned>(p.T * (p.ldq + 16));
+  const dim3 grid(static_cast<unsigned>((p.O + 16 * NB - 1) / (16 * NB)), static_cast<unsigned>((p.T + 15) / 16));
+  const unsigned lds = static_cast<unsigned>(std::min(p.T, 16) * (p.ldq + 16));
   if (p.rows_each > 0) hipLaunchKernelGGL((i8_fused_kernel<NB, kWaves, kUnroll, false>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
   else hipLaunchKernelGGL((i8_fused_kernel<NB, kWaves, kUnroll, true>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
   return hipGetLastError();

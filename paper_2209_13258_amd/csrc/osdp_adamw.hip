@@ -94,7 +94,7 @@ __device__ __forceinline__ int tensor_of(const Batch &b, uint32_t tile) {
 // take neighbouring elements, so that accesses of single elements still cover whole segments.  Either way a row is a block.
 template <bool kWide>
 __device__ __forceinline__ uint32_t element(int j) {
-  const uint32_t row = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  const uint32_t row = (threadIdx.x & (kThreads - 1)) >> 4, lane = threadIdx.x & 15;
   return row * kBlock + (kWide ? lane * kPerLane + j : j * 16u + lane);
 }
 
@@ -453,6 +453,7 @@ constexpr int kSumBlocks = 1024;  // workgroups, and so partial sums, of a launc
 constexpr int kSumTiles = 4;      // tiles that a workgroup has on their way at a time, where there are enough for all: 806 MB in 136 us
                                   // (5.9 TB/s), with one tile at a time in 214
 
+template <int kThreads = osdp::kThreads>
 __device__ __forceinline__ double block_sum(double x) {
   __shared__ double part[kThreads / 64];
 #pragma unroll
@@ -507,6 +508,39 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, 
   }
   sum = block_sum(sum);
   if (threadIdx.x == 0) out[blockIdx.x] = sum;
+}
+
+// All tiles of a small batch by one workgroup of four times the size, which has the sum itself: one launch instead of two.
+constexpr int kSmallThreads = 4 * kThreads;
+template <class Grad>
+__global__ __launch_bounds__(kSmallThreads) void sumsq_small_kernel(Batch b, int32_t accumulate, double *__restrict__ out) {
+  double sum = 0.0;
+  for (uint32_t first = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads); first < b.tiles; first += 4 * kSumTiles) {
+    float g[kSumTiles][8];
+#pragma unroll
+    for (int u = 0; u < kSumTiles; ++u) {
+      const uint32_t tile = min(first + 4 * u, b.tiles - 1);
+      const int i = tensor_of(b, tile);
+      const int64_t from = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile, rest = b.t[i].n - from;
+      if (((b.wide >> i) & 1u) && rest >= kTile) {
+        Eight<Grad, true> x;
+        x.load(b.t[i].grad, from, kTile);
+        x.get(g[u]);
+      } else {
+        Eight<Grad, false> x;
+        x.load(b.t[i].grad, from, rest < kTile ? static_cast<uint32_t>(rest) : kTile);
+        x.get(g[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kSumTiles; ++u)
+      if (first + 4 * u < b.tiles) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fma(static_cast<double>(g[u][j]), static_cast<double>(g[u][j]), sum);
+      }
+  }
+  sum = block_sum<kSmallThreads>(sum);
+  if (threadIdx.x == 0) *out = accumulate ? *out + sum : sum;
 }
 
 __global__ __launch_bounds__(kThreads) void sumsq_finish_kernel(const double *__restrict__ part, int32_t count, int32_t accumulate,
@@ -614,13 +648,21 @@ hipError_t launch_adamw(int form, bool state8, const Batch &b, const Step &s, hi
 }
 
 // Workgroups, and so partial sums, of the launch over a batch.
+// A call of so few tiles, in one batch, is the small kernel's: at 16 tiles a round, of two microseconds, it is the faster one up to two rounds.
+constexpr uint32_t kSmallTiles = 32;
 uint32_t sum_run(const Batch &b) { return b.tiles >= kSumTiles * kSumBlocks ? kSumTiles : 1; }
 unsigned sum_blocks(const Batch &b) { return std::min<unsigned>(b.tiles, kSumBlocks); }
 
-osdp_status sumsq_parts(const osdp_adamw_tensor *tensors, int32_t count, int64_t *parts) {
+// Partial sums of a call, and whether it is a small one.
+osdp_status sumsq_parts(const osdp_adamw_tensor *tensors, int32_t count, int64_t *parts, bool *small) {
   *parts = 0;
-  return for_batches(tensors, count, [](int32_t, Tensor *) { return false; },
-                     [&](const Batch &b) { *parts += sum_blocks(b); return OSDP_OK; });
+  *small = false;
+  int batches = 0;
+  return for_batches(tensors, count, [](int32_t, Tensor *) { return false; }, [&](const Batch &b) {
+    *parts += sum_blocks(b);
+    *small = ++batches == 1 && b.tiles <= kSmallTiles;
+    return OSDP_OK;
+  });
 }
 
 }  // namespace
@@ -696,7 +738,8 @@ osdp_status osdp_adamw_grad_sumsq_workspace_bytes(const osdp_adamw_tensor *tenso
   if (st != OSDP_OK) return st;
   if (!bytes) return fail(OSDP_ERR_INVALID_ARG, "bytes is NULL");
   int64_t parts = 0;
-  if ((st = sumsq_parts(tensors, count, &parts)) != OSDP_OK) return st;
+  bool small = false;
+  if ((st = sumsq_parts(tensors, count, &parts, &small)) != OSDP_OK) return st;
   *bytes = static_cast<size_t>(parts) * sizeof(double);
   return OSDP_OK;
 }
@@ -711,7 +754,8 @@ osdp_status osdp_adamw_grad_sumsq(const osdp_adamw_tensor *tensors, int32_t coun
   for (int32_t i = 0; i < count; ++i)
     if (tensors[i].n > 0 && (st = check_array(tensors[i].grad, size_of(grad_type), i, "grad")) != OSDP_OK) return st;
   int64_t parts = 0;
-  if ((st = sumsq_parts(tensors, count, &parts)) != OSDP_OK) return st;
+  bool small = false;
+  if ((st = sumsq_parts(tensors, count, &parts, &small)) != OSDP_OK) return st;
   if (parts > 0 && !workspace) return fail(OSDP_ERR_INVALID_ARG, "workspace is NULL");
   if (!aligned(workspace, 8)) return fail(OSDP_ERR_UNSUPPORTED, "workspace is not 8-byte aligned");
   if (workspace_bytes < static_cast<size_t>(parts) * sizeof(double))
@@ -727,12 +771,17 @@ osdp_status osdp_adamw_grad_sumsq(const osdp_adamw_tensor *tensors, int32_t coun
       },
       [&](const Batch &b) {
         const unsigned blocks = sum_blocks(b);
+        if (small) {
+          if (grad_type == OSDP_BF16) hipLaunchKernelGGL(sumsq_small_kernel<uint16_t>, dim3(1), dim3(kSmallThreads), 0, q, b, accumulate, sumsq);
+          else hipLaunchKernelGGL(sumsq_small_kernel<float>, dim3(1), dim3(kSmallThreads), 0, q, b, accumulate, sumsq);
+          return hip_status(hipGetLastError(), "launching the sum of squares");
+        }
         if (grad_type == OSDP_BF16) hipLaunchKernelGGL(sumsq_kernel<uint16_t>, dim3(blocks), dim3(kThreads), 0, q, b, sum_run(b), part);
         else hipLaunchKernelGGL(sumsq_kernel<float>, dim3(blocks), dim3(kThreads), 0, q, b, sum_run(b), part);
         part += blocks;
         return hip_status(hipGetLastError(), "launching the sum of squares");
       });
-  if (st != OSDP_OK) return st;
+  if (st != OSDP_OK || small) return st;
   hipLaunchKernelGGL(sumsq_finish_kernel, dim3(1), dim3(kThreads), 0, q, static_cast<const double *>(workspace),
                      static_cast<int32_t>(parts), accumulate, sumsq);
   return hip_status(hipGetLastError(), "launching the end of the sum of squares");

@@ -382,12 +382,15 @@ hipError_t launch_product(const I8Problem &p, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 
-// Whether tokens are rounded inside the product's launch: every 16 channels do it again, which 2^14 values are quick enough
-// for, and in all 2^27 / 16 of them (one token: any number; it is read by every workgroup anyway).  us in one launch / two: 1 token 512 -> 512
-// 4.1 / 5.5, 4096 -> 16384 14.9 / 16.8; 8 of 2048 -> 512 6.5 / 6.9; beyond the line, 3 of 4096 -> 16384 18.2 / 15.6.
+// Whether tokens are rounded inside the product's launch: every workgroup, of 16 tokens and 16 channels, does it again, which
+// 2^14 values are quick enough for as long as there are not too many workgroups.  (One token is always: it is read by all of them anyway.)  us in
+// two launches / one, one call behind another: 1 token 512 -> 512 9.0 / 6.3, 4096 -> 16384 16.8 / 14.9; 64 tokens 512 -> 1024 9.1 / 6.2; at the line
+// 512 of 512 -> 512 9.2 / 8.6 and 128 of 1024 -> 1024 9.2 / 7.7; beyond it 256 of 256 -> 2048 9.3 / 14.5, 3 of 4096 -> 16384 15.6 / 18.2.
 bool rounds_inside(const Weight &w) {
-  const int64_t values = w.T * w.I;
-  return w.T <= 16 && values <= (1 << 14) && (w.T == 1 || values * w.O <= (1ll << 27));
+  const int64_t values = std::min<int64_t>(w.T, 16) * w.I;
+  if (values > (1 << 14)) return false;
+  if (w.T == 1) return true;
+  return (w.T + 15) / 16 * ((w.O + 15) / 16) * std::max<int64_t>(values, 1 << 13) <= (1 << 23);
 }
 
 // Whether the product reads the shards where they lie.

@@ -111,7 +111,7 @@ def test_product_over_weight_shapes_and_cuts(T, I, O, N, k):
 
 
 # one that each of the kernels is chosen for, with the parts that its tiles' reductions are cut into
-CHOICES = [((5, 512, 512, 8), "i8_fused_kernel", 1), ((30, 400, 3456, 8), "i8_few_kernel", 1), ((300, 1152, 2048, 8), "i8_w4_kernelILi2ELi2ELi4", 1),
+CHOICES = [((5, 512, 512, 8), "i8_fused_kernel", 1), ((512, 512, 512, 8), "i8_fused_kernel", 1), ((30, 2048, 1024, 8), "i8_few_kernel", 1), ((300, 1152, 2048, 8), "i8_w4_kernelILi2ELi2ELi4", 1),
            ((161, 14448, 960, 8), "i8_w4_kernelILi2ELi2ELi4", 4), ((1000, 4096, 4096, 4), "i8_w4_kernelILi4ELi4ELi4", 1),
            ((300, 16384, 2048, 4), "i8_w4_kernelILi4ELi4ELi4", 4), ((500, 2560, 10240, 8), "i8_w4_kernelILi4ELi4ELi2", 1),
            ((1500, 1024, 16424, 8), "i8_w4_kernelILi8ELi8ELi2", 1)]
@@ -236,7 +236,8 @@ def quantize(W, I, O, N):
 
 
 @pytest.mark.parametrize("I,O,N", [(16, 8, 1), (16, 16, 16), (32, 24, 3), (64, 40, 8), (128, 128, 2), (144, 136, 4), (256, 1024, 2), (272, 264, 11),
-                                   (1040, 520, 5), (2560, 1280, 8), (4096, 8, 64), (16, 4096, 64), (336, 1000, 3), (131072, 16, 8), (1024, 4096, 8)])
+                                   (1040, 520, 5), (2560, 1280, 8), (4096, 8, 64), (16, 4096, 64), (336, 1000, 3), (131072, 16, 8), (1024, 4096, 8), (1008, 1032, 7),
+                                   (1040, 72, 2), (2048, 136, 4), (16, 8, 8), (512, 8, 64)])
 def test_weight_to_8_bits(I, O, N):
     print("int8 quantize", I, O, N, flush=True)
     g = np.random.default_rng([I, O])
