@@ -62,6 +62,11 @@ def parse():
                          "far larger than every cache): the known traffic that HBM counters of a profiled run are scaled by")
     ap.add_argument("--no-cpu", action="store_true", help="skip the CPU oracle baseline")
     ap.add_argument("--serial", action="store_true", help="one stream: no gather/GEMM overlap")
+    ap.add_argument("--adamw", choices=["32", "8"], default=None,
+                    help="also time the whole training step: after the backward pass the gradients' norm and an AdamW step on "
+                         "all shards, with fp32 master copies and moments in 32 or 8 bits")
+    ap.add_argument("--int8", action="store_true",
+                    help="also time the workload's forward pass with its weights in 8-bit integers, and making them from the shards")
     return ap.parse_args()
 
 
@@ -153,6 +158,85 @@ class Stack:
             if profile:
                 stats["_overlap"] = osdp.osdp_profile_overlap()
         return (t1 - t0) * 1e3 / steps, stats
+
+
+def median_ms(torch, call, iters, warmup):
+    """Median of `call` on the default stream, by events."""
+    for _ in range(warmup):
+        call()
+    ev = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in range(iters)]
+    for e0, e1 in ev:
+        e0.record()
+        call()
+        e1.record()
+    torch.cuda.synchronize()
+    return sorted(e0.elapsed_time(e1) for e0, e1 in ev)[iters // 2]
+
+
+def training_step(st, bits, iters, warmup):
+    """Forward, backward, norm of the gradients and AdamW on the shards, as one step and its last two parts alone."""
+    torch, osdp = st.torch, st.osdp
+    W, dW = [w for d in st.ops for w in d["W"]], [g for d in st.ops for g in d["dW"]]
+    masters = [w.float() for w in W]
+    kind = torch.float32 if bits == 32 else torch.uint8
+    m, v = ([torch.zeros(w.numel(), dtype=kind, device="cuda") for w in W] for _ in range(2))
+    exps = None if bits == 32 else [torch.zeros(2 * -(-w.numel() // osdp.OSDP_ADAMW_BLOCK), dtype=torch.uint8, device="cuda") for w in W]
+    table = osdp.AdamWTable(params=W, grads=dW, masters=masters, m=m, v=v, exps=exps, weight_decay=0.1)
+    sumsq = torch.zeros(1, dtype=torch.float64, device="cuda")
+    ws = torch.empty(max(256, osdp.osdp_adamw_grad_sumsq_workspace_bytes(table)), dtype=torch.uint8, device="cuda")
+    step = [0]
+
+    def update(stream=None):
+        step[0] += 1
+        osdp.osdp_adamw_grad_sumsq(table, sumsq, ws, stream=stream)
+        osdp.osdp_adamw_step(table, lr=1e-6, step=step[0], grad_sumsq=sumsq, max_norm=1.0, seed=1, stream=stream)
+
+    def whole():
+        st.step()
+        update(st.sc)
+    times = []
+    with torch.cuda.stream(st.sc):
+        for i in range(warmup + iters):
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            e0.record(st.sc)
+            whole()
+            e1.record(st.sc)
+            times.append((e0, e1))
+        torch.cuda.synchronize()
+    n = sum(w.numel() for w in W)
+    ms = sorted(e0.elapsed_time(e1) for e0, e1 in times[warmup:])[iters // 2]
+    alone = median_ms(torch, update, iters, warmup)
+    moved = n * (2 + 2 + 8 + 2 + (16 if bits == 32 else 4 + 4 / osdp.OSDP_ADAMW_BLOCK))  # the norm reads the gradients once more
+    return {"state_bits": bits, "parameters": n, "median_ms_per_step": round(ms, 4), "norm_and_adamw_ms": round(alone, 4),
+            "norm_and_adamw_gbs": round(moved / (alone * 1e-3) / 1e9, 1), "frac_hbm_peak": round(moved / (alone * 1e-3) / 1e9 / PEAK_HBM_GBS, 4)}
+
+
+def int8_forward(st, iters, warmup):
+    """Every operator's forward pass with its weight in 8-bit integers, and the same in bf16."""
+    torch, osdp, w = st.torch, st.osdp, st.w
+    need = max(max(osdp.osdp_split_linear_i8_workspace_bytes(w.T, op.I, op.O, w.N, op.k)[0],
+                   osdp.osdp_split_linear_i8_quantize_workspace_bytes(op.I, op.O, w.N)) for op in w.ops)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for d in st.ops:
+        d["Q"] = [torch.zeros(s.numel(), dtype=torch.int8, device="cuda") for s in d["W"]]
+        d["scale"] = torch.zeros(d["op"].O, device="cuda")
+
+    def make():
+        for d in st.ops:
+            osdp.osdp_split_linear_i8_quantize(d["op"].I, d["op"].O, d["W"], d["Q"], d["scale"], ws)
+
+    def forward():
+        for d in st.ops:
+            osdp.osdp_split_linear_i8_fwd(d["X"], d["Q"], d["scale"], d["Y"], max(d["op"].k, 1), ws)
+
+    def bf16():
+        for d in st.ops:
+            osdp.osdp_split_linear_fwd(d["X"], d["W"], d["Y"], 0, st.ws, plan=st.plan, op_index=d["n"])
+    make()
+    ops = w.layers * sum(2 * w.T * op.I * op.O for op in w.ops)
+    t8, t16, tq = median_ms(torch, forward, iters, warmup), median_ms(torch, bf16, iters, warmup), median_ms(torch, make, iters, warmup)
+    return {"median_ms": round(t8, 4), "tops": round(ops / (t8 * 1e-3) / 1e12, 2), "bf16_median_ms": round(t16, 4),
+            "bf16_tflops": round(ops / (t16 * 1e-3) / 1e12, 2), "quantize_ms": round(tq, 4)}
 
 
 def per_step_times(st, iters, warmup, serial):
@@ -608,6 +692,10 @@ def main():
             torch.cuda.empty_cache()
         out["zdp_slices_of_k"] = zmodes
         out["plan_search"] = plan_search(w, m["kernels"], staging, rows, torch, osdp, sub_steps, sub_warm)
+    if a.int8:
+        out["int8_forward"] = int8_forward(st, sub_steps, sub_warm)
+    if a.adamw:
+        out["training_step"] = training_step(st, int(a.adamw), sub_steps, sub_warm)
     if not a.no_auto:
         out["auto_granularity"] = auto_granularity(st, osdp, torch, sub_steps, sub_warm)
     if not a.no_sweep and default_plan:
