@@ -518,17 +518,20 @@ OSDP_API osdp_status osdp_split_linear_i8_quantize(const osdp_shape *shape, cons
                                                    float *w_scale, void *workspace, size_t workspace_bytes, void *stream);
 OSDP_API osdp_status osdp_split_linear_i8_quantize_workspace_bytes(const osdp_shape *shape, size_t *bytes);
 
-/* The forward pass.  Shards that are blocks of whole channels (N divides O) are read where they lie, and so are all shards
- * for few tokens (at most 64); otherwise the k slices of output channels, c0_j = floor(j*O/k), are gathered one after
- * another into one staging slot of a slice (size/k at one byte an element).
+/* The forward pass.  Up to 64 tokens read the weight where it lies, however it is cut; more tokens do where every shard is a
+ * block of whole channels (N divides O), at least 32 of them.  Otherwise, and from 257 tokens on where the library estimates
+ * it faster, the k slices of output channels, c0_j = floor(j*O/k), are gathered one after another into one staging slot of a
+ * slice (size/k at one byte an element).
  *   X : device [T x I] bf16, ldx >= I     Y : device [T x O] bf16, ldy >= O (every element written)
- *   workspace: device, 256-byte aligned, >= osdp_split_linear_i8_workspace_bytes: [Xq and s_t][staging slot]
- * T = 0 does nothing. */
+ *   workspace: device, 256-byte aligned, >= osdp_split_linear_i8_workspace_bytes: [Xq and s_t][sums of tiles whose reduction
+ *              workgroups share][staging slot]; what does for T tokens does for fewer
+ * T = 0 does nothing.  The slice bounds must be multiples of 8. */
 OSDP_API osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int64_t ldx,
                                               const void *const *q_shards, const float *w_scale, void *Y, int64_t ldy,
                                               void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes of workspace, and how many of them hold gathered weights.  Either pointer may be NULL.  Host only. */
+/* Bytes of workspace, and how many of them are for gathered weights (0: no slice is staged).  Either pointer may be NULL.
+ * Host only. */
 OSDP_API osdp_status osdp_split_linear_i8_workspace_bytes(const osdp_shape *shape, size_t *total, size_t *peak_weight_staging);
 
 /* ---- test and debug switches ------------------------------------------------

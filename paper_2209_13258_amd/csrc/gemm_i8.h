@@ -73,9 +73,9 @@ struct I8Problem {
 constexpr int64_t kI8MostTiles = 256;
 constexpr size_t kI8SumBytes = 16 << 20;
 
-// Up to this many tokens the product reads the weight where it lies, however it is cut; from there on if every shard is
-// a block of at least kI8ShardRows channels (tiles end with a shard).
-constexpr int64_t kI8FewTokens = 64, kI8ShardRows = 32;
+// Up to kI8FewTokens the product reads the weight where it lies, however it is cut; from there on if every shard is
+// a block of at least kI8ShardRows channels (tiles end with a shard); beyond kI8ManyTokens only if that is no slower than gathering.
+constexpr int64_t kI8FewTokens = 64, kI8ShardRows = 32, kI8ManyTokens = 256;
 
 // Eight sums as Y: both scales, then the rounding to bf16.
 __device__ __forceinline__ void i8_store8(uint16_t *y, const int *sums, float st, const float *so) {

@@ -81,7 +81,7 @@ hipError_t launch_quantize_tokens(const uint16_t *x, int64_t ldx, const I8Proble
 // ---- weight shards to 8 bits --------------------------------------------------------------------------------------
 // Two passes: the largest magnitude of every column over a range of rows, one range a workgroup (into the workspace); then,
 // over tiles of 128 x 128, their largest, the rounding, and the transposition through LDS.  Both run at the rate of a copy (8192 -> 32768,
-// 537 MB: 117 us at 4.6 TB/s, then 163 us at 4.9 read and written).  Taking the columns in strips small enough for the second pass to find
+// 537 MB: 117 us at 4.6 TB/s, then 142 us at 5.7 read and written).  Taking the columns in strips small enough for the second pass to find
 // them in the last-level cache did not pay: 298 us in strips of 128 MB, 307 of 96, 367 of 64, against 287 all at once.
 struct WeightShards {
   ShardTable w, q;          // bf16 [I x O], 8 bits [O x I]: flat, cut after every L elements
@@ -160,7 +160,10 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
     q_tab[threadIdx.x] = static_cast<uint8_t *>(p.q.p[threadIdx.x]);
   }
   __syncthreads();
-  const int o0 = blockIdx.x * kStrip, i0 = blockIdx.y * kStrip;
+  // (tiles that run together lie on a diagonal: their stores, a row of the result apart, then do not all meet the same memory
+  // channels; 149 -> 142 us)
+  const int ti = (blockIdx.y + blockIdx.x / 4) % gridDim.y;
+  const int o0 = blockIdx.x * kStrip, i0 = ti * kStrip;
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;  // 8 columns, 4 rows to a lane, twice
   uint4 v[2][4];  // (on their way while the columns' largest are looked up; beyond the edges anything, it is not stored)
   {
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
     const I8Scale s(max(most[0][threadIdx.x], most[1][threadIdx.x]));
     ratio[threadIdx.x] = s.r;
     up[threadIdx.x] = s.up;
-    if (blockIdx.y == 0 && o0 + static_cast<int>(threadIdx.x) < p.O) scale[o0 + threadIdx.x] = s.scale;
+    if (ti == 0 && o0 + static_cast<int>(threadIdx.x) < p.O) scale[o0 + threadIdx.x] = s.scale;
   }
   __syncthreads();
 #pragma unroll
@@ -317,6 +320,7 @@ enum class Kernel { kFew, k64, k128, k128Walk, k256Walk };
 struct Choice {
   Kernel kernel;
   int parts;
+  double us;  // estimated
 };
 
 // The kernel, and the parts of a tile's reduction, that are estimated fastest for T tokens and `shards` blocks of `rows`
@@ -342,8 +346,7 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
                                 {Kernel::k128Walk, 128, 512, 5.44, 1.048, 5.73, 0, 0},
                                 {Kernel::k256Walk, 256, 256, 0.95, 1.156, 12.8, 0, 0}};
   const int64_t blocks = (I + 127) / 128;
-  Choice best = {Kernel::k256Walk, 1};
-  double least = -1.0;
+  Choice best = {Kernel::k256Walk, 1, -1.0};
   for (const Prices &v : kPrices) {
     const bool few = v.kernel == Kernel::kFew;
     const int64_t across = few ? (rows * shards + 15) / 16 : shards * i8_shard_tiles(rows, v.side);
@@ -360,10 +363,7 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
       else if (v.room == 512 && groups % 512 != 0 && groups % 512 <= 256) rounds -= 0.4;  // (one workgroup to a CU is faster than two)
       double us = v.fixed + rounds * (static_cast<double>(each) * v.block + v.start);
       if (parts > 1) us += v.each * static_cast<double>(parts) + v.meet * static_cast<double>(groups) / 256.0;
-      if (least < 0.0 || us < least) {
-        least = us;
-        best = {v.kernel, static_cast<int>(parts)};
-      }
+      if (best.us < 0.0 || us < best.us) best = {v.kernel, static_cast<int>(parts), us};
     }
   }
   return best;
@@ -393,8 +393,22 @@ bool rounds_inside(const Weight &w) {
   return (w.T + 15) / 16 * ((w.O + 15) / 16) * std::max<int64_t>(values, 1 << 13) <= (1 << 23);
 }
 
-// Whether the product reads the shards where they lie.
-bool in_place(const Weight &w) { return w.T <= kI8FewTokens || w.rows_each >= kI8ShardRows; }
+// Whether slices have to be gathered, and whether they may be: with many tokens the tiles that end with each shard can cost more than a
+// dense copy of the weight does.
+bool has_to_gather(const Weight &w) { return w.T > kI8FewTokens && w.rows_each < kI8ShardRows; }
+bool may_gather(const Weight &w) { return has_to_gather(w) || (w.T > kI8ManyTokens && w.N > 1 && w.rows_each % 256 != 0); }
+
+// Gathers where that is estimated faster: a gather reads and writes a slice at 5.5 TB/s and takes 6 us besides.  Eight shards of 320 channels,
+// 16384 tokens: 2560 -> 2560 in place 167 us, gathered 144; 10240 -> 2560 565 and 474; of 125 channels, 4000 tokens 4096 -> 1000: 46 and 34.
+bool gathers(const Weight &w) {
+  if (!may_gather(w) || has_to_gather(w)) return has_to_gather(w);
+  double us = 0.0;
+  for (int64_t j = 0; j < w.k; ++j) {
+    const int64_t wide = (j + 1) * w.O / w.k - j * w.O / w.k;
+    us += choose(w.T, w.I, wide, 1, false).us + 2.0 * static_cast<double>(w.I * wide) / 5.5e6 + 6.0;
+  }
+  return us < 0.97 * choose(w.T, w.I, w.rows_each, w.N, false).us;
+}
 
 // The workspace up to the staging slot: [Xq][s_t][counters][sums of tiles whose reduction is shared].  The last two do not depend on
 // T, so that what does for many tokens does for fewer.
@@ -414,7 +428,7 @@ osdp_status check_slices(const osdp_shape *s, Weight *w, int64_t *widest) {
     if (c0 % 8 || c1 % 8) return fail(OSDP_ERR_UNSUPPORTED, "slice %lld = [%lld, %lld) is not aligned to 8 columns", (long long)j, (long long)c0, (long long)c1);
     *widest = std::max(*widest, c1 - c0);
   }
-  if (in_place(*w)) *widest = 0;
+  if (!may_gather(*w)) *widest = 0;
   return OSDP_OK;
 }
 
@@ -507,11 +521,9 @@ osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int
   }
   char *slot = ws + token_bytes(w);
   if ((st = hip_status(launch_quantize_tokens(x, ldx, p, xq, x_scale, q), "launching the tokens' quantization")) != OSDP_OK) return st;
-  if (in_place(w)) {
-    return hip_status(launch_product(p, q), "launching the product");
-  }
+  if (!gathers(w)) return hip_status(launch_product(p, q), "launching the product");
   ShardLayout lay{};  // (two bytes an element, as the gather counts)
-  lay.O = w.I / 2; lay.L = w.L / 2; lay.N = w.N; lay.rows_per_shard = 0;
+  lay.O = w.I / 2; lay.L = w.L / 2; lay.N = w.N; lay.rows_per_shard = static_cast<int32_t>(w.rows_each);
   for (int64_t j = 0; j < w.k; ++j) {
     const int64_t c0 = j * w.O / w.k, c1 = (j + 1) * w.O / w.k;
     if ((st = hip_status(launch_gather(tab, lay, c0, c1 - c0, 0, w.I / 2, slot, q), "gathering a slice")) != OSDP_OK) return st;

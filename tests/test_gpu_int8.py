@@ -140,7 +140,7 @@ def test_every_kernel_gives_the_same_whole_numbers(sizes, kernel, parts):
 
 
 @pytest.mark.parametrize("T,I,O,N", [(1, 32768, 1024, 8), (33, 131072, 128, 2), (1030, 1024, 2048, 8), (700, 8192, 776, 1), (2100, 384, 3080, 8),
-                                     (4096, 256, 5000, 5), (4096, 256, 5000, 16)])
+                                     (4096, 256, 5000, 5), (4096, 256, 5000, 16), (4000, 1024, 1000, 8), (3000, 512, 2560, 8)])
 def test_larger_products(T, I, O, N):
     print("int8 product", T, I, O, N, flush=True)
     w, x = Weight(I, O, N), tokens(T, I)
@@ -148,14 +148,14 @@ def test_larger_products(T, I, O, N):
 
 
 @pytest.mark.parametrize("T", [1, 5, 33, 130, 400])
-def test_strides(T):
+def test_strides(T):  # (in place, and from T = 400 on gathered)
     w, x = Weight(528, 392, 11), tokens(T, 528)
     want = expected(x, w.q, w.scale)
     for pad_x, pad_y in ((8, 0), (0, 8), (1000, 24)):
         same(forward(w, x, pad_x=pad_x, pad_y=pad_y), want)
 
 
-@pytest.mark.parametrize("T", [1, 4, 20, 70, 150, 300])
+@pytest.mark.parametrize("T", [1, 4, 20, 70, 150, 300, 3000])
 def test_slices_and_shards_do_not_change_a_bit(T):
     I, O = 336, 1000
     x = tokens(T, I)
