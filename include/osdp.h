@@ -59,7 +59,8 @@
  *     calls run on stream_compute alone, and work of the caller's on stream_copy
  *     that reuses the workspace has to wait for it.  Inputs must be ready on
  *     stream_compute when the call is made.
- *   - The forward, backward and gather calls can be captured into a HIP graph on
+ *   - The forward, backward and gather calls, and those of AdamW and of the operator in 8-bit
+ *     integers, can be captured into a HIP graph on
  *     stream_compute (after one eager call, which sets kernel attributes): they enqueue
  *     kernels and event records / waits only, and every use of stream_copy starts
  *     from and returns to stream_compute.  Not capturable: the profiling calls
@@ -459,7 +460,8 @@ typedef struct {
   const double *grad_sumsq;     /* device, or NULL: the squared norm of all gradients (over all ranks: add up the ranks'
                                    sums).  Where it is infinite or NaN the call leaves everything as it is */
   const int64_t *step_device;   /* device, or NULL: t, in place of `step`, read when the kernels run: a captured graph
-                                   that is replayed takes the step (and seeds its roundings by it) from here */
+                                   that is replayed takes the step (and seeds its roundings by it) from here.
+                                   What is below 1 counts as 1 */
   const float *lr_device;       /* device, or NULL: lr, in place of `lr`                             */
   int32_t grad_type;            /* an osdp_dtype                                                     */
   int32_t param_type;           /* an osdp_dtype                                                     */

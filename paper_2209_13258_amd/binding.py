@@ -558,6 +558,8 @@ def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=No
     """Y[T x O] = X[T x I] . W with W as int8 shards of Wq[O x I]; X, Y 2-D bf16 tensors (row stride = ld)."""
     T, I = X.shape
     O = Y.shape[1]
+    if X.stride(1) != 1 or Y.stride(1) != 1 or X.itemsize != 2 or Y.itemsize != 2 or Y.shape[0] != T:
+        _refuse("X and Y must be bf16 matrices of as many rows, with unit stride along them")
     if w_scale.nbytes < 4 * O:
         _refuse(f"w_scale must hold {O} float32")
     shape = osdp_shape(T, I, O, len(q_shards), k)

@@ -399,6 +399,46 @@ def test_streams_of_the_caller():
     b.check(1e-3, 0.9, 0.999, 1e-8, 7, 2)
 
 
+def test_more_elements_than_32_bits_count():
+    """Places beyond 2^31 and 2^32: their own numbers, powers of two and random bits, and no others'."""
+    n, step, seed = (1 << 32) + 4096 + 77, 3, 19
+    print("adamw", n, "elements", flush=True)
+    z = lambda t, k=n: torch.zeros(k, dtype=t, device="cuda")  # noqa: E731
+    p, g, m, v, e = z(torch.bfloat16), z(torch.bfloat16), z(torch.uint8), z(torch.uint8), z(torch.uint8, 2 * -(-n // 128))
+    starts = [0, (1 << 31) - 256, (1 << 32) - 256, n - 333]
+    rng = np.random.default_rng(4)
+    parts = {}
+    for a in starts:
+        a -= a % 128
+        k = min(512, n - a)
+        parts[a] = torch.from_numpy(rng.standard_normal((2, k)).astype(np.float32)).to(torch.bfloat16)
+        g[a:a + k], p[a:a + k] = parts[a][0].cuda(), parts[a][1].cuda()
+    table = osdp.AdamWTable(params=[p], grads=[g], m=[m], v=[v], exps=[e])
+    sumsq, ws = z(torch.float64, 1), z(torch.uint8, osdp.osdp_adamw_grad_sumsq_workspace_bytes(table))
+    osdp.osdp_adamw_grad_sumsq(table, sumsq, ws)
+    osdp.osdp_adamw_step(table, lr=1e-2, beta1=0.5, beta2=0.5, step=step, seed=seed)
+    torch.cuda.synchronize()
+    want = sum(float((x[0].double() ** 2).sum()) for x in parts.values())
+    assert abs(sumsq.item() / want - 1) < 2.0 ** -39
+    one, touched = np.float32, 0
+    for a, x in parts.items():
+        k = x.shape[1]
+        key = mix(mix(mix(mix(mix(seed) ^ 0) ^ step) ^ 0) ^ (a >> 32))
+        h = mix((np.arange(a, a + k, dtype=np.uint64) + key) & M32)   # (none of the parts crosses 2^32 within itself ...
+        if (a >> 32) != ((a + k - 1) >> 32):                          # ... but one, whose second half counts anew)
+            key2 = mix(mix(mix(mix(mix(seed) ^ 0) ^ step) ^ 0) ^ ((a >> 32) + 1))
+            h2 = mix((np.arange(a, a + k, dtype=np.uint64) + key2) & M32)
+            h = np.where(np.arange(a, a + k) >> 32 == a >> 32, h, h2)
+        gr = x[0].float().numpy()
+        m1, v1 = gr * one(0.5), (gr * gr) * one(0.5)
+        for name, val, r16, top, low, dev, col in (("m", m1, h & 0xFFFF, 15, 32, m, 0), ("v", v1, h >> 16, 31, 48, v, 1)):
+            code, b = encode(val, r16, top, low)
+            assert np.array_equal(dev[a:a + k].cpu().numpy(), code), (name, a)
+            assert np.array_equal(e[2 * (a // 128):2 * (a // 128) + 2 * b.size].cpu().numpy()[col::2], b), (name, a)
+        touched += int((m[a:a + k] != 0).sum())
+    assert int((m != 0).sum()) == touched, "moments outside the parts with gradients were written"
+
+
 @pytest.mark.parametrize("grad", ["bf16", "f32"])
 @pytest.mark.parametrize("lengths,gap", [([1], 0), ([7, 0, 4097], 3), (LENGTHS, 0), ([3000001], 1), ([40] * 130, 0)])
 def test_sum_of_squares(grad, lengths, gap):

@@ -185,6 +185,81 @@ def test_tokens_that_are_zeros_or_hold_no_numbers(T):
     assert (got[0] == 0).all() and np.isnan(got[1:4]).all() and np.isfinite(got[4:6]).all()
 
 
+def _few_columns(X, shards, scale, O, rows, cols):
+    """Y at some rows and columns, from the definition, in 64 bits on the GPU."""
+    I = X.shape[1]
+    x = X[rows].float().cpu().numpy()
+    L = shards[0].numel()
+    q = np.stack([np.concatenate([shards[s][a:b].cpu().numpy() for s, a, b in _pieces(c * I, I, L)]) for c in cols])
+    return expected(x, q, scale[cols].cpu().numpy())
+
+
+def _pieces(start, length, L):
+    """(shard, from, to) of the pieces that a run of a flat matrix lies in."""
+    out = []
+    while length > 0:
+        s, a = divmod(start, L)
+        b = min(L, a + length)
+        out.append((s, a, b))
+        start, length = start + b - a, length - (b - a)
+    return out
+
+
+@pytest.mark.parametrize("T,I,O,N", [(2, 131072, 40000, 5), (70, 131072, 40000, 5), (300, 131072, 33000, 16)])
+def test_weights_of_more_than_32_bits(T, I, O, N):
+    """5 GB of weights: whole channels in five shards of more than 2^29 bytes, and cut within channels in sixteen."""
+    print("int8 product", T, I, O, N, flush=True)
+    L = -(-I * O // N)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    base = torch.randint(-127, 128, (1000003,), dtype=torch.int8, device="cuda", generator=gen)
+    shards = [base.roll(s).repeat(-(-L // 1000003))[:L].contiguous() for s in range(N)]
+    scale = torch.rand(O, device="cuda", generator=gen) * 1e-3
+    X = torch.randn(T, I, device="cuda", generator=gen).to(torch.bfloat16)
+    Y = torch.zeros(T, O, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, 1)[0], dtype=torch.uint8, device="cuda")
+    osdp.osdp_split_linear_i8_fwd(X, shards, scale, Y, 1, ws)
+    torch.cuda.synchronize()
+    rows = [0, T // 2, T - 1]
+    cols = [0, 1, O // 3, (1 << 31) // I - 1, (1 << 31) // I, (1 << 32) // I - 1, (1 << 32) // I, O - 1]
+    same(Y[rows][:, cols].float().cpu().numpy(), _few_columns(X, shards, scale, O, rows, cols))
+
+
+def test_tokens_of_more_than_32_bits():
+    """4.9 GB of rounded tokens, 9.8 GB in bf16."""
+    T, I, O, N = 300000, 16384, 16, 1
+    print("int8 product", T, I, O, N, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    w = Weight(I, O, N)
+    X = torch.randn(1000, I, device="cuda", generator=gen).to(torch.bfloat16).repeat(300, 1)
+    Y = torch.zeros(T, O, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, 1)[0], dtype=torch.uint8, device="cuda")
+    osdp.osdp_split_linear_i8_fwd(X, w.shards, w.dev_scale, Y, 1, ws)
+    torch.cuda.synchronize()
+    want = expected(X[:1000].float().cpu().numpy(), w.q, w.scale)
+    for a in range(0, T, 1000):
+        assert torch.equal(Y[a:a + 1000], Y[:1000]), a
+    same(Y[:1000].float().cpu().numpy(), want)
+
+
+def test_weight_of_more_than_32_bits_to_8():
+    I, O, N = 131072, 40000, 5
+    print("int8 quantize", I, O, N, flush=True)
+    L = I * O // N
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    base = (torch.randn(1000003, device="cuda", generator=gen) * 0.02).to(torch.bfloat16)
+    W = [base.roll(s).repeat(-(-L // 1000003))[:L].contiguous() for s in range(N)]
+    q = [torch.zeros(L, dtype=torch.int8, device="cuda") for _ in range(N)]
+    scale = torch.zeros(O, device="cuda")
+    ws = torch.empty(osdp.osdp_split_linear_i8_quantize_workspace_bytes(I, O, N), dtype=torch.uint8, device="cuda")
+    osdp.osdp_split_linear_i8_quantize(I, O, W, q, scale, ws)
+    torch.cuda.synchronize()
+    full = torch.cat(W).view(I, O)
+    for c in (0, 1, 16383, 16384, 32767, 32768, O - 1):
+        want, want_scale = to_8_bits(full[:, c:c + 1].float().cpu().numpy(), 0)
+        s, off = c * I // L, c * I % L
+        assert np.array_equal(q[s][off:off + I].cpu().numpy(), want[:, 0]) and scale[c].item() == want_scale[0], c
+
+
 def test_extreme_sums_stay_exact():
     """Every number at its largest: 131072 * 127 * 127 = 2113929216 is below 2^31."""
     I, O = 131072, 32
