@@ -7,6 +7,11 @@
 // upload, and a captured graph keeps them).  Tensors are cut into tiles of 2048 elements, one to a workgroup of 256 at a time: 8
 // elements to a lane, so that a row of 16 lanes is one block of 128 that moments in 8 bits share a power of two over, and
 // its largest magnitude is found without leaving the row (four DPP steps, no LDS, no barrier).
+//
+// What bounds it: memory with moments in fp32 (78.7 million elements, 2.2 GB: 407 us, 5.4 TB/s) and with a master copy and moments in 8
+// bits (1.57 GB with their values read back: 291 us); without a master copy the 87 instructions that two codes, two random numbers and a
+// rounded parameter cost an element weigh as much as its 10 bytes (202 million elements: 450 us, 4.5 TB/s).  More waves to a SIMD
+// would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
@@ -99,7 +104,9 @@ __device__ __forceinline__ uint32_t element(int j) {
 }
 
 // A lane's eight elements as they lie in memory, asked for (load) apart from where they are taken to pieces (get), so that all of a
-// tile's loads are on their way before the first of them is waited for.
+// tile's loads are on their way before the first of them is waited for.  Wide loads and stores are marked as used once: nothing here
+// is touched again before far more than the caches hold has passed.  A step over 78.7 million elements with moments in fp32 takes 407 us
+// with the marks (5.4 TB/s) and 425 without, with moments in 8 bits 291 and 310; the sum of squares of 403 million 126 and 135.
 template <class T, bool kWide>
 struct Eight;
 
@@ -130,8 +137,8 @@ struct Eight<float, true> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t) {
     const f32x4 *q = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + at + element<true>(0));
-    a = q[0];
-    b = q[1];
+    a = __builtin_nontemporal_load(q);
+    b = __builtin_nontemporal_load(q + 1);
   }
   __device__ __forceinline__ void get(float (&out)[8]) const {
 #pragma unroll
@@ -143,7 +150,8 @@ template <>
 struct Eight<uint16_t, true> {
   uint4 a;
   __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t) {
-    a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + at + element<true>(0));
+    const osdp_u32x4 z = __builtin_nontemporal_load(reinterpret_cast<const osdp_u32x4 *>(static_cast<const uint16_t *>(p) + at + element<true>(0)));
+    a = uint4{z[0], z[1], z[2], z[3]};
   }
   __device__ __forceinline__ void get(float (&out)[8]) const {  // bf16
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -174,8 +182,8 @@ template <bool kWide>
 __device__ __forceinline__ void store8(float *p, int64_t at, uint32_t left, const float (&x)[8]) {
   if constexpr (kWide) {
     f32x4 *q = reinterpret_cast<f32x4 *>(p + at + element<true>(0));
-    q[0] = f32x4{x[0], x[1], x[2], x[3]};
-    q[1] = f32x4{x[4], x[5], x[6], x[7]};
+    __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, q);
+    __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, q + 1);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -190,7 +198,7 @@ __device__ __forceinline__ void store8(uint16_t *p, int64_t at, uint32_t left, c
     uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = (x[2 * j] >> 16) | (x[2 * j + 1] & 0xffff0000u);
-    *reinterpret_cast<uint4 *>(p + at + element<true>(0)) = uint4{w[0], w[1], w[2], w[3]};
+    __builtin_nontemporal_store(osdp_u32x4{w[0], w[1], w[2], w[3]}, reinterpret_cast<osdp_u32x4 *>(p + at + element<true>(0)));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -207,7 +215,7 @@ __device__ __forceinline__ void store8(uint8_t *p, int64_t at, uint32_t left, co
       w.x |= x[j] << (8 * j);
       w.y |= x[4 + j] << (8 * j);
     }
-    *reinterpret_cast<uint2 *>(p + at + element<true>(0)) = w;
+    __builtin_nontemporal_store(osdp_u32x2{w.x, w.y}, reinterpret_cast<osdp_u32x2 *>(p + at + element<true>(0)));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -450,8 +458,8 @@ __global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
 // Squares and sums are in double from the first product on (a bf16 gradient of 1e20 is one, its square in fp32 is not): the
 // vector unit multiplies and adds them as fast as fp32, and the pass stays bound by memory.
 constexpr int kSumBlocks = 1024;  // workgroups, and so partial sums, of a launch at most
-constexpr int kSumTiles = 4;      // tiles that a workgroup has on their way at a time, where there are enough for all: 806 MB in 136 us
-                                  // (5.9 TB/s), with one tile at a time in 214
+constexpr int kSumTiles = 4;      // tiles that a workgroup has on their way at a time, where there are enough for all: 806 MB in 126 us
+                                  // (6.4 TB/s); one tile at a time takes half as long again
 
 template <int kThreads = osdp::kThreads>
 __device__ __forceinline__ double block_sum(double x) {
