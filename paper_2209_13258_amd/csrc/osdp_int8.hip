@@ -79,10 +79,12 @@ hipError_t launch_quantize_tokens(const uint16_t *x, int64_t ldx, const I8Proble
 }
 
 // ---- weight shards to 8 bits --------------------------------------------------------------------------------------
-// Two passes: the largest magnitude of every column over a range of rows, one range a workgroup (into the workspace); then,
-// over tiles of 128 x 128, their largest, the rounding, and the transposition through LDS.  Both run at the rate of a copy (8192 -> 32768,
-// 537 MB: 117 us at 4.6 TB/s, then 142 us at 5.7 read and written).  Taking the columns in strips small enough for the second pass to find
-// them in the last-level cache did not pay: 298 us in strips of 128 MB, 307 of 96, 367 of 64, against 287 all at once.
+// Two passes: the largest magnitude of every column over the rows that a workgroup takes (into the workspace), 32 rows at a time,
+// the workgroups' side by side, so that all of them move down the matrix together; then, over tiles of 128 x 128, their largest,
+// the rounding, and the transposition through LDS.  The second pass begins at the bottom, where the first has left the last
+// 256 MB in the last-level cache, and marks its own loads and stores as used once, which keeps them there until they are read: 8192 -> 32768
+// (537 MB read twice, 268 written) takes 212 us, against 267 with ranges of rows to the workgroups and both passes from the top.
+// Taking the columns in strips of what the cache holds, pass after pass, did not pay (298 us in strips of 128 MB, 307 of 96, 367 of 64).
 struct WeightShards {
   ShardTable w, q;          // bf16 [I x O], 8 bits [O x I]: flat, cut after every L elements
   int64_t L;
@@ -90,6 +92,7 @@ struct WeightShards {
 };
 
 constexpr int kColumns = 256;  // of a workgroup of the first pass: 8 to a lane, 32 lanes side by side, 8 rows at a time
+constexpr int kAmaxRows = 32;  // of a step of the first pass: 8 rows at a time, four times
 constexpr int kStrip = 128;    // rows and columns of a tile of the second pass
 
 // A place in a flat matrix that is cut into shards.  One division finds a workgroup's first place; from there on places move
@@ -107,26 +110,26 @@ struct Place {
   }
 };
 
-__global__ __launch_bounds__(kThreads) void column_amax_kernel(WeightShards p, int32_t rows_each, uint32_t *__restrict__ part) {
+__global__ __launch_bounds__(kThreads) void column_amax_kernel(WeightShards p, uint32_t *__restrict__ part) {
   __shared__ const uint16_t *tab[OSDP_MAX_SHARDS];
   __shared__ uint32_t most[8][kColumns];
   if (threadIdx.x < OSDP_MAX_SHARDS) tab[threadIdx.x] = static_cast<const uint16_t *>(p.w.p[threadIdx.x]);
   __syncthreads();
   const int lane = threadIdx.x & 31, line = threadIdx.x >> 5;
   const int c = blockIdx.x * kColumns + lane * 8;
-  const int r0 = blockIdx.y * rows_each, r1 = min(r0 + rows_each, p.I);
+  const int r0 = blockIdx.y * kAmaxRows + line, turn = gridDim.y * kAmaxRows;
   uint32_t m[8] = {};
   if (c < p.O) {
-    Place at(static_cast<int64_t>(r0) * p.O, p.L);
-    at.ahead(static_cast<int64_t>(line) * p.O + c, p.L);
+    Place at(static_cast<int64_t>(r0) * p.O + c, p.L);
     // (rows beyond the last repeat it, so that the loads of four steps go out together)
-    for (int r = r0 + line; r < r1; r += 32) {
+    for (int r = r0; r < p.I; r += turn) {
       uint4 v[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         v[u] = load_global16(tab[at.shard] + at.off);
-        if (r + 8 * (u + 1) < r1) at.ahead(static_cast<int64_t>(8) * p.O, p.L);
+        if (u < 3 && r + 8 * (u + 1) < p.I) at.ahead(static_cast<int64_t>(8) * p.O, p.L);
       }
+      if (r + turn < p.I) at.ahead(static_cast<int64_t>(turn - 24) * p.O, p.L);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
@@ -160,9 +163,9 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
     q_tab[threadIdx.x] = static_cast<uint8_t *>(p.q.p[threadIdx.x]);
   }
   __syncthreads();
-  // (tiles that run together lie on a diagonal: their stores, a row of the result apart, then do not all meet the same memory
+  // (from the bottom up; tiles that run together lie on a diagonal: their stores, a row of the result apart, then do not all meet the same memory
   // channels; 149 -> 142 us)
-  const int ti = (blockIdx.y + blockIdx.x / 4) % gridDim.y;
+  const int ti = (gridDim.y - 1 - blockIdx.y + blockIdx.x / 4) % gridDim.y;
   const int o0 = blockIdx.x * kStrip, i0 = ti * kStrip;
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;  // 8 columns, 4 rows to a lane, twice
   uint4 v[2][4];  // (on their way while the columns' largest are looked up; beyond the edges anything, it is not stored)
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
       for (int j = 0; j < 4; ++j) {
         Place at = first;
         at.ahead(static_cast<int64_t>(min(half * 64 + rg * 4 + j, p.I - 1 - i0)) * p.O + min(cg * 8, p.O - 8 - o0), p.L);
-        v[half][j] = load_global16(tab[at.shard] + at.off);
+        v[half][j] = load_global16_once(tab[at.shard] + at.off);
       }
   }
   {
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
       const uint4 v = {tile[row][piece * 4], tile[row][piece * 4 + 1], tile[row][piece * 4 + 2], tile[row][piece * 4 + 3]};
       Place at = out;
       at.ahead(static_cast<int64_t>(row) * p.I + piece * 16, p.L);
-      store_global16(q_tab[at.shard] + at.off, v);
+      store_global16_once(q_tab[at.shard] + at.off, v);
     }
   }
 }
@@ -304,15 +307,10 @@ osdp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   return OSDP_OK;
 }
 
-// Ranges of rows that the first pass is cut into: enough workgroups for the card, at least 32 rows each.
-int32_t amax_rows(const Weight &w) {
-  const int64_t strips = (w.O + kColumns - 1) / kColumns;
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((w.I + 31) / 32, 1024 / std::min<int64_t>(strips, 1024)));
-  return static_cast<int32_t>(((w.I + parts - 1) / parts + 7) / 8 * 8);
-}
+// Workgroups that share the rows of a strip of columns in the first pass: enough for the card, with at least one step each.
 int32_t amax_parts(const Weight &w) {
-  const int32_t each = amax_rows(w);
-  return static_cast<int32_t>((w.I + each - 1) / each);
+  const int64_t strips = (w.O + kColumns - 1) / kColumns;
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>((w.I + kAmaxRows - 1) / kAmaxRows, 1024 / std::min<int64_t>(strips, 1024))));
 }
 
 // ---- which kernel ---------------------------------------------------------------------------------------------------
@@ -467,7 +465,7 @@ osdp_status osdp_split_linear_i8_quantize(const osdp_shape *shape, const void *c
   const hipStream_t q = static_cast<hipStream_t>(stream);
   uint32_t *part = static_cast<uint32_t *>(workspace);
   hipLaunchKernelGGL(column_amax_kernel, dim3(static_cast<unsigned>((w.O + kColumns - 1) / kColumns), static_cast<unsigned>(parts)),
-                     dim3(kThreads), 0, q, p, amax_rows(w), part);
+                     dim3(kThreads), 0, q, p, part);
   if ((st = hip_status(hipGetLastError(), "launching the columns' largest")) != OSDP_OK) return st;
   hipLaunchKernelGGL(quantize_weight_kernel, dim3(static_cast<unsigned>(tiles_o), static_cast<unsigned>(tiles_i)), dim3(kThreads), 0, q,
                      p, parts, part, w_scale);

@@ -21,6 +21,14 @@ __device__ __forceinline__ uint4 load_global16(const void *p) {
 __device__ __forceinline__ void store_global16(void *p, uint4 v) {
   *(__attribute__((address_space(1))) osdp_u32x4 *)(p) = osdp_u32x4{v.x, v.y, v.z, v.w};
 }
+// The same, marked as used once, so that the caches rather keep something else.
+__device__ __forceinline__ uint4 load_global16_once(const void *p) {
+  const osdp_u32x4 v = __builtin_nontemporal_load((const __attribute__((address_space(1))) osdp_u32x4 *)(p));
+  return uint4{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store_global16_once(void *p, uint4 v) {
+  __builtin_nontemporal_store(osdp_u32x4{v.x, v.y, v.z, v.w}, (__attribute__((address_space(1))) osdp_u32x4 *)(p));
+}
 __device__ __forceinline__ void store_global8(void *p, uint2 v) {
   *(__attribute__((address_space(1))) osdp_u32x2 *)(p) = osdp_u32x2{v.x, v.y};
 }

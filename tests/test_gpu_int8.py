@@ -312,7 +312,7 @@ def quantize(W, I, O, N):
 
 @pytest.mark.parametrize("I,O,N", [(16, 8, 1), (16, 16, 16), (32, 24, 3), (64, 40, 8), (128, 128, 2), (144, 136, 4), (256, 1024, 2), (272, 264, 11),
                                    (1040, 520, 5), (2560, 1280, 8), (4096, 8, 64), (16, 4096, 64), (336, 1000, 3), (131072, 16, 8), (1024, 4096, 8), (1008, 1032, 7),
-                                   (1040, 72, 2), (2048, 136, 4), (16, 8, 8), (512, 8, 64)])
+                                   (1040, 72, 2), (2048, 136, 4), (16, 8, 8), (512, 8, 64), (20016, 536, 3)])
 def test_weight_to_8_bits(I, O, N):
     print("int8 quantize", I, O, N, flush=True)
     g = np.random.default_rng([I, O])
