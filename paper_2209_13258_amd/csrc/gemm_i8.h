@@ -90,150 +90,105 @@ __device__ __forceinline__ void i8_store8(uint16_t *y, const int *sums, float st
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------
-// A workgroup owns 16 * NB output channels and 16 * MB tokens; its kWaves waves share the reduction, 64 * kUnroll bytes of
-// every row at a time, and add their sums up in LDS (integers: in any order).  Weights go from memory to registers, each lane 16
-// bytes of a row, the four lanes of a row 64 in sequence; nothing of them is used twice, so nothing is staged.
-template <int MB, int NB, int kWaves, int kUnroll, bool kFlat>
-__global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
-  constexpr int BM = 16 * MB, BN = 16 * NB, kStep = 64 * kUnroll;
-  __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
-  __shared__ int sums[BM * BN];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
-  if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
-  for (int i = tid; i < BM * BN; i += kWaves * 64) sums[i] = 0;
-  __syncthreads();
-  const int n0 = blockIdx.x * BN, m0 = blockIdx.y * BM;
-  // where this lane's rows of the weight begin (rows beyond the last repeat it; they are not stored)
-  const uint8_t *row[NB];
-  int64_t off[NB];
-  int shard[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int o = min(n0 + 16 * b + l16, p.O - 1);
-    if (!kFlat) {
-      const int s = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.rows_each));
-      row[b] = tab[s] + static_cast<int64_t>(o - s * p.rows_each) * p.I;
-    } else {
+// One output channel's row of the weight.  kFlat: the row may go on in the next shard, and every piece of 16 bytes looks for its own.
+template <bool kFlat>
+struct I8Row {
+  const uint8_t *row;
+  const uint8_t *const *tab;
+  int64_t off, L;
+  int shard;
+  __device__ __forceinline__ I8Row(const I8Problem &p, const uint8_t *const *shards, int o) : tab(shards), L(p.L) {
+    if constexpr (kFlat) {
       const uint64_t f = static_cast<uint64_t>(o) * p.I;
-      shard[b] = static_cast<int>(f / static_cast<uint64_t>(p.L));
-      off[b] = static_cast<int64_t>(f - static_cast<uint64_t>(shard[b]) * p.L);
+      shard = static_cast<int>(f / static_cast<uint64_t>(p.L));
+      off = static_cast<int64_t>(f - static_cast<uint64_t>(shard) * p.L);
+    } else {
+      shard = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.rows_each));
+      row = tab[shard] + static_cast<int64_t>(o - shard * p.rows_each) * p.I;
     }
   }
-  const uint8_t *token[MB];
-#pragma unroll
-  for (int b = 0; b < MB; ++b) token[b] = p.xq + static_cast<int64_t>(min(m0 + 16 * b + l16, p.T - 1)) * p.ldq;
-  i32x4 acc[MB][NB];
-#pragma unroll
-  for (int bm = 0; bm < MB; ++bm)
-#pragma unroll
-    for (int bn = 0; bn < NB; ++bn) acc[bm][bn] = i32x4{0, 0, 0, 0};
+  __device__ __forceinline__ uint4 load(int k) const {
+    if constexpr (!kFlat) return load_global16(row + k);
+    int64_t f = off + k;
+    int s = shard;
+    while (f >= L) {
+      f -= L;
+      ++s;
+    }
+    return load_global16(tab[s] + f);
+  }
+};
+
+// What the two kernels below have in common: a workgroup owns 16 output channels and 16 tokens; its kWaves waves share the
+// reduction, 64 * kUnroll bytes of every row at a time, and add their sums up in LDS (integers: in any order).  Weights go from memory
+// to registers, each lane 16 bytes of a row, the four lanes of a row 64 in sequence; nothing of them is used twice, so nothing is
+// staged.  Both are bound by the weight's bytes.
+//
+// Tokens that are in 8 bits already.  16 tokens, 4096 -> 16384, rounded in a launch before it: 25 us in all, 2.7 TB/s (2 tokens 17.5, 3.8);
+// where rows run over the ends of shards 28.  32 or 64 channels to a workgroup, which read the tokens half or a quarter as often, take
+// 22 and 25 there but 20 to 31 instead of 15 for 10240 -> 2560, whose workgroups then leave half the card or more idle.
+template <int kWaves, int kUnroll, bool kFlat>
+__global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
+  constexpr int kStep = 64 * kUnroll;
+  __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
+  __shared__ int sums[16 * 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
+  if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
+  for (int i = tid; i < 16 * 16; i += kWaves * 64) sums[i] = 0;
+  __syncthreads();
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
+  // (rows beyond the last repeat it; they are not stored)
+  const I8Row<kFlat> weight(p, tab, min(n0 + l16, p.O - 1));
+  const uint8_t *token = p.xq + static_cast<int64_t>(min(m0 + l16, p.T - 1)) * p.ldq;
+  i32x4 acc = {0, 0, 0, 0};
   for (int k0 = wave * kStep; k0 < p.I; k0 += kWaves * kStep) {
-    uint4 w[kUnroll][NB], x[kUnroll][MB];
+    uint4 w[kUnroll], x[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int k = k0 + 64 * u + 16 * q4;
-      const int kw = k < p.I ? k : 0;       // beyond the row's end: any weights, the tokens are zeros there
-      const int kx = k < p.ldq ? k : p.ldq - 16;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const uint8_t *at;
-        if (!kFlat) {
-          at = row[b] + kw;
-        } else {
-          int64_t f = off[b] + kw;
-          int s = shard[b];
-          while (f >= p.L) {
-            f -= p.L;
-            ++s;
-          }
-          at = tab[s] + f;
-        }
-        w[u][b] = load_global16(at);
-      }
-#pragma unroll
-      for (int b = 0; b < MB; ++b) x[u][b] = load_global16(token[b] + kx);
-      if (k >= p.ldq) {
-#pragma unroll
-        for (int b = 0; b < MB; ++b) x[u][b] = uint4{0u, 0u, 0u, 0u};
-      }
+      w[u] = weight.load(k < p.I ? k : 0);  // beyond the row's end: any weights, the tokens are zeros there
+      x[u] = load_global16(token + (k < p.ldq ? k : p.ldq - 16));
+      if (k >= p.ldq) x[u] = uint4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int bm = 0; bm < MB; ++bm)
-#pragma unroll
-        for (int bn = 0; bn < NB; ++bn)
-          acc[bm][bn] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u][bn]), __builtin_bit_cast(i32x4, x[u][bm]),
-                                                              acc[bm][bn], 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u]), __builtin_bit_cast(i32x4, x[u]), acc, 0, 0, 0);
   }
 #pragma unroll
-  for (int bm = 0; bm < MB; ++bm)
-#pragma unroll
-    for (int bn = 0; bn < NB; ++bn)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) atomicAdd(&sums[(16 * bm + l16) * BN + 16 * bn + 4 * q4 + i], acc[bm][bn][i]);
+  for (int i = 0; i < 4; ++i) atomicAdd(&sums[l16 * 16 + 4 * q4 + i], acc[i]);
   __syncthreads();
-  for (int i = tid; i < BM * BN / 8; i += kWaves * 64) {
-    const int r = i / (BN / 8), c = i % (BN / 8) * 8, m = m0 + r, n = n0 + c;
-    if (m >= p.T || n >= p.O) continue;
-    i8_store8(p.y + static_cast<int64_t>(m) * p.ldy + n, &sums[r * BN + c], p.x_scale[m], p.w_scale + n);
+  if (tid < 32) {
+    const int r = tid >> 1, c = (tid & 1) * 8, m = m0 + r, n = n0 + c;
+    if (m < p.T && n < p.O) i8_store8(p.y + static_cast<int64_t>(m) * p.ldy + n, &sums[r * 16 + c], p.x_scale[m], p.w_scale + n);
   }
 }
 
 // The same with the tokens' rounding in the launch, for tokens of so few features that the bytes of 16 of them fit in LDS and
 // that every workgroup may well round its 16 for itself: one launch instead of two, the first weights on their way meanwhile.
-template <int NB, int kWaves, int kUnroll, bool kFlat>
+// One token, 4096 -> 16384: 15.8 us (4.2 TB/s) in one launch, 23 in two.
+template <int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, const uint16_t *__restrict__ x, int64_t ldx) {
-  constexpr int BN = 16 * NB, kStep = 64 * kUnroll;
+  constexpr int kStep = 64 * kUnroll;
   extern __shared__ __attribute__((aligned(16))) uint8_t rows[];  // [T][ldq + 16]: 16 rows fall into 16 different bank groups
   __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
-  __shared__ int sums[16 * BN];
+  __shared__ int sums[16 * 16];
   __shared__ uint32_t most[16][kWaves];
   __shared__ float scale[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
-  const int n0 = blockIdx.x * BN, m0 = blockIdx.y * 16, pitch = p.ldq + 16, tokens = min(p.T - m0, 16);
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16, pitch = p.ldq + 16, tokens = min(p.T - m0, 16);
   x += static_cast<int64_t>(m0) * ldx;
   if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
-  for (int i = tid; i < 16 * BN; i += kWaves * 64) sums[i] = 0;
+  for (int i = tid; i < 16 * 16; i += kWaves * 64) sums[i] = 0;
   __syncthreads();
-  const uint8_t *row[NB];
-  int64_t off[NB];
-  int shard[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int o = min(n0 + 16 * b + l16, p.O - 1);
-    if (!kFlat) {
-      const int s = static_cast<int>(static_cast<uint32_t>(o) / static_cast<uint32_t>(p.rows_each));
-      row[b] = tab[s] + static_cast<int64_t>(o - s * p.rows_each) * p.I;
-    } else {
-      const uint64_t f = static_cast<uint64_t>(o) * p.I;
-      shard[b] = static_cast<int>(f / static_cast<uint64_t>(p.L));
-      off[b] = static_cast<int64_t>(f - static_cast<uint64_t>(shard[b]) * p.L);
-    }
-  }
-  auto load = [&](int k0, uint4 (&w)[kUnroll][NB]) {
+  const I8Row<kFlat> weight(p, tab, min(n0 + l16, p.O - 1));
+  auto load = [&](int k0, uint4 (&w)[kUnroll]) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int k = k0 + 64 * u + 16 * q4, kw = k < p.I ? k : 0;  // beyond the row's end: any weights, the tokens are zeros there
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const uint8_t *at;
-        if (!kFlat) {
-          at = row[b] + kw;
-        } else {
-          int64_t f = off[b] + kw;
-          int s = shard[b];
-          while (f >= p.L) {
-            f -= p.L;
-            ++s;
-          }
-          at = tab[s] + f;
-        }
-        w[u][b] = load_global16(at);
-      }
+      const int k = k0 + 64 * u + 16 * q4;
+      w[u] = weight.load(k < p.I ? k : 0);  // beyond the row's end: any weights, the tokens are zeros there
     }
   };
-  uint4 w[kUnroll][NB];
+  uint4 w[kUnroll];
   load(wave * kStep, w);
   // tokens to 8 bits: a row to a wave, or (fewer tokens than waves) to as many waves as there are for it
   const int share = tokens >= kWaves ? 1 : kWaves / tokens, part = wave % share;
@@ -255,49 +210,43 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
   }
   __syncthreads();
   const uint8_t *token = rows + min(l16, tokens - 1) * pitch + 16 * q4;
-  i32x4 acc[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) acc[b] = i32x4{0, 0, 0, 0};
+  i32x4 acc = {0, 0, 0, 0};
   for (int k0 = wave * kStep; k0 < p.I; k0 += kWaves * kStep) {
-    uint4 next[kUnroll][NB];
+    uint4 next[kUnroll];
     if (k0 + kWaves * kStep < p.I) load(k0 + kWaves * kStep, next);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       if (k0 + 64 * u >= p.I) break;
       const i32x4 a = *reinterpret_cast<const i32x4 *>(token + k0 + 64 * u);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u][b]), a, acc[b], 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u]), a, acc, 0, 0, 0);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) w[u][b] = next[u][b];
+    for (int u = 0; u < kUnroll; ++u) w[u] = next[u];
   }
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) atomicAdd(&sums[l16 * BN + 16 * b + 4 * q4 + i], acc[b][i]);
+  for (int i = 0; i < 4; ++i) atomicAdd(&sums[l16 * 16 + 4 * q4 + i], acc[i]);
   __syncthreads();
-  for (int i = tid; i < 2 * BN; i += kWaves * 64) {
-    const int m = i / (BN / 8), c = i % (BN / 8) * 8, n = n0 + c;
-    if (m < tokens && n < p.O) i8_store8(p.y + static_cast<int64_t>(m0 + m) * p.ldy + n, &sums[m * BN + c], scale[m], p.w_scale + n);
+  if (tid < 32) {
+    const int m = tid >> 1, c = (tid & 1) * 8, n = n0 + c;
+    if (m < tokens && n < p.O) i8_store8(p.y + static_cast<int64_t>(m0 + m) * p.ldy + n, &sums[m * 16 + c], scale[m], p.w_scale + n);
   }
 }
 
-template <int NB, int kWaves, int kUnroll>
+inline dim3 i8_few_grid(const I8Problem &p) { return dim3(static_cast<unsigned>((p.O + 15) / 16), static_cast<unsigned>((p.T + 15) / 16)); }
+
+// (eight waves with 128 bytes of a row on their way in the one, 256 in the other: 4 or 16 waves, or 512 bytes, were within 3 % or slower)
 hipError_t launch_fused(const I8Problem &p, const uint16_t *x, int64_t ldx, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>((p.O + 16 * NB - 1) / (16 * NB)), static_cast<unsigned>((p.T + 15) / 16));
+  constexpr int kWaves = 8, kUnroll = 2;
   const unsigned lds = static_cast<unsigned>(std::min(p.T, 16) * (p.ldq + 16));
-  if (p.rows_each > 0) hipLaunchKernelGGL((i8_fused_kernel<NB, kWaves, kUnroll, false>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
-  else hipLaunchKernelGGL((i8_fused_kernel<NB, kWaves, kUnroll, true>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
+  if (p.rows_each > 0) hipLaunchKernelGGL((i8_fused_kernel<kWaves, kUnroll, false>), i8_few_grid(p), dim3(kWaves * 64), lds, stream, p, x, ldx);
+  else hipLaunchKernelGGL((i8_fused_kernel<kWaves, kUnroll, true>), i8_few_grid(p), dim3(kWaves * 64), lds, stream, p, x, ldx);
   return hipGetLastError();
 }
 
-template <int MB, int NB, int kWaves, int kUnroll>
 hipError_t launch_few(const I8Problem &p, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>((p.O + 16 * NB - 1) / (16 * NB)), static_cast<unsigned>((p.T + 16 * MB - 1) / (16 * MB)));
-  if (p.rows_each > 0) hipLaunchKernelGGL((i8_few_kernel<MB, NB, kWaves, kUnroll, false>), grid, dim3(kWaves * 64), 0, stream, p);
-  else hipLaunchKernelGGL((i8_few_kernel<MB, NB, kWaves, kUnroll, true>), grid, dim3(kWaves * 64), 0, stream, p);
+  constexpr int kWaves = 8, kUnroll = 4;
+  if (p.rows_each > 0) hipLaunchKernelGGL((i8_few_kernel<kWaves, kUnroll, false>), i8_few_grid(p), dim3(kWaves * 64), 0, stream, p);
+  else hipLaunchKernelGGL((i8_few_kernel<kWaves, kUnroll, true>), i8_few_grid(p), dim3(kWaves * 64), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -361,7 +361,7 @@ hipError_t launch_i8_tiles(const I8Problem &p, int parts, hipStream_t stream) {
   t.arrived = p.arrived;
   int64_t grid = std::min<int64_t>(tiles, kI8Cus * kPerCu);
   if (kSlots > 2) grid = tiles * t.parts;
-  if (grid > (1 << 24) || (t.parts > 1 && (kSlots == 2 || tiles > kI8MostTiles || grid * (MB * NB * 4096) > static_cast<int64_t>(kI8SumBytes))))
+  if (grid > (1 << 24) || (t.parts > 1 && (kSlots == 2 || !t.sums || tiles > kI8MostTiles || grid * (MB * NB * 4096) > static_cast<int64_t>(kI8SumBytes))))
     return hipErrorInvalidValue;
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);

@@ -357,9 +357,13 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
                         static_cast<size_t>(groups) * v.side * v.side * 4 > kI8SumBytes))
         break;
       double rounds = static_cast<double>((groups + v.room - 1) / v.room);
-      if (few) rounds = std::max(static_cast<double>(groups) / v.room, groups <= 256 ? 0.35 : 0.5);
+      if (few) rounds = std::max(static_cast<double>(groups) / v.room, groups > 256 ? 0.5 : T > 16 ? 0.35 : 0.25);
       else if (v.room == 512 && groups % 512 != 0 && groups % 512 <= 256) rounds -= 0.4;  // (one workgroup to a CU is faster than two)
-      double us = v.fixed + rounds * (static_cast<double>(each) * v.block + v.start);
+      // (up to 16 tokens all workgroups read the same ones, and with fewer than 16 a wave's 16 rows of them are fewer lines: us by 16 / by
+      // 64 x 64 in four to eight parts, weight from memory: 16384 -> 4096 2 tokens 20.1 / 25.0, 10 22.1 / 25.5, 16 24.8 / 25.6; 12000 -> 1024
+      // 2 tokens 11.1 / 15.8, 16 14.1 / 15.9; 16000 -> 1000 40 tokens 21.4 / 17.9)
+      const double block = few && T < 16 ? v.block * (0.7 + 0.3 * static_cast<double>(T) / 16.0) : v.block;
+      double us = v.fixed + rounds * (static_cast<double>(each) * block + v.start);
       if (parts > 1) us += v.each * static_cast<double>(parts) + v.meet * static_cast<double>(groups) / 256.0;
       if (best.us < 0.0 || us < best.us) best = {v.kernel, static_cast<int>(parts), us};
     }
@@ -368,10 +372,10 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
 }
 
 hipError_t launch_product(const I8Problem &p, hipStream_t stream) {
-  if (p.rows_each == 0) return launch_few<1, 1, 8, 4>(p, stream);
+  if (p.rows_each == 0) return launch_few(p, stream);
   const Choice c = choose(p.T, p.I, p.rows_each, p.O / p.rows_each, p.sums != nullptr);
   switch (c.kernel) {
-    case Kernel::kFew: return launch_few<1, 1, 8, 4>(p, stream);
+    case Kernel::kFew: return launch_few(p, stream);
     case Kernel::k64: return launch_i8_tiles<2, 2, 4>(p, c.parts, stream);
     case Kernel::k128: return launch_i8_tiles<4, 4, 4>(p, c.parts, stream);
     case Kernel::k128Walk: return launch_i8_tiles<4, 4, 2>(p, 1, stream);
@@ -509,7 +513,7 @@ osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int
   p.shards = tab; p.L = w.L; p.rows_each = static_cast<int32_t>(w.rows_each);
   p.w_scale = w_scale; p.y = static_cast<uint16_t *>(Y); p.ldy = ldy;
   const uint16_t *x = static_cast<const uint16_t *>(X);
-  if (rounds_inside(w)) return hip_status(launch_fused<1, 8, 2>(p, x, ldx, q), "launching the product");
+  if (rounds_inside(w)) return hip_status(launch_fused(p, x, ldx, q), "launching the product");
   uint8_t *xq = reinterpret_cast<uint8_t *>(ws);
   float *x_scale = reinterpret_cast<float *>(ws + scale_offset(w));
   p.xq = xq; p.x_scale = x_scale;
