@@ -9,9 +9,8 @@
 // its largest magnitude is found without leaving the row (four DPP steps, no LDS, no barrier).
 //
 // What bounds it: memory with moments in fp32 (78.7 million elements, 2.2 GB: 407 us, 5.4 TB/s) and with a master copy and moments in 8
-// bits (1.57 GB with their values read back: 291 us); without a master copy the 87 instructions that two codes, two random numbers and a
-// rounded parameter cost an element weigh as much as its 10 bytes (202 million elements: 450 us, 4.5 TB/s).  More waves to a SIMD
-// would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
+// bits (1.57 GB with their values read back: 291 us); without a master copy the 60 instructions that two codes, a random number and a
+// rounded parameter cost an element keep the vector units as busy as its 10 bytes keep memory (201 million elements: 375 us, 5.4 TB/s).  More waves to a SIMD would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
@@ -49,6 +48,7 @@ struct Batch {
   int32_t count;
   uint32_t first;       // place of t[0] in the caller's array
   uint32_t tiles;
+  uint32_t run;         // tiles that a workgroup takes one after another
 };
 
 struct Step {
@@ -389,8 +389,14 @@ __device__ __forceinline__ bool scalars_of(const Step &s, Scalars *k) {
     const double sum = *s.sumsq;
     if (!(sum < std::numeric_limits<double>::infinity())) return false;  // (NaN too)
     if (s.max_norm > 0.0) {
-      const double norm = sqrt(sum);
-      if (norm > s.max_norm) k->coef = static_cast<float>(s.max_norm / norm);
+      // (1 / sqrt(sum) to some 50 bits, by two steps of Newton's from the instruction's 23 or more, which every wave works out for
+      // itself: a division and a root in double take three times the instructions)
+      if (sum > s.max_norm * s.max_norm) {
+        double y = __builtin_amdgcn_rsq(sum);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) y = fma(0.5 * y, fma(-(sum * y), y, 1.0), y);
+        k->coef = static_cast<float>(s.max_norm * y);
+      }
     }
   }
   k->rate = s.rate;
@@ -414,13 +420,16 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Batch b, Step s) {
   Scalars k;
   if (!scalars_of(s, &k)) return;
   const uint32_t stirred = k.key;
-  for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
-    const int i = tensor_of(b, tile);
-    const Tensor t = b.t[i];
-    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
-    k.key = mix(mix(stirred ^ (b.first + static_cast<uint32_t>(i))) ^ static_cast<uint32_t>(at >> 32));
-    if (((b.wide >> i) & 1u) && t.n - at >= kTile) adamw_tile<Grad, kForm, kState8, true>(t, s, k, at);
-    else adamw_tile<Grad, kForm, kState8, false>(t, s, k, at);
+  for (uint32_t first = blockIdx.x * b.run; first < b.tiles; first += gridDim.x * b.run) {
+    const uint32_t end = min(first + b.run, b.tiles);
+    for (uint32_t tile = first; tile < end; ++tile) {
+      const int i = tensor_of(b, tile);
+      const Tensor t = b.t[i];
+      const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
+      k.key = mix(mix(stirred ^ (b.first + static_cast<uint32_t>(i))) ^ static_cast<uint32_t>(at >> 32));
+      if (((b.wide >> i) & 1u) && t.n - at >= kTile) adamw_tile<Grad, kForm, kState8, true>(t, s, k, at);
+      else adamw_tile<Grad, kForm, kState8, false>(t, s, k, at);
+    }
   }
 }
 
@@ -611,7 +620,7 @@ size_t size_of(int32_t type) { return type == OSDP_BF16 ? 2 : 4; }
 template <class Fill, class Launch>
 osdp_status for_batches(const osdp_adamw_tensor *tensors, int32_t count, Fill &&fill, Launch &&launch) {
   Batch b;
-  b.count = 0; b.tiles = 0; b.wide = 0;
+  b.count = 0; b.tiles = 0; b.wide = 0; b.run = 1;
   int32_t last = -1;  // place of the batch's last tensor: places within a batch are consecutive
   auto flush = [&]() -> osdp_status {
     if (b.count == 0) return OSDP_OK;
@@ -639,12 +648,18 @@ osdp_status for_batches(const osdp_adamw_tensor *tensors, int32_t count, Fill &&
   return flush();
 }
 
-unsigned grid_of(const Batch &b, unsigned most) { return std::min<unsigned>(b.tiles, most); }
 constexpr unsigned kMostBlocks = 1u << 20;
+unsigned grid_of(const Batch &b, uint32_t run) { return std::min<unsigned>((b.tiles + run - 1) / run, kMostBlocks); }
 
 template <class Grad, int kForm, bool kState8>
 hipError_t launch_adamw(const Batch &b, const Step &s, hipStream_t stream) {
-  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(b, kMostBlocks)), dim3(kThreads), 0, stream, b, s);
+  // Every wave works the call's scalars out for itself, 40 to 250 operations.  Where arithmetic is the bound and there are workgroups enough
+  // (from 6144 tiles on; fewer leave compute units idle at the end), one takes four tiles, so that they weigh less: 201 million elements in
+  // 375 us, with the step on the device 406, one tile to a workgroup 458 and 535.  The other forms are bound by memory and are the
+  // slower for it (78.7 million elements, master copy: moments in 8 bits 312 us instead of 291, in fp32 442 instead of 407).
+  Batch batch = b;
+  batch.run = kForm == kBf16 && kState8 && b.tiles >= 6144 ? 4 : 1;
+  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(batch, batch.run)), dim3(kThreads), 0, stream, batch, s);
   return hipGetLastError();
 }
 
@@ -818,7 +833,7 @@ osdp_status osdp_adamw_state_values(const osdp_adamw_tensor *tensors, int32_t co
         return aligned(t->m, 8) && aligned(t->v, 8) && aligned(m_out[i], 16) && aligned(v_out[i], 16);
       },
       [&](const Batch &b) {
-        hipLaunchKernelGGL(values_kernel, dim3(grid_of(b, kMostBlocks)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), b);
+        hipLaunchKernelGGL(values_kernel, dim3(grid_of(b, 1)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), b);
         return hip_status(hipGetLastError(), "launching the values of the moments");
       });
 }

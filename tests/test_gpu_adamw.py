@@ -220,6 +220,31 @@ def test_no_tensors_and_empty_ones():
         assert out.item() == 0.0
 
 
+@pytest.mark.parametrize("param,state", [("bf16", 8), ("master", 32)])
+def test_a_large_step_whose_tensors_end_anywhere(param, state):
+    """Enough elements for a workgroup to take several tiles one after another, across the ends of tensors short and long."""
+    c = Case([5000003, 2047, 3000000, 1, 0, 4700001, 64, 129, 130000], state, param, seed=8)
+    osdp.osdp_adamw_step(c.table, lr=1e-3, step=7, seed=12)
+    c.check(1e-3, 0.9, 0.999, 1e-8, 7, 12)
+
+
+def test_the_factor_that_clips_is_the_quotient():
+    """m is the factor itself after a step over gradients of 1 with beta1 = 0."""
+    g = np.random.default_rng(4)
+    sums = list(10.0 ** g.uniform(-290, 300, 150)) + [1e-300, 1e308, 1.0, 4.0, 1.0 + 2.0 ** -52, 2.0]
+    m = torch.zeros(8, device="cuda")
+    table = osdp.AdamWTable(params=[torch.zeros(8, device="cuda")], grads=[torch.ones(8, device="cuda")], m=[m], v=[torch.zeros(8, device="cuda")])
+    for s in sums:
+        for bound in (np.sqrt(s) * g.uniform(1e-3, 1.0), np.sqrt(s) * 10.0 ** g.uniform(-30, 0), 2.0 * np.sqrt(s), 1.0):
+            total = torch.tensor([s], dtype=torch.float64, device="cuda")
+            osdp.osdp_adamw_step(table, lr=0.0, beta1=0.0, step=1, grad_sumsq=total, max_norm=float(bound))
+            q = float(bound) / np.sqrt(s) if np.sqrt(s) > bound else 1.0
+            with np.errstate(over="ignore", under="ignore"):  # (its own error, below 2^-40, may turn a rounding's tie)
+                ends = np.float32(q * (1 - 2.0 ** -40)), np.float32(q * (1 + 2.0 ** -40))
+            got = m[3].item()
+            assert ends[0] <= got <= ends[1], (s, bound, got, q)
+
+
 @pytest.mark.parametrize("factor", [0.5, 1.0, 7.0])
 def test_clipping_by_the_norm(factor):
     """The norm found by the one call is what the other clips by; a norm below the bound changes nothing."""
