@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void quantize_weight_kernel(WeightShards 
   __shared__ uint8_t *q_tab[OSDP_MAX_SHARDS];
   __shared__ uint32_t most[2][kStrip];
   __shared__ float ratio[kStrip], up[kStrip];
-  __shared__ uint32_t tile[kStrip][kStrip / 4 + 1];  // [o][i / 4]
+  __shared__ uint32_t tile[kStrip][kStrip / 4 + 1];  // [o][i / 4]; two lanes to a bank (an order without that takes as long: memory is the bound)
   if (threadIdx.x < OSDP_MAX_SHARDS) {
     tab[threadIdx.x] = static_cast<const uint16_t *>(p.w.p[threadIdx.x]);
     q_tab[threadIdx.x] = static_cast<uint8_t *>(p.q.p[threadIdx.x]);
