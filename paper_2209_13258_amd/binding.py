@@ -7,6 +7,7 @@ PyTorch fallback: if the library is missing the import of this module fails.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -418,6 +419,34 @@ def _refuse(message: str):
     raise OsdpError(OSDP_ERR_INVALID_ARG, message)
 
 
+_kinds = {}  # names of element types (asking torch for one anew costs as much as the rest of a check)
+
+
+def _is(t, kind: str) -> bool:
+    d = t.dtype
+    name = _kinds.get(d)
+    if name is None:
+        name = _kinds[d] = str(d)
+    return name == kind
+
+
+def _one(t, kind: str) -> bool:
+    return t.numel() == 1 and _is(t, kind) and t.is_cuda
+
+
+def _overlap(written, read) -> bool:
+    """Whether some array that is written shares memory with another of them, or with one that is read; (address, bytes) each."""
+    written = sorted(a for a in written if a[1])
+    starts = [a for a, _ in written]
+    if any(a + n > b for (a, n), b in zip(written, starts[1:])):
+        return True
+    for a, n in read:
+        i = bisect.bisect_left(starts, a + n)  # the first that begins behind it; the one before that must end ahead of it
+        if n and i and sum(written[i - 1]) > a:
+            return True
+    return False
+
+
 class AdamWTable:
     """The tensors of an AdamW step, as the library takes them: checked and put together once, used for every step.
 
@@ -425,7 +454,8 @@ class AdamWTable:
     None; ``m`` and ``v``: fp32, or uint8 together with ``exps`` (uint8, 2 * ceil(n / 128) of each tensor), all zeros at the
     start.  ``weight_decay``: one number, or one for each tensor.  The table keeps the tensors alive.  One that is only
     summed up (``osdp_adamw_grad_sumsq``) needs ``grads`` alone, one that is only looked at (``osdp_adamw_state_values``)
-    ``m``, ``v`` and ``exps``."""
+    ``m``, ``v`` and ``exps``.  A tensor may not be listed twice (two operators that share a weight have one gradient, the sum),
+    nor may any that are written share memory."""
 
     def __init__(self, params=None, grads=None, masters=None, m=None, v=None, exps=None, weight_decay=0.0):
         lists = dict(params=params, grads=grads, masters=masters, m=m, v=v, exps=exps)
@@ -458,6 +488,9 @@ class AdamWTable:
         decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
         if len(decay) != count:
             _refuse(f"{len(decay)} weight decays for {count} tensors")
+        spans = {name: [(t.data_ptr(), t.nbytes) for t in ts] for name, ts in lists.items()}
+        if _overlap(sum((ts for name, ts in spans.items() if name != "grads"), []), spans.get("grads", [])):
+            _refuse("a tensor is listed twice, or tensors of the table share memory")
         self._keep = lists
         self.tensors = (osdp_adamw_tensor * max(count, 1))()
         for i in range(count):
@@ -492,8 +525,8 @@ def osdp_adamw_grad_sumsq_workspace_bytes(table: AdamWTable) -> int:
 
 def osdp_adamw_grad_sumsq(table: AdamWTable, sumsq, workspace, *, accumulate: bool = False, stream=None) -> None:
     """``sumsq`` (one float64 on the GPU) = sum of the squares of all of the table's gradients; accumulate: is added to it."""
-    if sumsq.nbytes != 8 or sumsq.numel() != 1 or not sumsq.is_floating_point():
-        _refuse("sumsq must be one float64")
+    if not _one(sumsq, "torch.float64"):
+        _refuse("sumsq must be one float64 on the GPU")
     _check(lib.osdp_adamw_grad_sumsq(table.tensors, table.count, table.grad_type, int(bool(accumulate)), sumsq.data_ptr(),
                                      workspace.data_ptr(), _bytes(workspace), _stream(stream)))
 
@@ -502,12 +535,12 @@ def osdp_adamw_step(table: AdamWTable, *, lr: float, beta1: float = 0.9, beta2: 
                     grad_sumsq=None, max_norm: float = 0.0, seed: int = 0, step_device=None, lr_device=None, stream=None) -> None:
     """One AdamW step, in place.  ``grad_sumsq`` (one float64), ``step_device`` (one int64) and ``lr_device`` (one float32)
     are read on the GPU when the kernels run."""
-    if grad_sumsq is not None and (grad_sumsq.nbytes != 8 or grad_sumsq.numel() != 1 or not grad_sumsq.is_floating_point()):
-        _refuse("grad_sumsq must be one float64")
-    if step_device is not None and (step_device.nbytes != 8 or step_device.numel() != 1 or step_device.is_floating_point()):
-        _refuse("step_device must be one int64")
-    if lr_device is not None and (lr_device.nbytes != 4 or lr_device.numel() != 1 or not lr_device.is_floating_point()):
-        _refuse("lr_device must be one float32")
+    if grad_sumsq is not None and not _one(grad_sumsq, "torch.float64"):
+        _refuse("grad_sumsq must be one float64 on the GPU")
+    if step_device is not None and not _one(step_device, "torch.int64"):
+        _refuse("step_device must be one int64 on the GPU")
+    if lr_device is not None and not _one(lr_device, "torch.float32"):
+        _refuse("lr_device must be one float32 on the GPU")
     o = osdp_adamw_options(lr, beta1, beta2, eps, int(step), int(seed) & 0xFFFFFFFFFFFFFFFF, max_norm,
                            None if grad_sumsq is None else grad_sumsq.data_ptr(),
                            None if step_device is None else step_device.data_ptr(),
@@ -524,8 +557,8 @@ def osdp_adamw_state_values(table: AdamWTable, m_out, v_out, *, stream=None) -> 
         if len(outs) != table.count:
             _refuse(f"{len(outs)} {name} for {table.count} tensors")
         for i, t in enumerate(outs):
-            if t.numel() != table.lengths[i] or str(t.dtype) != "torch.bfloat16" or not t.is_contiguous():
-                _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values")
+            if t.numel() != table.lengths[i] or not _is(t, "torch.bfloat16") or not t.is_contiguous() or not t.is_cuda:
+                _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values on the GPU")
     _check(lib.osdp_adamw_state_values(table.tensors, table.count, _ptrs(m_out), _ptrs(v_out), _stream(stream)))
 
 
@@ -541,7 +574,7 @@ def osdp_split_linear_i8_quantize(I, O, w_shards, q_shards, w_scale, workspace, 
     shape = osdp_shape(0, I, O, N, 0)
     if len(q_shards) != N:
         _refuse(f"{len(q_shards)} q_shards for {N} w_shards")
-    if w_scale.nbytes < 4 * O:
+    if not _is(w_scale, "torch.float32") or w_scale.numel() < O or not w_scale.is_contiguous():
         _refuse(f"w_scale must hold {O} float32")
     _check(lib.osdp_split_linear_i8_quantize(ctypes.byref(shape), _ptrs(w_shards), _ptrs(q_shards), w_scale.data_ptr(),
                                              workspace.data_ptr(), _bytes(workspace), _stream(stream)))
@@ -558,9 +591,9 @@ def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=No
     """Y[T x O] = X[T x I] . W with W as int8 shards of Wq[O x I]; X, Y 2-D bf16 tensors (row stride = ld)."""
     T, I = X.shape
     O = Y.shape[1]
-    if X.stride(1) != 1 or Y.stride(1) != 1 or X.itemsize != 2 or Y.itemsize != 2 or Y.shape[0] != T:
+    if X.stride(1) != 1 or Y.stride(1) != 1 or not _is(X, "torch.bfloat16") or not _is(Y, "torch.bfloat16") or Y.shape[0] != T:
         _refuse("X and Y must be bf16 matrices of as many rows, with unit stride along them")
-    if w_scale.nbytes < 4 * O:
+    if not _is(w_scale, "torch.float32") or w_scale.numel() < O or not w_scale.is_contiguous():
         _refuse(f"w_scale must hold {O} float32")
     shape = osdp_shape(T, I, O, len(q_shards), k)
     _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), X.stride(0), _ptrs(q_shards), w_scale.data_ptr(),

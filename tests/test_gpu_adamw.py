@@ -501,3 +501,18 @@ def test_table_refusals():
         osdp.osdp_adamw_state_values(table, [t(4, torch.bfloat16)], [t(4, torch.bfloat16)])
     with pytest.raises(osdp.OsdpError):
         table.set_grads([t(5)])
+
+
+def test_tables_whose_tensors_share_memory():
+    t = lambda n: torch.zeros(n, device="cuda")  # noqa: E731
+    p, g, flat = t(64), t(64), t(256)
+    piece = lambda i, n=64: flat[i:i + n]  # noqa: E731
+    for kw in (dict(params=[p, p], grads=[g, t(64)], m=[t(64), t(64)], v=[t(64), t(64)]),            # listed twice
+               dict(params=[p], grads=[p], m=[t(64)], v=[t(64)]), dict(params=[p], grads=[g], m=[p], v=[t(64)]),
+               dict(params=[piece(0)], grads=[g], m=[piece(63)], v=[piece(128)]),                     # by one element
+               dict(params=[piece(0)], grads=[piece(191)], m=[piece(64)], v=[piece(128)])):
+        with pytest.raises(osdp.OsdpError, match="share memory"):
+            osdp.AdamWTable(**kw)
+    osdp.AdamWTable(params=[piece(0)], grads=[piece(192)], m=[piece(64)], v=[piece(128)])             # side by side
+    osdp.AdamWTable(params=[p, t(64)], grads=[g, g], m=[t(64), t(64)], v=[t(64), t(64)])              # read twice
+    osdp.AdamWTable(grads=[g, g])

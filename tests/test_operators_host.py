@@ -151,3 +151,50 @@ def test_the_binding_refuses_before_it_calls():
         osdp.AdamWTable(grads=[torch.zeros(4)])
     with pytest.raises(osdp.OsdpError):
         osdp.AdamWTable(grads=[torch.zeros(4)], params=[])
+
+
+def test_arrays_that_share_memory_are_found():
+    import random
+    rng = random.Random(3)
+    found = 0
+    for _ in range(2000):
+        spans = lambda k: [(rng.randrange(60), rng.randrange(9)) for _ in range(k)]  # noqa: E731
+        written, read = spans(rng.randrange(5)), spans(rng.randrange(4))
+        meet = lambda x, y: x[1] and y[1] and x[0] < sum(y) and y[0] < sum(x)  # noqa: E731
+        want = any(meet(x, y) for i, x in enumerate(written) for y in written[:i] + read)
+        assert B._overlap(written, read) == bool(want), (written, read)
+        found += bool(want)
+    assert 400 < found < 1600
+
+
+def test_the_binding_refuses_scalars_that_are_not_on_the_gpu():
+    import torch
+
+    class Table:
+        tensors, count, grad_type, param_type, state_bits, lengths = None, 0, 0, 0, 8, [4]
+    one = lambda kind: torch.ones(1, dtype=kind)  # noqa: E731
+    for kw in (dict(grad_sumsq=one(torch.float64)), dict(step_device=one(torch.int64)), dict(lr_device=one(torch.float32))):
+        with pytest.raises(osdp.OsdpError, match="on the GPU"):
+            osdp.osdp_adamw_step(Table, lr=1e-3, **kw)
+    with pytest.raises(osdp.OsdpError, match="on the GPU"):
+        osdp.osdp_adamw_grad_sumsq(Table, one(torch.float64), one(torch.uint8))
+    Table.count = 1
+    out = [torch.zeros(4, dtype=torch.bfloat16)]
+    with pytest.raises(osdp.OsdpError, match="on the GPU"):
+        osdp.osdp_adamw_state_values(Table, out, out)
+
+
+def test_the_binding_refuses_other_types_of_matrices():
+    import torch
+    z = lambda *n, d=torch.bfloat16: torch.zeros(*n, dtype=d)  # noqa: E731
+    q, scale, ws = [z(16 * 16, d=torch.int8)], z(16, d=torch.float32), z(1 << 16, d=torch.uint8)
+    for X, Y, s in ((z(2, 16, d=torch.float16), z(2, 16), scale), (z(2, 16), z(2, 16, d=torch.float16), scale), (z(2, 16), z(3, 16), scale),
+                    (z(16, 2).t(), z(2, 16), scale), (z(2, 16), z(2, 16), z(8, d=torch.float32)), (z(2, 16), z(2, 16), z(16, d=torch.float64)),
+                    (z(2, 16), z(2, 16), z(32, d=torch.float32)[::2])):
+        with pytest.raises(osdp.OsdpError) as e:
+            osdp.osdp_split_linear_i8_fwd(X, q, s, Y, 1, ws)
+        assert e.value.status == B.OSDP_ERR_INVALID_ARG
+    for w, qs, s in (([z(256)] * 2, q, scale), ([z(256)], q, z(15, d=torch.float32)), ([z(256)], q, z(16))):
+        with pytest.raises(osdp.OsdpError) as e:
+            osdp.osdp_split_linear_i8_quantize(16, 16, w, qs, s, ws)
+        assert e.value.status == B.OSDP_ERR_INVALID_ARG
