@@ -276,7 +276,7 @@ def test_extreme_sums_stay_exact():
 
 
 def test_halves_go_away_from_zero():
-    """All 256 x 127 quotients of significands, at every power of two that matters: none of them may be taken for the other side of a half."""
+    """Quotients of all significands by every sixteenth largest one, at eight powers of two: none may be taken for the other side of a half."""
     a = np.arange(128, 256)
     for b in range(128, 256):
         x = np.zeros((8, 144), np.float32)

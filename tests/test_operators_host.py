@@ -198,3 +198,18 @@ def test_the_binding_refuses_other_types_of_matrices():
         with pytest.raises(osdp.OsdpError) as e:
             osdp.osdp_split_linear_i8_quantize(16, 16, w, qs, s, ws)
         assert e.value.status == B.OSDP_ERR_INVALID_ARG
+
+
+def test_rounding_by_one_multiplication_and_one_addition_is_exact():
+    """trunc(fma(x, r, 1/2)), r = fp32(fp32(127 / amax) (1 + 2^-21)), against round(x * 127 / amax), halves upwards, in whole numbers: for every
+    significand of a bf16 x and amax at every power of two between them that leaves something."""
+    import numpy as np
+    a, b = np.meshgrid(np.arange(128, 256, dtype=np.int64), np.arange(128, 256, dtype=np.int64), indexing="ij")
+    r = (np.float32(127) / b.astype(np.float32)) * np.float32(1 + 2.0 ** -21)
+    assert r.dtype == np.float32
+    for j in range(12):
+        ok = a <= b * 2 ** j            # x = a 2^-j is no larger than amax = b
+        exact = (2 * 127 * a + b * 2 ** j) // (2 * b * 2 ** j)
+        t = (a * 2.0 ** -j * r.astype(np.float64) + 0.5).astype(np.float32)  # (32 bits of product and a half: exact in 64, rounded once)
+        assert (t.astype(np.int64) == exact)[ok].all(), j
+        assert t[ok].max() < 128
