@@ -438,7 +438,8 @@ OSDP_API osdp_status osdp_plan_search(const osdp_operator_cost *ops, int32_t n, 
  * is cut, v the upper 16, a bf16 parameter the upper 16 of h * 0x297A2D39.  Results are a function of the inputs alone.
  *
  * Tensors: any lengths (0 too) and, element by element, any alignment; exps must be 2-byte aligned.  The widest accesses are
- * used for those whose arrays are all 16-byte aligned (moments in 8 bits: 8-byte).  No two arrays of a call may overlap. */
+ * used for those whose arrays are all 16-byte aligned (moments in 8 bits: 8-byte).  No two arrays of a call may overlap.
+ * Where N does not divide I*O, n of the last shard leaves its padding out, which the backward pass does not write. */
 
 typedef enum { OSDP_BF16 = 0, OSDP_F32 = 1 } osdp_dtype;
 
