@@ -8,8 +8,8 @@
 // elements to a lane, so that a row of 16 lanes is one block of 128 that moments in 8 bits share a power of two over, and
 // its largest magnitude is found without leaving the row (four DPP steps, no LDS, no barrier).
 //
-// What bounds it: memory with moments in fp32 (78.7 million elements, 2.2 GB: 407 us, 5.4 TB/s) and with a master copy and moments in 8
-// bits (1.57 GB with their values read back: 291 us); without a master copy the 60 instructions that two codes, a random number and a
+// What bounds it: memory with moments in fp32 (78.7 million elements, 2.2 GB: 402 us, 5.5 TB/s) and with a master copy and moments in 8
+// bits (1.57 GB with their values read back: 283 us); without a master copy the 60 instructions that two codes, a random number and a
 // rounded parameter cost an element keep the vector units as busy as its 10 bytes keep memory (201 million elements: 375 us, 5.4 TB/s).  More waves to a SIMD would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
 #include <algorithm>
 #include <cmath>
@@ -39,11 +39,11 @@ struct Tensor {
   uint8_t *exps;
   int64_t n;
   float decay;          // weight_decay
-  uint32_t end_tile;    // tiles of this and all earlier tensors of the batch
 };
 
 struct Batch {
   Tensor t[kBatch];
+  uint32_t end[kBatch]; // tiles of this and all earlier tensors of the batch
   uint64_t wide;        // bit i: tensor i is aligned for 16-byte accesses
   int32_t count;
   uint32_t first;       // place of t[0] in the caller's array
@@ -84,16 +84,36 @@ __host__ __device__ inline double power(double base, int64_t n) {
   return r;
 }
 
-// Tensor and element of a tile: tensors are found by halving, on the scalar unit (the tile is common to the workgroup).
+// The tensor that a tile (the same in all lanes of a wave) belongs to: by halving, on the scalar unit.
 __device__ __forceinline__ int tensor_of(const Batch &b, uint32_t tile) {
   int lo = 0, hi = b.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if (tile < b.t[mid].end_tile) hi = mid;
+    if (tile < b.end[mid]) hi = mid;
     else lo = mid + 1;
   }
   return lo;
 }
+
+// The same where it is the greater part of the work: lane i holds the end of tensor i, and the ends that do not lie behind the tile are
+// counted.  (The arguments come from memory when a launch begins, and halving waits for it up to six times: sums of squares of 20 small
+// tensors 9.8 us, so 6.7; values of 78.7 million moments 72 us, 66.  The step itself, which is the slower for the register and whose waves wait for
+// much else, keeps halving: 78.7 million elements with moments in fp32 in 407 us, with a held end 419.)
+static_assert(kBatch <= 64, "a lane holds the end of a tensor");
+struct Ends {
+  uint32_t end;
+  __device__ __forceinline__ explicit Ends(const Batch &b) {
+    const int lane = threadIdx.x & 63;
+    end = lane < b.count ? b.end[lane < kBatch ? lane : 0] : ~0u;
+  }
+  // *from: the tile's first element in it
+  __device__ __forceinline__ int find(uint32_t tile, int64_t *from) const {
+    const int i = __popcll(__ballot(tile >= end));
+    const uint32_t start = i > 0 ? __builtin_amdgcn_readlane(end, i - 1) : 0u;
+    *from = static_cast<int64_t>(tile - start) * kTile;
+    return i;
+  }
+};
 
 // Element j of the lane's eight: side by side where a tile is read 16 bytes at a time; otherwise the lanes of a row of 16
 // take neighbouring elements, so that accesses of single elements still cover whole segments.  Either way a row is a block.
@@ -105,8 +125,8 @@ __device__ __forceinline__ uint32_t element(int j) {
 
 // A lane's eight elements as they lie in memory, asked for (load) apart from where they are taken to pieces (get), so that all of a
 // tile's loads are on their way before the first of them is waited for.  Wide loads and stores are marked as used once: nothing here
-// is touched again before far more than the caches hold has passed.  A step over 78.7 million elements with moments in fp32 takes 407 us
-// with the marks (5.4 TB/s) and 425 without, with moments in 8 bits 291 and 310; the sum of squares of 403 million 126 and 135.
+// is touched again before far more than the caches hold has passed.  A step over 78.7 million elements with moments in fp32 took 407 us
+// with the marks and 425 without, with moments in 8 bits 291 and 310; the sum of squares of 403 million 126 and 135.
 template <class T, bool kWide>
 struct Eight;
 
@@ -425,7 +445,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Batch b, Step s) {
     for (uint32_t tile = first; tile < end; ++tile) {
       const int i = tensor_of(b, tile);
       const Tensor t = b.t[i];
-      const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
+      const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.end[i - 1] : 0u)) * kTile;
       k.key = mix(mix(stirred ^ (b.first + static_cast<uint32_t>(i))) ^ static_cast<uint32_t>(at >> 32));
       if (((b.wide >> i) & 1u) && t.n - at >= kTile) adamw_tile<Grad, kForm, kState8, true>(t, s, k, at);
       else adamw_tile<Grad, kForm, kState8, false>(t, s, k, at);
@@ -454,10 +474,11 @@ __device__ __forceinline__ void values_tile(const Tensor &t, int64_t at) {
 }
 
 __global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
+  const Ends ends(b);
   for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
-    const int i = tensor_of(b, tile);
+    int64_t at;
+    const int i = ends.find(tile, &at);
     const Tensor t = b.t[i];
-    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile;
     if (((b.wide >> i) & 1u) && t.n - at >= kTile) values_tile<true>(t, at);
     else values_tile<false>(t, at);
   }
@@ -467,8 +488,8 @@ __global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
 // Squares and sums are in double from the first product on (a bf16 gradient of 1e20 is one, its square in fp32 is not): the
 // vector unit multiplies and adds them as fast as fp32, and the pass stays bound by memory.
 constexpr int kSumBlocks = 1024;  // workgroups, and so partial sums, of a launch at most
-constexpr int kSumTiles = 4;      // tiles that a workgroup has on their way at a time, where there are enough for all: 806 MB in 126 us
-                                  // (6.4 TB/s); one tile at a time takes half as long again
+constexpr int kSumTiles = 4;      // tiles that a workgroup has on their way at a time, where there are enough for all: 806 MB in 123 us
+                                  // (6.6 TB/s); one tile at a time takes half as long again
 
 template <int kThreads = osdp::kThreads>
 __device__ __forceinline__ double block_sum(double x) {
@@ -491,11 +512,11 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum = fma(static_cast<double>(g[j]), static_cast<double>(g[j]), sum);
   };
+  const Ends ends(b);
   for (uint32_t first = blockIdx.x * run; first < b.tiles; first += gridDim.x * run) {
     const uint32_t end = min(first + run, b.tiles);
-    int i = tensor_of(b, first);
-    const int64_t start = i > 0 ? b.t[i - 1].end_tile : 0;
-    const int64_t at = (first - start) * kTile;
+    int64_t at;
+    int i = ends.find(first, &at);
     float g[8];
     if (run == kSumTiles && first + kSumTiles <= b.tiles && ((b.wide >> i) & 1u) && b.t[i].n - at >= kSumTiles * kTile) {
       Eight<Grad, true> x[kSumTiles];
@@ -509,8 +530,9 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, 
       continue;
     }
     for (uint32_t tile = first; tile < end; ++tile) {
-      i = tensor_of(b, tile);
-      const int64_t from = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile, rest = b.t[i].n - from;
+      int64_t from;
+      i = ends.find(tile, &from);
+      const int64_t rest = b.t[i].n - from;
       if (((b.wide >> i) & 1u) && rest >= kTile) {
         Eight<Grad, true> x;
         x.load(b.t[i].grad, from, kTile);
@@ -531,14 +553,16 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, 
 constexpr int kSmallThreads = 4 * kThreads;
 template <class Grad>
 __global__ __launch_bounds__(kSmallThreads) void sumsq_small_kernel(Batch b, int32_t accumulate, double *__restrict__ out) {
+  const Ends ends(b);
   double sum = 0.0;
   for (uint32_t first = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads); first < b.tiles; first += 4 * kSumTiles) {
     float g[kSumTiles][8];
 #pragma unroll
     for (int u = 0; u < kSumTiles; ++u) {
       const uint32_t tile = min(first + 4 * u, b.tiles - 1);
-      const int i = tensor_of(b, tile);
-      const int64_t from = static_cast<int64_t>(tile - (i > 0 ? b.t[i - 1].end_tile : 0u)) * kTile, rest = b.t[i].n - from;
+      int64_t from;
+      const int i = ends.find(tile, &from);
+      const int64_t rest = b.t[i].n - from;
       if (((b.wide >> i) & 1u) && rest >= kTile) {
         Eight<Grad, true> x;
         x.load(b.t[i].grad, from, kTile);
@@ -641,7 +665,7 @@ osdp_status for_batches(const osdp_adamw_tensor *tensors, int32_t count, Fill &&
     t.n = tensors[i].n;
     if (fill(i, &t)) b.wide |= 1ull << b.count;
     b.tiles += static_cast<uint32_t>(tiles);
-    t.end_tile = b.tiles;
+    b.end[b.count] = b.tiles;
     ++b.count;
     last = i;
   }
@@ -656,10 +680,14 @@ hipError_t launch_adamw(const Batch &b, const Step &s, hipStream_t stream) {
   // Every wave works the call's scalars out for itself, 40 to 250 operations.  Where arithmetic is the bound and there are workgroups enough
   // (from 6144 tiles on; fewer leave compute units idle at the end), one takes four tiles, so that they weigh less: 201 million elements in
   // 375 us, with the step on the device 406, one tile to a workgroup 458 and 535.  The other forms are bound by memory and are the
-  // slower for it (78.7 million elements, master copy: moments in 8 bits 312 us instead of 291, in fp32 442 instead of 407).
+  // slower for it (78.7 million elements, master copy: moments in 8 bits 312 us instead of 291, in fp32 425 instead of 402).
+  // With moments in fp32 a launch asks for 64 KB of LDS that it does not use, so that no more than two workgroups run on a compute
+  // unit: their loads keep memory busy, and with more of them its reads and writes, to eight arrays, get in one another's way.  us
+  // with eight / three / two workgroups: 78.7 million elements with master copies 414 / 403 / 402, 201 million 1068 / 1035 / 989, bf16 alone 940 / 843 /
+  // 807, fp32 parameters 980 / 952 / 918, 12.6 million 66 / 65 / 66.  With moments in 8 bits the arithmetic needs the four that registers leave room for.
   Batch batch = b;
   batch.run = kForm == kBf16 && kState8 && b.tiles >= 6144 ? 4 : 1;
-  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(batch, batch.run)), dim3(kThreads), 0, stream, batch, s);
+  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(batch, batch.run)), dim3(kThreads), kState8 ? 0 : 64 << 10, stream, batch, s);
   return hipGetLastError();
 }
 
