@@ -266,9 +266,11 @@ __device__ __forceinline__ float decode(uint32_t code, uint32_t b, uint32_t nan)
 __device__ __forceinline__ uint32_t nan_bits(uint32_t b) { return b == 255u ? 0x7fc00000u : 0u; }
 
 // The power of two of a block whose largest magnitude has these bits: rounding up to 3 fraction bits may carry into the
-// next binade, or (FLT_MAX) out of the numbers, like a NaN or an infinity.
+// next binade, or (FLT_MAX) out of the numbers, like an infinity and a NaN, whatever its sign and payload.
 template <int kLow>
-__device__ __forceinline__ uint32_t block_exponent(uint32_t most) { return max((most + 0xfffffu) >> 23, static_cast<uint32_t>(kLow)); }
+__device__ __forceinline__ uint32_t block_exponent(uint32_t most) {
+  return max((min(most, 0x7f800000u) + 0xfffffu) >> 23, static_cast<uint32_t>(kLow));
+}
 
 // Codes of eight values (magnitudes' bits) of a block, rounded with 16 random bits each, from bit kShift of h on.  Above the smallest
 // binade the random bits are added below the last fraction bit and the sum is cut: a carry runs into the exponent as it should,

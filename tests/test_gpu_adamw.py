@@ -292,6 +292,32 @@ def test_numbers_that_are_none_stay_in_their_block():
                 assert torch.isnan(o[256:384]).all() and torch.isfinite(o[:256]).all() and torch.isfinite(o[384:]).all()
 
 
+@pytest.mark.parametrize("gap", [0, 3])
+@pytest.mark.parametrize("param,grad", [("bf16", "bf16"), ("bf16", "f32"), ("master", "f32"), ("f32", "f32"), ("master", "bf16")])
+def test_not_a_number_of_any_sign_and_payload(param, grad, gap):
+    """In 8 bits: the element's parameter is NaN, its block's powers say so and its codes are zeros; all else is as without it."""
+    c = Case([4096, 700], 8, param, grad, gap, seed=6)
+    at = [5, 128 + 127, 1280, 2047, 3500]
+    patterns = [0xFFFFFFFF, 0x7FFFFFFF, 0xFF800001, 0xFFC00000, 0x7FA00000]
+    whole = c.grad.view(torch.int32 if grad == "f32" else torch.int16)
+    for i, b in zip(at, patterns):
+        if grad == "bf16":
+            b = (b >> 16) | (1 if b & 0xFFFF else 0)
+        whole[c.start[0] + i] = b - (1 << (32 if grad == "f32" else 16)) if b >> (31 if grad == "f32" else 15) else b
+    assert c.grad.isnan().sum() == len(at)
+    c.before["grads"] = c.grad.clone()
+    osdp.osdp_adamw_step(c.table, lr=1e-3, step=3, seed=2)
+    torch.cuda.synchronize()
+    m, v, e = c.part("m", 0), c.part("v", 0), c.exps[0].cpu().numpy()
+    blocks = sorted({i // 128 for i in at})
+    assert sorted(np.flatnonzero(e[:, 0] == 255)) == blocks and sorted(np.flatnonzero(e[:, 1] == 255)) == blocks
+    for b in blocks:
+        assert not m[b * 128:b * 128 + 128].any() and not v[b * 128:b * 128 + 128].any()
+    for name in ("params", "masters") if param == "master" else ("params",):
+        assert sorted(np.flatnonzero(np.isnan(c.part(name, 0)))) == at
+        assert not np.isnan(c.part(name, 1)).any()
+
+
 @pytest.mark.parametrize("gap", [0, 5])
 def test_state_values_are_the_codes_values(gap):
     c = Case([1, 127, 128, 300, 4096, 0, 2051], 8, "bf16", gap=gap)
