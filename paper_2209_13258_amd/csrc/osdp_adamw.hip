@@ -9,8 +9,8 @@
 // its largest magnitude is found without leaving the row (four DPP steps, no LDS, no barrier).
 //
 // What bounds it: memory with moments in fp32 (78.7 million elements, 2.2 GB: 402 us, 5.5 TB/s) and with a master copy and moments in 8
-// bits (1.57 GB with their values read back: 283 us); without a master copy the 60 instructions that two codes, a random number and a
-// rounded parameter cost an element keep the vector units as busy as its 10 bytes keep memory (201 million elements: 375 us, 5.4 TB/s).  More waves to a SIMD would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
+// bits (1.57 GB with their values read back: 283 us); without a master copy the 55 instructions that two codes, a random number and a
+// rounded parameter cost an element keep the vector units as busy as its 10 bytes keep memory (201 million elements: 359 us, 5.6 TB/s).  More waves to a SIMD would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
@@ -226,10 +226,11 @@ __device__ __forceinline__ void store8(uint16_t *p, int64_t at, uint32_t left, c
   }
 }
 
+// bytes, and the bits of low and high (four bytes each) besides
 template <bool kWide>
-__device__ __forceinline__ void store8(uint8_t *p, int64_t at, uint32_t left, const uint32_t (&x)[8]) {
+__device__ __forceinline__ void store8(uint8_t *p, int64_t at, uint32_t left, const uint32_t (&x)[8], uint32_t low = 0, uint32_t high = 0) {
   if constexpr (kWide) {
-    uint2 w = {0u, 0u};
+    uint2 w = {low, high};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       w.x |= x[j] << (8 * j);
@@ -239,7 +240,7 @@ __device__ __forceinline__ void store8(uint8_t *p, int64_t at, uint32_t left, co
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (element<false>(j) < left) p[at + element<false>(j)] = static_cast<uint8_t>(x[j]);
+      if (element<false>(j) < left) p[at + element<false>(j)] = static_cast<uint8_t>(x[j] | (j < 4 ? low : high) >> 8 * (j & 3));
   }
 }
 
@@ -259,9 +260,8 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
 // is 0 fp32 reads them as it reads its own smallest numbers, which is what the format wants.  nan: a quiet NaN's bits for a block that is none, else 0.
 template <int kTop>
 __device__ __forceinline__ float decode(uint32_t code, uint32_t b, uint32_t nan) {
-  const uint32_t magnitude = kTop == 15 ? code & 127u : code;
-  const float x = __builtin_amdgcn_ldexpf(__uint_as_float((magnitude << 20) | nan), static_cast<int>(b) - kTop);
-  return kTop == 15 ? __uint_as_float(__float_as_uint(x) | ((code & 128u) << 24)) : x;
+  const uint32_t placed = kTop == 15 ? static_cast<uint32_t>(static_cast<int32_t>(code << 24) >> 4) & 0x87f00000u : code << 20;
+  return __builtin_amdgcn_ldexpf(__uint_as_float(placed | nan), static_cast<int>(b) - kTop);
 }
 __device__ __forceinline__ uint32_t nan_bits(uint32_t b) { return b == 255u ? 0x7fc00000u : 0u; }
 
@@ -276,8 +276,9 @@ __device__ __forceinline__ uint32_t block_exponent(uint32_t most) {
 // binade the random bits are added below the last fraction bit and the sum is cut: a carry runs into the exponent as it should,
 // and never beyond the block's own largest code.  A lane that has a value in the smallest binade (one in 10^4 of a bell curve's; zeros) takes
 // the general way, which is three times as long: in units of its binade's step a magnitude is x in [0, 16), and x plus the fraction is cut.
+// A block that is none (b = 255) has zeros for codes; true is returned where it has not.
 template <int kTop, int kShift>
-__device__ __forceinline__ void encode8(const uint32_t (&size)[8], uint32_t b, const uint32_t (&h)[8], uint32_t (&code)[8]) {
+__device__ __forceinline__ bool encode8(const uint32_t (&size)[8], uint32_t b, const uint32_t (&h)[8], uint32_t (&code)[8]) {
   const uint32_t least = b - (kTop - 1);
   uint32_t smallest = size[0];
 #pragma unroll
@@ -286,7 +287,8 @@ __device__ __forceinline__ void encode8(const uint32_t (&size)[8], uint32_t b, c
     const uint32_t r = kShift ? (h[j] >> 12) & 0xffff0u : (h[j] & 0xffffu) << 4;
     code[j] = ((size[j] + r) >> 20) - (least - 1) * 8u;
   }
-  if (smallest < least << 23) {
+  const bool number = b != 255u;
+  if (smallest < least << 23 || !number) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t e = max(size[j] >> 23, least);
@@ -294,8 +296,17 @@ __device__ __forceinline__ void encode8(const uint32_t (&size)[8], uint32_t b, c
       const uint32_t q = static_cast<uint32_t>(fmaf(static_cast<float>((h[j] >> kShift) & 0xffffu), 0x1p-16f, units));
       code[j] = (e - least) * 8u + q;
       if (kTop == 31) code[j] = max(code[j], min(size[j], 1u));  // (a positive v stays positive)
+      if (!number) code[j] = 0u;
     }
   }
+  return number;
+}
+
+// The upper bytes of four values: their signs, where codes have them, and other bits.
+__device__ __forceinline__ uint32_t signs_of(const float *m) {
+  const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(m[1]), __float_as_uint(m[0]), 0x0c0c0703u);
+  const uint32_t high = __builtin_amdgcn_perm(__float_as_uint(m[3]), __float_as_uint(m[2]), 0x07030c0cu);
+  return low | high;
 }
 
 struct Scalars {
@@ -366,23 +377,18 @@ __device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const
     for (int j = 0; j < 8; ++j) {
       if (!kWide && element<kWide>(j) >= left) m[j] = v[j] = 0.f;  // (0 * beta is NaN where the block was)
       sm[j] = __float_as_uint(m[j]) & 0x7fffffffu;
-      sv[j] = __float_as_uint(v[j]) & 0x7fffffffu;
+      sv[j] = __float_as_uint(v[j]);  // (no sign, but of a NaN)
       most_m = max(most_m, sm[j]);
       most_v = max(most_v, sv[j]);
     }
     most_m = row_max(most_m);
     most_v = row_max(most_v);
     const uint32_t bm = block_exponent<32>(most_m), bv = block_exponent<48>(most_v);
-    encode8<15, 0>(sm, bm, h, cm);
+    const uint32_t signs = encode8<15, 0>(sm, bm, h, cm) ? 0x80808080u : 0u;
     encode8<31, 16>(sv, bv, h, cv);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      cm[j] = bm == 255u ? 0u : cm[j] | ((__float_as_uint(m[j]) >> 24) & 128u);
-      cv[j] = bv == 255u ? 0u : cv[j];
-    }
     if ((threadIdx.x & 15) == 0 && block)
       *exps = static_cast<uint16_t>((most_m ? bm : 0u) | (most_v ? bv << 8 : 0u));
-    store8<kWide>(static_cast<uint8_t *>(t.m), at, left, cm);
+    store8<kWide>(static_cast<uint8_t *>(t.m), at, left, cm, signs_of(m) & signs, signs_of(m + 4) & signs);
     store8<kWide>(static_cast<uint8_t *>(t.v), at, left, cv);
   } else {
     store8<kWide>(static_cast<float *>(t.m), at, left, m);
@@ -396,9 +402,10 @@ __device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       // without a master copy to one of its neighbours, the one above with the probability that keeps the mean (an infinity
-      // keeps its upper half whatever is added, a NaN might not)
+      // keeps its upper half whatever is added, and so does a NaN whose lower half is 0, as any is that comes from bf16 or from a
+      // block; another might not)
       if constexpr (kForm == kMaster) w[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(p[j]))) << 16;
-      else w[j] = __float_as_uint(p[j]) + (p[j] == p[j] ? (h[j] * 0x297A2D39u) >> 16 : 0u);
+      else w[j] = __float_as_uint(p[j]) + ((kState8 && sizeof(Grad) == 2) || p[j] == p[j] ? (h[j] * 0x297A2D39u) >> 16 : 0u);
     }
     store8<kWide>(static_cast<uint16_t *>(t.param), at, left, w);
   }
@@ -681,15 +688,18 @@ template <class Grad, int kForm, bool kState8>
 hipError_t launch_adamw(const Batch &b, const Step &s, hipStream_t stream) {
   // Every wave works the call's scalars out for itself, 40 to 250 operations.  Where arithmetic is the bound and there are workgroups enough
   // (from 6144 tiles on; fewer leave compute units idle at the end), one takes four tiles, so that they weigh less: 201 million elements in
-  // 375 us, with the step on the device 406, one tile to a workgroup 458 and 535.  The other forms are bound by memory and are the
+  // 375 us, with the step on the device 406, one tile to a workgroup 458 and 535 (359 and 380 since codes take fewer operations).  The other forms are bound by memory and are the
   // slower for it (78.7 million elements, master copy: moments in 8 bits 312 us instead of 291, in fp32 425 instead of 402).
-  // With moments in fp32 a launch asks for 64 KB of LDS that it does not use, so that no more than two workgroups run on a compute
-  // unit: their loads keep memory busy, and with more of them its reads and writes, to eight arrays, get in one another's way.  us
-  // with eight / three / two workgroups: 78.7 million elements with master copies 414 / 403 / 402, 201 million 1068 / 1035 / 989, bf16 alone 940 / 843 /
-  // 807, fp32 parameters 980 / 952 / 918, 12.6 million 66 / 65 / 66.  With moments in 8 bits the arithmetic needs the four that registers leave room for.
+  // With moments in fp32 a launch asks for LDS that it does not use, so that no more than two workgroups run on a compute unit, or three where
+  // the scalars, and with them the wait before a tile's loads, are longer (step or rate on the device): their loads keep memory busy, and
+  // with more of them its reads and writes, to eight arrays, get in one another's way.  us with eight / three / two workgroups, and with the step on
+  // the device: 201 million elements with master copies 1069 / 1035 / 992 and 1074 / 1028 / 1138, bf16 alone 947 / 846 / 809 and 945 / 828 / 949, fp32
+  // parameters 983 / 951 / 921 and 986 / 937 / 1066; 78.7 million with master copies 415 / 403 / 402, 6.3 million 35 / 34 / 34 and 37 / 36 / 41.
+  // With moments in 8 bits the arithmetic needs the five that registers leave room for.
+  const unsigned lds = kState8 ? 0 : s.step_device || s.lr_device ? 52 << 10 : 64 << 10;
   Batch batch = b;
   batch.run = kForm == kBf16 && kState8 && b.tiles >= 6144 ? 4 : 1;
-  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(batch, batch.run)), dim3(kThreads), kState8 ? 0 : 64 << 10, stream, batch, s);
+  hipLaunchKernelGGL((adamw_kernel<Grad, kForm, kState8>), dim3(grid_of(batch, batch.run)), dim3(kThreads), lds, stream, batch, s);
   return hipGetLastError();
 }
 
@@ -701,7 +711,8 @@ hipError_t launch_adamw(int form, bool state8, const Batch &b, const Step &s, hi
 }
 
 // Workgroups, and so partial sums, of the launch over a batch.
-// A call of so few tiles, in one batch, is the small kernel's: at 16 tiles a round, of two microseconds, it is the faster one up to two rounds.
+// A call of so few tiles, in one batch, is the small kernel's, at 16 tiles a round: us captured / called 32 tiles 4.7 / 4.8, two launches 4.4 / 7.1; 48 tiles 6.0 / 6.1
+// and 4.4 / 7.0.
 constexpr uint32_t kSmallTiles = 32;
 uint32_t sum_run(const Batch &b) { return b.tiles >= kSumTiles * kSumBlocks ? kSumTiles : 1; }
 unsigned sum_blocks(const Batch &b) { return std::min<unsigned>(b.tiles, kSumBlocks); }
