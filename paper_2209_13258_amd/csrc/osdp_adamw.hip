@@ -95,10 +95,10 @@ __device__ __forceinline__ int tensor_of(const Batch &b, uint32_t tile) {
   return lo;
 }
 
-// The same where it is the greater part of the work: lane i holds the end of tensor i, and the ends that do not lie behind the tile are
-// counted.  (The arguments come from memory when a launch begins, and halving waits for it up to six times: sums of squares of 20 small
-// tensors 9.8 us, so 6.7; values of 78.7 million moments 72 us, 66.  The step itself, which is the slower for the register and whose waves wait for
-// much else, keeps halving: 78.7 million elements with moments in fp32 in 407 us, with a held end 419.)
+// The same for sums of squares, which do little else: lane i holds the end of tensor i, and the ends that do not lie behind the tile are
+// counted.  (The arguments come from memory when a launch begins, and halving waits for it up to six times: 20 small tensors 9.8 us, so
+// 6.7.)  The step and the values, whose waves wait for more, are the slower for the register: 78.7 million elements with moments in fp32 407 us,
+// with a held end 419; values of 201 million 200 and 207.
 static_assert(kBatch <= 64, "a lane holds the end of a tensor");
 struct Ends {
   uint32_t end;
@@ -483,10 +483,9 @@ __device__ __forceinline__ void values_tile(const Tensor &t, int64_t at) {
 }
 
 __global__ __launch_bounds__(kThreads) void values_kernel(Batch b) {
-  const Ends ends(b);
   for (uint32_t tile = blockIdx.x; tile < b.tiles; tile += gridDim.x) {
-    int64_t at;
-    const int i = ends.find(tile, &at);
+    const int i = tensor_of(b, tile);
+    const int64_t at = static_cast<int64_t>(tile - (i > 0 ? b.end[i - 1] : 0u)) * kTile;
     const Tensor t = b.t[i];
     if (((b.wide >> i) & 1u) && t.n - at >= kTile) values_tile<true>(t, at);
     else values_tile<false>(t, at);
