@@ -119,17 +119,29 @@ struct I8Row {
   }
 };
 
+// Rows of the weight that lie a multiple of 4 KB apart are asked for from the same few memory channels by all workgroups at a time, unless
+// these begin at different places of the reduction and go round.
+constexpr int kI8Turn = 4096;
+
+// Where a workgroup of the kernels for few tokens begins, whose waves take kSpan bytes of a row together: 32 workgroups that follow one
+// another, four to an XCD, at one place, the next 32 behind it.  One token, weight from memory: 4096 -> 16384 17.6 us, so 14.6; 8192 -> 32768 50.5
+// and 47.0, 16384 -> 16384 55.4 and 53.3, 24576 -> 8192 46.5 and 42.2; where neighbours, which run on different XCDs, differ instead: 15.3, 54.5, 72.8 and 47.8.
+template <int kSpan>
+__device__ __forceinline__ int i8_first(int I) {
+  return I % kI8Turn == 0 ? static_cast<int>(blockIdx.x >> 5) % ((I + kSpan - 1) / kSpan) * kSpan : 0;
+}
+
 // What the two kernels below have in common: a workgroup owns 16 output channels and 16 tokens; its kWaves waves share the
 // reduction, 64 * kUnroll bytes of every row at a time, and add their sums up in LDS (integers: in any order).  Weights go from memory
 // to registers, each lane 16 bytes of a row, the four lanes of a row 64 in sequence; nothing of them is used twice, so nothing is
 // staged.  Both are bound by the weight's bytes.
 //
-// Tokens that are in 8 bits already.  16 tokens, 4096 -> 16384, rounded in a launch before it: 25 us in all, 2.7 TB/s (2 tokens 17.5, 3.8);
-// where rows run over the ends of shards 28.  32 or 64 channels to a workgroup, which read the tokens half or a quarter as often, take
-// 22 and 25 there but 20 to 31 instead of 15 for 10240 -> 2560, whose workgroups then leave half the card or more idle.
+// Tokens that are in 8 bits already.  4 tokens, 4096 -> 16384, rounded in a launch before it: 18.0 us in all, 3.7 TB/s.  32 or 64 channels to a
+// workgroup, which read the tokens half or a quarter as often, took 22 and 25 us where 16 took 25 (16 tokens), but 20 to 31 instead of 15 for
+// 10240 -> 2560, whose workgroups then leave half the card or more idle.
 template <int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
-  constexpr int kStep = 64 * kUnroll;
+  constexpr int kStep = 64 * kUnroll, kSpan = kWaves * kStep;
   __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
   __shared__ int sums[16 * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
@@ -141,19 +153,24 @@ __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
   const I8Row<kFlat> weight(p, tab, min(n0 + l16, p.O - 1));
   const uint8_t *token = p.xq + static_cast<int64_t>(min(m0 + l16, p.T - 1)) * p.ldq;
   i32x4 acc = {0, 0, 0, 0};
-  for (int k0 = wave * kStep; k0 < p.I; k0 += kWaves * kStep) {
+  auto step = [&](int k0) {
     uint4 w[kUnroll], x[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int k = k0 + 64 * u + 16 * q4;
       w[u] = weight.load(k < p.I ? k : 0);  // beyond the row's end: any weights, the tokens are zeros there
       x[u] = load_global16(token + (k < p.ldq ? k : p.ldq - 16));
-      if (k >= p.ldq) x[u] = uint4{0u, 0u, 0u, 0u};
     }
+    __builtin_amdgcn_sched_barrier(0);  // (all of them on their way before the first is waited for)
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+    for (int u = 0; u < kUnroll; ++u) {
+      if (k0 + 64 * u + 16 * q4 >= p.ldq) x[u] = uint4{0u, 0u, 0u, 0u};
       acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u]), __builtin_bit_cast(i32x4, x[u]), acc, 0, 0, 0);
-  }
+    }
+  };
+  const int first = i8_first<kSpan>(p.I);
+  for (int k0 = first + wave * kStep; k0 < p.I; k0 += kSpan) step(k0);
+  for (int k0 = wave * kStep; k0 < first; k0 += kSpan) step(k0);
 #pragma unroll
   for (int i = 0; i < 4; ++i) atomicAdd(&sums[l16 * 16 + 4 * q4 + i], acc[i]);
   __syncthreads();
@@ -165,10 +182,11 @@ __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
 
 // The same with the tokens' rounding in the launch, for tokens of so few features that the bytes of 16 of them fit in LDS and
 // that every workgroup may well round its 16 for itself: one launch instead of two, the first weights on their way meanwhile.
-// One token, 4096 -> 16384: 14.9 us in one launch, 16.8 in two, one call behind another; 15.7 with the weight from memory (4.3 TB/s).
+// One token, 4096 -> 16384: 14.9 us in one launch, 16.8 in two, one call behind another, before both began at different places; 14.0 since, with
+// the weight from memory (4.8 TB/s).
 template <int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, const uint16_t *__restrict__ x, int64_t ldx) {
-  constexpr int kStep = 64 * kUnroll;
+  constexpr int kStep = 64 * kUnroll, kSpan = kWaves * kStep;
   extern __shared__ __attribute__((aligned(16))) uint8_t rows[];  // [T][ldq + 16]: 16 rows fall into 16 different bank groups
   __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
   __shared__ int sums[16 * 16];
@@ -188,8 +206,9 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
       w[u] = weight.load(k < p.I ? k : 0);  // beyond the row's end: any weights, the tokens are zeros there
     }
   };
+  const int first = i8_first<kSpan>(p.I);
   uint4 w[kUnroll];
-  load(wave * kStep, w);
+  load(first + wave * kStep, w);
   // tokens to 8 bits: a row to a wave, or (fewer tokens than waves) to as many waves as there are for it
   const int share = tokens >= kWaves ? 1 : kWaves / tokens, part = wave % share;
   for (int t = wave / share; t < tokens; t += kWaves / share) {
@@ -211,15 +230,18 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
   __syncthreads();
   const uint8_t *token = rows + min(l16, tokens - 1) * pitch + 16 * q4;
   i32x4 acc = {0, 0, 0, 0};
-  for (int k0 = wave * kStep; k0 < p.I; k0 += kWaves * kStep) {
+  for (int at = first;;) {  // (the kSpan bytes that the waves are at)
+    const int k0 = at + wave * kStep;
+    at = at + kSpan < p.I ? at + kSpan : 0;
     uint4 next[kUnroll];
-    if (k0 + kWaves * kStep < p.I) load(k0 + kWaves * kStep, next);
+    if (at != first) load(at + wave * kStep, next);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       if (k0 + 64 * u >= p.I) break;
       const i32x4 a = *reinterpret_cast<const i32x4 *>(token + k0 + 64 * u);
       acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u]), a, acc, 0, 0, 0);
     }
+    if (at == first) break;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) w[u] = next[u];
   }

@@ -6,7 +6,7 @@
 // at twice the products.
 //
 // What bounds them: 4096 tokens 8192 -> 32768 on walking tiles of 256 x 256 take 850 us (2.6e15 operations a second) with random
-// integers and 764 with zeros, so the card's power, not the schedule; 33 tokens of the same weight on tiles of 64 x 64 take 57 us (4.7 TB/s),
+// integers and 764 with zeros, so the card's power, not the schedule; 33 tokens of the same weight on tiles of 64 x 64 take 48 us (5.6 TB/s),
 // the weight's bytes; 500 tokens 2560 -> 10240, 320 tiles of 128 x 128 on 256 compute units, 21 us for the 13 that their
 // operations cost a full card: the second round of tiles.
 #pragma once
@@ -149,7 +149,13 @@ __device__ __forceinline__ void i8_store_tile(const I8Tiles &p, const I8Scales<M
 // part of its reduction, to a workgroup and loads further ahead.  The parts of a tile meet in memory: each writes its sums, and
 // the last one to arrive (a counter says which; nobody waits) adds the others' to its own and stores the tile.  They are
 // consecutive workgroups of one XCD, whose L2 then holds all of it.
-template <int MB, int NB, int kSlots>
+//
+// kTurn (with more than two slots, where the weight's bytes are the bound): a workgroup begins at another block of the reduction than those of
+// the next columns and takes the blocks ahead of it at the end (see kI8Turn).  us: 33 tokens 8192 -> 32768 59.1, with turns 52.9; 16384 -> 16384
+// 63.2 and 56.1, 24576 -> 8192 48.6 and 49.4; 100 tokens 8192 -> 32768 65.3 and 54.4.  Not so rows that lie apart otherwise, 33 tokens 6144 -> 24576
+// 36.4 and 37.2, or several rows of tiles, of which those of a column are to read the same weights at a time: 160 tokens 4096 -> 4096 14.3 and
+// 15.5, 1000 26.2 and 27.6.
+template <int MB, int NB, int kSlots, bool kTurn>
 __device__ __forceinline__ void i8_w4_tiles(const I8Tiles &p) {
   constexpr int WM = 16 * MB, WN = 16 * NB, BM = 2 * WM, BN = 2 * WN;
   using OpA = W4Operand<true, MB>;
@@ -179,19 +185,30 @@ __device__ __forceinline__ void i8_w4_tiles(const I8Tiles &p) {
   const int nb = (K + 63) / 64;
   const int my_tiles = kSlots == 2 ? __builtin_amdgcn_readfirstlane((tiles - first + G - 1) / G) : 1;
 
-  int lt = first;
+  static_assert(!kTurn || kSlots > 2);
+  int lt = first, turn = 0;  // (blocks that are left for the end)
+  if constexpr (kTurn) {
+    int tm, tn;
+    tile_of_pid(first, tiles_m, tiles_n, &tm, &tn);
+    turn = __builtin_amdgcn_readfirstlane(tn % nb);
+  }
   I8Source<OpA, OpB, BM, BN> src;
-  auto load_tile = [&](int tile) {
+  auto load_tile = [&](int tile, int from, int length) {
     int tm, tn;
     tile_of_pid(tile, tiles_m, tiles_n, &tm, &tn);
-    src.begin(p, tm * BM, tn, k0, K, wave, lane);
+    src.begin(p, tm * BM, tn, k0 + from, length, wave, lane);
   };
+  int length = K - turn * 64;  // of the reduction that the source is at
   auto block_issued = [&]() {
     if (kSlots == 2 && src.block + 1 == nb && lt + G < tiles) {
       lt += G;
-      load_tile(lt);
+      load_tile(lt, 0, K);
+    } else if (kTurn && turn > 0 && src.block + 1 == src.nb) {
+      length = turn * 64;
+      turn = 0;
+      load_tile(lt, 0, length);
     } else {
-      src.next(K, wave, lane);
+      src.next(length, wave, lane);
     }
   };
   const uint32_t lds_base = lds_address(smem);
@@ -227,7 +244,7 @@ __device__ __forceinline__ void i8_w4_tiles(const I8Tiles &p) {
     });
   };
 
-  load_tile(lt);
+  load_tile(lt, turn * 64, length);
   static_for<kAhead>([&](auto b) {
     static_for<L>([&](auto i) { issue(decltype(b)::value, i); });
     block_issued();
@@ -333,10 +350,10 @@ __device__ __forceinline__ void i8_w4_tiles(const I8Tiles &p) {
   }
 }
 
-template <int MB, int NB, int kSlots>
+template <int MB, int NB, int kSlots, bool kTurn>
 __global__ __launch_bounds__(256, kSlots * (32 * (MB + NB) * 128) <= 80 * 1024 ? 2 : 1)
 void i8_w4_kernel(I8Tiles p) {
-  i8_w4_tiles<MB, NB, kSlots>(p);
+  i8_w4_tiles<MB, NB, kSlots, kTurn>(p);
 }
 
 constexpr int kI8Cus = 256;
@@ -344,9 +361,11 @@ constexpr int kI8Cus = 256;
 // Columns of tiles of BN channels that cover all shards.
 inline int64_t i8_shard_tiles(int64_t rows_each, int BN) { return ((rows_each % 8 ? rows_each + 7 : rows_each) + BN - 1) / BN; }
 
-template <int MB, int NB, int kSlots>
+template <int MB, int NB, int kSlots, bool kTurn = false>
 hipError_t launch_i8_tiles(const I8Problem &p, int parts, hipStream_t stream) {
   constexpr int BM = 32 * MB, BN = 32 * NB, kLds = kSlots * (BM + BN) * 128;
+  if constexpr (kSlots > 2 && !kTurn)
+    if (p.I % kI8Turn == 0 && p.T <= 2 * BM) return launch_i8_tiles<MB, NB, kSlots, true>(p, parts, stream);
   constexpr int kPerCu = kLds <= 80 * 1024 ? 2 : 1;
   static std::atomic<uint64_t> ready{0};  // devices that know the kernel's LDS size
   I8Tiles t{};
@@ -373,11 +392,11 @@ hipError_t launch_i8_tiles(const I8Problem &p, int parts, hipStream_t stream) {
   if (e != hipSuccess) return e;
   if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
   if (!(ready.load(std::memory_order_relaxed) >> dev & 1)) {  // (a benign race sets the same attribute twice)
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(i8_w4_kernel<MB, NB, kSlots>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(i8_w4_kernel<MB, NB, kSlots, kTurn>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess) return e;
     ready.fetch_or(1ull << dev);
   }
-  hipLaunchKernelGGL((i8_w4_kernel<MB, NB, kSlots>), dim3(static_cast<unsigned>(grid)), dim3(256), kLds, stream, t);
+  hipLaunchKernelGGL((i8_w4_kernel<MB, NB, kSlots, kTurn>), dim3(static_cast<unsigned>(grid)), dim3(256), kLds, stream, t);
   return hipGetLastError();
 }
 
