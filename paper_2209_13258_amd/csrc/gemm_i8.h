@@ -182,8 +182,8 @@ __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
 
 // The same with the tokens' rounding in the launch, for tokens of so few features that the bytes of 16 of them fit in LDS and
 // that every workgroup may well round its 16 for itself: one launch instead of two, the first weights on their way meanwhile.
-// One token, 4096 -> 16384: 14.9 us in one launch, 16.8 in two, one call behind another, before both began at different places; 14.0 since, with
-// the weight from memory (4.8 TB/s).
+// One token, 4096 -> 16384: 14.9 us in one launch, 16.8 in two, one call behind another, before both began at different places; 12.4 since, with
+// the weight from memory (5.4 TB/s).
 template <int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, const uint16_t *__restrict__ x, int64_t ldx) {
   constexpr int kStep = 64 * kUnroll, kSpan = kWaves * kStep;

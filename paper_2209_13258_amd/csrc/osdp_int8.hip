@@ -358,7 +358,11 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
         break;
       double rounds = static_cast<double>((groups + v.room - 1) / v.room);
       if (few) rounds = std::max(static_cast<double>(groups) / v.room, groups > 256 ? 0.5 : T > 16 ? 0.35 : 0.25);
-      else if (v.room == 512 && groups % 512 != 0 && groups % 512 <= 256) rounds -= 0.4;  // (one workgroup to a CU is faster than two)
+      else if (v.room == 512 && groups % 512 != 0) {  // (one workgroup to a CU is faster than two; with so few tokens that bytes are the bound,
+                                                          // in proportion: 16 tokens 5120 -> 20480 38.3 us, so 31.0; 20480 -> 5120 37.5 and 34.4)
+        const double part = static_cast<double>(groups % 512) / 512.0;
+        rounds -= T <= 16 ? std::min(0.4, 0.5 - 0.5 * part) : part <= 0.5 ? 0.4 : 0.0;
+      }
       // (up to 16 tokens all workgroups read the same ones, and with fewer than 16 a wave's 16 rows of them are fewer lines: us by 16 / by
       // 64 x 64 in four to eight parts, weight from memory: 16384 -> 4096 2 tokens 20.1 / 25.0, 10 22.1 / 25.5, 16 24.8 / 25.6; 12000 -> 1024
       // 2 tokens 11.1 / 15.8, 16 14.1 / 15.9; 16000 -> 1000 40 tokens 21.4 / 17.9)
