@@ -110,6 +110,16 @@ def test_product_over_weight_shapes_and_cuts(T, I, O, N, k):
     same(forward(w, x, k), expected(x, w.q, w.scale))
 
 
+@pytest.mark.parametrize("T,I,O,N", [(1, 4096, 2056, 1), (1, 12288, 1024, 8), (2, 8192, 4104, 8), (9, 4096, 1032, 16), (40, 4096, 520, 16), (33, 4096, 8192, 8),
+                                     (64, 8192, 2048, 2), (100, 8192, 3000, 8), (128, 16384, 1024, 4), (129, 4096, 2048, 8), (250, 16384, 2048, 4),
+                                     (5, 131072, 72, 1), (60, 20480, 1000, 5)])
+def test_rows_a_multiple_of_4_kb_apart(T, I, O, N):
+    """Workgroups that begin at different places of the reduction, with and without parts."""
+    print("int8 product", T, I, O, N, flush=True)
+    w, x = Weight(I, O, N), tokens(T, I)
+    same(forward(w, x), expected(x, w.q, w.scale))
+
+
 # one that each of the kernels is chosen for, with the parts that its tiles' reductions are cut into
 CHOICES = [((5, 512, 512, 8), "i8_fused_kernel", 1), ((512, 512, 512, 8), "i8_fused_kernel", 1), ((30, 2048, 1024, 8), "i8_few_kernel", 1), ((300, 1152, 2048, 8), "i8_w4_kernelILi2ELi2ELi4", 1),
            ((161, 14448, 960, 8), "i8_w4_kernelILi2ELi2ELi4", 4), ((1000, 4096, 4096, 4), "i8_w4_kernelILi4ELi4ELi4", 1),
