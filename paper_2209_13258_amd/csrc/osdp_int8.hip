@@ -323,9 +323,10 @@ struct Choice {
 
 // The kernel, and the parts of a tile's reduction, that are estimated fastest for T tokens and `shards` blocks of `rows`
 // channels.  A launch takes `fixed` us, and for each round of workgroups over the card `start` and `block` for every 128 input
-// features; a tile's parts cost `each` apiece, and `meet` for every 256 workgroups' worth of sums.  The constants were fitted to 121 random sizes
-// (8 to 8192 tokens, 256 to 16384 input and output features), all of them timed with every kernel below and 1 to 8 parts: the choice is 1.4 % slower than
-// the best of them in the geometric mean and 28 % at most.  us for 16 / 64 x 64 / 128 x 128 / walking 128 x 128 / walking 256 x 256:
+// features; a tile's parts cost `each` apiece, and `meet` for every 256 workgroups' worth of sums.  The constants were fitted to 181 random sizes
+// (8 to 8192 tokens, 256 to 16384 input and output features), all of them timed with every kernel below and 1 to 8 parts, and those of the
+// walking tiles to 60 more with the weight from memory: the choice is 0.8 and 0.4 % slower than the best of them in the geometric mean, 30 and 12 %
+// at most.  us for 16 / 64 x 64 / 128 x 128 / walking 128 x 128 / walking 256 x 256:
 //     30 tokens   400 -> 3456       6.1 /  7.4 /   9.5 /   9.6 /  15.5
 //    162         1152 -> 1344      10.2 /  8.9 /  11.7 /  12.9 /  22.0
 //    161        14448 ->  960      37.5 / 35.1 (four parts 21.2) / 55.4 (30.0) / 85.8 / 135
@@ -341,8 +342,8 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
   constexpr Prices kPrices[] = {{Kernel::kFew, 16, 1024, 5.05, 0.364, 0.81, 0, 0},
                                 {Kernel::k64, 64, 512, 4.84, 0.429, 3.07, 0.83, 0.83},
                                 {Kernel::k128, 128, 256, 2.63, 0.447, 6.37, 0.89, 4.43},
-                                {Kernel::k128Walk, 128, 512, 5.44, 1.048, 5.73, 0, 0},
-                                {Kernel::k256Walk, 256, 256, 0.95, 1.156, 12.8, 0, 0}};
+                                {Kernel::k128Walk, 128, 512, 5.44, 0.9, 5.73, 0, 0},
+                                {Kernel::k256Walk, 256, 256, 0.95, 1.1, 15, 0, 0}};
   const int64_t blocks = (I + 127) / 128;
   Choice best = {Kernel::k256Walk, 1, -1.0};
   for (const Prices &v : kPrices) {
