@@ -139,42 +139,55 @@ __device__ __forceinline__ int i8_first(int I) {
 // Tokens that are in 8 bits already.  4 tokens, 4096 -> 16384, rounded in a launch before it: 18.0 us in all, 3.7 TB/s.  32 or 64 channels to a
 // workgroup, which read the tokens half or a quarter as often, took 22 and 25 us where 16 took 25 (16 tokens), but 20 to 31 instead of 15 for
 // 10240 -> 2560, whose workgroups then leave half the card or more idle.
-template <int kWaves, int kUnroll, bool kFlat>
+//
+// MB: 16 * MB tokens to a workgroup, for rows of the weight that may run over the ends of shards, which no tile reads.  us by sixteens and with all
+// tokens to a workgroup: 33 tokens 4096 -> 16392 in 16 shards 47.9 and 38.9, 64 tokens 8192 -> 32776 250 and 184, 48 tokens 16384 -> 4104 62.6 and 65.9.
+template <int MB, int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
   constexpr int kStep = 64 * kUnroll, kSpan = kWaves * kStep;
   __shared__ const uint8_t *tab[OSDP_MAX_SHARDS];
-  __shared__ int sums[16 * 16];
+  __shared__ int sums[MB * 16 * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
   if (tid < OSDP_MAX_SHARDS) tab[tid] = static_cast<const uint8_t *>(p.shards.p[tid]);
-  for (int i = tid; i < 16 * 16; i += kWaves * 64) sums[i] = 0;
+  for (int i = tid; i < MB * 16 * 16; i += kWaves * 64) sums[i] = 0;
   __syncthreads();
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MB);
   // (rows beyond the last repeat it; they are not stored)
   const I8Row<kFlat> weight(p, tab, min(n0 + l16, p.O - 1));
-  const uint8_t *token = p.xq + static_cast<int64_t>(min(m0 + l16, p.T - 1)) * p.ldq;
-  i32x4 acc = {0, 0, 0, 0};
+  const uint8_t *token[MB];
+  i32x4 acc[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    token[b] = p.xq + static_cast<int64_t>(min(m0 + 16 * b + l16, p.T - 1)) * p.ldq;
+    acc[b] = i32x4{0, 0, 0, 0};
+  }
   auto step = [&](int k0) {
-    uint4 w[kUnroll], x[kUnroll];
+    uint4 w[kUnroll], x[kUnroll][MB];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int k = k0 + 64 * u + 16 * q4;
       w[u] = weight.load(k < p.I ? k : 0);  // beyond the row's end: any weights, the tokens are zeros there
-      x[u] = load_global16(token + (k < p.ldq ? k : p.ldq - 16));
+#pragma unroll
+      for (int b = 0; b < MB; ++b) x[u][b] = load_global16(token[b] + (k < p.ldq ? k : p.ldq - 16));
     }
     __builtin_amdgcn_sched_barrier(0);  // (all of them on their way before the first is waited for)
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (k0 + 64 * u + 16 * q4 >= p.ldq) x[u] = uint4{0u, 0u, 0u, 0u};
-      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u]), __builtin_bit_cast(i32x4, x[u]), acc, 0, 0, 0);
-    }
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        if (k0 + 64 * u + 16 * q4 >= p.ldq) x[u][b] = uint4{0u, 0u, 0u, 0u};
+        acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w[u]), __builtin_bit_cast(i32x4, x[u][b]), acc[b], 0, 0, 0);
+      }
   };
   const int first = i8_first<kSpan>(p.I);
   for (int k0 = first + wave * kStep; k0 < p.I; k0 += kSpan) step(k0);
   for (int k0 = wave * kStep; k0 < first; k0 += kSpan) step(k0);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) atomicAdd(&sums[l16 * 16 + 4 * q4 + i], acc[i]);
+  for (int b = 0; b < MB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) atomicAdd(&sums[(16 * b + l16) * 16 + 4 * q4 + i], acc[b][i]);
   __syncthreads();
-  if (tid < 32) {
+  if (tid < 32 * MB) {
     const int r = tid >> 1, c = (tid & 1) * 8, m = m0 + r, n = n0 + c;
     if (m < p.T && n < p.O) i8_store8(p.y + static_cast<int64_t>(m) * p.ldy + n, &sums[r * 16 + c], p.x_scale[m], p.w_scale + n);
   }
@@ -254,22 +267,30 @@ __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, cons
   }
 }
 
-inline dim3 i8_few_grid(const I8Problem &p) { return dim3(static_cast<unsigned>((p.O + 15) / 16), static_cast<unsigned>((p.T + 15) / 16)); }
-
 // (eight waves with 128 bytes of a row on their way in the one, 256 in the other: 4 or 16 waves, or 512 bytes, were within 3 % or slower)
 hipError_t launch_fused(const I8Problem &p, const uint16_t *x, int64_t ldx, hipStream_t stream) {
   constexpr int kWaves = 8, kUnroll = 2;
   const unsigned lds = static_cast<unsigned>(std::min(p.T, 16) * (p.ldq + 16));
-  if (p.rows_each > 0) hipLaunchKernelGGL((i8_fused_kernel<kWaves, kUnroll, false>), i8_few_grid(p), dim3(kWaves * 64), lds, stream, p, x, ldx);
-  else hipLaunchKernelGGL((i8_fused_kernel<kWaves, kUnroll, true>), i8_few_grid(p), dim3(kWaves * 64), lds, stream, p, x, ldx);
+  const dim3 grid(static_cast<unsigned>((p.O + 15) / 16), static_cast<unsigned>((p.T + 15) / 16));
+  if (p.rows_each > 0) hipLaunchKernelGGL((i8_fused_kernel<kWaves, kUnroll, false>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
+  else hipLaunchKernelGGL((i8_fused_kernel<kWaves, kUnroll, true>), grid, dim3(kWaves * 64), lds, stream, p, x, ldx);
   return hipGetLastError();
 }
 
+template <int MB, bool kFlat>
 hipError_t launch_few(const I8Problem &p, hipStream_t stream) {
   constexpr int kWaves = 8, kUnroll = 4;
-  if (p.rows_each > 0) hipLaunchKernelGGL((i8_few_kernel<kWaves, kUnroll, false>), i8_few_grid(p), dim3(kWaves * 64), 0, stream, p);
-  else hipLaunchKernelGGL((i8_few_kernel<kWaves, kUnroll, true>), i8_few_grid(p), dim3(kWaves * 64), 0, stream, p);
+  const dim3 grid(static_cast<unsigned>((p.O + 15) / 16), static_cast<unsigned>((p.T + 16 * MB - 1) / (16 * MB)));
+  hipLaunchKernelGGL((i8_few_kernel<MB, kWaves, kUnroll, kFlat>), grid, dim3(kWaves * 64), 0, stream, p);
   return hipGetLastError();
+}
+hipError_t launch_few(const I8Problem &p, hipStream_t stream) {
+  static_assert(kI8FewTokens == 64, "rows that run over the ends of shards come with up to 64 tokens");
+  if (p.rows_each > 0) return launch_few<1, false>(p, stream);
+  if (p.T <= 16) return launch_few<1, true>(p, stream);
+  if (p.T <= 32) return launch_few<2, true>(p, stream);
+  if (p.T <= 48) return launch_few<3, true>(p, stream);
+  return launch_few<4, true>(p, stream);
 }
 
 }  // namespace

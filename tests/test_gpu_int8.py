@@ -110,6 +110,14 @@ def test_product_over_weight_shapes_and_cuts(T, I, O, N, k):
     same(forward(w, x, k), expected(x, w.q, w.scale))
 
 
+@pytest.mark.parametrize("T", [16, 17, 32, 33, 47, 48, 49, 63, 64])
+@pytest.mark.parametrize("I,O,N", [(336, 1000, 21), (4096, 520, 16), (2048, 40, 64)])
+def test_rows_that_run_over_the_ends_of_shards(T, I, O, N):
+    print("int8 product", T, I, O, N, flush=True)
+    w, x = Weight(I, O, N), tokens(T, I)
+    same(forward(w, x, pad_y=8), expected(x, w.q, w.scale))
+
+
 @pytest.mark.parametrize("T,I,O,N", [(1, 4096, 2056, 1), (1, 12288, 1024, 8), (2, 8192, 4104, 8), (9, 4096, 1032, 16), (40, 4096, 520, 16), (33, 4096, 8192, 8),
                                      (64, 8192, 2048, 2), (100, 8192, 3000, 8), (128, 16384, 1024, 4), (129, 4096, 2048, 8), (250, 16384, 2048, 4),
                                      (5, 131072, 72, 1), (60, 20480, 1000, 5)])
