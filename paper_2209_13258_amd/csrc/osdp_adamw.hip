@@ -127,6 +127,8 @@ __device__ __forceinline__ uint32_t element(int j) {
 // tile's loads are on their way before the first of them is waited for.  Wide loads and stores are marked as used once: nothing here
 // is touched again before far more than the caches hold has passed.  A step over 78.7 million elements with moments in fp32 took 407 us
 // with the marks and 425 without, with moments in 8 bits 291 and 310; the sum of squares of 403 million 126 and 135.
+// load_anywhere: 16 bytes at a time from any element on (global memory is read so at any address), and not marked, since neighbouring lanes meet
+// in a cache line that would be fetched twice (sum of squares of 403 million fp32 values off by one element 257 us, marked 300).
 template <class T, bool kWide>
 struct Eight;
 
@@ -160,6 +162,12 @@ struct Eight<float, true> {
     a = __builtin_nontemporal_load(q);
     b = __builtin_nontemporal_load(q + 1);
   }
+  __device__ __forceinline__ void load_anywhere(const void *p, int64_t at) {
+    typedef f32x4 Any __attribute__((aligned(4)));
+    const Any *q = reinterpret_cast<const Any *>(static_cast<const float *>(p) + at + element<true>(0));
+    a = q[0];
+    b = q[1];
+  }
   __device__ __forceinline__ void get(float (&out)[8]) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) out[j] = a[j], out[4 + j] = b[j];
@@ -171,6 +179,11 @@ struct Eight<uint16_t, true> {
   uint4 a;
   __device__ __forceinline__ void load(const void *p, int64_t at, uint32_t) {
     const osdp_u32x4 z = __builtin_nontemporal_load(reinterpret_cast<const osdp_u32x4 *>(static_cast<const uint16_t *>(p) + at + element<true>(0)));
+    a = uint4{z[0], z[1], z[2], z[3]};
+  }
+  __device__ __forceinline__ void load_anywhere(const void *p, int64_t at) {
+    typedef osdp_u32x4 Any __attribute__((aligned(2)));
+    const osdp_u32x4 z = *reinterpret_cast<const Any *>(static_cast<const uint16_t *>(p) + at + element<true>(0));
     a = uint4{z[0], z[1], z[2], z[3]};
   }
   __device__ __forceinline__ void get(float (&out)[8]) const {  // bf16
@@ -512,6 +525,23 @@ __device__ __forceinline__ double block_sum(double x) {
   return sum;
 }
 
+// A lane's eight elements of a tile, which ones depending on the tile's length alone, not on where the tensor lies: the same gradients are summed
+// in the same order in tensors of their own and packed side by side.
+template <class Grad>
+__device__ __forceinline__ void load_tile(const Tensor &t, int64_t from, bool wide, float (&g)[8]) {
+  const int64_t rest = t.n - from;
+  if (rest >= kTile) {
+    Eight<Grad, true> x;
+    if (wide) x.load(t.grad, from, kTile);
+    else x.load_anywhere(t.grad, from);
+    x.get(g);
+  } else {
+    Eight<Grad, false> x;
+    x.load(t.grad, from, static_cast<uint32_t>(rest));
+    x.get(g);
+  }
+}
+
 // Tiles in runs of kSumTiles, or alone, one run after another to the workgroups.
 template <class Grad>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, double *__restrict__ out) {
@@ -540,16 +570,7 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, uint32_t run, 
     for (uint32_t tile = first; tile < end; ++tile) {
       int64_t from;
       i = ends.find(tile, &from);
-      const int64_t rest = b.t[i].n - from;
-      if (((b.wide >> i) & 1u) && rest >= kTile) {
-        Eight<Grad, true> x;
-        x.load(b.t[i].grad, from, kTile);
-        x.get(g);
-      } else {
-        Eight<Grad, false> x;
-        x.load(b.t[i].grad, from, rest < kTile ? static_cast<uint32_t>(rest) : kTile);
-        x.get(g);
-      }
+      load_tile<Grad>(b.t[i], from, (b.wide >> i) & 1u, g);
       add(g);
     }
   }
@@ -570,16 +591,7 @@ __global__ __launch_bounds__(kSmallThreads) void sumsq_small_kernel(Batch b, int
       const uint32_t tile = min(first + 4 * u, b.tiles - 1);
       int64_t from;
       const int i = ends.find(tile, &from);
-      const int64_t rest = b.t[i].n - from;
-      if (((b.wide >> i) & 1u) && rest >= kTile) {
-        Eight<Grad, true> x;
-        x.load(b.t[i].grad, from, kTile);
-        x.get(g[u]);
-      } else {
-        Eight<Grad, false> x;
-        x.load(b.t[i].grad, from, rest < kTile ? static_cast<uint32_t>(rest) : kTile);
-        x.get(g[u]);
-      }
+      load_tile<Grad>(b.t[i], from, (b.wide >> i) & 1u, g[u]);
     }
 #pragma unroll
     for (int u = 0; u < kSumTiles; ++u)

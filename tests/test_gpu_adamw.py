@@ -509,6 +509,38 @@ def test_sum_of_squares(grad, lengths, gap):
     assert out.item() == first
 
 
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [[9000], [70000], [5, 4099, 30001], [1 << 20, 300001], [5000003, 2047, 1, 4700001, 129]])
+def test_sum_of_squares_at_any_alignment(grad, lengths):
+    """The order of the sum depends on the lengths alone: the same gradients give the same bits wherever they lie, in tensors of their own and packed
+    side by side, in one launch, in two, and in runs of four tiles."""
+    kind = torch.bfloat16 if grad == "bf16" else torch.float32
+    # (of magnitudes far enough apart that 53 bits do not hold their squares' sums exactly, whatever their order)
+    values = [torch.randn(2, n, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda") for n in lengths]
+    values = [(x[0] * torch.exp2(8 * x[1])).to(kind) for x in values]
+    total = sum(float((x.double() ** 2).sum()) for x in values)
+    out = torch.full((1,), float("nan"), dtype=torch.float64, device="cuda")
+    sums = {}
+    for first in (0, 1, 2, 3, 8):
+        for packed in (False, True):
+            grads = []
+            if packed:
+                flat = torch.full((first + sum(lengths) + 8,), 1e4, dtype=kind, device="cuda")
+                at = first
+                for x in values:
+                    grads.append(flat[at:at + x.numel()].copy_(x))
+                    at += x.numel()
+            else:
+                grads = [torch.full((first + x.numel() + 8,), 1e4, dtype=kind, device="cuda")[first:first + x.numel()].copy_(x) for x in values]
+            table = osdp.AdamWTable(grads=grads)
+            ws = torch.full((max(8, osdp.osdp_adamw_grad_sumsq_workspace_bytes(table)),), 255, dtype=torch.uint8, device="cuda")
+            osdp.osdp_adamw_grad_sumsq(table, out, ws)
+            sums[first, packed] = out.item()
+    # either side: chains of fewer than 2^13 additions, all of one sign, each off by at most 2^-53 of the sum
+    assert abs(sums[0, False] / total - 1) < 2.0 ** -39
+    assert len(set(sums.values())) == 1, sums
+
+
 def test_table_refusals():
     t = lambda n, d=torch.float32: torch.zeros(n, dtype=d, device="cuda")  # noqa: E731
     bad = [dict(grads=[t(4)], params=[t(5)]), dict(grads=[t(4)], params=[t(4), t(4)]), dict(grads=[t(4, torch.float16)]),
