@@ -463,7 +463,7 @@ typedef struct {
   const int64_t *step_device;   /* device, or NULL: t, in place of `step`, read when the kernels run: a captured graph
                                    that is replayed takes the step (and seeds its roundings by it) from here.
                                    What is below 1 counts as 1 */
-  const float *lr_device;       /* device, or NULL: lr, in place of `lr`                             */
+  const float *lr_device;       /* device, or NULL: lr, in place of `lr`.  A NaN makes NaN of every parameter */
   int32_t grad_type;            /* an osdp_dtype                                                     */
   int32_t param_type;           /* an osdp_dtype                                                     */
   int32_t state_bits;           /* 32 or 8                                                           */

@@ -415,13 +415,19 @@ __device__ __forceinline__ void adamw_tile(const Tensor &t, const Step &s, const
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       // without a master copy to one of its neighbours, the one above with the probability that keeps the mean (an infinity
-      // keeps its upper half whatever is added, and so does a NaN whose lower half is 0, as any is that comes from bf16 or from a
-      // block; another might not)
+      // keeps its upper half whatever is added, and so does a NaN whose lower half is 0, as any is that comes from bf16, from a
+      // block or from the rate; another might not)
       if constexpr (kForm == kMaster) w[j] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(p[j]))) << 16;
       else w[j] = __float_as_uint(p[j]) + ((kState8 && sizeof(Grad) == 2) || p[j] == p[j] ? (h[j] * 0x297A2D39u) >> 16 : 0u);
     }
     store8<kWide>(static_cast<uint16_t *>(t.param), at, left, w);
   }
+}
+
+// The number, or a NaN whose lower half is 0 for any NaN: what is rounded stochastically counts on that.
+__device__ __forceinline__ float with_plain_nan(float x) {
+  const uint32_t w = __float_as_uint(x);
+  return __uint_as_float((w & 0x7fffffffu) > 0x7f800000u ? 0x7fc00000u : w);
 }
 
 // Scalars of a call: one for all lanes.
@@ -446,7 +452,7 @@ __device__ __forceinline__ bool scalars_of(const Step &s, Scalars *k) {
   k->lr = static_cast<float>(s.lr);
   int64_t step = s.step;
   if (s.step_device || s.lr_device) {
-    const double lr = s.lr_device ? static_cast<double>(*s.lr_device) : s.lr;
+    const double lr = s.lr_device ? static_cast<double>(with_plain_nan(*s.lr_device)) : s.lr;
     if (s.step_device) step = *s.step_device;
     if (step < 1) step = 1;
     k->lr = static_cast<float>(lr);

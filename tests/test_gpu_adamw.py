@@ -318,6 +318,23 @@ def test_not_a_number_of_any_sign_and_payload(param, grad, gap):
         assert not np.isnan(c.part(name, 1)).any()
 
 
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+@pytest.mark.parametrize("state,param", [(8, "bf16"), (32, "bf16"), (8, "master"), (32, "master"), (8, "f32"), (32, "f32")])
+def test_a_rate_that_is_not_a_number(state, param, grad):
+    """Whatever its sign and payload every parameter becomes NaN, none a number, and the moments are those of any rate."""
+    for pattern in (0x7FFFFFFF, 0xFFFFFFFF, 0x7F800001, 0xFFC00000):
+        rate = torch.tensor([pattern - (1 << 32 if pattern >> 31 else 0)], dtype=torch.int64, device="cuda").to(torch.int32).view(torch.float32)
+        c, other = (Case([3000, 129], state, param, grad, gap=1, seed=9) for _ in range(2))
+        osdp.osdp_adamw_step(c.table, lr=0.0, lr_device=rate, step=3, seed=2)
+        osdp.osdp_adamw_step(other.table, lr=1e-3, step=3, seed=2)
+        torch.cuda.synchronize()
+        for name in ("params", "masters") if param == "master" else ("params",):
+            for i in range(2):
+                assert np.isnan(c.part(name, i)).all(), (hex(pattern), name, i)
+        for name in ("m", "v"):
+            assert torch.equal(c.flat[name], other.flat[name])
+
+
 @pytest.mark.parametrize("gap", [0, 5])
 def test_state_values_are_the_codes_values(gap):
     c = Case([1, 127, 128, 300, 4096, 0, 2051], 8, "bf16", gap=gap)
