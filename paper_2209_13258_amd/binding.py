@@ -14,6 +14,11 @@ from typing import Optional, Sequence
 
 from . import build as _build
 
+try:
+    from ._pointers import pointers as _checked_pointers
+except ImportError as e:
+    raise ImportError(f"{_build.POINTERS} is missing or of another Python: build it first (python paper_2209_13258_amd/build.py)") from e
+
 OSDP_OK = 0
 OSDP_ERR_INVALID_ARG = -1
 OSDP_ERR_UNSUPPORTED = -2
@@ -434,6 +439,49 @@ def _one(t, kind: str) -> bool:
     return t.numel() == 1 and _is(t, kind) and t.is_cuda
 
 
+class _Allowed(dict):
+    """Whether shards may have an element type, of ``size`` bytes."""
+    def __init__(self, size, *kinds):
+        super().__init__()
+        self.size, self.kinds = size, kinds
+
+    def __missing__(self, dtype):
+        ok = self[dtype] = str(dtype) in self.kinds
+        return ok
+
+
+_SHARDS = {"w_shards": _Allowed(2, "torch.bfloat16"), "q_shards": _Allowed(1, "torch.int8", "torch.uint8")}
+
+
+def _shard_ptrs(name: str, shards, I: int, O: int, device: int):
+    """Addresses of shards that are what the library takes them for, and as long as what it reads or writes there."""
+    allowed, N = _SHARDS[name], len(shards)
+    L = -(-I * O // N) if N else 0
+    out = _checked_pointers(shards, L * allowed.size, allowed, device)
+    if out is None:
+        for i, t in enumerate(shards):
+            n = max(min(L, I * O - i * L), 0)  # (what is behind the last element of the weight may be missing)
+            if t.nbytes < n * allowed.size or not allowed[t.dtype] or t.get_device() != device or not t.is_contiguous():
+                _refuse(f"{name}[{i}] must be a contiguous tensor of at least {n} elements, {' or '.join(allowed.kinds)}, on the GPU that the others are on")
+        out = _ptrs(shards)
+    return out
+
+
+def _check_scale(w_scale, O: int) -> int:
+    """The device that the scales are on."""
+    device = w_scale.get_device()
+    if device < 0 or not _is(w_scale, "torch.float32") or w_scale.numel() < O or not w_scale.is_contiguous():
+        _refuse(f"w_scale must hold {O} float32 on the GPU")
+    return device
+
+
+def _check_workspace(workspace, device: int) -> int:
+    """Its bytes."""
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        _refuse("the workspace must be a contiguous tensor on the GPU that the others are on")
+    return workspace.nbytes
+
+
 def _overlap(written, read) -> bool:
     """Whether some array that is written shares memory with another of them, or with one that is read; (address, bytes) each."""
     written = sorted(a for a in written if a[1])
@@ -513,10 +561,6 @@ class AdamWTable:
         self._keep["grads"] = grads
 
 
-def _bytes(workspace) -> int:
-    return workspace.nbytes
-
-
 def osdp_adamw_grad_sumsq_workspace_bytes(table: AdamWTable) -> int:
     need = ctypes.c_size_t()
     _check(lib.osdp_adamw_grad_sumsq_workspace_bytes(table.tensors, table.count, ctypes.byref(need)))
@@ -527,8 +571,9 @@ def osdp_adamw_grad_sumsq(table: AdamWTable, sumsq, workspace, *, accumulate: bo
     """``sumsq`` (one float64 on the GPU) = sum of the squares of all of the table's gradients; accumulate: is added to it."""
     if not _one(sumsq, "torch.float64"):
         _refuse("sumsq must be one float64 on the GPU")
+    nbytes = _check_workspace(workspace, sumsq.get_device())
     _check(lib.osdp_adamw_grad_sumsq(table.tensors, table.count, table.grad_type, int(bool(accumulate)), sumsq.data_ptr(),
-                                     workspace.data_ptr(), _bytes(workspace), _stream(stream)))
+                                     workspace.data_ptr(), nbytes, _stream(stream)))
 
 
 def osdp_adamw_step(table: AdamWTable, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1,
@@ -569,15 +614,16 @@ def osdp_split_linear_i8_quantize_workspace_bytes(I, O, N) -> int:
 
 
 def osdp_split_linear_i8_quantize(I, O, w_shards, q_shards, w_scale, workspace, *, stream=None) -> None:
-    """bf16 shards of W[I x O] -> int8 shards of Wq[O x I] and the channels' scales (fp32 [O])."""
+    """bf16 shards of W[I x O] -> int8 shards of Wq[O x I] and the channels' scales (fp32 [O]).  Tensors of another type, length or device are
+    refused; the last shards may leave out what is behind the weight's end."""
     N = len(w_shards)
     shape = osdp_shape(0, I, O, N, 0)
     if len(q_shards) != N:
         _refuse(f"{len(q_shards)} q_shards for {N} w_shards")
-    if not _is(w_scale, "torch.float32") or w_scale.numel() < O or not w_scale.is_contiguous():
-        _refuse(f"w_scale must hold {O} float32")
-    _check(lib.osdp_split_linear_i8_quantize(ctypes.byref(shape), _ptrs(w_shards), _ptrs(q_shards), w_scale.data_ptr(),
-                                             workspace.data_ptr(), _bytes(workspace), _stream(stream)))
+    device = _check_scale(w_scale, O)
+    _check(lib.osdp_split_linear_i8_quantize(ctypes.byref(shape), _shard_ptrs("w_shards", w_shards, I, O, device),
+                                             _shard_ptrs("q_shards", q_shards, I, O, device), w_scale.data_ptr(),
+                                             workspace.data_ptr(), _check_workspace(workspace, device), _stream(stream)))
 
 
 def osdp_split_linear_i8_workspace_bytes(T, I, O, N, k):
@@ -590,14 +636,17 @@ def osdp_split_linear_i8_workspace_bytes(T, I, O, N, k):
 def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=None) -> None:
     """Y[T x O] = X[T x I] . W with W as int8 shards of Wq[O x I]; X, Y 2-D bf16 tensors (row stride = ld)."""
     T, I = X.shape
-    O = Y.shape[1]
-    if X.stride(1) != 1 or Y.stride(1) != 1 or not _is(X, "torch.bfloat16") or not _is(Y, "torch.bfloat16") or Y.shape[0] != T:
+    rows, O = Y.shape
+    ldx, x_step = X.stride()
+    ldy, y_step = Y.stride()
+    if x_step != 1 or y_step != 1 or not _is(X, "torch.bfloat16") or not _is(Y, "torch.bfloat16") or rows != T:
         _refuse("X and Y must be bf16 matrices of as many rows, with unit stride along them")
-    if not _is(w_scale, "torch.float32") or w_scale.numel() < O or not w_scale.is_contiguous():
-        _refuse(f"w_scale must hold {O} float32")
+    device = _check_scale(w_scale, O)
+    if X.get_device() != device or Y.get_device() != device:
+        _refuse("X and Y must be on the GPU that the others are on")
     shape = osdp_shape(T, I, O, len(q_shards), k)
-    _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), X.stride(0), _ptrs(q_shards), w_scale.data_ptr(),
-                                        Y.data_ptr(), Y.stride(0), workspace.data_ptr(), _bytes(workspace), _stream(stream)))
+    _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), ldx, _shard_ptrs("q_shards", q_shards, I, O, device), w_scale.data_ptr(),
+                                        Y.data_ptr(), ldy, workspace.data_ptr(), _check_workspace(workspace, device), _stream(stream)))
 
 
 def osdp_debug_option(name: str, value: int) -> None:

@@ -200,6 +200,107 @@ def test_the_binding_refuses_other_types_of_matrices():
         assert e.value.status == B.OSDP_ERR_INVALID_ARG
 
 
+class OnGpu:
+    """What the binding asks a tensor for, of one that would lie on a GPU."""
+    def __init__(self, shape, dtype="bfloat16", device=0, contiguous=True):
+        import torch
+        self.shape = shape if isinstance(shape, tuple) else (shape,)
+        self.dtype, self.device, self.contiguous, self.is_cuda = getattr(torch, dtype), device, contiguous, device >= 0
+        self.nbytes = self.numel() * self.dtype.itemsize
+
+    def numel(self):
+        n = 1
+        for s in self.shape:
+            n *= s
+        return n
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def stride(self):
+        return self.shape[-1], 1
+
+    def data_ptr(self):
+        return P if self.device >= 0 else 0
+
+
+@pytest.fixture
+def no_gpu_work(monkeypatch):
+    """Calls that pass all checks, the binding's and the library's, end here with OSDP_ERR_HIP: there is no GPU to ask for."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a call that passes the checks would run")
+
+
+@pytest.mark.parametrize("name", ["w_shards", "q_shards", "fwd"])
+@pytest.mark.parametrize("bad", [dict(dtype="float32"), dict(dtype="float16"), dict(dtype="int16"), dict(n=-1), dict(device=-1), dict(device=1),
+                                 dict(contiguous=False), dict(dtype="other")])
+@pytest.mark.parametrize("place", [0, 2, 3])
+def test_the_binding_refuses_other_shards(no_gpu_work, name, bad, place):
+    I, O, N = 272, 24, 4
+    L = I * O // N
+    bad = dict(bad)
+    if bad.get("dtype") == "other":   # the other matrix's shards
+        bad["dtype"] = "int8" if name == "w_shards" else "bfloat16"
+    w, q = [OnGpu(L) for _ in range(N)], [OnGpu(L, "int8") for _ in range(N)]
+    scale, ws = OnGpu(O, "float32"), OnGpu(1 << 30, "uint8")
+
+    def call():
+        if name == "fwd":
+            osdp.osdp_split_linear_i8_fwd(OnGpu((2, I)), q, scale, OnGpu((2, O)), 1, ws)
+        else:
+            osdp.osdp_split_linear_i8_quantize(I, O, w, q, scale, ws)
+    with pytest.raises(osdp.OsdpError) as e:   # what is right gets as far as the GPU
+        call()
+    assert e.value.status in (B.OSDP_ERR_HIP, B.OSDP_ERR_UNSUPPORTED) and "aligned" not in str(e.value)
+    shards = w if name == "w_shards" else q
+    kind = dict(n=0, dtype="bfloat16" if name == "w_shards" else "int8")
+    kind.update(bad)
+    shards[place] = OnGpu(L + kind.pop("n"), **kind)
+    with pytest.raises(osdp.OsdpError, match=r"_shards\[%d\]" % place) as e:
+        call()
+    assert e.value.status == B.OSDP_ERR_INVALID_ARG
+
+
+def test_the_last_shard_may_hold_less_and_bytes_may_have_no_sign(no_gpu_work):
+    """112 x 8 elements in 19 shards of 48, of which the last holds 32; 16 x 16 in 17 of 16, of which the last holds none."""
+    for I, O, N, L in ((112, 8, 19, 48), (16, 16, 17, 16)):
+        for kind in ("int8", "uint8"):
+            for less in (0, 1):
+                q = [OnGpu(L, kind) for _ in range(N - 1)] + [OnGpu(max(I * O - (N - 1) * L - less, 0), kind)]
+                with pytest.raises(osdp.OsdpError) as e:
+                    osdp.osdp_split_linear_i8_fwd(OnGpu((2, I)), q, OnGpu(O, "float32"), OnGpu((2, O)), 1, OnGpu(1 << 30, "uint8"))
+                assert ("q_shards[18]" in str(e.value)) == bool(less and N == 19), e.value
+
+
+@pytest.mark.parametrize("place", ["X", "Y", "scale", "ws"])
+@pytest.mark.parametrize("device", [-1, 1])
+def test_the_binding_refuses_other_devices(no_gpu_work, place, device):
+    I, O = 64, 32
+    at = {name: device if name == place else 0 for name in ("X", "Y", "scale", "ws")}
+    args = dict(X=OnGpu((2, I), device=at["X"]), Y=OnGpu((2, O), device=at["Y"]), scale=OnGpu(O, "float32", at["scale"]),
+                ws=OnGpu(1 << 30, "uint8", at["ws"]))
+    q, w = [OnGpu(I * O, "int8")], [OnGpu(I * O)]
+    with pytest.raises(osdp.OsdpError, match="GPU") as e:
+        osdp.osdp_split_linear_i8_fwd(args["X"], q, args["scale"], args["Y"], 1, args["ws"])
+    assert e.value.status == B.OSDP_ERR_INVALID_ARG
+    if place in ("scale", "ws"):
+        with pytest.raises(osdp.OsdpError, match="GPU") as e:
+            osdp.osdp_split_linear_i8_quantize(I, O, w, q, args["scale"], args["ws"])
+        assert e.value.status == B.OSDP_ERR_INVALID_ARG
+
+
+def test_the_sum_of_squares_refuses_a_workspace_that_is_not_on_the_gpu():
+    class Table:
+        tensors, count, grad_type = (B.osdp_adamw_tensor * 1)(), 0, 0
+    for ws in (OnGpu(1024, "uint8", -1), OnGpu(1024, "uint8", 0, False)):
+        with pytest.raises(osdp.OsdpError, match="workspace must be"):
+            osdp.osdp_adamw_grad_sumsq(Table, OnGpu(1, "float64"), ws)
+
+
 def test_rounding_by_one_multiplication_and_one_addition_is_exact():
     """trunc(fma(x, r, 1/2)), r = fp32(fp32(127 / amax) (1 + 2^-21)), against round(x * 127 / amax), halves upwards, in whole numbers: for every
     significand of a bf16 x and amax at every power of two between them that leaves something."""
