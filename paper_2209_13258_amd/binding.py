@@ -482,6 +482,10 @@ def _check_workspace(workspace, device: int) -> int:
     return workspace.nbytes
 
 
+def _spans(tensors):
+    return [(t.data_ptr(), t.nbytes) for t in tensors]
+
+
 def _overlap(written, read) -> bool:
     """Whether some array that is written shares memory with another of them, or with one that is read; (address, bytes) each."""
     written = sorted(a for a in written if a[1])
@@ -536,8 +540,8 @@ class AdamWTable:
         decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * count
         if len(decay) != count:
             _refuse(f"{len(decay)} weight decays for {count} tensors")
-        spans = {name: [(t.data_ptr(), t.nbytes) for t in ts] for name, ts in lists.items()}
-        if _overlap(sum((ts for name, ts in spans.items() if name != "grads"), []), spans.get("grads", [])):
+        self._written = sorted(sum((_spans(ts) for name, ts in lists.items() if name != "grads"), []))
+        if _overlap(self._written, _spans(lists.get("grads", []))):
             _refuse("a tensor is listed twice, or tensors of the table share memory")
         self._keep = lists
         self.tensors = (osdp_adamw_tensor * max(count, 1))()
@@ -556,6 +560,8 @@ class AdamWTable:
         for i, g in enumerate(grads):
             if g.numel() != self.lengths[i] or str(g.dtype) != want or not g.is_contiguous() or not g.is_cuda:
                 _refuse(f"grads[{i}] must be a contiguous GPU tensor of {self.lengths[i]} elements, {want}")
+        if _overlap(self._written, _spans(grads)):
+            _refuse("gradients share memory with tensors of the table")
         for i, g in enumerate(grads):
             self.tensors[i].grad = g.data_ptr() if self.lengths[i] else None
         self._keep["grads"] = grads

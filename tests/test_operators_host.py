@@ -202,11 +202,11 @@ def test_the_binding_refuses_other_types_of_matrices():
 
 class OnGpu:
     """What the binding asks a tensor for, of one that would lie on a GPU."""
-    def __init__(self, shape, dtype="bfloat16", device=0, contiguous=True):
+    def __init__(self, shape, dtype="bfloat16", device=0, contiguous=True, address=P):
         import torch
         self.shape = shape if isinstance(shape, tuple) else (shape,)
         self.dtype, self.device, self.contiguous, self.is_cuda = getattr(torch, dtype), device, contiguous, device >= 0
-        self.nbytes = self.numel() * self.dtype.itemsize
+        self.nbytes, self.address = self.numel() * self.dtype.itemsize, address
 
     def numel(self):
         n = 1
@@ -224,7 +224,7 @@ class OnGpu:
         return self.shape[-1], 1
 
     def data_ptr(self):
-        return P if self.device >= 0 else 0
+        return self.address if self.device >= 0 else 0
 
 
 @pytest.fixture
@@ -291,6 +291,29 @@ def test_the_binding_refuses_other_devices(no_gpu_work, place, device):
         with pytest.raises(osdp.OsdpError, match="GPU") as e:
             osdp.osdp_split_linear_i8_quantize(I, O, w, q, args["scale"], args["ws"])
         assert e.value.status == B.OSDP_ERR_INVALID_ARG
+
+
+def test_new_gradients_may_not_share_memory_with_what_is_written():
+    """set_grads refuses what the constructor does."""
+    at = lambda name, i: P * (1 + ("param", "master", "m", "v", "exps", "grad").index(name)) + 4096 * i  # noqa: E731
+    make = lambda name, n, kind: [OnGpu(n, kind, address=at(name, i)) for i in range(2)]  # noqa: E731
+    table = osdp.AdamWTable(params=make("param", 256, "bfloat16"), grads=make("grad", 256, "bfloat16"), masters=make("master", 256, "float32"),
+                            m=make("m", 256, "uint8"), v=make("v", 256, "uint8"), exps=make("exps", 4, "uint8"))
+    bf16 = lambda address: OnGpu(256, address=address)  # noqa: E731
+    before = [table.tensors[i].grad for i in range(2)]
+    sizes = dict(param=512, master=1024, m=256, v=256, exps=4)
+    for name, size in sizes.items():
+        for i in range(2):
+            for bad in (at(name, i), at(name, i) + size - 2, at(name, i) - 510):
+                for place in range(2):
+                    new = [bf16(1 << 30), bf16(1 << 30)]
+                    new[place] = bf16(bad)
+                    with pytest.raises(osdp.OsdpError, match="share memory"):
+                        table.set_grads(new)
+                    assert [table.tensors[i].grad for i in range(2)] == before
+            table.set_grads([bf16(at(name, i) + size), bf16(at(name, i) - 512)])   # side by side
+            before = [table.tensors[i].grad for i in range(2)]
+    table.set_grads([bf16(1 << 30), bf16(1 << 30)])                                # read twice
 
 
 def test_the_sum_of_squares_refuses_a_workspace_that_is_not_on_the_gpu():
