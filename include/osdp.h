@@ -509,7 +509,7 @@ OSDP_API osdp_status osdp_adamw_state_values(const osdp_adamw_tensor *tensors, i
  * made from them again.
  *
  * Shapes (else OSDP_ERR_UNSUPPORTED): I a multiple of 16 and at most 131072 (the sums fit 32 bits), O a multiple of 8, L a
- * multiple of 16, leading dimensions multiples of 8; pointers 16-byte aligned; N <= 64; T, O < 2^31. */
+ * multiple of 16, leading dimensions multiples of 8; pointers 16-byte aligned; N <= 64; T < 2^31, O <= 2^31 - 512. */
 
 /* 8-bit shards and the channels' scales from bf16 shards (the layout of osdp_split_linear_fwd).
  *   w_shards : host array of N device pointers, bf16, L elements each
@@ -521,7 +521,7 @@ OSDP_API osdp_status osdp_split_linear_i8_quantize(const osdp_shape *shape, cons
                                                    float *w_scale, void *workspace, size_t workspace_bytes, void *stream);
 OSDP_API osdp_status osdp_split_linear_i8_quantize_workspace_bytes(const osdp_shape *shape, size_t *bytes);
 
-/* The forward pass.  Up to 64 tokens read the weight where it lies, however it is cut; more tokens do where every shard is a
+/* The forward pass.  Up to 64 tokens read the weight (of up to 2^27 - 16 channels) where it lies, however it is cut; more tokens do where every shard is a
  * block of whole channels (N divides O), at least 32 of them.  Otherwise, and from 257 tokens on where the library estimates
  * it faster, the k slices of output channels, c0_j = floor(j*O/k), are gathered one after another into one staging slot of a
  * slice (size/k at one byte an element).

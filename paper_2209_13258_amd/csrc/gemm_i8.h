@@ -77,6 +77,9 @@ constexpr size_t kI8SumBytes = 16 << 20;
 // a block of at least kI8ShardRows channels (tiles end with a shard); beyond kI8ManyTokens only if that is no slower than gathering.
 constexpr int64_t kI8FewTokens = 64, kI8ShardRows = 32, kI8ManyTokens = 256;
 
+// What the kernels for few tokens, of 512 threads for 16 channels, can be launched over: threads along a grid are counted in 32 bits.
+constexpr int64_t kI8FewChannels = (int64_t{1} << 27) - 16;
+
 // Eight sums as Y: both scales, then the rounding to bf16.
 __device__ __forceinline__ void i8_store8(uint16_t *y, const int *sums, float st, const float *so) {
   uint32_t out[4];

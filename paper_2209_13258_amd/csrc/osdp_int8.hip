@@ -264,7 +264,8 @@ osdp_status check_weight(const osdp_shape *s, Weight *w) {
     return fail(OSDP_ERR_INVALID_ARG, "I, O must be positive and T non-negative (got T %lld, I %lld, O %lld)", (long long)s->T, (long long)s->I, (long long)s->O);
   if (s->N < 1) return fail(OSDP_ERR_INVALID_ARG, "N must be >= 1 (got %d)", s->N);
   if (s->N > OSDP_MAX_SHARDS) return fail(OSDP_ERR_UNSUPPORTED, "N = %d exceeds %d shards", s->N, OSDP_MAX_SHARDS);
-  if (s->T >= (1ll << 31) || s->O >= (1ll << 31)) return fail(OSDP_ERR_UNSUPPORTED, "T and O must be below 2^31");
+  // (columns of the tile that ends last are counted too, up to 263 behind O)
+  if (s->T >= (1ll << 31) || s->O > (1ll << 31) - 512) return fail(OSDP_ERR_UNSUPPORTED, "T must be below 2^31, O at most 2^31 - 512");
   if (s->I % 16 || s->I > kMaxFeatures)
     return fail(OSDP_ERR_UNSUPPORTED, "I must be a multiple of 16 and at most %lld (got %lld)", (long long)kMaxFeatures, (long long)s->I);
   if (s->O % 8) return fail(OSDP_ERR_UNSUPPORTED, "O must be a multiple of 8 (got %lld)", (long long)s->O);
@@ -350,7 +351,7 @@ Choice choose(int64_t T, int64_t I, int64_t rows, int64_t shards, bool may_share
     const bool few = v.kernel == Kernel::kFew;
     const int64_t across = few ? (rows * shards + 15) / 16 : shards * i8_shard_tiles(rows, v.side);
     const int64_t tiles = across * ((T + v.side - 1) / v.side);
-    if (few && T > 4096) continue;
+    if (few && (T > 4096 || rows * shards > kI8FewChannels)) continue;
     if ((v.kernel == Kernel::k64 || v.kernel == Kernel::k128) && tiles > (1 << 20)) continue;
     for (int asked : {1, 2, 3, 4, 6, 8}) {
       const int64_t each = (blocks + asked - 1) / asked, parts = (blocks + each - 1) / each, groups = tiles * parts;
@@ -395,14 +396,14 @@ hipError_t launch_product(const I8Problem &p, hipStream_t stream) {
 // 512 of 512 -> 512 9.2 / 8.6 and 128 of 1024 -> 1024 9.2 / 7.7; beyond it 256 of 256 -> 2048 9.3 / 14.5, 3 of 4096 -> 16384 15.6 / 18.2.
 bool rounds_inside(const Weight &w) {
   const int64_t values = std::min<int64_t>(w.T, 16) * w.I;
-  if (values > (1 << 14)) return false;
+  if (values > (1 << 14) || w.O > kI8FewChannels) return false;
   if (w.T == 1) return true;
   return (w.T + 15) / 16 * ((w.O + 15) / 16) * std::max<int64_t>(values, 1 << 13) <= (1 << 23);
 }
 
 // Whether slices have to be gathered, and whether they may be: with many tokens the tiles that end with each shard can cost more than a
 // dense copy of the weight does.
-bool has_to_gather(const Weight &w) { return w.T > kI8FewTokens && w.rows_each < kI8ShardRows; }
+bool has_to_gather(const Weight &w) { return (w.T > kI8FewTokens || w.O > kI8FewChannels) && w.rows_each < kI8ShardRows; }
 bool may_gather(const Weight &w) { return has_to_gather(w) || (w.T > kI8ManyTokens && w.N > 1 && w.rows_each % 256 != 0); }
 
 // Gathers where that is estimated faster: a gather reads and writes a slice at 5.5 TB/s and takes 6 us besides.  Eight shards of 320 channels,

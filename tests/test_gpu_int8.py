@@ -242,6 +242,26 @@ def test_weights_of_more_than_32_bits(T, I, O, N):
     same(Y[rows][:, cols].float().cpu().numpy(), _few_columns(X, shards, scale, O, rows, cols))
 
 
+@pytest.mark.parametrize("T,I,O,N", [(1, 16, (1 << 27) + 64, 1), (5, 16, (1 << 27) + 64, 8), (3, 48, (1 << 27) + 8, 3), (2, 16, (1 << 31) - 512, 1)])
+def test_most_channels(T, I, O, N):
+    """More channels than a launch of the kernels for few tokens has threads for."""
+    print("int8 product", T, I, O, N, flush=True)
+    L = -(-I * O // N)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    base = torch.randint(-127, 128, (1000003,), dtype=torch.int8, device="cuda", generator=gen)
+    shards = [base.roll(s).repeat(-(-L // 1000003))[:L].contiguous() for s in range(N)]
+    scale = (torch.rand(1000, device="cuda", generator=gen) * 1e-3).repeat(-(-O // 1000))[:O].contiguous()
+    X = torch.randn(T, I, device="cuda", generator=gen).to(torch.bfloat16)
+    Y = torch.zeros(T, O, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, 1)[0], dtype=torch.uint8, device="cuda")
+    osdp.osdp_split_linear_i8_fwd(X, shards, scale, Y, 1, ws)
+    torch.cuda.synchronize()
+    rows = sorted({0, T - 1})
+    cols = [0, 1, 255, 256, O // N - 1, O // N % O, O // N % O + 1, O // 3, (1 << 27) - 17, (1 << 27) - 1, 1 << 27, O - 9, O - 1]
+    assert all(0 <= c < O for c in cols)
+    same(Y[rows][:, cols].float().cpu().numpy(), _few_columns(X, shards, scale, O, rows, cols))
+
+
 def test_tokens_of_more_than_32_bits():
     """4.9 GB of rounded tokens, 9.8 GB in bf16."""
     T, I, O, N = 300000, 16384, 16, 1

@@ -129,6 +129,22 @@ def test_i8_workspace_follows_the_law(T, I, O, N, k):
     assert fewer == sorted(fewer) and max(fewer) <= total, "what does for T tokens has to do for fewer"
 
 
+def test_i8_weights_of_most_channels():
+    """A launch counts its threads in 32 bits, so 16 channels to a workgroup of 512 ends at 2^27: a weight of more that is cut within channels is
+    gathered for any number of tokens.  Tile numbers and columns behind the last one are 32-bit numbers too."""
+    I, O, N = 48, (1 << 27) + 8, 3
+    for T in (1, 5, 64, 65):
+        assert osdp.osdp_split_linear_i8_workspace_bytes(T, I, O, N, 1)[1] == I * O
+        assert osdp.osdp_split_linear_i8_workspace_bytes(T, I, 1 << 27, N, 8)[1] == I * (1 << 24)
+    assert osdp.osdp_split_linear_i8_workspace_bytes(64, 112, (1 << 27) - 16, 7, 1)[1] == 0
+    fits = (1 << 31) - 512
+    assert osdp.osdp_split_linear_i8_workspace_bytes(1, 16, fits, 1, 1)[1] == 0
+    for O in (fits + 8, (1 << 31) - 8):
+        with pytest.raises(osdp.OsdpError) as e:
+            osdp.osdp_split_linear_i8_workspace_bytes(1, 16, O, 1, 1)
+        assert e.value.status == B.OSDP_ERR_UNSUPPORTED
+
+
 def test_i8_quantize_refuses():
     def call(I=64, O=32, N=2, w=P, q=P, scale=P, ws=P, ws_bytes=1 << 30):
         shape = B.osdp_shape(0, I, O, N, 0)
