@@ -455,6 +455,36 @@ def test_captured_step_takes_step_and_rate_from_the_device(state):
             assert torch.equal(eager.flat[name], graph.flat[name]), (k, name)
 
 
+@pytest.mark.parametrize("lengths", [[3000, 129], [12500003, 100001, 1]])
+@pytest.mark.parametrize("state,param", [(8, "bf16"), (32, "bf16"), (8, "f32"), (32, "f32"), (8, "master"), (32, "master")])
+def test_step_and_rate_on_the_device_one_by_one(state, param, lengths):
+    """Either alone and both, in a graph that is replayed, against eager calls with the same numbers from the host; what is below 1 counts as step 1.
+    The longer list has enough tiles for a workgroup of the bf16 form in 8 bits to take four."""
+    host, dev = (Case(lengths, state, param, gap=1, seed=5) for _ in range(2))
+    step, rate = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.zeros(1, device="cuda")
+    stream = torch.cuda.Stream()
+    kwargs = dict(beta1=0.9, beta2=0.95, seed=21)
+    for which in ("step", "rate", "both"):
+        on_device = dict(step_device=step if which != "rate" else None, lr_device=rate if which != "step" else None)
+        at = {"step": 1, "rate": 6, "both": 1}[which]  # (what the graph holds: a step that is not read, and one that is)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            osdp.osdp_adamw_step(dev.table, lr=2.0 ** -10 if which == "step" else 0.0, step=at, stream=stream, **on_device, **kwargs)
+        for t in (-3, 0, 1, 2, 1000, 10 ** 7) if len(lengths) == 2 else (2, 1000):
+            lr = float(np.float32(3e-4 / max(t, 1) ** 0.25))
+            step.fill_(t)
+            rate.fill_(lr)
+            torch.cuda.synchronize()
+            g.replay()
+            osdp.osdp_adamw_step(host.table, lr=2.0 ** -10 if which == "step" else lr, step=6 if which == "rate" else max(t, 1), **kwargs)
+            torch.cuda.synchronize()
+            for name, x in host.flat.items():
+                assert torch.equal(x, dev.flat[name]), (which, t, name)
+            for a, b in zip(host.exps or [], dev.exps or []):
+                assert torch.equal(a, b), (which, t)
+
+
 def test_streams_of_the_caller():
     a, b = Case([200000], 32, "master", seed=1), Case([200000], 8, "bf16", seed=2)
     sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
