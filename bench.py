@@ -122,20 +122,25 @@ class Stack:
         self.ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
         self.sc, self.sp = torch.cuda.Stream(), torch.cuda.Stream()
 
-    def step(self, serial=False):
+    def forward(self, serial=False):
         osdp, sp = self.osdp, (None if serial else self.sp)
-        if self.mixed:
-            for d in self.ops:
+        for d in self.ops:
+            if self.mixed:
                 osdp.osdp_split_linear_fwd_mixed(d["X"], d["W"], d["w_dp"], d["op"].O, d["Y"], 0, self.ws, plan=self.plan,
                                                  op_index=d["n"], stream_compute=self.sc, stream_copy=sp)
+            else:
+                osdp.osdp_split_linear_fwd(d["X"], d["W"], d["Y"], 0, self.ws, plan=self.plan, op_index=d["n"],
+                                           stream_compute=self.sc, stream_copy=sp)
+
+    def step(self, serial=False):
+        osdp, sp = self.osdp, (None if serial else self.sp)
+        self.forward(serial)
+        if self.mixed:
             for d in reversed(self.ops):
                 osdp.osdp_split_linear_bwd_mixed(d["X"], d["dY"], d["W"], d["w_dp"], d["op"].O, d["dX"], d["dW"],
                                                  d["dw_dp"], 0, self.ws, plan=self.plan, op_index=d["n"],
                                                  stream_compute=self.sc, stream_copy=sp)
             return
-        for d in self.ops:
-            osdp.osdp_split_linear_fwd(d["X"], d["W"], d["Y"], 0, self.ws, plan=self.plan, op_index=d["n"],
-                                       stream_compute=self.sc, stream_copy=sp)
         for d in reversed(self.ops):
             osdp.osdp_split_linear_bwd(d["X"], d["dY"], d["W"], d["dX"], d["dW"], 0, self.ws, plan=self.plan,
                                        op_index=d["n"], stream_compute=self.sc, stream_copy=sp)
@@ -160,15 +165,16 @@ class Stack:
         return (t1 - t0) * 1e3 / steps, stats
 
 
-def median_ms(torch, call, iters, warmup):
-    """Median of `call` on the default stream, by events."""
+def median_ms(torch, call, iters, warmup, stream):
+    """Median of `call`, which works on `stream`, by events, once everything before it is done."""
+    torch.cuda.synchronize()
     for _ in range(warmup):
         call()
     ev = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in range(iters)]
     for e0, e1 in ev:
-        e0.record()
+        e0.record(stream)
         call()
-        e1.record()
+        e1.record(stream)
     torch.cuda.synchronize()
     return sorted(e0.elapsed_time(e1) for e0, e1 in ev)[iters // 2]
 
@@ -186,33 +192,23 @@ def training_step(st, bits, iters, warmup):
     ws = torch.empty(max(256, osdp.osdp_adamw_grad_sumsq_workspace_bytes(table)), dtype=torch.uint8, device="cuda")
     step = [0]
 
-    def update(stream=None):
+    def update():
         step[0] += 1
-        osdp.osdp_adamw_grad_sumsq(table, sumsq, ws, stream=stream)
-        osdp.osdp_adamw_step(table, lr=1e-6, step=step[0], grad_sumsq=sumsq, max_norm=1.0, seed=1, stream=stream)
+        osdp.osdp_adamw_grad_sumsq(table, sumsq, ws, stream=st.sc)
+        osdp.osdp_adamw_step(table, lr=1e-6, step=step[0], grad_sumsq=sumsq, max_norm=1.0, seed=1, stream=st.sc)
 
     def whole():
         st.step()
-        update(st.sc)
-    times = []
-    with torch.cuda.stream(st.sc):
-        for i in range(warmup + iters):
-            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-            e0.record(st.sc)
-            whole()
-            e1.record(st.sc)
-            times.append((e0, e1))
-        torch.cuda.synchronize()
+        update()
     n = sum(w.numel() for w in W)
-    ms = sorted(e0.elapsed_time(e1) for e0, e1 in times[warmup:])[iters // 2]
-    alone = median_ms(torch, update, iters, warmup)
+    ms, alone = median_ms(torch, whole, iters, warmup, st.sc), median_ms(torch, update, iters, warmup, st.sc)
     moved = n * (2 + 2 + 8 + 2 + (16 if bits == 32 else 4 + 4 / osdp.OSDP_ADAMW_BLOCK))  # the norm reads the gradients once more
     return {"state_bits": bits, "parameters": n, "median_ms_per_step": round(ms, 4), "norm_and_adamw_ms": round(alone, 4),
             "norm_and_adamw_gbs": round(moved / (alone * 1e-3) / 1e9, 1), "frac_hbm_peak": round(moved / (alone * 1e-3) / 1e9 / PEAK_HBM_GBS, 4)}
 
 
 def int8_forward(st, iters, warmup):
-    """Every operator's forward pass with its weight in 8-bit integers, and the same in bf16."""
+    """Every operator's forward pass with its weight in 8-bit integers, and the same in bf16, as a step runs it."""
     torch, osdp, w = st.torch, st.osdp, st.w
     need = max(max(osdp.osdp_split_linear_i8_workspace_bytes(w.T, op.I, op.O, w.N, op.k)[0],
                    osdp.osdp_split_linear_i8_quantize_workspace_bytes(op.I, op.O, w.N)) for op in w.ops)
@@ -223,18 +219,13 @@ def int8_forward(st, iters, warmup):
 
     def make():
         for d in st.ops:
-            osdp.osdp_split_linear_i8_quantize(d["op"].I, d["op"].O, d["W"], d["Q"], d["scale"], ws)
+            osdp.osdp_split_linear_i8_quantize(d["op"].I, d["op"].O, d["W"], d["Q"], d["scale"], ws, stream=st.sc)
 
     def forward():
         for d in st.ops:
-            osdp.osdp_split_linear_i8_fwd(d["X"], d["Q"], d["scale"], d["Y"], max(d["op"].k, 1), ws)
-
-    def bf16():
-        for d in st.ops:
-            osdp.osdp_split_linear_fwd(d["X"], d["W"], d["Y"], 0, st.ws, plan=st.plan, op_index=d["n"])
-    make()
+            osdp.osdp_split_linear_i8_fwd(d["X"], d["Q"], d["scale"], d["Y"], max(d["op"].k, 1), ws, stream=st.sc)
     ops = w.layers * sum(2 * w.T * op.I * op.O for op in w.ops)
-    t8, t16, tq = median_ms(torch, forward, iters, warmup), median_ms(torch, bf16, iters, warmup), median_ms(torch, make, iters, warmup)
+    tq, t8, t16 = (median_ms(torch, call, iters, warmup, st.sc) for call in (make, forward, st.forward))
     return {"median_ms": round(t8, 4), "tops": round(ops / (t8 * 1e-3) / 1e12, 2), "bf16_median_ms": round(t16, 4),
             "bf16_tflops": round(ops / (t16 * 1e-3) / 1e12, 2), "quantize_ms": round(tq, 4)}
 
