@@ -435,8 +435,8 @@ def _is(t, kind: str) -> bool:
     return name == kind
 
 
-def _one(t, kind: str) -> bool:
-    return t.numel() == 1 and _is(t, kind) and t.is_cuda
+def _one(t, kind: str, table) -> bool:
+    return t.numel() == 1 and _is(t, kind) and t.is_cuda and t.get_device() == table.device
 
 
 class _Allowed(dict):
@@ -516,6 +516,7 @@ class AdamWTable:
         if first is None:
             _refuse("a table needs tensors")
         count, lengths = len(first), [t.numel() for t in first]
+        self.device = first[0].get_device() if first else 0
         types = {}
         for name, ts in lists.items():
             if len(ts) != count:
@@ -524,6 +525,8 @@ class AdamWTable:
                 want = 2 * -(-lengths[i] // OSDP_ADAMW_BLOCK) if name == "exps" else lengths[i]
                 if not t.is_contiguous() or not t.is_cuda or (t.numel() < want if name == "exps" else t.numel() != want):
                     _refuse(f"{name}[{i}] must be a contiguous GPU tensor of {want} elements")
+                if t.get_device() != self.device:
+                    _refuse(f"{name}[{i}] is on another GPU than the table's first tensor")
                 if types.setdefault(name, t.dtype) != t.dtype:
                     _refuse(f"{name} are of different types")
         for name, allowed in (("params", ("torch.bfloat16", "torch.float32")), ("grads", ("torch.bfloat16", "torch.float32")),
@@ -559,8 +562,8 @@ class AdamWTable:
             _refuse(f"{len(grads)} gradients for {self.count} tensors")
         want = "torch.float32" if self.grad_type == OSDP_F32 else "torch.bfloat16"
         for i, g in enumerate(grads):
-            if g.numel() != self.lengths[i] or str(g.dtype) != want or not g.is_contiguous() or not g.is_cuda:
-                _refuse(f"grads[{i}] must be a contiguous GPU tensor of {self.lengths[i]} elements, {want}")
+            if g.numel() != self.lengths[i] or str(g.dtype) != want or not g.is_contiguous() or g.get_device() != self.device:
+                _refuse(f"grads[{i}] must be a contiguous tensor of {self.lengths[i]} elements, {want}, on the GPU that the others are on")
         if _overlap(self._written, _spans(grads)):
             _refuse("gradients share memory with tensors of the table")
         for i, g in enumerate(grads):
@@ -576,22 +579,22 @@ def osdp_adamw_grad_sumsq_workspace_bytes(table: AdamWTable) -> int:
 
 def osdp_adamw_grad_sumsq(table: AdamWTable, sumsq, workspace, *, accumulate: bool = False, stream=None) -> None:
     """``sumsq`` (one float64 on the GPU) = sum of the squares of all of the table's gradients; accumulate: is added to it."""
-    if not _one(sumsq, "torch.float64"):
-        _refuse("sumsq must be one float64 on the GPU")
     nbytes = _check_workspace(workspace, sumsq.get_device())
+    if not _one(sumsq, "torch.float64", table):
+        _refuse("sumsq must be one float64 on the GPU")
     _check(lib.osdp_adamw_grad_sumsq(table.tensors, table.count, table.grad_type, int(bool(accumulate)), sumsq.data_ptr(),
                                      workspace.data_ptr(), nbytes, _stream(stream)))
 
 
 def osdp_adamw_step(table: AdamWTable, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1,
                     grad_sumsq=None, max_norm: float = 0.0, seed: int = 0, step_device=None, lr_device=None, stream=None) -> None:
-    """One AdamW step, in place.  ``grad_sumsq`` (one float64), ``step_device`` (one int64) and ``lr_device`` (one float32)
+    """One AdamW step, in place, of tensors on the current device.  ``grad_sumsq`` (one float64), ``step_device`` (one int64) and ``lr_device`` (one float32)
     are read on the GPU when the kernels run."""
-    if grad_sumsq is not None and not _one(grad_sumsq, "torch.float64"):
+    if grad_sumsq is not None and not _one(grad_sumsq, "torch.float64", table):
         _refuse("grad_sumsq must be one float64 on the GPU")
-    if step_device is not None and not _one(step_device, "torch.int64"):
+    if step_device is not None and not _one(step_device, "torch.int64", table):
         _refuse("step_device must be one int64 on the GPU")
-    if lr_device is not None and not _one(lr_device, "torch.float32"):
+    if lr_device is not None and not _one(lr_device, "torch.float32", table):
         _refuse("lr_device must be one float32 on the GPU")
     o = osdp_adamw_options(lr, beta1, beta2, eps, int(step), int(seed) & 0xFFFFFFFFFFFFFFFF, max_norm,
                            None if grad_sumsq is None else grad_sumsq.data_ptr(),
@@ -609,8 +612,8 @@ def osdp_adamw_state_values(table: AdamWTable, m_out, v_out, *, stream=None) -> 
         if len(outs) != table.count:
             _refuse(f"{len(outs)} {name} for {table.count} tensors")
         for i, t in enumerate(outs):
-            if t.numel() != table.lengths[i] or not _is(t, "torch.bfloat16") or not t.is_contiguous() or not t.is_cuda:
-                _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values on the GPU")
+            if t.numel() != table.lengths[i] or not _is(t, "torch.bfloat16") or not t.is_contiguous() or not t.is_cuda or t.get_device() != table.device:
+                _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values on the GPU that the moments are on")
     if _overlap(_spans(m_out) + _spans(v_out), table._state):
         _refuse("m_out and v_out share memory, with each other or with the moments")
     _check(lib.osdp_adamw_state_values(table.tensors, table.count, _ptrs(m_out), _ptrs(v_out), _stream(stream)))

@@ -345,6 +345,32 @@ def test_values_may_not_share_memory_with_the_moments_or_each_other(no_gpu_work)
     assert "share memory" not in str(e.value)
 
 
+def test_a_table_and_its_scalars_are_on_one_gpu(no_gpu_work):
+    def lists(place=None, device=1):
+        at = lambda i, n, kind, name: OnGpu(n, kind, device if (name, i) == place else 0, address=P * (1 + 2 * len(name) + i) + 4096 * ord(name[0]))  # noqa: E731
+        pair = lambda name, n, kind: [at(i, n, kind, name) for i in range(2)]  # noqa: E731
+        return dict(params=pair("params", 256, "bfloat16"), grads=pair("grads", 256, "bfloat16"), masters=pair("masters", 256, "float32"),
+                    m=pair("m", 256, "uint8"), v=pair("v", 256, "uint8"), exps=pair("exps", 4, "uint8"))
+    for name in lists():
+        for i in range(2):
+            with pytest.raises(osdp.OsdpError, match="GPU") as e:
+                osdp.AdamWTable(**lists((name, i)))
+            assert e.value.status == B.OSDP_ERR_INVALID_ARG
+    table = osdp.AdamWTable(**lists())
+    with pytest.raises(osdp.OsdpError, match="GPU"):
+        table.set_grads(lists(("grads", 1))["grads"])
+    away = lambda kind: OnGpu(1, kind, 1)  # noqa: E731
+    for kw in (dict(grad_sumsq=away("float64")), dict(step_device=away("int64")), dict(lr_device=away("float32"))):
+        with pytest.raises(osdp.OsdpError, match="on the GPU"):
+            osdp.osdp_adamw_step(table, lr=1e-3, **kw)
+    with pytest.raises(osdp.OsdpError, match="on the GPU"):
+        osdp.osdp_adamw_grad_sumsq(table, away("float64"), OnGpu(1024, "uint8", 1))
+    here, there = ([OnGpu(256, device=d, address=(30 + i) * P) for i in range(4)] for d in (0, 1))
+    for m_out, v_out in ((here[:2], there[2:]), (there[:2], here[2:])):
+        with pytest.raises(osdp.OsdpError, match="on the GPU"):
+            osdp.osdp_adamw_state_values(table, m_out, v_out)
+
+
 def test_the_sum_of_squares_refuses_a_workspace_that_is_not_on_the_gpu():
     class Table:
         tensors, count, grad_type = (B.osdp_adamw_tensor * 1)(), 0, 0
