@@ -546,7 +546,6 @@ class AdamWTable:
         self._written = sorted(sum((_spans(ts) for name, ts in lists.items() if name != "grads"), []))
         if _overlap(self._written, _spans(lists.get("grads", []))):
             _refuse("a tensor is listed twice, or tensors of the table share memory")
-        self._state = sum((_spans(lists[name]) for name in ("m", "v", "exps") if name in lists), [])
         self._keep = lists
         self.tensors = (osdp_adamw_tensor * max(count, 1))()
         for i in range(count):
@@ -614,8 +613,6 @@ def osdp_adamw_state_values(table: AdamWTable, m_out, v_out, *, stream=None) -> 
         for i, t in enumerate(outs):
             if t.numel() != table.lengths[i] or not _is(t, "torch.bfloat16") or not t.is_contiguous() or not t.is_cuda or t.get_device() != table.device:
                 _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values on the GPU that the moments are on")
-    if _overlap(_spans(m_out) + _spans(v_out), table._state):
-        _refuse("m_out and v_out share memory, with each other or with the moments")
     _check(lib.osdp_adamw_state_values(table.tensors, table.count, _ptrs(m_out), _ptrs(v_out), _stream(stream)))
 
 

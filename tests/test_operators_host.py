@@ -332,19 +332,6 @@ def test_new_gradients_may_not_share_memory_with_what_is_written():
     table.set_grads([bf16(1 << 30), bf16(1 << 30)])                                # read twice
 
 
-def test_values_may_not_share_memory_with_the_moments_or_each_other(no_gpu_work):
-    m, v, e = OnGpu(256, "uint8", address=P), OnGpu(256, "uint8", address=2 * P), OnGpu(4, "uint8", address=3 * P)
-    table = osdp.AdamWTable(m=[m], v=[v], exps=[e])
-    out = lambda address: [OnGpu(256, address=address)]  # noqa: E731
-    for a, b in ((4 * P, 4 * P), (4 * P, 4 * P + 510), (P, 5 * P), (P - 510, 5 * P), (4 * P, 2 * P + 254), (4 * P, 3 * P + 2)):
-        with pytest.raises(osdp.OsdpError, match="share memory") as e:
-            osdp.osdp_adamw_state_values(table, out(a), out(b))
-        assert e.value.status == B.OSDP_ERR_INVALID_ARG
-    with pytest.raises(osdp.OsdpError) as e:   # side by side: as far as the GPU
-        osdp.osdp_adamw_state_values(table, out(4 * P), out(4 * P + 512))
-    assert "share memory" not in str(e.value)
-
-
 def test_a_table_and_its_scalars_are_on_one_gpu(no_gpu_work):
     def lists(place=None, device=1):
         at = lambda i, n, kind, name: OnGpu(n, kind, device if (name, i) == place else 0, address=P * (1 + 2 * len(name) + i) + 4096 * ord(name[0]))  # noqa: E731
