@@ -439,30 +439,21 @@ def _one(t, kind: str, table) -> bool:
     return t.numel() == 1 and _is(t, kind) and t.is_cuda and t.get_device() == table.device
 
 
-class _Allowed(dict):
-    """Whether shards may have an element type, of ``size`` bytes."""
-    def __init__(self, size, *kinds):
-        super().__init__()
-        self.size, self.kinds = size, kinds
-
-    def __missing__(self, dtype):
-        ok = self[dtype] = str(dtype) in self.kinds
-        return ok
-
-
-_SHARDS = {"w_shards": _Allowed(2, "torch.bfloat16"), "q_shards": _Allowed(1, "torch.int8", "torch.uint8")}
+# element types that shards may have, with their bytes, and the same as DLPack's type codes and bits
+_SHARDS = {"w_shards": (2, ("torch.bfloat16",), bytes((4, 16))), "q_shards": (1, ("torch.int8", "torch.uint8"), bytes((0, 8, 1, 8)))}
 
 
 def _shard_ptrs(name: str, shards, I: int, O: int, device: int):
     """Addresses of shards that are what the library takes them for, and as long as what it reads or writes there."""
-    allowed, N = _SHARDS[name], len(shards)
+    size, kinds, codes = _SHARDS[name]
+    N = len(shards)
     L = -(-I * O // N) if N else 0
-    out = _checked_pointers(shards, L * allowed.size, allowed, device)
+    out = _checked_pointers(shards, L * size, codes, device)
     if out is None:
         for i, t in enumerate(shards):
             n = max(min(L, I * O - i * L), 0)  # (what is behind the last element of the weight may be missing)
-            if t.nbytes < n * allowed.size or not allowed[t.dtype] or t.get_device() != device or not t.is_contiguous():
-                _refuse(f"{name}[{i}] must be a contiguous tensor of at least {n} elements, {' or '.join(allowed.kinds)}, on the GPU that the others are on")
+            if t.numel() < n or not any(_is(t, kind) for kind in kinds) or t.get_device() != device or not t.is_contiguous():
+                _refuse(f"{name}[{i}] must be a contiguous tensor of at least {n} elements, {' or '.join(kinds)}, on the GPU that the others are on")
         out = _ptrs(shards)
     return out
 

@@ -369,6 +369,31 @@ def test_weight_to_8_bits(I, O, N):
     assert got[4, 1] == 64 and got[4, 2] == -64 and np.isnan(scale[1]) and np.isnan(scale[2]) and scale[0] == 0
 
 
+def test_shards_are_looked_at_before_their_addresses_are_taken():
+    """Tensors as a program may have them: views, parameters, several dimensions; and those that do not do."""
+    look = osdp.binding._checked_pointers
+    z = lambda *n, d=torch.int8: torch.zeros(*n, dtype=d, device="cuda")  # noqa: E731
+    flat, weight = z(4096), torch.nn.Parameter(z(64, 8, d=torch.bfloat16))
+    good = [z(1024), flat[7:1031], flat.view(4, 1024)[1], flat.view(torch.uint8)[:1024], z(8, 1, 128), z(1, 1024).t()]
+    bits8, bf16 = bytes((0, 8, 1, 8)), bytes((4, 16))
+    out = look(good, 1024, bits8, 0)
+    assert np.frombuffer(out, np.uint64).tolist() == [t.data_ptr() for t in good]
+    assert np.frombuffer(look([weight, weight.detach()], 1024, bf16, 0), np.uint64).tolist() == [weight.data_ptr()] * 2
+    for bad in (z(1023), flat[::2], flat.view(64, 64).t(), z(1).expand(1024), z(1024, d=torch.bfloat16), z(1024, d=torch.int16), z(1024).cpu(),
+                z(1024, d=torch.bool)):
+        for place in range(2):
+            ts = [z(1024), z(1024)]
+            ts[place] = bad
+            assert look(ts, 1024, bits8, 0) is None
+            w = [z(1024, d=torch.bfloat16) for _ in range(2)]
+            with pytest.raises(osdp.OsdpError, match=r"q_shards\[%d\]" % place):
+                osdp.osdp_split_linear_i8_quantize(64, 32, w, ts, z(32, d=torch.float32), z(1 << 16, d=torch.uint8))
+    for bad in (z(1024, d=torch.float32), z(1024, d=torch.float16), z(511, d=torch.bfloat16)):
+        with pytest.raises(osdp.OsdpError, match="w_shards"):
+            osdp.osdp_split_linear_i8_quantize(64, 32, [z(1024, d=torch.bfloat16), bad], [z(1024), z(1024)], z(32, d=torch.float32), z(1 << 16, d=torch.uint8))
+    assert look([z(1024)], 1024, bits8, 1) is None
+
+
 def test_graph_of_two_products_sharing_a_workspace():
     """Captured one after another on one stream, replayed with other inputs and the program's own work between."""
     a, b = Weight(512, 768, 8), Weight(768, 520, 5)

@@ -292,6 +292,18 @@ def test_the_last_shard_may_hold_less_and_bytes_may_have_no_sign(no_gpu_work):
                 assert ("q_shards[18]" in str(e.value)) == bool(less and N == 19), e.value
 
 
+def test_the_look_at_shards_leaves_to_python_what_it_cannot_answer():
+    import torch
+    look, kinds = B._checked_pointers, bytes((0, 8))
+    assert look([], 64, kinds, 0) == b""
+    for ts in ([torch.zeros(64, dtype=torch.int8)], (torch.zeros(64),), [OnGpu(64, "int8")], [None], [3, "x"],
+               [torch.zeros(4).to_sparse()], [torch.zeros(64, dtype=torch.int8, device="meta")]):
+        assert look(ts, 1, kinds, 0) is None
+    for args in (([], 1, kinds), ([], 1, "x", 0), (3, 1, kinds, 0), ([], "1", kinds, 0), ([], 1, kinds, None), ([], 1 << 70, kinds, 0)):
+        with pytest.raises((TypeError, OverflowError)):
+            look(*args)
+
+
 @pytest.mark.parametrize("place", ["X", "Y", "scale", "ws"])
 @pytest.mark.parametrize("device", [-1, 1])
 def test_the_binding_refuses_other_devices(no_gpu_work, place, device):
