@@ -439,8 +439,9 @@ def _one(t, kind: str, table) -> bool:
     return t.numel() == 1 and _is(t, kind) and t.is_cuda and t.get_device() == table.device
 
 
+_BF16 = bytes((4, 16))  # DLPack's type code, bits
 # element types that shards may have, with their bytes, and the same as DLPack's type codes and bits
-_SHARDS = {"w_shards": (2, ("torch.bfloat16",), bytes((4, 16))), "q_shards": (1, ("torch.int8", "torch.uint8"), bytes((0, 8, 1, 8)))}
+_SHARDS = {"w_shards": (2, ("torch.bfloat16",), _BF16), "q_shards": (1, ("torch.int8", "torch.uint8"), bytes((0, 8, 1, 8)))}
 
 
 def _shard_ptrs(name: str, shards, I: int, O: int, device: int):
@@ -598,13 +599,18 @@ def osdp_adamw_state_values(table: AdamWTable, m_out, v_out, *, stream=None) -> 
     """The bf16 values of moments in 8 bits: ``m_out`` and ``v_out`` hold one bf16 tensor for each of the table's."""
     if table.state_bits != 8:
         _refuse("the table's moments are not in 8 bits")
+    places = []
     for name, outs in (("m_out", m_out), ("v_out", v_out)):
         if len(outs) != table.count:
             _refuse(f"{len(outs)} {name} for {table.count} tensors")
-        for i, t in enumerate(outs):
-            if t.numel() != table.lengths[i] or not _is(t, "torch.bfloat16") or not t.is_contiguous() or not t.is_cuda or t.get_device() != table.device:
-                _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values on the GPU that the moments are on")
-    _check(lib.osdp_adamw_state_values(table.tensors, table.count, _ptrs(m_out), _ptrs(v_out), _stream(stream)))
+        at = _checked_pointers(outs, 0, _BF16, outs[0].get_device()) if outs else b""
+        if at is None or [t.numel() for t in outs] != table.lengths or (outs and outs[0].get_device() != table.device):
+            for i, t in enumerate(outs):
+                if t.numel() != table.lengths[i] or not _is(t, "torch.bfloat16") or not t.is_contiguous() or not t.is_cuda or t.get_device() != table.device:
+                    _refuse(f"{name}[{i}] must be {table.lengths[i]} contiguous bf16 values on the GPU that the moments are on")
+            at = _ptrs(outs)
+        places.append(at)
+    _check(lib.osdp_adamw_state_values(table.tensors, table.count, *places, _stream(stream)))
 
 
 def osdp_split_linear_i8_quantize_workspace_bytes(I, O, N) -> int:
