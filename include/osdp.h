@@ -528,6 +528,7 @@ OSDP_API osdp_status osdp_split_linear_i8_quantize_workspace_bytes(const osdp_sh
  *   X : device [T x I] bf16, ldx >= I     Y : device [T x O] bf16, ldy >= O (every element written)
  *   workspace: device, 256-byte aligned, >= osdp_split_linear_i8_workspace_bytes: [Xq and s_t][sums of tiles whose reduction
  *              workgroups share][staging slot]; what does for T tokens does for fewer
+ * Y overlaps no input and not the workspace (one that overlaps X is refused: each token is read more than once).
  * T = 0 does nothing.  The slice bounds must be multiples of 8. */
 OSDP_API osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int64_t ldx,
                                               const void *const *q_shards, const float *w_scale, void *Y, int64_t ldy,

@@ -301,6 +301,17 @@ osdp_status check_matrix(const void *p, int64_t ld, int64_t cols, const char *na
   return OSDP_OK;
 }
 
+// Whether T rows of I elements, ldx apart, and T of O, ldy apart, share any.  Rows of one length apart meet where those of the one fall into
+// columns of the other; of different lengths, anywhere (nobody lays matrices into one another so).
+bool overlap(const void *x, int64_t ldx, int64_t I, const void *y, int64_t ldy, int64_t O, int64_t T) {
+  const int64_t d = (static_cast<int64_t>(reinterpret_cast<uintptr_t>(y)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(x))) / 2;
+  if (d >= (T - 1) * ldx + I || -d >= (T - 1) * ldy + O) return false;
+  if (ldx != ldy || T == 1) return true;
+  // rows i of X and j of Y meet where (i - j) ld lies in (d - I, d + O)
+  auto floor_div = [ldx](int64_t a) { return a / ldx - (a % ldx < 0); };
+  return std::max(floor_div(d - I) + 1, 1 - T) <= std::min(-floor_div(-d - O) - 1, T - 1);
+}
+
 osdp_status check_workspace(const void *ws, size_t bytes, size_t need) {
   if (!ws) return fail(OSDP_ERR_INVALID_ARG, "workspace is NULL");
   if (!aligned(ws, kAlign)) return fail(OSDP_ERR_UNSUPPORTED, "workspace is not 256-byte aligned");
@@ -509,6 +520,7 @@ osdp_status osdp_split_linear_i8_fwd(const osdp_shape *shape, const void *X, int
   if ((st = fill_table(q_shards, w.N, "q_shards", &tab)) != OSDP_OK) return st;
   if ((st = check_scale(w_scale)) != OSDP_OK) return st;
   if (!no_tokens && (st = check_workspace(workspace, workspace_bytes, token_bytes(w) + round_up(static_cast<size_t>(widest) * w.I, kAlign))) != OSDP_OK) return st;
+  if (!no_tokens && overlap(X, ldx, w.I, Y, ldy, w.O, w.T)) return fail(OSDP_ERR_INVALID_ARG, "Y overlaps X");
   if ((st = device_ok()) != OSDP_OK) return st;
   if (no_tokens) return OSDP_OK;
   const hipStream_t q = static_cast<hipStream_t>(stream);

@@ -114,6 +114,29 @@ def test_i8_forward_refuses(more, status):
     assert osdp.lib.osdp_last_error()
 
 
+def test_i8_forward_refuses_outputs_that_overlap_its_tokens():
+    """Every workgroup reads the tokens while others store.  Against sets of addresses: rows of one length apart, matrices beside, between, behind and
+    in one another."""
+    import random
+    rng = random.Random(11)
+    seen = {True: 0, False: 0}
+    for _ in range(3000):
+        T, I, O = rng.randrange(1, 5), 16 * rng.randrange(1, 4), 8 * rng.randrange(1, 5)
+        ldx = I + 8 * rng.randrange(0, 8)
+        ldy = max(ldx, O) if rng.random() < 0.8 else O + 8 * rng.randrange(0, 8)
+        d = 8 * rng.randrange(-T * ldy // 8 - 2, T * ldx // 8 + 3)
+        cells = lambda at, ld, n: {(at + t * ld + c) for t in range(T) for c in range(0, n, 8)}  # noqa: E731
+        meet = bool(cells(0, ldx, I) & cells(d, ldy, O))
+        status = i8_fwd(T=T, I=I, O=O, N=1, X=P, ldx=ldx, Y=P + 2 * d, ldy=ldy, shards=[8 * P], ws_bytes=1 << 40)
+        if ldx == ldy or T == 1:
+            assert (status == B.OSDP_ERR_INVALID_ARG) == meet, (T, I, O, ldx, ldy, d)
+        elif meet or status == B.OSDP_ERR_INVALID_ARG:   # rows of different lengths: where the matrices reach into one another at all
+            assert status == B.OSDP_ERR_INVALID_ARG and -((T - 1) * ldy + O) < d < (T - 1) * ldx + I, (T, I, O, ldx, ldy, d)
+        seen[meet] += 1
+    assert min(seen.values()) > 300
+    assert i8_fwd(T=0, X=P, Y=P) != B.OSDP_ERR_INVALID_ARG
+
+
 @pytest.mark.parametrize("T,I,O,N,k", [(1, 16, 8, 1, 0), (500, 2560, 10240, 8, 4), (500, 2560, 10248, 16, 3), (64, 4096, 24, 64, 1),
                                        (65, 4096, 24, 16, 3), (0, 64, 32, 2, 1), (300, 4096, 256, 16, 1), (300, 4096, 1000, 8, 1)])
 def test_i8_workspace_follows_the_law(T, I, O, N, k):
@@ -266,7 +289,7 @@ def test_the_binding_refuses_other_shards(no_gpu_work, name, bad, place):
 
     def call():
         if name == "fwd":
-            osdp.osdp_split_linear_i8_fwd(OnGpu((2, I)), q, scale, OnGpu((2, O)), 1, ws)
+            osdp.osdp_split_linear_i8_fwd(OnGpu((2, I)), q, scale, OnGpu((2, O), address=2 * P), 1, ws)
         else:
             osdp.osdp_split_linear_i8_quantize(I, O, w, q, scale, ws)
     with pytest.raises(osdp.OsdpError) as e:   # what is right gets as far as the GPU
@@ -288,7 +311,7 @@ def test_the_last_shard_may_hold_less_and_bytes_may_have_no_sign(no_gpu_work):
             for less in (0, 1):
                 q = [OnGpu(L, kind) for _ in range(N - 1)] + [OnGpu(max(I * O - (N - 1) * L - less, 0), kind)]
                 with pytest.raises(osdp.OsdpError) as e:
-                    osdp.osdp_split_linear_i8_fwd(OnGpu((2, I)), q, OnGpu(O, "float32"), OnGpu((2, O)), 1, OnGpu(1 << 30, "uint8"))
+                    osdp.osdp_split_linear_i8_fwd(OnGpu((2, I)), q, OnGpu(O, "float32"), OnGpu((2, O), address=2 * P), 1, OnGpu(1 << 30, "uint8"))
                 assert ("q_shards[18]" in str(e.value)) == bool(less and N == 19), e.value
 
 
