@@ -435,7 +435,8 @@ OSDP_API osdp_status osdp_plan_search(const osdp_operator_cost *ops, int32_t n, 
  * Random numbers: with mix(x) = { x *= 0x9E3779B1; x ^= x >> 15; x *= 0x2C1B3C6D; x ^= x >> 13 } on 32 bits, element i of the
  * tensor at place j of the array has h = mix(lo(i) + mix(mix(mix(mix(mix(lo(seed)) ^ hi(seed)) ^ lo(t)) ^ j) ^ hi(i))),
  * lo / hi = lower / upper 32 bits: m adds the lower 16 bits of h (below its last fraction bit, as a fraction of it) before it
- * is cut, v the upper 16, a bf16 parameter the upper 16 of h * 0x297A2D39.  Results are a function of the inputs alone.
+ * is cut, v the upper 16, a bf16 parameter the upper 16 of h * 0x297A2D39.  Results are a function of the inputs alone: replicas on
+ * several ranks stay equal if they are given the same seed, step and gradients, and each tensor the same place in the array.
  *
  * Tensors: any lengths (0 too) and, element by element, any alignment; exps must be 2-byte aligned.  The widest accesses are
  * used for those whose arrays are all 16-byte aligned (moments in 8 bits: 8-byte).  No two arrays of a call may overlap.
@@ -498,7 +499,8 @@ OSDP_API osdp_status osdp_adamw_state_values(const osdp_adamw_tensor *tensors, i
  *     Y[t, o] = bf16( (sum_i Xq[t, i] Wq[o, i]) * s_t * s_o )
  * round: to the nearest whole number, halves away from zero, exactly (the quotient of two bf16 numbers is never so close to
  * a half that fp32 could not tell).  The sum is one of whole numbers, so exact: Y does not depend on the shards, on k or on
- * the kernel.  A token of zeros gives 0; a token or channel that holds a NaN or an infinity gives NaN in all of its outputs.
+ * the kernel.  It is rounded to fp32 and multiplied by s_t and then by s_o in fp32, which is off by 2^-22 at most (before the rounding to bf16) for tokens whose largest
+ * magnitude lies between 2^-119 and 2^104; beyond 2^104 the first product may be infinite, below 2^-119 s_t has fewer bits.  A token of zeros gives 0; a token or channel that holds a NaN or an infinity gives NaN in all of its outputs.
  *
  * Layout: Wq lies [O x I], input features contiguous, in N flat shards as elsewhere: f = o*I + i in shard f / L at f % L,
  * L = ceil(I*O/N), the last shard's tail neither read nor written by the product (the quantization leaves it as it is).

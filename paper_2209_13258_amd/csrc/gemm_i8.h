@@ -127,7 +127,7 @@ struct I8Row {
 constexpr int kI8Turn = 4096;
 
 // Where a workgroup of the kernels for few tokens begins, whose waves take kSpan bytes of a row together: 32 workgroups that follow one
-// another, four to an XCD, at one place, the next 32 behind it.  One token, weight from memory: 4096 -> 16384 17.6 us, so 14.6; 8192 -> 32768 50.5
+// another, four to an XCD, at one place, the next 32 behind it.  One token, weight from memory: 4096 -> 16384 17.2 us, so 15.1; 8192 -> 32768 50.5
 // and 47.0, 16384 -> 16384 55.4 and 53.3, 24576 -> 8192 46.5 and 42.2; where neighbours, which run on different XCDs, differ instead: 15.3, 54.5, 72.8 and 47.8.
 template <int kSpan>
 __device__ __forceinline__ int i8_first(int I) {
@@ -139,7 +139,8 @@ __device__ __forceinline__ int i8_first(int I) {
 // to registers, each lane 16 bytes of a row, the four lanes of a row 64 in sequence; nothing of them is used twice, so nothing is
 // staged.  Both are bound by the weight's bytes.
 //
-// Tokens that are in 8 bits already.  4 tokens, 4096 -> 16384, rounded in a launch before it: 18.0 us in all, 3.7 TB/s.  32 or 64 channels to a
+// Tokens that are in 8 bits already.  4 tokens, 4096 -> 16384, rounded in a launch before it: 17.9 us in all with the weight from memory (3.7 TB/s), 22.4
+// before workgroups began at different places.  Before that too, 32 or 64 channels to a
 // workgroup, which read the tokens half or a quarter as often, took 22 and 25 us where 16 took 25 (16 tokens), but 20 to 31 instead of 15 for
 // 10240 -> 2560, whose workgroups then leave half the card or more idle.
 //
@@ -198,8 +199,8 @@ __global__ __launch_bounds__(kWaves * 64) void i8_few_kernel(I8Problem p) {
 
 // The same with the tokens' rounding in the launch, for tokens of so few features that the bytes of 16 of them fit in LDS and
 // that every workgroup may well round its 16 for itself: one launch instead of two, the first weights on their way meanwhile.
-// One token, 4096 -> 16384: 14.9 us in one launch, 16.8 in two, one call behind another, before both began at different places; 12.4 since, with
-// the weight from memory (5.4 TB/s).
+// One token, 4096 -> 16384, one call behind another: 15.1 us in one launch, 17.4 in two, with the weight from memory (4.4 TB/s); 12.5 and 15.4 from the
+// last-level cache.
 template <int kWaves, int kUnroll, bool kFlat>
 __global__ __launch_bounds__(kWaves * 64) void i8_fused_kernel(I8Problem p, const uint16_t *__restrict__ x, int64_t ldx) {
   constexpr int kStep = 64 * kUnroll, kSpan = kWaves * kStep;

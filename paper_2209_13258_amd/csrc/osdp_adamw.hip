@@ -10,7 +10,7 @@
 //
 // What bounds it: memory with moments in fp32 (78.7 million elements, 2.2 GB: 402 us, 5.5 TB/s) and with a master copy and moments in 8
 // bits (1.57 GB with their values read back: 283 us); without a master copy the 55 instructions that two codes, a random number and a
-// rounded parameter cost an element keep the vector units as busy as its 10 bytes keep memory (201 million elements: 359 us, 5.6 TB/s).  More waves to a SIMD would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
+// rounded parameter cost an element keep the vector units as busy as its 10 bytes keep memory (201 million elements: 362 us, 5.6 TB/s).  More waves to a SIMD would have to spill: a bound of six costs 7 % there and 12 % with a master copy.
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
@@ -65,7 +65,8 @@ struct Step {
 
 enum Form { kMaster = 0, kBf16 = 1, kF32 = 2 };
 
-// 32 bits stirred: multiplications by odd numbers and shifted sums without carry, each of them one to one.
+// 32 bits stirred: multiplications by odd numbers and shifted sums without carry, each of them one to one.  The first number is 2^32 over the golden ratio
+// (Knuth's multiplicative hashing); 0x2C1B3C6D and 0x297A2D39 were published by Chris Wellons, from a search for numbers that let every bit reach every other.
 constexpr uint32_t kStir = 0x9E3779B1u;
 __device__ __forceinline__ uint32_t stir(uint32_t x) {  // mix() behind its first product
   x ^= x >> 15;

@@ -403,8 +403,9 @@ hipError_t launch_product(const I8Problem &p, hipStream_t stream) {
 
 // Whether tokens are rounded inside the product's launch: every workgroup, of 16 tokens and 16 channels, does it again, which
 // 2^14 values are quick enough for as long as there are not too many workgroups.  (One token is always: it is read by all of them anyway.)  us in
-// two launches / one, one call behind another: 1 token 512 -> 512 9.0 / 6.3, 4096 -> 16384 16.8 / 14.9; 64 tokens 512 -> 1024 9.1 / 6.2; at the line
-// 512 of 512 -> 512 9.2 / 8.6 and 128 of 1024 -> 1024 9.2 / 7.7; beyond it 256 of 256 -> 2048 9.3 / 14.5, 3 of 4096 -> 16384 15.6 / 18.2.
+// two launches / one, one call behind another, and captured: 1 token 512 -> 512 8.9 / 6.8 and 4.7 / 3.4, 4096 -> 16384 17.4 / 15.1 and 16.7 / 14.6; 64 tokens
+// 512 -> 1024 8.5 / 6.6 and 5.6 / 5.0; at the line 512 of 512 -> 512 8.8 / 8.9 and 7.0 / 8.3, 128 of 1024 -> 1024 8.5 / 7.7 and 7.2 / 7.6; beyond it 256 of
+// 256 -> 2048 8.8 / 14.6 and 6.4 / 14.6, 3 of 4096 -> 16384 17.4 / 17.4 and 17.4 / 17.4.
 bool rounds_inside(const Weight &w) {
   const int64_t values = std::min<int64_t>(w.T, 16) * w.I;
   if (values > (1 << 14) || w.O > kI8FewChannels) return false;
@@ -413,7 +414,9 @@ bool rounds_inside(const Weight &w) {
 }
 
 // Whether slices have to be gathered, and whether they may be: with many tokens the tiles that end with each shard can cost more than a
-// dense copy of the weight does.
+// dense copy of the weight does.  Cut within channels, us in place (up to 64 tokens) / gathered (65), 16 shards: 4096 -> 16392 33 tokens 39 / 47, 64
+// 56 / 47; 8192 -> 32776 33 tokens 122 / 180, 64 185 / 180; 16384 -> 4104 48 tokens 66 / 53, 64 82 / 53: the line is right for wide weights, and
+// too far for long ones.
 bool has_to_gather(const Weight &w) { return (w.T > kI8FewTokens || w.O > kI8FewChannels) && w.rows_each < kI8ShardRows; }
 bool may_gather(const Weight &w) { return has_to_gather(w) || (w.T > kI8ManyTokens && w.N > 1 && w.rows_each % 256 != 0); }
 
