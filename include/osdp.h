@@ -295,6 +295,76 @@ OSDP_API osdp_status osdp_split_linear_bwd_mixed(const osdp_shape *shape, const 
                                                  void *workspace, size_t workspace_bytes, void *stream_compute,
                                                  void *stream_copy);
 
+/* ---- what stands around the product ------------------------------------------
+ * The same operators with a bias b, an activation and a residual R [T x O], as a transformer layer has them around its linear
+ * operators, in the product's own epilogue: the sum in fp32 is not rounded before them.
+ *     forward  : z = X . W + b      Y = bf16( act(z) + R )      Z = bf16( z ), kept for the backward pass
+ *     backward : dZ = bf16( dY * act'(Z) )   db = sum over tokens of dY * act'(Z)   dX, dW from dZ as above   (dR is dY)
+ *     act(z) : none    z
+ *              relu    max(z, 0); its slope at 0 is 0
+ *              gelu    z * Phi(z), Phi the normal distribution function
+ *              gelu_tanh  z / 2 * (1 + tanh( sqrt(2 / pi) * (z + 0.044715 z^3) ))
+ *              silu    z / (1 + exp(-z))
+ * Activations and slopes are computed in fp32, off by less than 2^-15 relative (the slopes: of 1) before the rounding.  NaN in
+ * gives NaN out (relu's slope at NaN is 1); z of minus infinity gives NaN in gelu, gelu_tanh and silu, as minus infinity
+ * times 0 does.  Without bias, activation, residual and Z the calls are osdp_split_linear_fwd_mixed and _bwd_mixed, bit for bit.
+ * b and db are replicated vectors: fp32 or bf16, alike, 16-byte aligned, O elements. */
+
+typedef enum { OSDP_BF16 = 0, OSDP_F32 = 1 } osdp_dtype;
+
+typedef enum {
+  OSDP_ACT_NONE = 0,
+  OSDP_ACT_RELU = 1,
+  OSDP_ACT_GELU = 2,
+  OSDP_ACT_GELU_TANH = 3,
+  OSDP_ACT_SILU = 4
+} osdp_activation;
+
+typedef struct {
+  const void *bias;     /* device [O] of bias_type, or NULL                                          */
+  const void *residual; /* device [T x O] bf16, or NULL.  May be Y itself (the same pointer and leading dimension) */
+  int64_t ld_residual;  /* >= O                                                                      */
+  void *z;              /* device [T x O] bf16, written, or NULL                                     */
+  int64_t ldz;          /* >= O                                                                      */
+  int32_t activation;   /* an osdp_activation                                                        */
+  int32_t bias_type;    /* an osdp_dtype                                                             */
+} osdp_epilogue;
+
+typedef struct {
+  const void *z;        /* device [T x O] bf16: what the forward pass kept; NULL without an activation */
+  int64_t ldz;          /* >= O                                                                      */
+  void *dz;             /* device [T x O] bf16, written; may be dY or z itself (the same pointer and leading dimension).
+                           NULL without an activation: dZ is dY                                      */
+  int64_t lddz;         /* >= O                                                                      */
+  void *dbias;          /* device [O] of bias_type, written, or NULL                                 */
+  int32_t activation;   /* an osdp_activation                                                        */
+  int32_t bias_type;    /* an osdp_dtype                                                             */
+} osdp_epilogue_grad;
+
+/* Bytes of workspace of the two calls below: those of osdp_split_linear_workspace_bytes, and, backward, the partial sums of
+ * db behind them. */
+OSDP_API osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape *shape, const osdp_plan *plan,
+                                                                int32_t op_index, int32_t is_bwd, size_t *total,
+                                                                size_t *peak_weight_staging);
+
+/* Forward.  Plans, modes (w_dp: NULL when no slice is DP), few tokens and streams as osdp_split_linear_fwd_mixed.  Y and Z
+ * overlap no input, each other or the workspace, but for a residual that is Y. */
+OSDP_API osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
+                                                    const osdp_epilogue *epilogue, const void *X, int64_t ldx,
+                                                    const void *const *w_shards, const void *const *w_dp, int64_t ld_dp,
+                                                    void *Y, int64_t ldy, void *workspace, size_t workspace_bytes,
+                                                    void *stream_compute, void *stream_copy);
+
+/* Backward: one pass for dZ and db, then osdp_split_linear_bwd_mixed with dZ in the place of dY (which also says what dX may
+ * take the place of: X, or with few tokens dZ).  db is the sum in fp32 in an order that T and O alone decide, rounded once if
+ * bias_type asks for it.  T = 0 stores db = 0 and dW = 0. */
+OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
+                                                    const osdp_epilogue_grad *epilogue, const void *X, int64_t ldx,
+                                                    const void *dY, int64_t lddy, const void *const *w_shards,
+                                                    const void *const *w_dp, int64_t ld_dp, void *dX, int64_t lddx,
+                                                    void *const *dw_shards, void *const *dw_dp, void *workspace,
+                                                    size_t workspace_bytes, void *stream_compute, void *stream_copy);
+
 /* ---- automatic slice granularity ------------------------------------------
  * Section 4.3 (effectiveness of operator splitting) observes that the best
  * granularity depends on the operator: small operators pay time for every extra
@@ -441,8 +511,6 @@ OSDP_API osdp_status osdp_plan_search(const osdp_operator_cost *ops, int32_t n, 
  * Tensors: any lengths (0 too) and, element by element, any alignment; exps must be 2-byte aligned.  The widest accesses are
  * used for those whose arrays are all 16-byte aligned (moments in 8 bits: 8-byte).  No two arrays of a call may overlap.
  * Where N does not divide I*O, n of the last shard leaves its padding out, which the backward pass does not write. */
-
-typedef enum { OSDP_BF16 = 0, OSDP_F32 = 1 } osdp_dtype;
 
 typedef struct {
   int64_t n;          /* elements, 0 <= n < 2^40                                                     */

@@ -39,6 +39,13 @@ OSDP_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 OSDP_BF16 = 0
 OSDP_F32 = 1
+
+OSDP_ACT_NONE = 0
+OSDP_ACT_RELU = 1
+OSDP_ACT_GELU = 2       # z Phi(z), Phi the normal distribution function
+OSDP_ACT_GELU_TANH = 3  # its approximation by tanh
+OSDP_ACT_SILU = 4
+
 OSDP_ADAMW_BLOCK = 128  # elements that share a power of two in moments of 8 bits
 
 OSDP_KERNEL_GATHER = 0
@@ -60,6 +67,7 @@ EXPORTS = (
     "osdp_adamw_step", "osdp_adamw_grad_sumsq", "osdp_adamw_grad_sumsq_workspace_bytes", "osdp_adamw_state_values",
     "osdp_split_linear_i8_quantize", "osdp_split_linear_i8_quantize_workspace_bytes", "osdp_split_linear_i8_fwd",
     "osdp_split_linear_i8_workspace_bytes",
+    "osdp_split_linear_epilogue_workspace_bytes", "osdp_split_linear_fwd_epilogue", "osdp_split_linear_bwd_epilogue",
 )
 
 
@@ -115,6 +123,16 @@ class osdp_adamw_options(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class osdp_epilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64), ("z", ctypes.c_void_p),
+                ("ldz", ctypes.c_int64), ("activation", ctypes.c_int32), ("bias_type", ctypes.c_int32)]
+
+
+class osdp_epilogue_grad(ctypes.Structure):
+    _fields_ = [("z", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64),
+                ("dbias", ctypes.c_void_p), ("activation", ctypes.c_int32), ("bias_type", ctypes.c_int32)]
+
+
 class OsdpError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"libosdp status {status}: {message}")
@@ -163,6 +181,13 @@ def _load() -> ctypes.CDLL:
     lib.osdp_split_linear_i8_quantize_workspace_bytes.argtypes = [shp, ctypes.POINTER(ctypes.c_size_t)]
     lib.osdp_split_linear_i8_fwd.argtypes = [shp, vp, i64, vp, vp, vp, i64, vp, ctypes.c_size_t, vp]
     lib.osdp_split_linear_i8_workspace_bytes.argtypes = [shp, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]
+    epi, epg = ctypes.POINTER(osdp_epilogue), ctypes.POINTER(osdp_epilogue_grad)
+    lib.osdp_split_linear_epilogue_workspace_bytes.argtypes = [shp, pln, i32, i32, ctypes.POINTER(ctypes.c_size_t),
+                                                               ctypes.POINTER(ctypes.c_size_t)]
+    lib.osdp_split_linear_fwd_epilogue.argtypes = [shp, pln, i32, epi, vp, i64, vp, vp, i64, vp, i64, vp, ctypes.c_size_t, vp, vp]
+    lib.osdp_split_linear_bwd_epilogue.argtypes = [shp, pln, i32, epg, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp,
+                                                   ctypes.c_size_t, vp, vp]
+    lib.hipGetDevice.argtypes = [ctypes.POINTER(ctypes.c_int)]  # (the HIP runtime, which the library brings along)
     lib.osdp_debug_option.argtypes = [ctypes.c_char_p, i32]
     lib.osdp_debug_option.restype = ctypes.c_int
     lib.osdp_profile_begin.argtypes = [i32]
@@ -177,7 +202,8 @@ def _load() -> ctypes.CDLL:
                  "osdp_profile_begin", "osdp_profile_end", "osdp_adamw_step", "osdp_adamw_grad_sumsq",
                  "osdp_adamw_grad_sumsq_workspace_bytes", "osdp_adamw_state_values", "osdp_split_linear_i8_quantize",
                  "osdp_split_linear_i8_quantize_workspace_bytes", "osdp_split_linear_i8_fwd",
-                 "osdp_split_linear_i8_workspace_bytes"):
+                 "osdp_split_linear_i8_workspace_bytes", "osdp_split_linear_epilogue_workspace_bytes",
+                 "osdp_split_linear_fwd_epilogue", "osdp_split_linear_bwd_epilogue"):
         getattr(lib, name).restype = ctypes.c_int
     lib.osdp_strerror.argtypes = [ctypes.c_int]
     lib.osdp_strerror.restype = ctypes.c_char_p
@@ -441,7 +467,7 @@ def _one(t, kind: str, table) -> bool:
 
 _BF16 = bytes((4, 16))  # DLPack's type code, bits
 # element types that shards may have, with their bytes, and the same as DLPack's type codes and bits
-_SHARDS = {"w_shards": (2, ("torch.bfloat16",), _BF16), "q_shards": (1, ("torch.int8", "torch.uint8"), bytes((0, 8, 1, 8)))}
+_SHARDS = {"w_shards": (2, ("torch.bfloat16",), _BF16), "dw_shards": (2, ("torch.bfloat16",), _BF16), "q_shards": (1, ("torch.int8", "torch.uint8"), bytes((0, 8, 1, 8)))}
 
 
 def _shard_ptrs(name: str, shards, I: int, O: int, device: int):
@@ -653,6 +679,116 @@ def osdp_split_linear_i8_fwd(X, q_shards, w_scale, Y, k, workspace, *, stream=No
     shape = osdp_shape(T, I, O, len(q_shards), k)
     _check(lib.osdp_split_linear_i8_fwd(ctypes.byref(shape), X.data_ptr(), ldx, _shard_ptrs("q_shards", q_shards, I, O, device), w_scale.data_ptr(),
                                         Y.data_ptr(), ldy, workspace.data_ptr(), _check_workspace(workspace, device), _stream(stream)))
+
+
+@dataclass
+class Epilogue:
+    """What a forward product's result goes through: Y = activation(X W + bias) + residual, z = X W + bias.
+
+    ``bias``: O contiguous bf16 or fp32; ``residual`` (may be Y itself) and ``z`` (written): bf16 matrices like Y."""
+    bias: Optional[object] = None
+    activation: int = OSDP_ACT_NONE
+    residual: Optional[object] = None
+    z: Optional[object] = None
+
+
+@dataclass
+class EpilogueGrad:
+    """The backward pass in front of the products': dz = dY activation'(z), dbias = the sum of that over the tokens.
+
+    ``z`` (what the forward pass kept) and ``dz`` (written; may be dY or z itself) are bf16 matrices like dY, both None without an
+    activation; ``dbias`` (written, or None): O contiguous bf16 or fp32."""
+    activation: int = OSDP_ACT_NONE
+    z: Optional[object] = None
+    dz: Optional[object] = None
+    dbias: Optional[object] = None
+
+
+def _current_device() -> int:
+    device = ctypes.c_int(-1)
+    lib.hipGetDevice(ctypes.byref(device))
+    return device.value
+
+
+def _here(t, name: str) -> int:
+    """The device that the tensor is on, which has to be the current one: that is where the kernels run."""
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        _refuse(f"{name} must be on the current GPU")
+    return device
+
+
+def _matrix(t, name: str, rows: int, cols: int, device: int):
+    """(address, leading dimension) of a bf16 matrix."""
+    if tuple(t.shape) != (rows, cols) or not _is(t, "torch.bfloat16") or t.get_device() != device:
+        _refuse(f"{name} must be a bf16 matrix of {rows} x {cols} on the GPU that X is on")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse(f"{name} must have unit stride along its rows")
+    return t.data_ptr(), ld if rows > 1 else cols  # (the stride of a single row means nothing)
+
+
+def _vector(t, name: str, n: int, device: int):
+    """(address, osdp_dtype) of a contiguous bf16 or fp32 vector."""
+    kind = OSDP_BF16 if _is(t, "torch.bfloat16") else OSDP_F32 if _is(t, "torch.float32") else -1
+    if kind < 0 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        _refuse(f"{name} must be {n} contiguous bf16 or float32 on the GPU that the others are on")
+    return t.data_ptr(), kind
+
+
+def osdp_split_linear_epilogue_workspace_bytes(T, I, O, N, k, is_bwd: bool, plan: Optional[Plan] = None, op_index: int = 0):
+    """Returns (total workspace bytes, peak gathered-weight staging bytes)."""
+    shape = _shape(T, I, O, N, k)
+    total, peak = ctypes.c_size_t(), ctypes.c_size_t()
+    pref, _keep = _plan_ref(plan)
+    _check(lib.osdp_split_linear_epilogue_workspace_bytes(ctypes.byref(shape), pref, op_index, int(bool(is_bwd)),
+                                                          ctypes.byref(total), ctypes.byref(peak)))
+    return total.value, peak.value
+
+
+def osdp_split_linear_fwd_epilogue(X, w_shards, Y, k, workspace, *, epilogue: Epilogue, plan: Optional[Plan] = None,
+                                   op_index: int = 0, w_dp=None, ld_dp: int = 0, stream_compute=None, stream_copy=None):
+    """Y[T x O] = activation(X[T x I] . W + bias) + residual; W as N shard tensors, and ``w_dp`` for slices in DP mode."""
+    T, I = X.shape
+    O = Y.shape[1]
+    device = _here(X, "X")
+    x, ldx = _matrix(X, "X", T, I, device)
+    y, ldy = _matrix(Y, "Y", T, O, device)
+    bias, kind = (None, OSDP_BF16) if epilogue.bias is None else _vector(epilogue.bias, "bias", O, device)
+    residual, ldr = (None, 0) if epilogue.residual is None else _matrix(epilogue.residual, "residual", T, O, device)
+    z, ldz = (None, 0) if epilogue.z is None else _matrix(epilogue.z, "z", T, O, device)
+    e = osdp_epilogue(bias, residual, ldr, z, ldz, epilogue.activation, kind)
+    shape = _shape(T, I, O, len(w_shards), k)
+    pref, _keep = _plan_ref(plan)
+    _check(lib.osdp_split_linear_fwd_epilogue(ctypes.byref(shape), pref, op_index, ctypes.byref(e), x, ldx,
+                                              _shard_ptrs("w_shards", w_shards, I, O, device), _opt_ptrs(w_dp), int(ld_dp), y, ldy,
+                                              workspace.data_ptr(), _check_workspace(workspace, device), _stream(stream_compute),
+                                              _stream(stream_copy)))
+
+
+def osdp_split_linear_bwd_epilogue(X, dY, w_shards, dX, dw_shards, k, workspace, *, epilogue: EpilogueGrad,
+                                   plan: Optional[Plan] = None, op_index: int = 0, w_dp=None, ld_dp: int = 0, dw_dp=None,
+                                   stream_compute=None, stream_copy=None):
+    """dz and dbias, then dX[T x I] and the shard-major dW from them; ``w_dp`` and ``dw_dp`` for slices in DP mode."""
+    T, I = X.shape
+    O = dY.shape[1]
+    device = _here(X, "X")
+    x, ldx = _matrix(X, "X", T, I, device)
+    dy, lddy = _matrix(dY, "dY", T, O, device)
+    dx, lddx = _matrix(dX, "dX", T, I, device)
+    z, ldz = (None, 0) if epilogue.z is None else _matrix(epilogue.z, "z", T, O, device)
+    dz, lddz = (None, 0) if epilogue.dz is None else _matrix(epilogue.dz, "dz", T, O, device)
+    db, kind = (None, OSDP_BF16) if epilogue.dbias is None else _vector(epilogue.dbias, "dbias", O, device)
+    e = osdp_epilogue_grad(z, ldz, dz, lddz, db, epilogue.activation, kind)
+    shape = _shape(T, I, O, len(w_shards), k)
+    if len(dw_shards) != len(w_shards):
+        _refuse(f"{len(dw_shards)} dw_shards for {len(w_shards)} w_shards")
+    pref, _keep = _plan_ref(plan)
+    _check(lib.osdp_split_linear_bwd_epilogue(ctypes.byref(shape), pref, op_index, ctypes.byref(e), x, ldx, dy, lddy,
+                                              _shard_ptrs("w_shards", w_shards, I, O, device), _opt_ptrs(w_dp), int(ld_dp), dx, lddx,
+                                              _shard_ptrs("dw_shards", dw_shards, I, O, device), _opt_ptrs(dw_dp),
+                                              workspace.data_ptr(), _check_workspace(workspace, device), _stream(stream_compute),
+                                              _stream(stream_copy)))
 
 
 def osdp_debug_option(name: str, value: int) -> None:

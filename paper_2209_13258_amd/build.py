@@ -5,6 +5,8 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -12,11 +14,11 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libosdp.so"
 POINTERS = PKG / "_pointers.so"
-SOURCES = ["osdp_api.hip", "osdp_gather.hip", "osdp_gemm.hip", "osdp_search.hip", "osdp_adamw.hip", "osdp_int8.hip"]
-HEADERS = [CSRC / "osdp_internal.h", CSRC / "gemm_common.h", CSRC / "gemm_dma.h", CSRC / "gemm_i8.h", CSRC / "gemm_i8_w4.h", CSRC / "gemm_skinny.h", CSRC / "gemm_w4.h", CSRC / "gemm_w4p.h", ROOT / "include" / "osdp.h"]
+SOURCES = ["osdp_api.hip", "osdp_gather.hip", "osdp_gemm.hip", "osdp_epilogue.hip", "osdp_search.hip", "osdp_adamw.hip", "osdp_int8.hip"]
+HEADERS = [CSRC / "osdp_internal.h", CSRC / "activation.h", CSRC / "gemm_launch.h", CSRC / "gemm_common.h", CSRC / "gemm_dma.h", CSRC / "gemm_i8.h", CSRC / "gemm_i8_w4.h", CSRC / "gemm_skinny.h", CSRC / "gemm_w4.h", CSRC / "gemm_w4p.h", ROOT / "include" / "osdp.h"]
 
 HIPCC_FLAGS = [
-    "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950", "-fvisibility=hidden",
+    "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-fvisibility=hidden",
     "-Wall", "-Wno-unused-function",
     # keep the compiler from forming packed-fp32 VALU ops
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -54,8 +56,16 @@ def build(force: bool = True, verbose: bool = False) -> Path:
     if not force and not is_stale():
         return LIB
     tmp = LIB.with_suffix(f".so.tmp{os.getpid()}")
-    cmd = [hipcc(), *HIPCC_FLAGS, f"-I{ROOT / 'include'}", f"-I{CSRC}",
-           *[str(CSRC / s) for s in SOURCES], "-o", str(tmp)]
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        made = [str(Path(objects) / Path(s).with_suffix(".o")) for s in SOURCES]
+        list(pool.map(lambda s, o: _hipcc(["-c", str(CSRC / s), "-o", o], verbose), SOURCES, made))
+        _hipcc(["-shared", *made, "-o", str(tmp)], verbose)
+    os.replace(tmp, LIB)
+    return LIB
+
+
+def _hipcc(args, verbose: bool) -> None:
+    cmd = [hipcc(), *HIPCC_FLAGS, f"-I{ROOT / 'include'}", f"-I{CSRC}", *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -65,8 +75,6 @@ def build(force: bool = True, verbose: bool = False) -> Path:
         raise RuntimeError(f"hipcc failed:\n{err}")
     if verbose and err.strip():
         print(err)
-    os.replace(tmp, LIB)
-    return LIB
 
 
 if __name__ == "__main__":

@@ -3,6 +3,7 @@
 #pragma once
 #include <utility>
 
+#include "activation.h"
 #include "osdp_internal.h"
 
 namespace osdp {
@@ -72,6 +73,7 @@ struct GemmParams {
   int64_t c0;          // shard-major epilogue: column of the full matrix where C starts
   int64_t r0;          // shard-major epilogue: row of the full matrix where C starts
   ShardTable shards;
+  FusedEpilogue fused; // only read by launches with that epilogue
   GatherJob job;       // only read by kernels instantiated to carry one
 };
 
@@ -142,6 +144,49 @@ __device__ __forceinline__ void load_acc_tile(const GemmParams &p, f32x4 (&acc)[
     }
 }
 
+// W (4 or 8) consecutive columns' bias from column n on; zeros without one.
+template <int W>
+__device__ __forceinline__ void load_bias(const FusedEpilogue &e, int n, float (&b)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) b[i] = 0.0f;
+  if (!e.bias) return;
+  if (e.bias_f32) {
+    const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(e.bias) + n);
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const float4 v = src[i];
+      b[4 * i] = v.x; b[4 * i + 1] = v.y; b[4 * i + 2] = v.z; b[4 * i + 3] = v.w;
+    }
+  } else {
+    const uint2 *src = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(e.bias) + n);
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const uint2 v = src[i];
+      b[4 * i] = bf16_low(v.x); b[4 * i + 1] = bf16_high(v.x); b[4 * i + 2] = bf16_low(v.y); b[4 * i + 3] = bf16_high(v.y);
+    }
+  }
+}
+
+// One row's 4 columns through the fused epilogue.
+__device__ __forceinline__ uint2 fused4(const FusedEpilogue &e, f32x4 c, int64_t m, int n) {
+  float b[4];
+  load_bias<4>(e, n, b);
+  uint2 r = {0u, 0u};
+  if (e.residual) r = *reinterpret_cast<const uint2 *>(e.residual + m * e.ld_residual + n);
+  float z[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = c[i] + b[i];
+  if (e.z) store_global8(e.z + m * e.ldz + n, uint2{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])});
+  with_activation(e.activation, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = activate<decltype(act)::value>(z[i]);
+  });
+  if (e.residual) {
+    z[0] += bf16_low(r.x); z[1] += bf16_high(r.x); z[2] += bf16_low(r.y); z[3] += bf16_high(r.y);
+  }
+  return uint2{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+}
+
 // Stores 4 consecutive columns of row m starting at column n according to the epilogue.
 template <int kEpi>
 __device__ __forceinline__ void store_acc4(const GemmParams &p, f32x4 c, int m, int n, uint16_t *const *s_tab) {
@@ -152,7 +197,10 @@ __device__ __forceinline__ void store_acc4(const GemmParams &p, f32x4 c, int m, 
   }
   uint2 o = {pack_bf16x2(c[0], c[1]), pack_bf16x2(c[2], c[3])};
   uint16_t *dst;
-  if (kEpi == static_cast<int>(Epilogue::kBf16RowMajor)) {
+  if constexpr (kEpi == static_cast<int>(Epilogue::kBf16Fused)) {
+    o = fused4(p.fused, c, m, n);
+    dst = static_cast<uint16_t *>(p.C) + static_cast<int64_t>(m) * p.ldc + n;
+  } else if (kEpi == static_cast<int>(Epilogue::kBf16RowMajor)) {
     dst = static_cast<uint16_t *>(p.C) + static_cast<int64_t>(m) * p.ldc + n;
   } else {
     int s;
@@ -268,6 +316,94 @@ __device__ __forceinline__ void store_tile(const GemmParams &p, Read &&read, int
     if constexpr (kShards) off += static_cast<int64_t>(16) * p.lay.O;
     else dst += static_cast<int64_t>(16) * p.ldc;
   });
+}
+
+// One wave's share through the fused epilogue: the same rows and columns as store_tile's.  `scratch`: this wave's own
+// fused_scratch_bytes(NB) of LDS.
+//
+// Straight-line code as above would hold an activation for each of the 256 values of a lane, for each activation.  Here one
+// loop turns to the row blocks in turn: 16 rows of accumulators go through LDS, from where the lanes take 8 columns of a row
+// each, so that bias and column addresses are one register set for the whole tile, residual, Z and Y are whole 16-byte
+// pieces, rows of 32 NB contiguous bytes, and the code is short.  The residual of the next row block is under way meanwhile.
+// Written down the rows and read along them, the 16-byte pieces of a row are permuted by its number, or (rows that are no
+// power of two) the rows padded by one.
+constexpr int fused_row(int NB) { return 16 * NB + (NB % 4 == 0 ? 0 : 4); }
+constexpr size_t fused_scratch_bytes(int NB) { return static_cast<size_t>(16) * fused_row(NB) * sizeof(float); }
+
+template <int MB, int NB, class Read>
+__device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, int m_base, int n_base, int n_end, int l16, int q,
+                                            float *scratch) {
+  constexpr int kVecs = 2 * NB;               // pieces of 8 columns in a row
+  constexpr int kRows = 64 / kVecs;           // rows that the wave takes at once
+  constexpr int kPasses = (16 + kRows - 1) / kRows;
+  constexpr int kRowLd = fused_row(NB), kPerm = NB % 4 == 0 ? 15 : 0;
+  static_assert(kPerm == 0 || (4 * NB) % 16 == 0, "a row is whole groups of permuted pieces");
+  const FusedEpilogue &e = p.fused;
+  const int lane = 16 * q + l16, row0 = lane / kVecs, vec = lane - row0 * kVecs;
+  const int n = n_base + 8 * vec;
+  const bool columns = row0 < kRows && n < n_end;
+  float bias[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+  if (columns) load_bias<8>(e, n, bias);
+  auto inside = [&](int bm, int pass) {
+    const int r = pass * kRows + row0;
+    return columns && r < 16 && m_base + 16 * bm + r < p.M;
+  };
+  uint4 next[kPasses];
+  auto ask = [&](int bm) {
+    static_for<kPasses>([&](auto pass_) {
+      constexpr int pass = decltype(pass_)::value;
+      next[pass] = uint4{0u, 0u, 0u, 0u};
+      if (e.residual && bm < MB && inside(bm, pass))
+        next[pass] = load_global16(e.residual + static_cast<int64_t>(m_base + 16 * bm + pass * kRows + row0) * e.ld_residual + n);
+    });
+  };
+  ask(0);
+#pragma unroll 1
+  for (int bm = 0; bm < MB; ++bm) {
+    static_for<MB>([&](auto b_) {
+      constexpr int b = decltype(b_)::value;
+      if (bm == b) {
+        static_for<NB>([&](auto bn_) {
+          constexpr int bn = decltype(bn_)::value;
+          const f32x4 c = read(Int<b>{}, Int<bn>{});
+          *reinterpret_cast<f32x4 *>(scratch + l16 * kRowLd + 4 * ((4 * bn + q) ^ (l16 & kPerm))) = c;
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      }
+    });
+    uint4 residual[kPasses];
+    static_for<kPasses>([&](auto pass) { residual[decltype(pass)::value] = next[decltype(pass)::value]; });
+    ask(bm + 1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (one wave's LDS accesses keep their order: no barrier)
+    static_for<kPasses>([&](auto pass_) {
+      constexpr int pass = decltype(pass_)::value;
+      const int r = pass * kRows + row0;
+      if (inside(bm, pass)) {
+        const float *row = scratch + r * kRowLd;
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(row + 4 * ((2 * vec) ^ (r & kPerm)));
+        const f32x4 hi = *reinterpret_cast<const f32x4 *>(row + 4 * ((2 * vec + 1) ^ (r & kPerm)));
+        float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += bias[i];
+        const int64_t m = m_base + 16 * bm + r;
+        if (e.z)
+          store_global16(e.z + m * e.ldz + n, uint4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])});
+        with_activation(e.activation, [&](auto act) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] = activate<decltype(act)::value>(z[i]);
+        });
+        if (e.residual) {
+          const uint4 v = residual[pass];
+          z[0] += bf16_low(v.x); z[1] += bf16_high(v.x); z[2] += bf16_low(v.y); z[3] += bf16_high(v.y);
+          z[4] += bf16_low(v.z); z[5] += bf16_high(v.z); z[6] += bf16_low(v.w); z[7] += bf16_high(v.w);
+        }
+        store_global16(static_cast<uint16_t *>(p.C) + m * p.ldc + n, uint4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])});
+      }
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
 }
 
 }  // namespace

@@ -31,6 +31,7 @@ struct SkinnyParams {
   uint16_t *C;           // Y or dX
   int64_t ldc;
   WeightMap w;
+  FusedEpilogue fused;   // only read by kernels instantiated with it
   int32_t tiles_m;       // row tiles; more than one only where that spreads a small product over more CUs
   int32_t by_lane;       // some K block may lie in more than one array: lanes need the tables
 };
@@ -173,7 +174,7 @@ struct SkinnyOperand {
 };
 
 // block(): which workgroup of the product this is (asked for where it is used: in front of everything else it costs 0.3 us).
-template <int BM, int BN, int BK, int kStages, bool kBKc, class Block>
+template <int BM, int BN, int BK, int kStages, bool kBKc, bool kEpilogue, class Block>
 __device__ __forceinline__ void skinny_tile(const SkinnyParams &p, Block &&block) {
   constexpr int MB = BM / 16, NB = BN / 16, KS = BK / 32;
   using OpA = SkinnyOperand<true, BM, BK>;
@@ -342,14 +343,17 @@ __device__ __forceinline__ void skinny_tile(const SkinnyParams &p, Block &&block
 #pragma unroll
       for (int e = 0; e < 4; ++e) c[e] += d[e];
     }
-    store_global8(p.C + static_cast<int64_t>(m0 + m) * p.ldc + n0 + n, uint2{pack_bf16x2(c[0], c[1]), pack_bf16x2(c[2], c[3])});
+    uint2 o;
+    if constexpr (kEpilogue) o = fused4(p.fused, c, m0 + m, n0 + n);
+    else o = uint2{pack_bf16x2(c[0], c[1]), pack_bf16x2(c[2], c[3])};
+    store_global8(p.C + static_cast<int64_t>(m0 + m) * p.ldc + n0 + n, o);
   }
 }
 
-template <int BM, int BN, int BK, int kStages, bool kBKc>
+template <int BM, int BN, int BK, int kStages, bool kBKc, bool kEpilogue>
 __global__ __launch_bounds__(kSkinnyWaves * 64, 1)
 void gemm_skinny_kernel(SkinnyParams p) {
-  skinny_tile<BM, BN, BK, kStages, kBKc>(p, [] { return logical_block(); });
+  skinny_tile<BM, BN, BK, kStages, kBKc, kEpilogue>(p, [] { return logical_block(); });
 }
 
 // The backward of few tokens as one launch: workgroups [0, n_dx) are those of dX, the others 128 x 128 tiles of dW into the
@@ -359,7 +363,7 @@ template <int BM, int BK, int kStages>
 __global__ __launch_bounds__(kSkinnyWaves * 64, 1)
 void few_token_backward_kernel(SkinnyParams dx, GemmParams dw, int n_dx, int tiles_m, int tiles_n) {
   const int id = blockIdx.x;
-  if (id < n_dx) skinny_tile<BM, 64, BK, kStages, true>(dx, [&] { return id; });
+  if (id < n_dx) skinny_tile<BM, 64, BK, kStages, true, false>(dx, [&] { return id; });
   else gemm_w4_tile<4, 4, 4, false, false, static_cast<int>(Epilogue::kBf16ShardMajor), false, false>(dw, tiles_m, tiles_n, id - n_dx);
 }
 

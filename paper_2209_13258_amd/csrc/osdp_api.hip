@@ -650,7 +650,8 @@ hipError_t gather_now(const GatherRequest &g, hipStream_t stream) {
 hipError_t do_gemm(int kind, const GemmProblem &g, hipStream_t stream) {
   const double M = g.M, N = g.N, K = g.K;
   const double out_bytes = g.epilogue == Epilogue::kF32Workspace ? 4.0 : 2.0;
-  const double bytes = 2.0 * M * K + 2.0 * K * N + out_bytes * M * N + (g.acc_in ? 4.0 * M * N : 0.0);
+  const double beside = g.epilogue == Epilogue::kBf16Fused ? (g.fused.residual ? 2.0 : 0.0) + (g.fused.z ? 2.0 : 0.0) : 0.0;
+  const double bytes = 2.0 * M * K + 2.0 * K * N + (out_bytes + beside) * M * N + (g.acc_in ? 4.0 * M * N : 0.0);
   bool carried = false;
   GemmProblem q = g;
   q.carried = &carried;
@@ -711,6 +712,13 @@ GemmProblem weight_gemm(const Resolved &r, bool is_fwd, int j0, int j1, WeightVi
     }
   }
   return g;
+}
+
+// A forward launch that stores the result goes through the epilogue; col: the first of its columns in Y.
+void fuse(GemmProblem *g, const FusedEpilogue *ep, int64_t col) {
+  if (!ep || g->epilogue != Epilogue::kBf16RowMajor) return;
+  g->epilogue = Epilogue::kBf16Fused;
+  g->fused = fused_from(*ep, 0, col);
 }
 
 // dW over the sub-slices [j0, j1), written into the shard-major gradient: column slices give
@@ -997,7 +1005,8 @@ osdp_status osdp_split_linear_gather_row_slice(const osdp_shape *shape, int32_t 
 
 static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index, bool allow_dp, const void *X,
                            int64_t ldx, const void *const *w_shards, const Replicas &rep, void *Y, int64_t ldy,
-                           void *workspace, size_t workspace_bytes, void *stream_compute, void *stream_copy) {
+                           void *workspace, size_t workspace_bytes, void *stream_compute, void *stream_copy,
+                           const FusedEpilogue *ep = nullptr) {
   hipStream_t sc = static_cast<hipStream_t>(stream_compute), sp = static_cast<hipStream_t>(stream_copy);
   const bool two_streams = sp != nullptr && sp != sc;
   Resolved r;
@@ -1015,17 +1024,26 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
   if (skinny_takes(false, r.T, ldx, r.layout, r.I)) {  // few tokens: one launch that reads the weights where they lie
     const double T = r.T, I = r.I, O = r.O;
     OSDP_HIP(timed(OSDP_KERNEL_GEMM_FWD, 2.0 * T * I * O, 2.0 * (T * I + I * O + T * O), sc,
-                   [&] { return launch_skinny(false, weight_map(r, tab, rep), r.T, X, ldx, Y, ldy, sc); }));
+                   [&] {
+                     return ep ? launch_skinny_fused(weight_map(r, tab, rep), r.T, X, ldx, Y, ldy, *ep, sc)
+                               : launch_skinny(false, weight_map(r, tab, rep), r.T, X, ldx, Y, ldy, sc);
+                   }));
     return OSDP_OK;
   }
   const bool in_place = one_chain(r, true) && gemm_reads_shards(r.T, ldx, r.layout) && switches_pay(r);
   if (in_place && !r.any_dp) {
-    OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, shard_gemm(r, true, tab, X, ldx, Y, ldy), sc));
+    GemmProblem g = shard_gemm(r, true, tab, X, ldx, Y, ldy);
+    fuse(&g, ep, 0);
+    OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
     return OSDP_OK;
   }
   if (in_place && r.any_dp && r.T <= kSkinnyMaxTokens) {
     const std::vector<Slice> runs = runs_in_place(r, true);
-    for (const Slice &l : runs) OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, run_gemm(r, true, l, tab, rep, X, ldx, Y, ldy), sc));
+    for (const Slice &l : runs) {
+      GemmProblem g = run_gemm(r, true, l, tab, rep, X, ldx, Y, ldy);
+      fuse(&g, ep, r.sub[l.c0].c0);
+      OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
+    }
     if (!runs.empty()) return OSDP_OK;
   }
   Resolved other;
@@ -1054,6 +1072,7 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
       if (j == 0 && !r.dp[0]) OSDP_HIP(do_gather(r, tab, r.sub[0], slot, sc));
       GemmProblem g = weight_gemm(r, /*is_fwd=*/true, j, j + 1, weights_of(r, rep, j, slot), WeightView{nullptr, 0}, X, ldx,
                                   Y, ldy, acc, static_cast<size_t>(j), static_cast<size_t>(n));
+      fuse(&g, ep, r.rows ? 0 : r.sub[j].c0);
       GatherRequest next;
       if (j + 1 < n && !r.dp[j + 1]) {
         next = gather_request(r, tab, r.sub[j + 1], ws + static_cast<size_t>((j + 1) % 2) * r.slot_bytes);
@@ -1091,6 +1110,7 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
                             li, r.fwd.size())
               : weight_gemm(r, /*is_fwd=*/true, j0, j1, weights_of(r, rep, j0, slot_of[0]),
                             weights_of(r, rep, j1 - 1, slot_of[1]), X, ldx, Y, ldy, acc, li, r.fwd.size());
+    fuse(&g, ep, r.rows ? 0 : r.sub[j0].c0);
     g.parts = planes; g.parts_bytes = planes_bytes;
     OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
     if (poison && gathered) {  // the slices this launch read are dead: poison their slots before they are handed back
@@ -1170,10 +1190,83 @@ osdp_status osdp_split_linear_fwd_mixed(const osdp_shape *shape, const osdp_plan
                  workspace_bytes, stream_compute, stream_copy);
 }
 
+// ---- bias, activation and residual ---------------------------------------------------------------------------------
+namespace {
+// Whether two matrices of T rows share memory: by their extents, or, with one leading dimension, by their columns (parts of one
+// wide matrix lie side by side).
+bool share_memory(const void *a, int64_t lda, int64_t cols_a, const void *b, int64_t ldb, int64_t cols_b, int64_t T) {
+  if (!a || !b || T <= 0) return false;
+  typedef __int128 wide;
+  const wide a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  const wide a1 = a0 + 2 * (static_cast<wide>(T - 1) * lda + cols_a), b1 = b0 + 2 * (static_cast<wide>(T - 1) * ldb + cols_b);
+  if (a1 <= b0 || b1 <= a0) return false;
+  if (T == 1 || lda != ldb) return true;
+  wide d = (b0 - a0) % (2 * static_cast<wide>(lda));
+  if (d < 0) d += 2 * static_cast<wide>(lda);
+  return d < 2 * static_cast<wide>(cols_a) || d + 2 * static_cast<wide>(cols_b) > 2 * static_cast<wide>(lda);
+}
+
+osdp_status check_vector(const void *p, int32_t activation, int32_t type, const char *name) {
+  if (activation < OSDP_ACT_NONE || activation > OSDP_ACT_SILU) return fail(OSDP_ERR_INVALID_ARG, "unknown activation %d", activation);
+  if (!p) return OSDP_OK;
+  if (type != OSDP_BF16 && type != OSDP_F32) return fail(OSDP_ERR_INVALID_ARG, "unknown bias_type %d", type);
+  if (!aligned16(p)) return fail(OSDP_ERR_UNSUPPORTED, "%s is not 16-byte aligned", name);
+  return OSDP_OK;
+}
+
+// A vector of O elements as a matrix of one row of 16-bit halves.
+int64_t halves(int64_t O, int32_t type) { return type == OSDP_F32 ? 2 * O : O; }
+bool vector_shares(const void *v, int64_t O, int32_t type, const void *m, int64_t ld, int64_t cols, int64_t T) {
+  if (!v || !m || T <= 0) return false;
+  const __int128 v0 = reinterpret_cast<uintptr_t>(v), m0 = reinterpret_cast<uintptr_t>(m);
+  const __int128 v1 = v0 + 2 * static_cast<__int128>(halves(O, type)), m1 = m0 + 2 * (static_cast<__int128>(T - 1) * ld + cols);
+  return v0 < m1 && m0 < v1;
+}
+}  // namespace
+
+osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
+                                                       int32_t is_bwd, size_t *total, size_t *peak_weight_staging) {
+  size_t base = 0;
+  const osdp_status st = osdp_split_linear_workspace_bytes(shape, plan, op_index, is_bwd, &base, peak_weight_staging);
+  if (st != OSDP_OK) return st;
+  if (total) *total = is_bwd ? round_up(base, kSlotAlign) + slope_workspace_bytes(shape->T, shape->O) : base;
+  return OSDP_OK;
+}
+
+osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
+                                           const osdp_epilogue *epilogue, const void *X, int64_t ldx,
+                                           const void *const *w_shards, const void *const *w_dp, int64_t ld_dp, void *Y,
+                                           int64_t ldy, void *workspace, size_t workspace_bytes, void *stream_compute,
+                                           void *stream_copy) {
+  osdp_status st = check_shape(shape);
+  if (st != OSDP_OK) return st;
+  if (!epilogue) return fail(OSDP_ERR_INVALID_ARG, "epilogue is NULL");
+  const osdp_epilogue &e = *epilogue;
+  const int64_t T = shape->T, I = shape->I, O = shape->O;
+  if ((st = check_vector(e.bias, e.activation, e.bias_type, "bias")) != OSDP_OK) return st;
+  if (T > 0) {
+    if (e.residual && (st = check_matrix(e.residual, e.ld_residual, O, "residual")) != OSDP_OK) return st;
+    if (e.z && (st = check_matrix(e.z, e.ldz, O, "z")) != OSDP_OK) return st;
+    const bool in_place = e.residual == Y && e.ld_residual == ldy;
+    if ((!in_place && share_memory(e.residual, e.ld_residual, O, Y, ldy, O, T)) || share_memory(X, ldx, I, Y, ldy, O, T) ||
+        vector_shares(e.bias, O, e.bias_type, Y, ldy, O, T))
+      return fail(OSDP_ERR_INVALID_ARG, "Y overlaps an input");
+    if (share_memory(e.z, e.ldz, O, Y, ldy, O, T) || share_memory(e.z, e.ldz, O, e.residual, e.ld_residual, O, T) ||
+        share_memory(X, ldx, I, e.z, e.ldz, O, T) || vector_shares(e.bias, O, e.bias_type, e.z, e.ldz, O, T))
+      return fail(OSDP_ERR_INVALID_ARG, "z overlaps Y or an input");
+  }
+  const FusedEpilogue f = {e.bias, static_cast<const uint16_t *>(e.residual), e.ld_residual, static_cast<uint16_t *>(e.z), e.ldz,
+                           e.activation, e.bias_type == OSDP_F32};
+  const bool plain = !e.bias && !e.residual && !e.z && e.activation == OSDP_ACT_NONE;
+  return forward(shape, plan, op_index, true, X, ldx, w_shards, Replicas{w_dp, nullptr, ld_dp}, Y, ldy, workspace,
+                 workspace_bytes, stream_compute, stream_copy, plain ? nullptr : &f);
+}
+
 static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index, bool allow_dp, const void *X,
                             int64_t ldx, const void *dY, int64_t lddy, const void *const *w_shards, const Replicas &rep,
                             void *dX, int64_t lddx, void *const *dw_shards, void *workspace, size_t workspace_bytes,
-                            void *stream_compute, void *stream_copy) {
+                            void *stream_compute, void *stream_copy, const SlopeProblem *slope = nullptr,
+                            void *slope_workspace = nullptr) {
   hipStream_t sc = static_cast<hipStream_t>(stream_compute), sp = static_cast<hipStream_t>(stream_copy);
   const bool two_streams = sp != nullptr && sp != sc;
   Resolved r;
@@ -1190,6 +1283,13 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
   if ((st = check_workspace(r, workspace, workspace_bytes)) != OSDP_OK) return st;
   if ((st = device_ok()) != OSDP_OK) return st;
 
+  if (slope) {  // the products' dY is the gradient in front of the activation
+    OSDP_HIP(launch_slope(*slope, slope_workspace, sc));
+    if (slope->dZ) {
+      dY = slope->dZ;
+      lddy = slope->lddz;
+    }
+  }
   if (no_tokens) {
     // dW = X^T . dY summed over no tokens is zero: the dW launches run with an empty reduction and store the
     // zeros where the gradient belongs; dX is empty, so no weight is gathered.
@@ -1324,6 +1424,52 @@ osdp_status osdp_split_linear_bwd_mixed(const osdp_shape *shape, const osdp_plan
                                         size_t workspace_bytes, void *stream_compute, void *stream_copy) {
   return backward(shape, plan, op_index, true, X, ldx, dY, lddy, w_shards, Replicas{w_dp, dw_dp, ld_dp}, dX, lddx,
                   dw_shards, workspace, workspace_bytes, stream_compute, stream_copy);
+}
+
+osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
+                                           const osdp_epilogue_grad *epilogue, const void *X, int64_t ldx, const void *dY,
+                                           int64_t lddy, const void *const *w_shards, const void *const *w_dp, int64_t ld_dp,
+                                           void *dX, int64_t lddx, void *const *dw_shards, void *const *dw_dp,
+                                           void *workspace, size_t workspace_bytes, void *stream_compute, void *stream_copy) {
+  osdp_status st = check_shape(shape);
+  if (st != OSDP_OK) return st;
+  if (!epilogue) return fail(OSDP_ERR_INVALID_ARG, "epilogue is NULL");
+  const osdp_epilogue_grad &e = *epilogue;
+  const int64_t T = shape->T, I = shape->I, O = shape->O;
+  if ((st = check_vector(e.dbias, e.activation, e.bias_type, "dbias")) != OSDP_OK) return st;
+  const bool active = e.activation != OSDP_ACT_NONE;
+  if (!active && e.dz) return fail(OSDP_ERR_INVALID_ARG, "dz is given without an activation: dZ is dY then");
+  if (T > 0 && active) {
+    if ((st = check_matrix(e.z, e.ldz, O, "z")) != OSDP_OK) return st;
+    if ((st = check_matrix(e.dz, e.lddz, O, "dz")) != OSDP_OK) return st;
+    const bool at_dy = e.dz == dY && e.lddz == lddy, at_z = e.dz == e.z && e.lddz == e.ldz;
+    if ((!at_dy && share_memory(dY, lddy, O, e.dz, e.lddz, O, T)) || (!at_z && share_memory(e.z, e.ldz, O, e.dz, e.lddz, O, T)) ||
+        share_memory(X, ldx, I, e.dz, e.lddz, O, T))
+      return fail(OSDP_ERR_INVALID_ARG, "dz overlaps an input");
+  }
+  if (T > 0 && (vector_shares(e.dbias, O, e.bias_type, dY, lddy, O, T) || vector_shares(e.dbias, O, e.bias_type, X, ldx, I, T) ||
+                (active && (vector_shares(e.dbias, O, e.bias_type, e.z, e.ldz, O, T) || vector_shares(e.dbias, O, e.bias_type, e.dz, e.lddz, O, T))) ||
+                vector_shares(e.dbias, O, e.bias_type, dX, lddx, I, T)))
+    return fail(OSDP_ERR_INVALID_ARG, "dbias overlaps an input or another output");
+  size_t base = 0, total = 0;
+  if ((st = osdp_split_linear_workspace_bytes(shape, plan, op_index, 1, &base, nullptr)) != OSDP_OK) return st;
+  total = round_up(base, kSlotAlign) + slope_workspace_bytes(T, O);
+  if (e.dbias && workspace && workspace_bytes < total)
+    return fail(OSDP_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace_bytes, total);
+  SlopeProblem q{};
+  q.T = T; q.O = O;
+  q.activation = T > 0 ? e.activation : static_cast<int32_t>(OSDP_ACT_NONE);  // (no rows: only db = 0 is left to store)
+  q.db_f32 = e.bias_type == OSDP_F32;
+  q.dY = dY; q.lddy = lddy;
+  if (T > 0 && active) {
+    q.Z = e.z; q.ldz = e.ldz;
+    q.dZ = e.dz; q.lddz = e.lddz;
+  }
+  q.db = e.dbias;
+  const bool plain = !active && !e.dbias;
+  return backward(shape, plan, op_index, true, X, ldx, dY, lddy, w_shards, Replicas{w_dp, dw_dp, ld_dp}, dX, lddx, dw_shards,
+                  workspace, workspace_bytes, stream_compute, stream_copy, plain ? nullptr : &q,
+                  static_cast<char *>(workspace) + round_up(base, kSlotAlign));
 }
 
 osdp_status osdp_granularity_candidates(const osdp_shape *shape, const int32_t *k_list, int32_t n_k,

@@ -1,0 +1,205 @@
+// What stands around the products of the split operator:
+//   forward   Z = X . W + b,  Y = act(Z) + R      in the product's epilogue (store_fused in gemm_common.h)
+//   backward  dZ = dY * act'(Z),  db = sum over tokens of dZ      in one pass in front of the product's backward
+// The products are those of osdp_gemm.hip, in the same order of additions: without bias, activation and residual Y has the same bits.
+#include "gemm_launch.h"
+
+namespace osdp {
+
+hipError_t launch_gemm_fused(const GemmProblem &q, hipStream_t stream, bool *carry) {
+  GemmParams p;
+  const hipError_t e = launch_params(q, *carry, &p);
+  if (e != hipSuccess) return e;
+  constexpr int kFused = static_cast<int>(Epilogue::kBf16Fused);
+  return q.acc_in ? launch_planned<true, false, kFused, true>(p, stream, carry, nullptr, 0)
+                  : launch_planned<true, false, kFused, false>(p, stream, carry, nullptr, 0);
+}
+
+hipError_t launch_combine_fused(const GemmProblem &q, int parts, const float *planes, hipStream_t stream) {
+  return launch_combine<static_cast<int>(Epilogue::kBf16Fused)>(gemm_params(q), parts, planes, stream);
+}
+
+hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int64_t ldx, void *Y, int64_t ldy,
+                               const FusedEpilogue &fused, hipStream_t stream) {
+  SkinnyParams p = skinny_params(false, w, T, X, ldx, Y, ldy);
+  p.fused = fused;
+  return launch_skinny_forward<true>(p, stream);
+}
+
+namespace {
+
+// ---- dZ and db ------------------------------------------------------------------------------------------------
+// A workgroup takes `lanes` x 8 columns (as many lanes side by side as the columns need, 64 at most) and a range of rows, 256 /
+// lanes of them at a time; every lane keeps the sums of its 8 columns.  The sums of its row groups are added up through LDS in
+// ascending order, and, where more than one workgroup shares a column, written to a plane of the workspace; sum_planes_kernel
+// adds the planes in ascending order.  No atomics: the same inputs give the same bits.
+struct SlopeParams {
+  int64_t T;
+  int32_t O, activation, lanes_log2, rows_per_group;
+  const uint16_t *dY;
+  int64_t lddy;
+  const uint16_t *Z;
+  int64_t ldz;
+  uint16_t *dZ;
+  int64_t lddz;
+  float *planes;   // nullptr: db is stored
+  void *db;
+  int32_t db_f32;
+};
+
+__device__ __forceinline__ void store_sums(void *db, int db_f32, int n, const float (&s)[8]) {
+  if (db_f32) {
+    float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(db) + n);
+    dst[0] = float4{s[0], s[1], s[2], s[3]};
+    dst[1] = float4{s[4], s[5], s[6], s[7]};
+  } else {
+    store_global16(static_cast<uint16_t *>(db) + n, uint4{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]), pack_bf16x2(s[4], s[5]), pack_bf16x2(s[6], s[7])});
+  }
+}
+
+template <int kAct, bool kSums>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeParams p) {
+  constexpr bool kSlope = kAct != OSDP_ACT_NONE;
+  constexpr int kAtOnce = 4;  // rows of a lane under way together
+  __shared__ float s_sum[kSums ? 256 * 8 : 1];
+  const int lanes = 1 << p.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log2;
+  const int groups = 256 >> p.lanes_log2;
+  const int n = (static_cast<int>(blockIdx.x) * lanes + lane) * 8;
+  const bool columns = n < p.O;
+  const int64_t first = static_cast<int64_t>(blockIdx.y) * p.rows_per_group;
+  const int64_t end = first + p.rows_per_group < p.T ? first + p.rows_per_group : p.T;
+  float sum[8] = {};
+  if (columns) {
+    for (int64_t m0 = first + group; m0 < end; m0 += kAtOnce * groups) {
+      uint4 dy[kAtOnce], z[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t m = m0 + i * groups;
+        if (m < end) {
+          dy[i] = load_global16(p.dY + m * p.lddy + n);
+          if constexpr (kSlope) z[i] = load_global16(p.Z + m * p.ldz + n);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t m = m0 + i * groups;
+        if (m >= end) continue;
+        const uint32_t d[4] = {dy[i].x, dy[i].y, dy[i].z, dy[i].w};
+        float g[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          g[2 * e] = bf16_low(d[e]);
+          g[2 * e + 1] = bf16_high(d[e]);
+        }
+        if constexpr (kSlope) {
+          const uint32_t zw[4] = {z[i].x, z[i].y, z[i].z, z[i].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            g[2 * e] *= activation_slope<kAct>(bf16_low(zw[e]));
+            g[2 * e + 1] *= activation_slope<kAct>(bf16_high(zw[e]));
+          }
+          store_global16(p.dZ + m * p.lddz + n, uint4{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7])});
+        }
+        if constexpr (kSums)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[e] += g[e];
+      }
+    }
+  }
+  if constexpr (kSums) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s_sum[e * 256 + threadIdx.x] = sum[e];
+    __syncthreads();
+    if (group != 0 || !columns) return;
+    for (int g = 1; g < groups; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += s_sum[e * 256 + (g << p.lanes_log2) + lane];
+    if (!p.planes) {
+      store_sums(p.db, p.db_f32, n, sum);
+    } else {
+      float4 *dst = reinterpret_cast<float4 *>(p.planes + static_cast<int64_t>(blockIdx.y) * p.O + n);
+      dst[0] = float4{sum[0], sum[1], sum[2], sum[3]};
+      dst[1] = float4{sum[4], sum[5], sum[6], sum[7]};
+    }
+  }
+}
+
+// db[n] = the sum over the planes: four waves take a quarter of them each, 64 columns to a workgroup.
+__global__ __launch_bounds__(256) void sum_planes_kernel(const float *planes, int count, int O, void *db, int db_f32) {
+  __shared__ float s_sum[256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+  const int per = (count + 3) / 4, first = wave * per, end = first + per < count ? first + per : count;
+  float sum = 0.0f;
+  if (n < O) {
+    const float *src = planes + static_cast<int64_t>(first) * O + n;
+#pragma unroll 8
+    for (int s = first; s < end; ++s, src += O) sum += *src;
+  }
+  s_sum[threadIdx.x] = sum;
+  __syncthreads();
+  if (wave != 0 || n >= O) return;
+  for (int w = 1; w < 4; ++w) sum += s_sum[w * 64 + lane];
+  if (db_f32) static_cast<float *>(db)[n] = sum;
+  else static_cast<__bf16 *>(db)[n] = static_cast<__bf16>(sum);
+}
+
+// How rows and columns are dealt out.
+struct SlopeGrid {
+  int lanes_log2;
+  int blocks;     // of columns
+  int parts;      // of rows
+  int rows;       // in a part
+};
+SlopeGrid slope_grid(int64_t T, int64_t O) {
+  SlopeGrid g{};
+  while (g.lanes_log2 < 6 && (int64_t{8} << g.lanes_log2) < O) ++g.lanes_log2;
+  const int64_t columns = int64_t{8} << g.lanes_log2;
+  const int64_t blocks = (O + columns - 1) / columns, least = 16 * (256 >> g.lanes_log2);  // (16 rows to a lane at least)
+  const int64_t wanted = std::max<int64_t>(1, 2048 / blocks), possible = std::max<int64_t>(1, (T + least - 1) / least);
+  const int64_t parts = std::min<int64_t>({wanted, possible, 1024});
+  g.blocks = static_cast<int>(blocks);
+  g.rows = static_cast<int>(std::max<int64_t>(1, (T + parts - 1) / parts));
+  g.parts = static_cast<int>(std::max<int64_t>(1, (T + g.rows - 1) / g.rows));
+  return g;
+}
+
+template <int kAct>
+void launch_slope_as(const SlopeParams &p, const SlopeGrid &g, hipStream_t stream) {
+  const dim3 grid(g.blocks, g.parts);
+  if (p.db) hipLaunchKernelGGL((slope_kernel<kAct, true>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((slope_kernel<kAct, false>), grid, dim3(256), 0, stream, p);
+}
+
+}  // namespace
+
+size_t slope_workspace_bytes(int64_t T, int64_t O) {
+  const SlopeGrid g = slope_grid(T, O);
+  return g.parts > 1 ? static_cast<size_t>(g.parts) * static_cast<size_t>(O) * sizeof(float) : 0;
+}
+
+hipError_t launch_slope(const SlopeProblem &q, void *workspace, hipStream_t stream) {
+  const SlopeGrid g = slope_grid(q.T, q.O);
+  SlopeParams p{};
+  p.T = q.T; p.O = static_cast<int32_t>(q.O);
+  p.activation = q.activation; p.lanes_log2 = g.lanes_log2; p.rows_per_group = g.rows;
+  p.dY = static_cast<const uint16_t *>(q.dY); p.lddy = q.lddy;
+  p.Z = static_cast<const uint16_t *>(q.Z); p.ldz = q.ldz;
+  p.dZ = static_cast<uint16_t *>(q.dZ); p.lddz = q.lddz;
+  p.db = q.db; p.db_f32 = q.db_f32;
+  p.planes = q.db && g.parts > 1 ? static_cast<float *>(workspace) : nullptr;
+  switch (q.activation) {
+    case OSDP_ACT_RELU: launch_slope_as<OSDP_ACT_RELU>(p, g, stream); break;
+    case OSDP_ACT_GELU: launch_slope_as<OSDP_ACT_GELU>(p, g, stream); break;
+    case OSDP_ACT_GELU_TANH: launch_slope_as<OSDP_ACT_GELU_TANH>(p, g, stream); break;
+    case OSDP_ACT_SILU: launch_slope_as<OSDP_ACT_SILU>(p, g, stream); break;
+    default:
+      if (!q.db) return hipSuccess;  // dZ is dY, and nobody asks for its sums
+      hipLaunchKernelGGL((slope_kernel<OSDP_ACT_NONE, true>), dim3(g.blocks, g.parts), dim3(256), 0, stream, p);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.planes) return e;
+  hipLaunchKernelGGL(sum_planes_kernel, dim3((p.O + 63) / 64), dim3(256), 0, stream, p.planes, g.parts, p.O, p.db, p.db_f32);
+  return hipGetLastError();
+}
+
+}  // namespace osdp

@@ -62,8 +62,29 @@ struct WeightMap {
 enum class Epilogue : int32_t {
   kBf16RowMajor = 0,   // C -> bf16, row-major with ldc
   kBf16ShardMajor = 1, // C -> bf16, scattered into the shard-major layout at column offset c0
-  kF32Workspace = 2    // C -> fp32, row-major with ldc (the dX accumulator between slices)
+  kF32Workspace = 2,   // C -> fp32, row-major with ldc (the dX accumulator between slices)
+  kBf16Fused = 3       // forward: C -> act(C + bias) + residual -> bf16, row-major with ldc (FusedEpilogue)
 };
+
+// What a forward launch does with its result in fp32 before it is rounded, z = C + bias: Z = z, C = act(z) + residual.  All
+// pointers are those of the launch's first row and column; matrices are 16-byte aligned, their leading dimensions multiples of 8.
+struct FusedEpilogue {
+  const void *bias;          // of C's columns: fp32 where bias_f32 is set, else bf16; 16-byte aligned, or nullptr
+  const uint16_t *residual;  // bf16, or nullptr
+  int64_t ld_residual;
+  uint16_t *z;               // bf16, or nullptr
+  int64_t ldz;
+  int32_t activation;        // an osdp_activation
+  int32_t bias_f32;
+};
+// The same from another row and column on.
+inline FusedEpilogue fused_from(const FusedEpilogue &e, int64_t row, int64_t col) {
+  FusedEpilogue f = e;
+  if (f.bias) f.bias = static_cast<const char *>(f.bias) + col * (f.bias_f32 ? 4 : 2);
+  if (f.residual) f.residual += row * f.ld_residual + col;
+  if (f.z) f.z += row * f.ldz + col;
+  return f;
+}
 
 // A slice gather: Ws[r, c] = W[r0 + r, c0 + c] for r < rows, c < w, into the dense row-major staging [rows x w].
 struct GatherRequest {
@@ -97,6 +118,7 @@ struct GemmProblem {
   const float *acc_in;  // fp32 [M x N] with ld_acc added to the product first, or nullptr
   int64_t ld_acc;
   Epilogue epilogue;
+  FusedEpilogue fused;  // kBf16Fused only
   ShardLayout layout;   // kBf16ShardMajor only
   ShardTable shards;    // kBf16ShardMajor: of the result; b_shard_rows: of the weight
   int64_t c0;           // kBf16ShardMajor only: column offset of C inside the full matrix
@@ -127,12 +149,31 @@ constexpr int64_t kSkinnyMaxTokens = 128, kSkinnyMaxWideTokens = 64, kSkinnyMaxC
 bool skinny_takes(bool dx, int64_t T, int64_t ld_act, const ShardLayout &lay, int64_t I);
 hipError_t launch_skinny(bool dx, const WeightMap &w, int64_t T, const void *act, int64_t ld_act, void *out, int64_t ld_out,
                          hipStream_t stream);
+// The forward product with an epilogue.
+hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int64_t ldx, void *Y, int64_t ldy,
+                               const FusedEpilogue &fused, hipStream_t stream);
 
 // dX of few tokens (skinny_takes) and dW of the whole matrix into the shards as one launch; takes: whether dW is the small
 // product that this is meant for (at most one 128 x 128 tile per CU) and the two fit beside each other.
 bool few_token_backward_takes(const GemmProblem &dw, int64_t T);
 hipError_t launch_few_token_backward(const GemmProblem &dw, const WeightMap &w, int64_t T, const void *dY, int64_t lddy, void *dX,
                                      int64_t lddx, hipStream_t stream);
+
+// dZ = dY act'(Z) and db = the sum over the rows of dZ, one pass over [T x O].  dZ may lie where dY or Z does.  Without an
+// activation Z and dZ are not looked at and the sums are dY's; db nullptr: no sums.  T = 0 stores db = 0.
+struct SlopeProblem {
+  int64_t T, O;
+  int32_t activation, db_f32;
+  const void *dY;
+  int64_t lddy;
+  const void *Z;
+  int64_t ldz;
+  void *dZ;
+  int64_t lddz;
+  void *db;
+};
+size_t slope_workspace_bytes(int64_t T, int64_t O);
+hipError_t launch_slope(const SlopeProblem &q, void *workspace, hipStream_t stream);
 
 // Whether a product of T tokens with the whole weight may read it from the shards (GemmProblem::b_shard_rows).
 // Up to four rows of 128-row tiles: the workgroups an XCD runs together walk the rows of a panel of weight columns
@@ -167,6 +208,12 @@ double gemm_planned_us(int64_t M, int64_t N, int64_t K, bool dx, bool acc_in);
 
 // Launches of the calling thread that ran as the persistent four-wave kernel so far (for the profile).
 int64_t gemm_persistent_launches();
+void gemm_count_persistent_launch();
+
+// Parts of launch_gemm: a forward launch whose epilogue is kBf16Fused (osdp_epilogue.hip), and the sum of the planes of one
+// that ran in parts of the reduction through that epilogue.
+hipError_t launch_gemm_fused(const GemmProblem &q, hipStream_t stream, bool *carry);
+hipError_t launch_combine_fused(const GemmProblem &q, int parts, const float *planes, hipStream_t stream);
 
 // Bytes of fp32 planes that launch_gemm needs in GemmProblem::parts for a forward product (A K-contiguous, B
 // N-contiguous, bf16 row-major result, no accumulator) of M x N x K; 0: that product is not split along K.  The
