@@ -59,8 +59,8 @@
  *     calls run on stream_compute alone, and work of the caller's on stream_copy
  *     that reuses the workspace has to wait for it.  Inputs must be ready on
  *     stream_compute when the call is made.
- *   - The forward, backward and gather calls, and those of AdamW and of the operator in 8-bit
- *     integers, can be captured into a HIP graph on
+ *   - The forward, backward and gather calls, and those of AdamW, of the operator in 8-bit
+ *     integers and of the norms of queries and keys, can be captured into a HIP graph on
  *     stream_compute (after one eager call, which sets kernel attributes): they enqueue
  *     kernels and event records / waits only, and every use of stream_copy starts
  *     from and returns to stream_compute.  Not capturable: the profiling calls
@@ -364,6 +364,59 @@ OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, con
                                                     const void *const *w_dp, int64_t ld_dp, void *dX, int64_t lddx,
                                                     void *const *dw_shards, void *const *dw_dp, void *workspace,
                                                     size_t workspace_bytes, void *stream_compute, void *stream_copy);
+
+/* ---- norms of queries and keys, and their rotation by position ------------------
+ * What a transformer layer does with the queries and keys in the qkv operator's output, in one pass over them: every head x of D
+ * elements is divided by its root mean square and multiplied by a learned weight g (norm = 1; 0: not so), then its first `rotary`
+ * elements are turned in pairs (a, b), by the angle  position * freqs[i]  for pair i:
+ *     n_j = x_j * g_j / sqrt( mean_j x_j^2 + eps )        (a, b) -> (a cos - b sin, b cos + a sin)
+ * Pair i is (i, i + rotary / 2), or (2 i, 2 i + 1) with interleaved = 1.  The backward pass, from the gradients of the turned heads
+ * (dn: turned back), r = 1 / sqrt(..), xh = x r, t = dn * g:
+ *     dx = r * (t - xh * mean_j(t_j xh_j))         dg_j = sum over tokens and heads of dn_j xh_j
+ * Everything is computed in fp32 and rounded once, angles in 64 bits until less than a turn is left of them (then cos and sin to 2^-20).
+ * Squares that leave the range of fp32 are taken of x / 2^70 instead.  dg is summed in an order that the sizes alone decide.
+ *
+ * A negative position marks a row of padding: it is neither read nor written and adds nothing to dg.
+ *
+ * Heads lie anywhere: element d of head h of token t at p + t * ld + h * head_stride + d.  Outputs may be the inputs of the same
+ * name (the same pointer and strides; backward: dq may be q or dq_out, dk alike), otherwise they overlap no input, nor each
+ * other, nor themselves.  The parts of one wide row (queries, keys, values side by side) do not overlap.
+ * Shapes (else OSDP_ERR_UNSUPPORTED): D a multiple of 8 and at most 512; rotary a multiple of 16 (interleaved: 8), at most D;
+ * strides multiples of 8, pointers 16-byte aligned; T < 2^31; heads at most 65535, either may be 0 (then its pointers are ignored). */
+
+typedef struct {
+  void *p;             /* device, bf16                                                               */
+  int64_t ld;          /* elements from a token to the next                                          */
+  int64_t head_stride; /* elements from a head to the next                                           */
+} osdp_heads;
+
+typedef struct {
+  int64_t T;           /* tokens; 0 is allowed (the backward call stores dg = 0)                     */
+  int32_t q_heads, k_heads;
+  int32_t D;           /* elements of a head                                                         */
+  int32_t rotary;      /* of them turned; 0: none, freqs is ignored                                  */
+  int32_t interleaved; /* 0 or 1                                                                     */
+  int32_t norm;        /* 1 or 0; 0: the weights must be NULL                                        */
+  int32_t weight_type; /* an osdp_dtype: of the weights and their gradients                          */
+  int32_t reserved;    /* 0                                                                          */
+  double eps;          /* >= 1e-12                                                                   */
+  const int64_t *positions; /* device [T], or NULL: row t has position t                             */
+  const double *freqs;      /* device [rotary / 2], radians a position                               */
+  const void *q_weight, *k_weight; /* device [D], 16-byte aligned, or NULL: ones                     */
+} osdp_qk;
+
+OSDP_API osdp_status osdp_qk_norm_rope_fwd(const osdp_qk *qk, const osdp_heads *q, const osdp_heads *k,
+                                           const osdp_heads *q_out, const osdp_heads *k_out, void *stream);
+
+/* q and k are the forward call's inputs.  dq_weight, dk_weight: device [D] of weight_type, 16-byte aligned, written, or NULL.
+ *   workspace: device, 256-byte aligned, >= osdp_qk_norm_rope_bwd_workspace_bytes; may be NULL when that is not asked for (no
+ *              weight gradients) */
+OSDP_API osdp_status osdp_qk_norm_rope_bwd(const osdp_qk *qk, const osdp_heads *q, const osdp_heads *k,
+                                           const osdp_heads *dq_out, const osdp_heads *dk_out, const osdp_heads *dq,
+                                           const osdp_heads *dk, void *dq_weight, void *dk_weight, void *workspace,
+                                           size_t workspace_bytes, void *stream);
+/* Of `qk`, T, the heads and D are looked at. Host only. */
+OSDP_API osdp_status osdp_qk_norm_rope_bwd_workspace_bytes(const osdp_qk *qk, size_t *bytes);
 
 /* ---- automatic slice granularity ------------------------------------------
  * Section 4.3 (effectiveness of operator splitting) observes that the best

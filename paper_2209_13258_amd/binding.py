@@ -68,6 +68,7 @@ EXPORTS = (
     "osdp_split_linear_i8_quantize", "osdp_split_linear_i8_quantize_workspace_bytes", "osdp_split_linear_i8_fwd",
     "osdp_split_linear_i8_workspace_bytes",
     "osdp_split_linear_epilogue_workspace_bytes", "osdp_split_linear_fwd_epilogue", "osdp_split_linear_bwd_epilogue",
+    "osdp_qk_norm_rope_fwd", "osdp_qk_norm_rope_bwd", "osdp_qk_norm_rope_bwd_workspace_bytes",
 )
 
 
@@ -133,6 +134,18 @@ class osdp_epilogue_grad(ctypes.Structure):
                 ("dbias", ctypes.c_void_p), ("activation", ctypes.c_int32), ("bias_type", ctypes.c_int32)]
 
 
+class osdp_heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class osdp_qk(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("rotary", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("reserved", ctypes.c_int32), ("eps", ctypes.c_double),
+                ("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p)]
+
+
 class OsdpError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"libosdp status {status}: {message}")
@@ -187,6 +200,10 @@ def _load() -> ctypes.CDLL:
     lib.osdp_split_linear_fwd_epilogue.argtypes = [shp, pln, i32, epi, vp, i64, vp, vp, i64, vp, i64, vp, ctypes.c_size_t, vp, vp]
     lib.osdp_split_linear_bwd_epilogue.argtypes = [shp, pln, i32, epg, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp,
                                                    ctypes.c_size_t, vp, vp]
+    qkp, hds = ctypes.POINTER(osdp_qk), ctypes.POINTER(osdp_heads)
+    lib.osdp_qk_norm_rope_fwd.argtypes = [qkp, hds, hds, hds, hds, vp]
+    lib.osdp_qk_norm_rope_bwd.argtypes = [qkp, hds, hds, hds, hds, hds, hds, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.osdp_qk_norm_rope_bwd_workspace_bytes.argtypes = [qkp, ctypes.POINTER(ctypes.c_size_t)]
     lib.hipGetDevice.argtypes = [ctypes.POINTER(ctypes.c_int)]  # (the HIP runtime, which the library brings along)
     lib.osdp_debug_option.argtypes = [ctypes.c_char_p, i32]
     lib.osdp_debug_option.restype = ctypes.c_int
@@ -203,7 +220,8 @@ def _load() -> ctypes.CDLL:
                  "osdp_adamw_grad_sumsq_workspace_bytes", "osdp_adamw_state_values", "osdp_split_linear_i8_quantize",
                  "osdp_split_linear_i8_quantize_workspace_bytes", "osdp_split_linear_i8_fwd",
                  "osdp_split_linear_i8_workspace_bytes", "osdp_split_linear_epilogue_workspace_bytes",
-                 "osdp_split_linear_fwd_epilogue", "osdp_split_linear_bwd_epilogue"):
+                 "osdp_split_linear_fwd_epilogue", "osdp_split_linear_bwd_epilogue", "osdp_qk_norm_rope_fwd",
+                 "osdp_qk_norm_rope_bwd", "osdp_qk_norm_rope_bwd_workspace_bytes"):
         getattr(lib, name).restype = ctypes.c_int
     lib.osdp_strerror.argtypes = [ctypes.c_int]
     lib.osdp_strerror.restype = ctypes.c_char_p
@@ -789,6 +807,75 @@ def osdp_split_linear_bwd_epilogue(X, dY, w_shards, dX, dw_shards, k, workspace,
                                               _shard_ptrs("dw_shards", dw_shards, I, O, device), _opt_ptrs(dw_dp),
                                               workspace.data_ptr(), _check_workspace(workspace, device), _stream(stream_compute),
                                               _stream(stream_copy)))
+
+
+def _heads(t, name: str, shape, device: int):
+    """Heads as the library takes them: a bf16 tensor [tokens, heads, D] with unit stride along D."""
+    if t.shape != shape or not _is(t, "torch.bfloat16") or t.get_device() != device:
+        _refuse(f"{name} must be a bf16 tensor of {tuple(shape)} on the GPU that q is on")
+    ld, head_stride, step = t.stride()
+    if step != 1:
+        _refuse(f"{name} must have unit stride along its heads")
+    return osdp_heads(t.data_ptr(), ld, head_stride)
+
+
+def _qk(q, k, device, positions, freqs, q_weight, k_weight, eps, norm, interleaved):
+    T, q_heads, D = q.shape
+    if k.dim() != 3 or k.shape[0] != T or k.shape[2] != D:
+        _refuse("q and k must be [tokens, heads, D] with tokens and D alike")
+    if positions is not None and (positions.numel() != T or not _is(positions, "torch.int64") or not positions.is_contiguous() or
+                                  positions.get_device() != device):
+        _refuse(f"positions must be {T} contiguous int64 on the GPU that q is on")
+    if freqs is not None and (not _is(freqs, "torch.float64") or not freqs.is_contiguous() or freqs.get_device() != device):
+        _refuse("freqs must be contiguous float64 on the GPU that q is on")
+    at, kind = [None, None], OSDP_BF16
+    for i, (name, w) in enumerate((("q_weight", q_weight), ("k_weight", k_weight))):
+        if w is not None:
+            at[i], kind = _vector(w, name, D, device)
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        _refuse("q_weight and k_weight must be of one type")
+    return osdp_qk(T, q_heads, k.shape[1], D, 0 if freqs is None else 2 * freqs.numel(), int(bool(interleaved)), int(bool(norm)),
+                   kind, 0, eps, None if positions is None else positions.data_ptr(), None if freqs is None else freqs.data_ptr(),
+                   at[0], at[1])
+
+
+def osdp_qk_norm_rope_fwd(q, k, q_out, k_out, *, positions=None, freqs=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                          norm: bool = True, interleaved: bool = False, stream=None) -> None:
+    """Norms of queries and keys and their rotation: bf16 tensors [tokens, heads, D] of any strides (views of the qkv operator's
+    output); ``positions`` int64 [tokens] (None: 0, 1, ..; negative: padding), ``freqs`` float64 [rotary / 2] (None: no rotation),
+    weights bf16 or fp32 [D] (None: ones).  ``q_out`` may be q and ``k_out`` k."""
+    device = _here(q, "q")
+    desc = _qk(q, k, device, positions, freqs, q_weight, k_weight, eps, norm, interleaved)
+    _check(lib.osdp_qk_norm_rope_fwd(desc, _heads(q, "q", q.shape, device), _heads(k, "k", k.shape, device),
+                                     _heads(q_out, "q_out", q.shape, device), _heads(k_out, "k_out", k.shape, device), _stream(stream)))
+
+
+def osdp_qk_norm_rope_bwd_workspace_bytes(T, q_heads, k_heads, D) -> int:
+    need, desc = ctypes.c_size_t(), osdp_qk(T=int(T), q_heads=int(q_heads), k_heads=int(k_heads), D=int(D))
+    _check(lib.osdp_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(need)))
+    return need.value
+
+
+def osdp_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, *, positions=None, freqs=None, q_weight=None,
+                          k_weight=None, eps: float = 1e-6, norm: bool = True, interleaved: bool = False, stream=None) -> None:
+    """The pass back: ``q``, ``k`` and the rest as the forward call had them; ``dq`` (may be q or dq_out), ``dk``, and the weights'
+    gradients (written, or None; of one type with the weights) from ``dq_out`` and ``dk_out``."""
+    device = _here(q, "q")
+    desc = _qk(q, k, device, positions, freqs, q_weight, k_weight, eps, norm, interleaved)
+    at = [None, None]
+    for i, (name, g) in enumerate((("dq_weight", dq_weight), ("dk_weight", dk_weight))):
+        if g is None:
+            continue
+        at[i], kind = _vector(g, name, q.shape[2], device)
+        if q_weight is None and k_weight is None and (i == 0 or dq_weight is None):
+            desc.weight_type = kind
+        if kind != desc.weight_type:
+            _refuse(f"{name} must be of the weights' type")
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), _check_workspace(workspace, device))
+    _check(lib.osdp_qk_norm_rope_bwd(desc, _heads(q, "q", q.shape, device), _heads(k, "k", k.shape, device),
+                                     _heads(dq_out, "dq_out", q.shape, device), _heads(dk_out, "dk_out", k.shape, device),
+                                     _heads(dq, "dq", q.shape, device), _heads(dk, "dk", k.shape, device), at[0], at[1], ws, size,
+                                     _stream(stream)))
 
 
 def osdp_debug_option(name: str, value: int) -> None:

@@ -14,7 +14,7 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libosdp.so"
 POINTERS = PKG / "_pointers.so"
-SOURCES = ["osdp_api.hip", "osdp_gather.hip", "osdp_gemm.hip", "osdp_epilogue.hip", "osdp_search.hip", "osdp_adamw.hip", "osdp_int8.hip"]
+SOURCES = ["osdp_api.hip", "osdp_gather.hip", "osdp_gemm.hip", "osdp_epilogue.hip", "osdp_search.hip", "osdp_adamw.hip", "osdp_int8.hip", "osdp_qk.hip"]
 HEADERS = [CSRC / "osdp_internal.h", CSRC / "activation.h", CSRC / "gemm_launch.h", CSRC / "gemm_common.h", CSRC / "gemm_dma.h", CSRC / "gemm_i8.h", CSRC / "gemm_i8_w4.h", CSRC / "gemm_skinny.h", CSRC / "gemm_w4.h", CSRC / "gemm_w4p.h", ROOT / "include" / "osdp.h"]
 
 HIPCC_FLAGS = [

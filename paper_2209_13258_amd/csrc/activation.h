@@ -1,5 +1,7 @@
 // Activations and their slopes in fp32, for the epilogue of the forward product and the pass in front of the backward one.
 #pragma once
+#include <type_traits>
+
 #include "osdp_internal.h"
 
 namespace osdp {
@@ -67,7 +69,7 @@ __device__ __forceinline__ float activation_slope(float z) {
   return 1.0f;
 }
 
-// f(Int<activation>{}) with the launch's activation, which all lanes share, as a compile-time number.
+// f(an integral constant) with the launch's activation, which all lanes share, as a compile-time number.
 template <class F>
 __device__ __forceinline__ void with_activation(int act, F &&f) {
   switch (act) {
