@@ -376,7 +376,7 @@ OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, con
  * Everything is computed in fp32 and rounded once, angles in 64 bits until less than a turn is left of them (then cos and sin to 2^-20).
  * Squares that leave the range of fp32 are taken of x / 2^70 instead.  dg is summed in an order that the sizes alone decide.
  *
- * A negative position marks a row of padding: it is neither read nor written and adds nothing to dg.
+ * A negative position marks a row of padding: its outputs are left as they are, and it adds nothing to dg, whatever it holds.
  *
  * Heads lie anywhere: element d of head h of token t at p + t * ld + h * head_stride + d.  Outputs may be the inputs of the same
  * name (the same pointer and strides; backward: dq may be q or dq_out, dk alike), otherwise they overlap no input, nor each

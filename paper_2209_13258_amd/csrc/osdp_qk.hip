@@ -27,17 +27,18 @@ struct QkSide {
   HeadsOut y;          // forward: the turned heads; backward: dx
   const void *weight;
   void *dweight;       // backward, or nullptr
-  int32_t heads, chunks;  // chunks: kU head groups each
+  int32_t heads, chunks, waves_log2;  // chunks: kU head groups each; waves of a workgroup that share a token tile (backward)
 };
 struct QkParams {
   QkSide side[2];
   const int64_t *positions;
   const double *freqs;
-  int64_t T, units;    // units: token tiles x chunks of both sides
+  int64_t T, tiles;    // tiles: of the tokens that a wave's lane groups hold
   float eps;
   int32_t D, slots;    // slots: lanes of a group that hold elements
   int32_t rotary, interleaved, norm, weight_f32;
   int32_t heads_log2;  // head groups of a wave; the other lane groups hold the next tokens
+  int32_t waves_log2;  // waves of a workgroup that share a token tile (forward)
   float *planes;       // backward: sums of workgroups, [gridDim.x][2][D]
 };
 
@@ -63,94 +64,105 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-// What a lane holds of every head, and the angles of its token.
-template <int kG>
+// How pairs lie, and whether every element is in one.  Elements that are not turned are kept from their neighbours, which may
+// be infinite, by selections that heads turned as a whole do not need.
+enum Pairs { kHalves = 0, kNeighbours = 1, kHalvesPartly = 2, kNeighboursPartly = 3 };
+constexpr bool neighbours(int pairs) { return pairs & 1; }
+constexpr bool partly(int pairs) { return pairs & 2; }
+
+// A lane's elements 0..7 are its first piece, 8..15 its second; its pair e (of 8) is made of
+constexpr int low_of(int pairs, int e) { return neighbours(pairs) ? 2 * e : e; }
+constexpr int high_of(int pairs, int e) { return neighbours(pairs) ? 2 * e + 1 : 8 + e; }
+
+// What a lane holds of every head.
+template <int kG, int kPairs>
 struct Lane {
-  int i, first, second;  // its slot, where its two pieces begin (elements)
-  bool has_first, has_second, turns_low, turns_high;  // turns: pairs 0..3 and 4..7 of its own
+  int i, first, second;          // its slot, where its two pieces begin (elements; where there is none: the head's first one)
+  bool has_first, has_second, turns_low, turns_high;  // turns: its pairs 0..3 and 4..7
   __device__ __forceinline__ void begin(const QkParams &p, int lane) {
     i = lane & (kG - 1);
     const int pairs = p.rotary / 2;
-    if (!p.interleaved && i < p.rotary / 16) {
+    if (!neighbours(kPairs) && i < p.rotary / 16) {
       first = 8 * i;
       second = first + pairs;
     } else {
-      first = p.interleaved ? 16 * i : p.rotary + 16 * (i - p.rotary / 16);
+      first = neighbours(kPairs) ? 16 * i : p.rotary + 16 * (i - p.rotary / 16);
       second = first + 8;
     }
     has_first = i < p.slots && first < p.D;
     has_second = has_first && second < p.D;
-    turns_low = 8 * i < pairs;
-    turns_high = 8 * i + 4 < pairs;
+    first = has_first ? first : 0;
+    second = has_second ? second : 0;
+    turns_low = has_first && 8 * i < pairs;
+    turns_high = has_first && 8 * i + 4 < pairs;
   }
+  __device__ __forceinline__ bool turns(int e) const { return neighbours(kPairs) && e >= 4 ? turns_high : turns_low; }
   __device__ __forceinline__ void weights(const QkParams &p, const void *w, float (&g)[16]) const {
 #pragma unroll
     for (int e = 0; e < 16; ++e) g[e] = 1.0f;
     if (!w) return;
+    const int at[2] = {first, second};
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      if (!(half ? has_second : has_first)) continue;
-      const int at = half ? second : first;
       if (p.weight_f32) {
-        const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(w) + at);
+        const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(w) + at[half]);
         const float4 a = src[0], b = src[1];
-        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[8 * half + e] = v[e];
+        g[8 * half] = a.x; g[8 * half + 1] = a.y; g[8 * half + 2] = a.z; g[8 * half + 3] = a.w;
+        g[8 * half + 4] = b.x; g[8 * half + 5] = b.y; g[8 * half + 6] = b.z; g[8 * half + 7] = b.w;
       } else {
-        const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(w) + at);
-        const uint32_t v[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          g[8 * half + 2 * e] = bf16_low(v[e]);
-          g[8 * half + 2 * e + 1] = bf16_high(v[e]);
-        }
+        const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(w) + at[half]);
+        g[8 * half] = bf16_low(a.x); g[8 * half + 1] = bf16_high(a.x); g[8 * half + 2] = bf16_low(a.y); g[8 * half + 3] = bf16_high(a.y);
+        g[8 * half + 4] = bf16_low(a.z); g[8 * half + 5] = bf16_high(a.z); g[8 * half + 6] = bf16_low(a.w); g[8 * half + 7] = bf16_high(a.w);
       }
     }
   }
+  // Cosines and sines of its pairs; 1 and 0 of those that do not turn.
   __device__ __forceinline__ void angles(const QkParams &p, int64_t position, float (&c)[8], float (&s)[8]) const {
     constexpr double kTurn = 0.15915494309189533577;  // 1 / (2 pi)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       c[e] = 1.0f;
       s[e] = 0.0f;
-      if (e < 4 ? !turns_low : !turns_high) continue;
-      const double turns = static_cast<double>(position) * p.freqs[8 * i + e] * kTurn;
-      const float rest = static_cast<float>(turns - __builtin_rint(turns));
-      c[e] = __builtin_amdgcn_cosf(rest);  // (of turns)
-      s[e] = __builtin_amdgcn_sinf(rest);
+    }
+    if (!turns_low) return;
+    const double at = static_cast<double>(position) * kTurn;
+    const double *freqs = p.freqs + 8 * i;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool there = e < 4 || !neighbours(kPairs) || turns_high;
+      const double turned = at * freqs[there ? e : e - 4];
+      const float rest = static_cast<float>(turned - __builtin_rint(turned));
+      c[e] = there ? __builtin_amdgcn_cosf(rest) : 1.0f;  // (of turns)
+      s[e] = there ? __builtin_amdgcn_sinf(rest) : 0.0f;
     }
   }
-  __device__ __forceinline__ void load(const HeadsIn &h, int64_t t, int head, bool valid, uint4 &a, uint4 &b) const {
-    a = b = uint4{0u, 0u, 0u, 0u};
-    if (!valid) return;
-    const uint16_t *row = h.p + t * h.ld + head * h.hs;
-    if (has_first) a = load_global16(row + first);
-    if (has_second) b = load_global16(row + second);
+  __device__ __forceinline__ void store(uint16_t *head, bool valid, const float (&v)[16]) const {
+    if (valid && has_first) store_global16(head + first, uint4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])});
+    if (valid && has_second) store_global16(head + second, uint4{pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]), pack2(v[14], v[15])});
   }
-  __device__ __forceinline__ void store(const HeadsOut &h, int64_t t, int head, bool valid, const float (&v)[16]) const {
-    if (!valid) return;
-    uint16_t *row = h.p + t * h.ld + head * h.hs;
-    if (has_first) store_global16(row + first, uint4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])});
-    if (has_second) store_global16(row + second, uint4{pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]), pack2(v[14], v[15])});
-  }
-  // v turned by the angles, or (back) by their negatives.  Elements that are not turned are left alone, whatever their neighbours hold.
-  template <bool kBack>
-  __device__ __forceinline__ void turn(const QkParams &p, const float (&c)[8], const float (&s_)[8], float (&v)[16]) const {
-    auto pair = [&](float &a, float &b, int e) {
-      const float s = kBack ? -s_[e] : s_[e], x = a, y = b;
-      if (e < 4 ? turns_low : turns_high) {
-        a = x * c[e] - y * s;
-        b = y * c[e] + x * s;
-      }
-    };
-    if (p.interleaved) {
+  // The sum over the head of products of what the lanes hold (pieces that are not there hold the head's first ones).
+  __device__ __forceinline__ float dot(const float (&a)[16], const float (&b)[16]) const {
+    float lo = 0.0f, hi = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) pair(v[2 * e], v[2 * e + 1], e);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pair(v[e], v[8 + e], e);
+    for (int e = 0; e < 8; ++e) {
+      lo = __builtin_fmaf(a[e], b[e], lo);
+      hi = __builtin_fmaf(a[8 + e], b[8 + e], hi);
     }
+    return group_sum<kG>((has_first ? lo : 0.0f) + (has_second ? hi : 0.0f));
+  }
+  // 1 / sqrt(mean v^2 + eps) over the head.  Where squares leave the range in which the rest is safe, v is scaled by 2^-70 first,
+  // and so is *scale (eps is nothing beside such squares).
+  __device__ __forceinline__ float factor(const QkParams &p, float (&v)[16], float *scale) const {
+    float s = dot(v, v), eps = p.eps;
+    *scale = 1.0f;
+    if (__builtin_expect(s > 0x1p60f, 0)) {  // (all lanes of the group or none)
+      *scale = 0x1p-70f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] *= 0x1p-70f;
+      s = dot(v, v);
+      eps = 0.0f;
+    }
+    return rsqrtf(__builtin_fmaf(s, 1.0f / static_cast<float>(p.D), eps));
   }
 };
 
@@ -162,137 +174,156 @@ __device__ __forceinline__ void widen(uint4 a, uint4 b, float (&v)[16]) {
     v[2 * e + 1] = bf16_high(w[e]);
   }
 }
+__device__ __forceinline__ uint4 only_if(bool c, uint4 v) { return uint4{c ? v.x : 0u, c ? v.y : 0u, c ? v.z : 0u, c ? v.w : 0u}; }
 
-// v times 1 / sqrt(mean v^2 + eps), over the group; the factor.
-template <int kG>
-__device__ __forceinline__ float normalize(const QkParams &p, float (&v)[16]) {
-  auto squares = [&] {
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s = __builtin_fmaf(v[e], v[e], s);
-    return group_sum<kG>(s);
-  };
-  float s = squares(), scale = 1.0f;
-  const float per = 1.0f / static_cast<float>(p.D);
-  float eps = p.eps;
-  if (__builtin_expect(s == __builtin_inff(), 0)) {  // (all lanes of the group or none: 2^70 of them still fit)
-    scale = 0x1p-70f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] *= scale;
-    s = squares();
-    eps = 0.0f;
-  }
-  const float r = rsqrtf(__builtin_fmaf(s, per, eps));
-#pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] *= r;
-  return r * scale;
-}
-
-// Where a wave's unit lies: its token tile and its head groups of one side.
-template <int kG, int kU>
-struct Unit {
-  int which, head0;
-  int64_t t;
-  __device__ __forceinline__ void find(const QkParams &p, int64_t unit, int lane) {
-    const int chunks = p.side[0].chunks + p.side[1].chunks;
-    const int64_t tile = unit / chunks;
-    int chunk = static_cast<int>(unit - tile * chunks);
-    which = chunk >= p.side[0].chunks;
-    if (which) chunk -= p.side[0].chunks;
-    const int group = lane / kG, heads = 1 << p.heads_log2;
-    t = tile * ((64 / kG) >> p.heads_log2) + (group >> p.heads_log2);
-    head0 = chunk * kU * heads + (group & (heads - 1));
-  }
-};
-
-template <int kG, int kU>
+// Forward.  With g the weight and r the head's factor a pair becomes r (a g_a c - b g_b s), r (b g_b c + a g_a s): the products
+// of weights, cosines and sines are made once for a token's heads.  A wave takes kU head groups of a token tile; the waves of a
+// workgroup those of one token tile, or of several where it has few.
+template <int kG, int kU, int kPairs>
 __global__ __launch_bounds__(256) void qk_forward_kernel(QkParams p) {
   const int lane_id = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Lane<kG> lane;
+  Lane<kG, kPairs> lane;
   lane.begin(p, lane_id);
-  for (int64_t u = static_cast<int64_t>(blockIdx.x) * 4 + wave; u < p.units; u += static_cast<int64_t>(gridDim.x) * 4) {
-    Unit<kG, kU> unit;
-    unit.find(p, u, lane_id);
-    const QkSide &side = p.side[unit.which];
-    const int64_t position = unit.t >= p.T ? -1 : p.positions ? p.positions[unit.t] : unit.t;
-    const bool row = position >= 0;
+  const int group = lane_id / kG, step = 1 << p.heads_log2, tile_tokens = (64 / kG) >> p.heads_log2;
+  const int chunk = (blockIdx.y << p.waves_log2) + (wave & ((1 << p.waves_log2) - 1));
+  if (chunk >= p.side[0].chunks + p.side[1].chunks) return;
+  const bool keys = chunk >= p.side[0].chunks;
+  const HeadsIn x = keys ? p.side[1].x : p.side[0].x;
+  const HeadsOut y = keys ? p.side[1].y : p.side[0].y;
+  const int heads = keys ? p.side[1].heads : p.side[0].heads;
+  const int head0 = (keys ? chunk - p.side[0].chunks : chunk) * kU * step + (group & (step - 1));
+  const int tiles_at_once = 4 >> p.waves_log2;
+  for (int64_t tile = static_cast<int64_t>(blockIdx.x) * tiles_at_once + (wave >> p.waves_log2); tile < p.tiles;
+       tile += static_cast<int64_t>(gridDim.x) * tiles_at_once) {
+    const int64_t t = tile * tile_tokens + (group >> p.heads_log2), t_in = t < p.T ? t : p.T - 1;
+    const uint16_t *src = x.p + t_in * x.ld;
     uint4 a[kU], b[kU];
-    const int step = 1 << p.heads_log2;
 #pragma unroll
-    for (int i = 0; i < kU; ++i)
-      lane.load(side.x, unit.t, unit.head0 + i * step, row && unit.head0 + i * step < side.heads, a[i], b[i]);
-    float c[8], s[8], g[16];
-    lane.angles(p, position, c, s);
-    lane.weights(p, side.weight, g);
+    for (int i = 0; i < kU; ++i) {  // (lanes without a head load one that is there)
+      const int head = head0 + i * step;
+      const uint16_t *at = src + (head < heads ? head : heads - 1) * x.hs;
+      a[i] = load_global16(at + lane.first);
+      b[i] = load_global16(at + lane.second);
+    }
+    const int64_t position = p.positions ? p.positions[t_in] : t;
+    const bool row = t < p.T && position >= 0;
+    float g[16], same[16], cross[16];  // what an element is multiplied by in its own place, and in its partner's
+    lane.weights(p, keys ? p.side[1].weight : p.side[0].weight, g);
+    {
+      float c[8], s[8];
+      lane.angles(p, position, c, s);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        constexpr int kP = kPairs;
+        const int lo = low_of(kP, e), hi = high_of(kP, e);
+        same[lo] = g[lo] * c[e];
+        cross[lo] = g[lo] * s[e];
+        same[hi] = g[hi] * c[e];
+        cross[hi] = g[hi] * s[e];
+      }
+    }
+    uint16_t *dst = y.p + t_in * y.ld;
 #pragma unroll
     for (int i = 0; i < kU; ++i) {
-      float v[16];
+      float v[16], o[16], r = 1.0f, scale;
       widen(a[i], b[i], v);
-      if (p.norm) {
-        normalize<kG>(p, v);
+      if (p.norm) r = lane.factor(p, v, &scale);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] *= g[e];
+      for (int e = 0; e < 8; ++e) {
+        const int lo = low_of(kPairs, e), hi = high_of(kPairs, e);
+        float to_lo = v[hi], to_hi = v[lo];
+        if constexpr (partly(kPairs)) {
+          to_lo = lane.turns(e) ? to_lo : 0.0f;
+          to_hi = lane.turns(e) ? to_hi : 0.0f;
+        }
+        o[lo] = r * __builtin_fmaf(v[lo], same[lo], -(to_lo * cross[hi]));
+        o[hi] = r * __builtin_fmaf(v[hi], same[hi], to_hi * cross[lo]);
       }
-      lane.template turn<false>(p, c, s, v);
-      lane.store(side.y, unit.t, unit.head0 + i * step, row && unit.head0 + i * step < side.heads, v);
+      const int head = head0 + i * step;
+      lane.store(dst + head * y.hs, row && head < heads, o);
     }
   }
 }
 
-// The pass back.  Workgroups [0, split) take units of the queries, the others of the keys, each every so many of them, and keep the
-// sums for their weight in registers; the lane groups' sums are added up through LDS, in order, into the workgroup's plane.
-template <int kG, int kU, bool kSums>
+// The pass back.  Workgroups [0, split) take token tiles of the queries, the others of the keys, each every so many of them, and keep
+// the sums for their weight in registers; the lane groups' sums are added up through LDS, in order, into the workgroup's plane.
+// With d the gradients turned back, x the head and r its factor:  u = d r,  sum += u x,  t = u g,  dx = t - x r^2 mean(t x).
+template <int kG, int kU, int kPairs, bool kSums>
 __global__ __launch_bounds__(256) void qk_backward_kernel(QkParams p, int split) {
   __shared__ float s_sum[kSums ? 256 * 16 : 1];
   const int lane_id = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int which = static_cast<int>(blockIdx.x) >= split;
-  const QkSide &side = p.side[which];
-  const int first = which ? split : 0, count = which ? gridDim.x - split : split;
-  const int groups = 1 << p.heads_log2, tile_tokens = (64 / kG) >> p.heads_log2;
-  Lane<kG> lane;
+  const bool keys = static_cast<int>(blockIdx.x) >= split;
+  const HeadsIn x = keys ? p.side[1].x : p.side[0].x, dy = keys ? p.side[1].dy : p.side[0].dy;
+  const HeadsOut y = keys ? p.side[1].y : p.side[0].y;
+  const int heads = keys ? p.side[1].heads : p.side[0].heads, chunks = keys ? p.side[1].chunks : p.side[0].chunks;
+  const int waves_log2 = keys ? p.side[1].waves_log2 : p.side[0].waves_log2;
+  const int first = keys ? split : 0, count = keys ? gridDim.x - split : split;
+  const int group = lane_id / kG, step = 1 << p.heads_log2, tile_tokens = (64 / kG) >> p.heads_log2;
+  Lane<kG, kPairs> lane;
   lane.begin(p, lane_id);
   float g[16], sum[16] = {};
-  lane.weights(p, side.weight, g);
-  const int64_t tiles = (p.T + tile_tokens - 1) / tile_tokens, units = tiles * side.chunks;
+  lane.weights(p, keys ? p.side[1].weight : p.side[0].weight, g);
   const float per = 1.0f / static_cast<float>(p.D);
-  for (int64_t u = static_cast<int64_t>(blockIdx.x - first) * 4 + wave; u < units; u += static_cast<int64_t>(count) * 4) {
-    const int64_t tile = u / side.chunks;
-    const int group = lane_id / kG;
-    const int64_t t = tile * tile_tokens + (group >> p.heads_log2);
-    const int head0 = static_cast<int>(u - tile * side.chunks) * kU * groups + (group & (groups - 1));
-    const int64_t position = t >= p.T ? -1 : p.positions ? p.positions[t] : t;
-    const bool row = position >= 0;
-    uint4 a[kU], b[kU], da[kU], db[kU];
-#pragma unroll
-    for (int i = 0; i < kU; ++i) {
-      const bool valid = row && head0 + i * groups < side.heads;
-      if (p.norm) lane.load(side.x, t, head0 + i * groups, valid, a[i], b[i]);
-      lane.load(side.dy, t, head0 + i * groups, valid, da[i], db[i]);
-    }
+  const int tiles_at_once = 4 >> waves_log2;
+  for (int64_t tile = static_cast<int64_t>(blockIdx.x - first) * tiles_at_once + (wave >> waves_log2); tile < p.tiles;
+       tile += static_cast<int64_t>(count) * tiles_at_once) {
+    const int64_t t = tile * tile_tokens + (group >> p.heads_log2), t_in = t < p.T ? t : p.T - 1;
+    const int64_t position = p.positions ? p.positions[t_in] : t;
+    const bool row = t < p.T && position >= 0;
     float c[8], s[8];
     lane.angles(p, position, c, s);
+    const uint16_t *src_x = x.p + t_in * x.ld, *src_dy = dy.p + t_in * dy.ld;
+    uint16_t *dst = y.p + t_in * y.ld;
+    for (int chunk = wave & ((1 << waves_log2) - 1); chunk < chunks; chunk += 1 << waves_log2) {
+      const int head0 = chunk * kU * step + (group & (step - 1));
+      uint4 a[kU], b[kU], da[kU], db[kU];
 #pragma unroll
-    for (int i = 0; i < kU; ++i) {
-      const bool valid = row && head0 + i * groups < side.heads;
-      float d[16];
-      widen(da[i], db[i], d);
-      lane.template turn<true>(p, c, s, d);
-      if (p.norm) {
-        float x[16];
-        widen(a[i], b[i], x);
-        const float r = normalize<kG>(p, x);
-        float dot = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if constexpr (kSums) sum[e] = __builtin_fmaf(d[e], x[e], sum[e]);  // (a head that is not there is all zeros)
-          d[e] *= g[e];
-          dot = __builtin_fmaf(d[e], x[e], dot);
+      for (int i = 0; i < kU; ++i) {
+        const int head = head0 + i * step, in = head < heads ? head : heads - 1;
+        a[i] = b[i] = uint4{0u, 0u, 0u, 0u};
+        if (p.norm) {
+          a[i] = load_global16(src_x + in * x.hs + lane.first);
+          b[i] = load_global16(src_x + in * x.hs + lane.second);
         }
-        dot = group_sum<kG>(dot) * per;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) d[e] = r * __builtin_fmaf(-x[e], dot, d[e]);
+        da[i] = load_global16(src_dy + in * dy.hs + lane.first);
+        db[i] = load_global16(src_dy + in * dy.hs + lane.second);
       }
-      lane.store(side.y, t, head0 + i * groups, valid, d);
+#pragma unroll
+      for (int i = 0; i < kU; ++i) {
+        const int head = head0 + i * step;
+        const bool valid = row && head < heads;
+        float w[16], d[16];
+        widen(kSums ? only_if(valid, da[i]) : da[i], kSums ? only_if(valid, db[i]) : db[i], w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int lo = low_of(kPairs, e), hi = high_of(kPairs, e);
+          float to_lo = w[hi], to_hi = w[lo];
+          if constexpr (partly(kPairs)) {
+            to_lo = lane.turns(e) ? to_lo : 0.0f;
+            to_hi = lane.turns(e) ? to_hi : 0.0f;
+          }
+          d[lo] = __builtin_fmaf(w[lo], c[e], to_lo * s[e]);
+          d[hi] = __builtin_fmaf(w[hi], c[e], -(to_hi * s[e]));
+        }
+        if (p.norm) {
+          float v[16], scale;
+          widen(kSums ? only_if(valid, a[i]) : a[i], kSums ? only_if(valid, b[i]) : b[i], v);
+          const float r = lane.factor(p, v, &scale);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            d[e] *= r;
+            if constexpr (kSums) sum[e] = __builtin_fmaf(d[e], v[e], sum[e]);
+            d[e] *= g[e];
+          }
+          const float k = lane.dot(d, v) * per * (r * r);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) d[e] = __builtin_fmaf(-v[e], k, d[e]);
+          if (__builtin_expect(scale != 1.0f, 0))
+#pragma unroll
+            for (int e = 0; e < 16; ++e) d[e] *= scale;
+        }
+        lane.store(dst + head * y.hs, valid, d);
+      }
     }
   }
   if constexpr (kSums) {
@@ -302,7 +333,7 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkParams p, int split)
     // element e of slot i: the sum over the workgroup's 256 / kG lane groups
     for (int at = threadIdx.x; at < 16 * kG; at += 256) {
       const int e = at / kG, i = at - e * kG;
-      Lane<kG> of;
+      Lane<kG, kPairs> of;
       of.begin(p, i);
       if (!(e < 8 ? of.has_first : of.has_second)) continue;
       float total = 0.0f;
@@ -340,6 +371,8 @@ int log2_up(int64_t n) {
   return l;
 }
 
+int waves_log2_of(int chunks) { return std::min(2, log2_up(std::max(1, chunks))); }
+
 // Workgroups of the pass back, those of the queries first.
 struct BackwardGrid {
   int queries, all;
@@ -359,7 +392,10 @@ BackwardGrid backward_grid(int64_t T, int q_heads, int k_heads, int D) {
   const int group = 1 << log2_up((D + 15) / 16), hl = heads_log2_of(q_heads, k_heads, group);
   const int tile = (64 / group) >> hl;
   const int64_t tiles = (T + tile - 1) / tile;
-  const int64_t uq = (tiles * chunks_of(q_heads, hl, kBackwardUnroll) + 3) / 4, uk = (tiles * chunks_of(k_heads, hl, kBackwardUnroll) + 3) / 4;
+  const int cq = chunks_of(q_heads, hl, kBackwardUnroll), ck = chunks_of(k_heads, hl, kBackwardUnroll);
+  // (workgroups that the work could keep busy, and that of a side with no heads none)
+  const int64_t uq = cq ? (tiles + (4 >> waves_log2_of(cq)) - 1) / (4 >> waves_log2_of(cq)) * ((cq + 3) / 4) : 0;
+  const int64_t uk = ck ? (tiles + (4 >> waves_log2_of(ck)) - 1) / (4 >> waves_log2_of(ck)) * ((ck + 3) / 4) : 0;
   BackwardGrid g{};
   if (uq + uk <= kMaxBackwardGroups) {
     g.queries = static_cast<int>(uq);
@@ -470,8 +506,11 @@ QkParams params_of(const osdp_qk &q, int group, int unroll) {
   for (int i = 0; i < 2; ++i) {
     p.side[i].heads = heads[i];
     p.side[i].chunks = chunks_of(heads[i], p.heads_log2, unroll);
+    p.side[i].waves_log2 = waves_log2_of(p.side[i].chunks);
     p.side[i].weight = weight[i];
   }
+  const int tile = (64 / group) >> p.heads_log2;
+  p.tiles = (q.T + tile - 1) / tile;
   return p;
 }
 HeadsIn in(const osdp_heads *h) { return h ? HeadsIn{static_cast<const uint16_t *>(h->p), h->ld, h->head_stride} : HeadsIn{nullptr, 0, 0}; }
@@ -480,36 +519,44 @@ HeadsOut out(const osdp_heads *h) { return h ? HeadsOut{static_cast<uint16_t *>(
 // Tokens times head groups from which a wave takes four head groups, with their angles worked out once, rather than one.
 constexpr int64_t kManyUnits = 8192;
 
-template <int kG>
-void launch_forward(QkParams &p, const osdp_qk &q, hipStream_t stream) {
-  const int tile = (64 / kG) >> p.heads_log2;
-  const int64_t tiles = (q.T + tile - 1) / tile;
-  const bool many = tiles * (p.side[0].chunks + p.side[1].chunks) >= kManyUnits;
+template <int kG, int kPairs>
+void launch_forward(QkParams &p, hipStream_t stream) {
+  const bool many = p.tiles * (p.side[0].chunks + p.side[1].chunks) >= kManyUnits;
   if (many)
     for (QkSide &s : p.side) s.chunks = chunks_of(s.heads, p.heads_log2, 4);
-  p.units = tiles * (p.side[0].chunks + p.side[1].chunks);
-  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((p.units + 3) / 4, 1 << 22));
-  if (many) hipLaunchKernelGGL((qk_forward_kernel<kG, 4>), dim3(grid), dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((qk_forward_kernel<kG, 1>), dim3(grid), dim3(256), 0, stream, p);
+  const int chunks = p.side[0].chunks + p.side[1].chunks;
+  p.waves_log2 = waves_log2_of(chunks);
+  const int at_once = 4 >> p.waves_log2, rows = (chunks + (1 << p.waves_log2) - 1) >> p.waves_log2;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((p.tiles + at_once - 1) / at_once, (1 << 22) / std::min(rows, 1 << 12))), rows);
+  if (many) hipLaunchKernelGGL((qk_forward_kernel<kG, 4, kPairs>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((qk_forward_kernel<kG, 1, kPairs>), grid, dim3(256), 0, stream, p);
 }
 
-template <int kG>
+template <int kG, int kPairs>
 void launch_backward(const QkParams &p, BackwardGrid grid, hipStream_t stream) {
-  if (p.planes) hipLaunchKernelGGL((qk_backward_kernel<kG, kBackwardUnroll, true>), dim3(grid.all), dim3(256), 0, stream, p, grid.queries);
-  else hipLaunchKernelGGL((qk_backward_kernel<kG, kBackwardUnroll, false>), dim3(grid.all), dim3(256), 0, stream, p, grid.queries);
+  constexpr int kU = kBackwardUnroll;
+  if (p.planes) hipLaunchKernelGGL((qk_backward_kernel<kG, kU, kPairs, true>), dim3(grid.all), dim3(256), 0, stream, p, grid.queries);
+  else hipLaunchKernelGGL((qk_backward_kernel<kG, kU, kPairs, false>), dim3(grid.all), dim3(256), 0, stream, p, grid.queries);
 }
 
-// f(integral_constant<kG>) for the lanes that hold a head.
-template <class F>
+// f(integral_constant<kG>, integral_constant<kPairs>) for the lanes that hold a head and the pairs that are turned.
+template <int kPairs, class F>
 void with_group(int D, F &&f) {
+  std::integral_constant<int, kPairs> pairs;
   switch (log2_up((D + 15) / 16)) {
-    case 0: f(std::integral_constant<int, 1>{}); break;
-    case 1: f(std::integral_constant<int, 2>{}); break;
-    case 2: f(std::integral_constant<int, 4>{}); break;
-    case 3: f(std::integral_constant<int, 8>{}); break;
-    case 4: f(std::integral_constant<int, 16>{}); break;
-    default: f(std::integral_constant<int, 32>{}); break;
+    case 0: f(std::integral_constant<int, 1>{}, pairs); break;
+    case 1: f(std::integral_constant<int, 2>{}, pairs); break;
+    case 2: f(std::integral_constant<int, 4>{}, pairs); break;
+    case 3: f(std::integral_constant<int, 8>{}, pairs); break;
+    case 4: f(std::integral_constant<int, 16>{}, pairs); break;
+    default: f(std::integral_constant<int, 32>{}, pairs); break;
   }
+}
+template <class F>
+void with_kernel(const osdp_qk &q, F &&f) {
+  const bool part = q.rotary < q.D;
+  if (q.interleaved) part ? with_group<kNeighboursPartly>(q.D, f) : with_group<kNeighbours>(q.D, f);
+  else part ? with_group<kHalvesPartly>(q.D, f) : with_group<kHalves>(q.D, f);
 }
 
 osdp_status hip_status(hipError_t e, const char *what) {
@@ -543,12 +590,12 @@ osdp_status osdp_qk_norm_rope_fwd(const osdp_qk *qk, const osdp_heads *q, const 
     return bad(OSDP_ERR_INVALID_ARG, "an output overlaps an input or the other output");
   if ((st = right_device()) != OSDP_OK) return st;
   if (d.T == 0 || d.q_heads + d.k_heads == 0) return OSDP_OK;
-  with_group(d.D, [&](auto group) {
+  with_kernel(d, [&](auto group, auto pairs) {
     constexpr int kG = decltype(group)::value;
     QkParams p = params_of(d, kG, 1);
     p.side[0].x = in(q); p.side[0].y = out(q_out);
     p.side[1].x = in(k); p.side[1].y = out(k_out);
-    launch_forward<kG>(p, d, static_cast<hipStream_t>(stream));
+    launch_forward<kG, decltype(pairs)::value>(p, static_cast<hipStream_t>(stream));
   });
   return hip_status(hipGetLastError(), "launching the norms of queries and keys");
 }
@@ -596,13 +643,13 @@ osdp_status osdp_qk_norm_rope_bwd(const osdp_qk *qk, const osdp_heads *q, const 
   if ((st = right_device()) != OSDP_OK) return st;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   QkParams last{};
-  with_group(d.D, [&](auto group) {
+  with_kernel(d, [&](auto group, auto pairs) {
     constexpr int kG = decltype(group)::value;
     QkParams p = params_of(d, kG, kBackwardUnroll);
     p.side[0].x = in(d.norm ? q : nullptr); p.side[0].dy = in(dq_out); p.side[0].y = out(dq); p.side[0].dweight = dq_weight;
     p.side[1].x = in(d.norm ? k : nullptr); p.side[1].dy = in(dk_out); p.side[1].y = out(dk); p.side[1].dweight = dk_weight;
     p.planes = sums ? static_cast<float *>(workspace) : nullptr;
-    if (grid.all > 0) launch_backward<kG>(p, grid, hs);
+    if (grid.all > 0) launch_backward<kG, decltype(pairs)::value>(p, grid, hs);
     last = p;
   });
   hipError_t e = hipGetLastError();
