@@ -318,91 +318,83 @@ __device__ __forceinline__ void store_tile(const GemmParams &p, Read &&read, int
   });
 }
 
-// One wave's share through the fused epilogue: the same rows and columns as store_tile's.  `scratch`: this wave's own
-// fused_scratch_bytes(NB) of LDS.
+// One wave's share through the fused epilogue: the same rows and columns as store_tile's.
 //
 // Straight-line code as above would hold an activation for each of the 256 values of a lane, for each activation.  Here one
-// loop turns to the row blocks in turn: 16 rows of accumulators go through LDS, from where the lanes take 8 columns of a row
-// each, so that bias and column addresses are one register set for the whole tile, residual, Z and Y are whole 16-byte
-// pieces, rows of 32 NB contiguous bytes, and the code is short.  The residual of the next row block is under way meanwhile.
-// Written down the rows and read along them, the 16-byte pieces of a row are permuted by its number, or (rows that are no
-// power of two) the rows padded by one.
-constexpr int fused_row(int NB) { return 16 * NB + (NB % 4 == 0 ? 0 : 4); }
-constexpr size_t fused_scratch_bytes(int NB) { return static_cast<size_t>(16) * fused_row(NB) * sizeof(float); }
-
+// loop takes the row blocks in turn, so that the code is that of one of them and a copy of its accumulators out of the register
+// file for each.  Bias, activation and residual work on the accumulators' own layout (a lane: 4 columns of each block, row l16),
+// Z and Y change lanes as above on their way out.  The residual of the next row block is under way meanwhile.
 template <int MB, int NB, class Read>
-__device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, int m_base, int n_base, int n_end, int l16, int q,
-                                            float *scratch) {
-  constexpr int kVecs = 2 * NB;               // pieces of 8 columns in a row
-  constexpr int kRows = 64 / kVecs;           // rows that the wave takes at once
-  constexpr int kPasses = (16 + kRows - 1) / kRows;
-  constexpr int kRowLd = fused_row(NB), kPerm = NB % 4 == 0 ? 15 : 0;
-  static_assert(kPerm == 0 || (4 * NB) % 16 == 0, "a row is whole groups of permuted pieces");
+__device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, int m_base, int n_base, int n_end, int l16, int q) {
   const FusedEpilogue &e = p.fused;
-  const int lane = 16 * q + l16, row0 = lane / kVecs, vec = lane - row0 * kVecs;
-  const int n = n_base + 8 * vec;
-  const bool columns = row0 < kRows && n < n_end;
-  float bias[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
-  if (columns) load_bias<8>(e, n, bias);
-  auto inside = [&](int bm, int pass) {
-    const int r = pass * kRows + row0;
-    return columns && r < 16 && m_base + 16 * bm + r < p.M;
-  };
-  uint4 next[kPasses];
+  const int n = n_base + 4 * q, col = 16 * (q & 1) + 8 * (q >> 1);
+  f32x4 bias[NB];
+  static_for<NB>([&](auto bn_) {
+    constexpr int bn = decltype(bn_)::value;
+    float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (n + 16 * bn < n_end) load_bias<4>(e, n + 16 * bn, b);
+    bias[bn] = f32x4{b[0], b[1], b[2], b[3]};
+  });
+  uint2 next[NB];
   auto ask = [&](int bm) {
-    static_for<kPasses>([&](auto pass_) {
-      constexpr int pass = decltype(pass_)::value;
-      next[pass] = uint4{0u, 0u, 0u, 0u};
-      if (e.residual && bm < MB && inside(bm, pass))
-        next[pass] = load_global16(e.residual + static_cast<int64_t>(m_base + 16 * bm + pass * kRows + row0) * e.ld_residual + n);
+    const int m = m_base + 16 * bm + l16;
+    const uint16_t *src = e.residual + static_cast<int64_t>(m) * e.ld_residual + n;
+    static_for<NB>([&](auto bn_) {
+      constexpr int bn = decltype(bn_)::value;
+      next[bn] = uint2{0u, 0u};
+      if (e.residual && bm < MB && m < p.M && n + 16 * bn < n_end) next[bn] = load_global8(src + 16 * bn);
     });
+  };
+  // two neighbouring blocks' packed values change lanes and are stored; a last block without a neighbour as it is
+  auto store = [&](uint16_t *row, bool there, const uint2 (&v)[NB]) {
+    static_for<NB / 2>([&](auto i_) {
+      constexpr int i = decltype(i_)::value;
+      const auto lo = __builtin_amdgcn_permlane16_swap(v[2 * i].x, v[2 * i + 1].x, false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(v[2 * i].y, v[2 * i + 1].y, false, false);
+      if (there && n_base + 32 * i + col < n_end) store_global16(row + 32 * i + col, uint4{lo[0], hi[0], lo[1], hi[1]});
+    });
+    if constexpr (NB % 2)
+      if (there && n + 16 * (NB - 1) < n_end) store_global8(row + 16 * (NB - 1) + 4 * q, v[NB - 1]);
   };
   ask(0);
 #pragma unroll 1
   for (int bm = 0; bm < MB; ++bm) {
+    f32x4 c[NB];
     static_for<MB>([&](auto b_) {
       constexpr int b = decltype(b_)::value;
-      if (bm == b) {
-        static_for<NB>([&](auto bn_) {
-          constexpr int bn = decltype(bn_)::value;
-          const f32x4 c = read(Int<b>{}, Int<bn>{});
-          *reinterpret_cast<f32x4 *>(scratch + l16 * kRowLd + 4 * ((4 * bn + q) ^ (l16 & kPerm))) = c;
-          __builtin_amdgcn_sched_barrier(0);
-        });
-      }
+      if (bm == b) static_for<NB>([&](auto bn) { c[decltype(bn)::value] = read(Int<b>{}, bn); });
     });
-    uint4 residual[kPasses];
-    static_for<kPasses>([&](auto pass) { residual[decltype(pass)::value] = next[decltype(pass)::value]; });
+    uint2 residual[NB], packed[NB];
+    static_for<NB>([&](auto bn) { residual[decltype(bn)::value] = next[decltype(bn)::value]; });
     ask(bm + 1);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (one wave's LDS accesses keep their order: no barrier)
-    static_for<kPasses>([&](auto pass_) {
-      constexpr int pass = decltype(pass_)::value;
-      const int r = pass * kRows + row0;
-      if (inside(bm, pass)) {
-        const float *row = scratch + r * kRowLd;
-        const f32x4 lo = *reinterpret_cast<const f32x4 *>(row + 4 * ((2 * vec) ^ (r & kPerm)));
-        const f32x4 hi = *reinterpret_cast<const f32x4 *>(row + 4 * ((2 * vec + 1) ^ (r & kPerm)));
-        float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    const int64_t m = m_base + 16 * bm + l16;
+    const bool there = m < p.M;
+    static_for<NB>([&](auto bn_) {
+      constexpr int bn = decltype(bn_)::value;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] += bias[i];
-        const int64_t m = m_base + 16 * bm + r;
-        if (e.z)
-          store_global16(e.z + m * e.ldz + n, uint4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])});
-        with_activation(e.activation, [&](auto act) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) z[i] = activate<decltype(act)::value>(z[i]);
-        });
-        if (e.residual) {
-          const uint4 v = residual[pass];
-          z[0] += bf16_low(v.x); z[1] += bf16_high(v.x); z[2] += bf16_low(v.y); z[3] += bf16_high(v.y);
-          z[4] += bf16_low(v.z); z[5] += bf16_high(v.z); z[6] += bf16_low(v.w); z[7] += bf16_high(v.w);
-        }
-        store_global16(static_cast<uint16_t *>(p.C) + m * p.ldc + n, uint4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])});
-      }
+      for (int i = 0; i < 4; ++i) c[bn][i] += bias[bn][i];
     });
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (e.z) {
+      static_for<NB>([&](auto bn_) {
+        constexpr int bn = decltype(bn_)::value;
+        packed[bn] = uint2{pack_bf16x2(c[bn][0], c[bn][1]), pack_bf16x2(c[bn][2], c[bn][3])};
+      });
+      store(e.z + m * e.ldz + n_base, there, packed);
+    }
+    with_activation(e.activation, [&](auto act) {
+      static_for<NB>([&](auto bn_) {
+        constexpr int bn = decltype(bn_)::value;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[bn][i] = activate<decltype(act)::value>(c[bn][i]);
+      });
+    });
+    static_for<NB>([&](auto bn_) {
+      constexpr int bn = decltype(bn_)::value;
+      const uint2 r = residual[bn];
+      packed[bn] = uint2{pack_bf16x2(c[bn][0] + bf16_low(r.x), c[bn][1] + bf16_high(r.x)),
+                         pack_bf16x2(c[bn][2] + bf16_low(r.y), c[bn][3] + bf16_high(r.y))};
+    });
+    store(static_cast<uint16_t *>(p.C) + m * p.ldc + n_base, there, packed);
   }
 }
 

@@ -419,10 +419,8 @@ void gemm_dma_kernel(GemmParams p, int tiles_m, int tiles_n) {
   wait_vmcnt<0>();  // surplus loads must have landed before the workgroup gives its LDS back
 
   if constexpr (kEpi == static_cast<int>(Epilogue::kBf16Fused)) {
-    __builtin_amdgcn_s_barrier();  // no wave needs what it reads from the stages any more
-    asm volatile("" ::: "memory");
     store_fused<MB, NB>(p, [&](auto bm, auto bn) { return acc[decltype(bm)::value][decltype(bn)::value]; }, m0 + wm, n0 + wn,
-                        n_end, l16, q4, reinterpret_cast<float *>(smem) + wave * (fused_scratch_bytes(NB) / 4));
+                        n_end, l16, q4);
   } else {
     store_tile<MB, NB, kEpi>(p, [&](auto bm, auto bn) { return acc[decltype(bm)::value][decltype(bn)::value]; }, m0 + wm, n0 + wn,
                              n_end, plane_row, l16, q4, s_tab);

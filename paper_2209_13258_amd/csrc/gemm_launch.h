@@ -181,7 +181,6 @@ hipError_t launch_dma(const GemmParams &p, hipStream_t stream) {
   constexpr int kWaves = (BM / WM) * (BN / WN);
   constexpr size_t lds = static_cast<size_t>(kStages) * (BM + BN) * BK * sizeof(uint16_t);
   static_assert(lds + OSDP_MAX_SHARDS * 8 <= 160 * 1024, "tile does not fit the 160 KB of LDS");
-  static_assert(kEpi != static_cast<int>(Epilogue::kBf16Fused) || kWaves * fused_scratch_bytes(WN / 16) <= lds, "the fused epilogue reuses the stages");
   auto kernel = gemm_dma_kernel<BM, BN, WM, WN, BK, kStages, kAK, kBK, kEpi, kAccIn>;
   static bool configured[kMaxDevices] = {};
   hipError_t e = allow_lds(kernel, lds, configured);
@@ -197,7 +196,6 @@ template <int MB, int NB, bool kAK, bool kBK, int kEpi, bool kAccIn, bool kCopy>
 hipError_t launch_w4(const GemmParams &p, hipStream_t stream) {
   constexpr size_t lds = 2 * (W4Operand<kAK, MB>::kElems + W4Operand<kBK, NB>::kElems) * sizeof(uint16_t);
   static_assert(lds + 2 * OSDP_MAX_SHARDS * 8 <= 160 * 1024, "tile does not fit the 160 KB of LDS");
-  static_assert(4 * fused_scratch_bytes(NB) <= lds, "the fused epilogue reuses the slots");
   auto kernel = [] {
     if constexpr (MB == 8 && NB == 8) return gemm_w4_kernel<kAK, kBK, kEpi, kAccIn, kCopy>;
     else return gemm_w4_small_kernel<MB, NB, kAK, kBK, kEpi, kAccIn, kCopy>;
@@ -215,7 +213,6 @@ hipError_t launch_w4(const GemmParams &p, hipStream_t stream) {
 template <int kSlots, bool kAK, bool kBK, int kEpi, bool kAccIn>
 hipError_t launch_w4_128(const GemmParams &p, hipStream_t stream) {
   constexpr size_t lds = static_cast<size_t>(kSlots) * (W4Operand<kAK, 4>::kElems + W4Operand<kBK, 4>::kElems) * sizeof(uint16_t);
-  static_assert(4 * fused_scratch_bytes(4) <= lds, "the fused epilogue reuses the slots");
   static_assert((kSlots == 2 ? 2 : 1) * (lds + OSDP_MAX_SHARDS * 8) <= 160 * 1024, "tile does not fit the 160 KB of LDS");
   auto kernel = gemm_w4_128_kernel<kSlots, kAK, kBK, kEpi, kAccIn>;
   static bool configured[kMaxDevices] = {};
@@ -275,10 +272,7 @@ constexpr int kCUs = 256;
 // The persistent form of the four-wave kernel: one workgroup per CU walks through the tiles.
 template <int MB, int NB, bool kAK, bool kBK, int kEpi, bool kAccIn>
 hipError_t launch_w4p(const GemmParams &p, hipStream_t stream) {
-  constexpr size_t lds = 2 * (W4Operand<kAK, MB>::kElems + W4Operand<kBK, NB>::kElems) * sizeof(uint16_t) +
-                         (kEpi == static_cast<int>(Epilogue::kBf16Fused) ? 4 * fused_scratch_bytes(NB) : 0);
-  static_assert(lds + (kEpi == static_cast<int>(Epilogue::kBf16ShardMajor) ? OSDP_MAX_SHARDS * 8 : 0) <= 160 * 1024,
-                "tile does not fit the 160 KB of LDS");
+  constexpr size_t lds = 2 * (W4Operand<kAK, MB>::kElems + W4Operand<kBK, NB>::kElems) * sizeof(uint16_t);
   auto kernel = [] {
     if constexpr (MB == 8 && NB == 8) return gemm_w4p_kernel<kAK, kBK, kEpi, kAccIn>;
     else return gemm_w4p_small_kernel<MB, NB, kAK, kBK, kEpi, kAccIn>;
@@ -401,15 +395,17 @@ enum class TileUse {
 // Cheapest tile for M x N; a column split must fall on a tile boundary.
 // parts > 1: the launch has that many workgroups per tile (parts of the reduction); the cost is in tile passes over
 // the whole reduction all the same, so the caller divides it by parts.
-int best_tile(int M, int N, int K, int n_split, int kind, double *cost, int parts = 1, TileUse use = TileUse::kLaunch) {
+// seg_n: columns that come in runs of this many, which tiles do not reach over (GemmParams); 0: not so.
+int best_tile(int M, int N, int K, int n_split, int kind, double *cost, int parts = 1, TileUse use = TileUse::kLaunch, int seg_n = 0) {
   const bool lone = use != TileUse::kSumLaunch && debug_options().deep.load(std::memory_order_relaxed) != 0;
   const int shapes = lone && use == TileUse::kLaunch ? kTileShapes : kPricedShapes;
   int best = -1;
   double best_cost = 0.0;
   for (int i = 0; i < shapes; ++i) {
-    if (i >= kPricedShapes && tile_count(M, N, kTiles[i].bm, kTiles[i].bn) * parts > kCUs) continue;  // lone tiles only
+    const int N_tiled = seg_n ? N / seg_n * ((seg_n + kTiles[i].bn - 1) / kTiles[i].bn) * kTiles[i].bn : N;
+    if (i >= kPricedShapes && tile_count(M, N_tiled, kTiles[i].bm, kTiles[i].bn) * parts > kCUs) continue;  // lone tiles only
     if (n_split % kTiles[i].bn || !tile_offered(i, kind, K / parts, use == TileUse::kFirstShapes ? kNarrowPricedK : kNarrowMinK)) continue;
-    const double c = tile_cost(M, N, kTiles[i].bm, kTiles[i].bn, kTiles[i].penalty[kind], parts, lone ? kTiles[i].lone[kind] : 0.0);
+    const double c = tile_cost(M, N_tiled, kTiles[i].bm, kTiles[i].bn, kTiles[i].penalty[kind], parts, lone ? kTiles[i].lone[kind] : 0.0);
     if (best < 0 || c < best_cost) {
       best = i;
       best_cost = c;
@@ -471,8 +467,9 @@ hipError_t launch_best(const GemmParams &p, hipStream_t stream, bool *carry) {
   constexpr int kind = layout_kind(kAK, kBK);
   const int parts = p.k_parts > 1 ? p.k_parts : 1;  // parts of the reduction run as further tiles of the same launch
   if (fast_path(p.K, p.k_split, p.n_split) && fits_offsets(p)) {
+    const bool few = p.M <= kShardReadMaxTokens;  // (of those the launches over shards keep the tiles that they were measured with)
     int best = best_tile(p.M, p.N, p.K, p.n_split, kind, nullptr, parts,
-                         kAccIn ? TileUse::kSumLaunch : p.seg_n ? TileUse::kFirstShapes : TileUse::kLaunch);
+                         kAccIn ? TileUse::kSumLaunch : p.seg_n && few ? TileUse::kFirstShapes : TileUse::kLaunch, few ? 0 : p.seg_n);
     const int forced = debug_options().tile.load(std::memory_order_relaxed);  // testing: tile 0..3 where it fits the segments of B
     bool force = forced >= 0 && forced <= 3;
     if (force && p.n_split % kTiles[forced].bn == 0) best = forced;
@@ -542,6 +539,8 @@ GemmParams column_range(const GemmParams &p, int n0, int n1) {
   if (kEpi == static_cast<int>(Epilogue::kBf16ShardMajor)) s.c0 = p.c0 + n0;
   else if (kEpi == static_cast<int>(Epilogue::kF32Workspace)) s.C = static_cast<float *>(p.C) + n0;
   else s.C = static_cast<uint16_t *>(p.C) + n0;
+  if (p.seg_k)  // (the same columns of every shard)
+    for (void *&shard : s.shards.p) shard = shard ? static_cast<uint16_t *>(shard) + n0 : nullptr;
   if (kEpi == static_cast<int>(Epilogue::kBf16Fused)) s.fused = fused_from(p.fused, 0, n0);
   if (p.acc_in) s.acc_in = p.acc_in + n0;
   return s;
@@ -571,22 +570,23 @@ GemmParams row_range(const GemmParams &p, int m0, int m1) {
 // here: 10241 x 3136 over K = 512 224 / 199, 6131 x 3008 over 3264 385 / 363, 5652 x 2944 over 1024 184 / 170).  The shapes that both
 // kinds of launches run keep their prices as lone tiles, although best_tile picks those launches without: with both alike 60
 // dX passes are as fast within 0.4 %, and 39 forward passes 3 % slower, some by 15.
-double plan_launches(int M, int N, int K, int kind, bool acc_in, int *axis, int *cut) {
+// seg_n: as in best_tile; such a launch is cut by rows only.
+double plan_launches(int M, int N, int K, int kind, bool acc_in, int *axis, int *cut, int seg_n = 0) {
   const TileUse use = acc_in ? TileUse::kSumPlan : TileUse::kLaunch;
   double whole = 0.0;
   *axis = -1;
   *cut = 0;
-  best_tile(M, N, K, 0, kind, &whole, 1, use);
+  best_tile(M, N, K, 0, kind, &whole, 1, use, seg_n);
   // testing: split_launch = 0 keeps every problem in one launch, as does a forced tile shape
   if (debug_options().split_launch.load(std::memory_order_relaxed) == 0 ||
       debug_options().tile.load(std::memory_order_relaxed) >= 0)
     return whole;
-  const int tm = (M + 255) / 256, tn = (N + 255) / 256;
+  const int tm = (M + 255) / 256, tn = seg_n ? N / seg_n * ((seg_n + 255) / 256) : (N + 255) / 256;
   const double between = 1.0e7 / K;  // about 5 us from one launch to the next, in the cost's units of tile area
   double best = 0.95 * whole;        // only for a clear gain
   double rest = 0.0;
   // candidate cuts: for every number of rounds r, the most tile columns (rows) that r rounds of large tiles hold
-  for (int r = 1; r <= 16; ++r) {
+  for (int r = 1; r <= 16 && !seg_n; ++r) {
     const int cn = static_cast<int>(static_cast<long>(kCUs) * r / tm);
     if (cn <= 0) continue;
     if (cn >= tn) break;
@@ -598,8 +598,8 @@ double plan_launches(int M, int N, int K, int kind, bool acc_in, int *axis, int 
     const int cm = static_cast<int>(static_cast<long>(kCUs) * r / tn);
     if (cm <= 0) continue;
     if (cm >= tm) break;
-    best_tile(M - cm * 256, N, K, 0, kind, &rest, 1, use);
-    const double c = tile_cost(cm * 256, N, 256, 256, 1.0) + rest + between;
+    best_tile(M - cm * 256, N, K, 0, kind, &rest, 1, use, seg_n);
+    const double c = tile_cost(cm * 256, tn * 256, 256, 256, 1.0) + rest + between;
     if (c < best) { best = c; *axis = 0; *cut = cm * 256; }
   }
   return *axis >= 0 ? best : whole;
@@ -636,9 +636,10 @@ hipError_t launch_planned(const GemmParams &p, hipStream_t stream, bool *carry, 
       return e != hipSuccess ? e : launch_combine<kEpi>(p, parts, planes, stream);
     }
   }
-  if (!p.k_split && !p.n_split && !p.seg_k && !p.seg_n && fast_path(p.K, 0, 0) && fits_offsets(p)) {
+  const bool planned = !(p.seg_k || p.seg_n) || p.M > kShardReadMaxTokens;
+  if (!p.k_split && !p.n_split && planned && fast_path(p.K, 0, 0) && fits_offsets(p)) {
     int axis, cut;
-    plan_launches(p.M, p.N, p.K, layout_kind(kAK, kBK), kAccIn, &axis, &cut);
+    plan_launches(p.M, p.N, p.K, layout_kind(kAK, kBK), kAccIn, &axis, &cut, p.seg_n);
     if (axis == 1) {
       hipError_t e = launch_best<kAK, kBK, kEpi, kAccIn>(column_range<kBK, kEpi>(p, 0, cut), stream, carry);
       if (e != hipSuccess) return e;

@@ -336,10 +336,8 @@ __device__ __forceinline__ void gemm_w4_tile(const GemmParams &p, int tiles_m, i
   asm volatile("s_nop 15");
   asm volatile("s_nop 15");
   if constexpr (kEpi == static_cast<int>(Epilogue::kBf16Fused)) {
-    __builtin_amdgcn_s_barrier();  // no wave needs what it reads from the slots any more
-    asm volatile("" ::: "memory");
     store_fused<MB, NB>(p, [&](auto bm, auto bn) { return acc_read(acc[decltype(bm)::value][decltype(bn)::value]); }, m0 + wm,
-                        n0 + wn, n_end, l16, q4, reinterpret_cast<float *>(smem) + wave * (fused_scratch_bytes(NB) / 4));
+                        n0 + wn, n_end, l16, q4);
   } else {
     store_tile<MB, NB, kEpi>(p, [&](auto bm, auto bn) { return acc_value<kEpi>(acc[decltype(bm)::value][decltype(bn)::value]); },
                              m0 + wm, n0 + wn, n_end, plane_row, l16, q4, s_tab);

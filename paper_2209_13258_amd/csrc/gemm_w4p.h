@@ -188,10 +188,9 @@ __device__ __forceinline__ void gemm_w4p_tiles(const GemmParams &p, int tiles_m,
       asm volatile("" : "+v"(l16e), "+v"(q4e));
       // (a block or two at a time, a scheduling fence after each: read all at once, the 256 values would push the K
       // loop's fragments out of their registers)
-      if constexpr (kEpi == static_cast<int>(Epilogue::kBf16Fused)) {  // (its LDS lies behind the slots, which hold the next tile's blocks)
+      if constexpr (kEpi == static_cast<int>(Epilogue::kBf16Fused)) {
         store_fused<MB, NB>(p, [&](auto bm, auto bn) { return acc_read(acc[decltype(bm)::value][decltype(bn)::value]); }, m0c + wm,
-                            n0c + wn, n_endc, l16e, q4e,
-                            reinterpret_cast<float *>(smem + 2 * kSlotElems) + wave * (fused_scratch_bytes(NB) / 4));
+                            n0c + wn, n_endc, l16e, q4e);
       } else {
         store_tile<MB, NB, kEpi>(p, [&](auto bm, auto bn) { return acc_value<kEpi>(acc[decltype(bm)::value][decltype(bn)::value]); },
                                  m0c + wm, n0c + wn, n_endc, plane_row, l16e, q4e, s_tab);

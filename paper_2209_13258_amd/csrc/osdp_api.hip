@@ -857,6 +857,13 @@ bool switches_pay(const Resolved &r) {
   return 0.18 * r.N < copies;
 }
 
+// dX over the shards in place: its tiles do not reach over the end of a shard, which may cost more than the copies.
+bool shards_pay_dx(const Resolved &r) {
+  double copies = 0.0;
+  for (size_t j = 0; j < r.sub.size(); ++j) copies += gather_estimate_us(r.D * (r.sub[j].c1 - r.sub[j].c0));
+  return gemm_shards_dx_us(r.T, r.I, r.O, r.layout.rows_per_shard) <= gemm_planned_us(r.T, r.I, r.O, true, false) + copies;
+}
+
 osdp_status check_replicas(const Resolved &r, const Replicas &rep, bool need_dw) {
   if (!r.any_dp) return OSDP_OK;
   if (!rep.w) return fail(OSDP_ERR_INVALID_ARG, "w_dp is NULL but the plan has slices in DP mode");
@@ -1030,7 +1037,8 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
                    }));
     return OSDP_OK;
   }
-  const bool in_place = one_chain(r, true) && gemm_reads_shards(r.T, ldx, r.layout) && switches_pay(r);
+  const bool in_place = ep ? !r.any_dp && gemm_reads_shards(r.T, ldx, r.layout, true) && switches_pay(r)
+                           : one_chain(r, true) && gemm_reads_shards(r.T, ldx, r.layout) && switches_pay(r);
   if (in_place && !r.any_dp) {
     GemmProblem g = shard_gemm(r, true, tab, X, ldx, Y, ldy);
     fuse(&g, ep, 0);
@@ -1301,7 +1309,8 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
   }
   // Few tokens: nothing is staged (see forward()), and dW is one launch per destination.
   const bool skinny = skinny_takes(true, r.T, lddy, r.layout, r.I);
-  const bool in_place = !skinny && one_chain(r, false) && gemm_reads_shards(r.T, lddy, r.layout);
+  const bool in_place = !skinny && (slope ? !r.any_dp && gemm_reads_shards(r.T, lddy, r.layout, true) && shards_pay_dx(r)
+                                          : one_chain(r, false) && gemm_reads_shards(r.T, lddy, r.layout));
   std::vector<Slice> runs;
   if (in_place && r.any_dp && r.T <= kSkinnyMaxTokens) runs = runs_in_place(r, false);
   if (skinny || (in_place && (!r.any_dp || !runs.empty()))) {

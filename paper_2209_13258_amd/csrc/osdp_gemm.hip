@@ -18,12 +18,12 @@ namespace {
 bool shards_are_k_blocks(const ShardLayout &lay) { return lay.rows_per_shard > 0 && lay.rows_per_shard % 64 == 0; }
 }  // namespace
 
-bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay) {
+bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay, bool any_tokens) {
   const DebugOptions &d = debug_options();
   const bool forced = d.gemm_generic.load(std::memory_order_relaxed) != 0 || d.tile.load(std::memory_order_relaxed) >= 0 ||
                       d.fwd_pair.load(std::memory_order_relaxed) >= 0 || d.fused_gather.load(std::memory_order_relaxed) >= 0 ||
                       d.poison_staging.load(std::memory_order_relaxed) != 0;  // (these ask for the staged schedule)
-  return !forced && T <= kShardReadMaxTokens && shards_are_k_blocks(lay) && ld_act < kMaxLd && lay.O < kMaxLd;
+  return !forced && (any_tokens || T <= kShardReadMaxTokens) && shards_are_k_blocks(lay) && ld_act < kMaxLd && lay.O < kMaxLd;
 }
 
 int gemm_forward_parts(int64_t M, int64_t K) { return forward_k_parts(M, K); }
@@ -66,6 +66,12 @@ double gemm_planned_us(int64_t M, int64_t N, int64_t K, bool dx, bool acc_in) {
 namespace {
 thread_local int64_t t_persistent_launches = 0;
 }  // namespace
+double gemm_shards_dx_us(int64_t M, int64_t N, int64_t K, int64_t shard_rows) {
+  int axis, cut;
+  const double cost = plan_launches(static_cast<int>(M), static_cast<int>(N), static_cast<int>(K), 2, false, &axis, &cut, static_cast<int>(shard_rows));
+  return cost * 2.0 * static_cast<double>(K) / 5.0e6 + 6.0;
+}
+
 int64_t gemm_persistent_launches() { return t_persistent_launches; }
 void gemm_count_persistent_launch() { t_persistent_launches += 1; }
 

@@ -18,6 +18,10 @@ __device__ __forceinline__ uint4 load_global16(const void *p) {
   const osdp_u32x4 v = *(const __attribute__((address_space(1))) osdp_u32x4 *)(p);
   return uint4{v[0], v[1], v[2], v[3]};
 }
+__device__ __forceinline__ uint2 load_global8(const void *p) {
+  const osdp_u32x2 v = *(const __attribute__((address_space(1))) osdp_u32x2 *)(p);
+  return uint2{v[0], v[1]};
+}
 __device__ __forceinline__ void store_global16(void *p, uint4 v) {
   *(__attribute__((address_space(1))) osdp_u32x4 *)(p) = osdp_u32x4{v.x, v.y, v.z, v.w};
 }
@@ -184,7 +188,8 @@ hipError_t launch_slope(const SlopeProblem &q, void *workspace, hipStream_t stre
 // (256 to 512 tokens, 1024 to 16384 features, 8 to 64 shards, k = 1 and 4: 1.05 to 2.5 times as fast as staged, but for
 // unsplit forwards over shards of 64 rows, see switches_pay; more than 512 tokens have not been timed in place.)
 constexpr int64_t kShardReadMaxTokens = 512;
-bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay);
+// any_tokens: the number of tokens does not count (calls with an epilogue, see reads_in_place in osdp_api.hip).
+bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay, bool any_tokens = false);
 
 // Number of parts of the reduction that a concatenating product of M x K is the sum of (1: one chain).
 int gemm_forward_parts(int64_t M, int64_t K);
@@ -205,6 +210,9 @@ double gemm_estimate_us(int64_t M, int64_t N, int64_t K, bool forward_parts = fa
 // The same for a forward or (dx) dX product of one segment as launch_gemm runs it, whole rounds and a remainder as two
 // launches where that is faster.
 double gemm_planned_us(int64_t M, int64_t N, int64_t K, bool dx, bool acc_in);
+
+// Of dX as one product over shards of this many rows, which its tiles do not reach over.
+double gemm_shards_dx_us(int64_t M, int64_t N, int64_t K, int64_t shard_rows);
 
 // Launches of the calling thread that ran as the persistent four-wave kernel so far (for the profile).
 int64_t gemm_persistent_launches();
