@@ -857,11 +857,20 @@ bool switches_pay(const Resolved &r) {
   return 0.18 * r.N < copies;
 }
 
-// dX over the shards in place: its tiles do not reach over the end of a shard, which may cost more than the copies.
+// dX over the shards in place: its tiles do not reach over the end of a shard, which may cost more than the copies, and the trips
+// of a sum through memory (see recut), that it saves.  us in place / staged: 16384 tokens 2560 -> 10240 over 8 shards (320 rows,
+// two tiles of 160), k = 4 XX / 907; unsplit, staged in one piece, XX.
 bool shards_pay_dx(const Resolved &r) {
-  double copies = 0.0;
-  for (size_t j = 0; j < r.sub.size(); ++j) copies += gather_estimate_us(r.D * (r.sub[j].c1 - r.sub[j].c0));
-  return gemm_shards_dx_us(r.T, r.I, r.O, r.layout.rows_per_shard) <= gemm_planned_us(r.T, r.I, r.O, true, false) + copies;
+  double staged = 0.0;
+  for (size_t j = 0; j < r.sub.size(); ++j) staged += gather_estimate_us(r.D * (r.sub[j].c1 - r.sub[j].c0));
+  bool first = true;
+  for (const Slice &l : r.pass) {
+    const int64_t span = r.sub[l.c1 - 1].c1 - r.sub[l.c0].c0;
+    staged += r.rows ? gemm_planned_us(r.T, span, r.D, true, false) : gemm_planned_us(r.T, r.D, span, true, !first);
+    if (!r.rows && !first) staged += 8.0 * static_cast<double>(r.T) * static_cast<double>(r.D) / 4.5e6;
+    first = false;
+  }
+  return gemm_shards_dx_us(r.T, r.I, r.O, r.layout.rows_per_shard) <= staged;
 }
 
 osdp_status check_replicas(const Resolved &r, const Replicas &rep, bool need_dw) {

@@ -150,12 +150,16 @@ struct SlopeGrid {
   int parts;      // of rows
   int rows;       // in a part
 };
+// Narrow blocks of many row groups: the sums of a block's rows meet in LDS, so that few planes are left to add up, and small
+// problems spread over the CUs.  Up to 256 rows a block takes them all, in 128-byte pieces, and there is no second launch; beyond,
+// 256-byte pieces, 4 rows to a lane at least, some 4096 workgroups.
 SlopeGrid slope_grid(int64_t T, int64_t O) {
   SlopeGrid g{};
-  while (g.lanes_log2 < 6 && (int64_t{8} << g.lanes_log2) < O) ++g.lanes_log2;
+  const int most = T <= 256 ? 3 : 4;
+  while (g.lanes_log2 < most && (int64_t{8} << g.lanes_log2) < O) ++g.lanes_log2;
   const int64_t columns = int64_t{8} << g.lanes_log2;
-  const int64_t blocks = (O + columns - 1) / columns, least = 16 * (256 >> g.lanes_log2);  // (16 rows to a lane at least)
-  const int64_t wanted = std::max<int64_t>(1, 2048 / blocks), possible = std::max<int64_t>(1, (T + least - 1) / least);
+  const int64_t blocks = (O + columns - 1) / columns, least = (T <= 256 ? 8 : 4) * (256 >> g.lanes_log2);
+  const int64_t wanted = std::max<int64_t>(1, 4096 / blocks), possible = std::max<int64_t>(1, (T + least - 1) / least);
   const int64_t parts = std::min<int64_t>({wanted, possible, 1024});
   g.blocks = static_cast<int>(blocks);
   g.rows = static_cast<int>(std::max<int64_t>(1, (T + parts - 1) / parts));
