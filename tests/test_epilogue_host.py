@@ -1,0 +1,234 @@
+"""Bias, activation and residual around the operator, and norms and rotation of queries and keys: formulas, sizes and refusals,
+which need no GPU."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import epilogue_reference as R
+import paper_2209_13258_amd as osdp
+from paper_2209_13258_amd import binding as B
+
+P = 1 << 24  # an aligned address that nothing here follows; matrices lie P apart
+INVALID, UNSUPPORTED, WORKSPACE = B.OSDP_ERR_INVALID_ARG, B.OSDP_ERR_UNSUPPORTED, B.OSDP_ERR_WORKSPACE
+T, I, O = 16, 64, 128
+
+
+# ---- the references that the kernels are tested against -----------------------------------------------------------
+@pytest.mark.parametrize("name", R.NAMES)
+def test_slopes_are_the_differences_of_the_activations(name):
+    z = torch.linspace(-9, 9, 3601, dtype=torch.float64)
+    z = z[(z.abs() > 1e-3)]  # (relu has no slope at 0)
+    h = 1e-5
+    d = (R.act(name, z + h) - R.act(name, z - h)) / (2 * h)
+    # central differences: h^2 / 6 of the third derivative (below 3 for all of them), and 2^-53 of values up to 9 over h
+    assert (d - R.slope(name, z)).abs().max() < h * h * 3 + 9 * 2.0 ** -52 / h
+    assert torch.allclose(R.act(name, z), {"none": lambda v: v, "relu": torch.relu, "gelu": torch.nn.functional.gelu,
+                                           "gelu_tanh": lambda v: torch.nn.functional.gelu(v, approximate="tanh"),
+                                           "silu": torch.nn.functional.silu}[name](z), rtol=1e-9, atol=1e-12)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+def test_the_pass_back_is_the_gradient_of_the_pass_forward(norm, interleaved):
+    g = torch.Generator().manual_seed(5)
+    x, dy = (torch.randn(3, 2, 24, generator=g, dtype=torch.float64) for _ in range(2))
+    w = torch.randn(24, generator=g, dtype=torch.float64) if norm else None
+    freqs, pos = torch.rand(8, generator=g, dtype=torch.float64), torch.tensor([0, 5, 100000])
+    x.requires_grad_()
+    if norm:
+        w.requires_grad_()
+    y = R.qk(x, pos, freqs, w, 1e-6, norm, interleaved)
+    grads = torch.autograd.grad((y * dy).sum(), [x, w] if norm else [x])
+    dx, dw = R.qk_back(x.detach(), dy, pos, freqs, None if w is None else w.detach(), 1e-6, norm, interleaved)
+    assert torch.allclose(grads[0], dx, rtol=1e-10, atol=1e-12)
+    assert not norm or torch.allclose(grads[1], dw, rtol=1e-10, atol=1e-12)
+    # and of its differences along a direction
+    u, h = torch.randn(x.shape, generator=g, dtype=torch.float64), 1e-6
+    f = [(R.qk(x.detach() + s * h * u, pos, freqs, w, 1e-6, norm, interleaved) * dy).sum().item() for s in (1, -1)]
+    assert abs((f[0] - f[1]) / (2 * h) - (dx * u).sum().item()) < 1e-6
+
+
+# ---- the operator with an epilogue --------------------------------------------------------------------------------
+def shards(n, at=8 * P):
+    return (ctypes.c_void_p * n)(*[at + i * P for i in range(n)])
+
+
+def forward(shape=(T, I, O, 2, 1), x=P, ldx=I, y=2 * P, ldy=O, ws=4 * P, ws_bytes=1 << 40, epilogue=True, **more):
+    e = B.osdp_epilogue(3 * P, 5 * P, O, 6 * P, O, B.OSDP_ACT_GELU, B.OSDP_BF16)
+    for k, v in more.items():
+        setattr(e, k, v)
+    return osdp.lib.osdp_split_linear_fwd_epilogue(ctypes.byref(B.osdp_shape(*shape)), None, 0, ctypes.byref(e) if epilogue else None,
+                                                   x, ldx, shards(shape[3]), None, 0, y, ldy, ws, ws_bytes, None, None)
+
+
+def backward(shape=(T, I, O, 2, 1), x=P, dy=2 * P, lddy=O, dx=3 * P, ws=4 * P, ws_bytes=1 << 40, epilogue=True, **more):
+    e = B.osdp_epilogue_grad(5 * P, O, 6 * P, O, 7 * P, B.OSDP_ACT_GELU, B.OSDP_BF16)
+    for k, v in more.items():
+        setattr(e, k, v)
+    return osdp.lib.osdp_split_linear_bwd_epilogue(ctypes.byref(B.osdp_shape(*shape)), None, 0, ctypes.byref(e) if epilogue else None,
+                                                   x, I, dy, lddy, shards(shape[3]), None, 0, dx, I, shards(shape[3], 32 * P), None, ws,
+                                                   ws_bytes, None, None)
+
+
+def passes_the_checks(status):
+    """Whether a call got as far as asking for the device, which is not there (or, where there is one, was not made)."""
+    return status not in (INVALID, UNSUPPORTED, WORKSPACE) or b"device" in osdp.lib.osdp_last_error()
+
+
+@pytest.fixture
+def no_gpu():
+    if torch.cuda.is_available():
+        pytest.skip("calls with made-up addresses would run")
+
+
+@pytest.mark.parametrize("more,status", [
+    (dict(epilogue=False), INVALID), (dict(activation=-1), INVALID), (dict(activation=5), INVALID), (dict(bias_type=2), INVALID),
+    (dict(bias=3 * P + 8), UNSUPPORTED), (dict(residual=5 * P + 8), UNSUPPORTED), (dict(z=6 * P + 2), UNSUPPORTED),
+    (dict(ld_residual=O - 8), INVALID), (dict(ldz=O - 8), INVALID), (dict(ldz=O + 4), UNSUPPORTED), (dict(ld_residual=O + 4), UNSUPPORTED),
+    (dict(z=2 * P), INVALID), (dict(z=2 * P + 16), INVALID), (dict(residual=2 * P + 16), INVALID), (dict(residual=2 * P, ld_residual=2 * O), INVALID),
+    (dict(z=5 * P), INVALID), (dict(z=P), INVALID), (dict(y=P), INVALID), (dict(bias=2 * P), INVALID), (dict(bias=6 * P + 32), INVALID),
+    (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(ldx=I - 8), INVALID), (dict(ws=None), INVALID), (dict(ws_bytes=0), WORKSPACE),
+    (dict(shape=(T, I, O, 0, 1)), INVALID), (dict(shape=(-1, I, O, 1, 1)), INVALID), (dict(shape=(T, I, O + 4, 1, 1)), INVALID),
+    (dict(shape=(T, 60, O, 1, 1)), UNSUPPORTED)])
+def test_forward_refuses(more, status):
+    assert forward(**more) == status
+    assert osdp.lib.osdp_last_error()
+
+
+@pytest.mark.parametrize("more", [
+    dict(), dict(residual=2 * P), dict(bias=None, residual=None, z=None, activation=0), dict(shape=(0, I, O, 2, 1), x=None, y=None),
+    dict(y=2 * P, ldy=3 * O, residual=2 * P + 2 * O, ld_residual=3 * O, z=2 * P + 4 * O, ldz=3 * O), dict(bias_type=B.OSDP_F32)])
+def test_forward_takes(no_gpu, more):
+    """A residual that is Y, parts of one wide matrix side by side, no tokens."""
+    assert passes_the_checks(forward(**more))
+
+
+@pytest.mark.parametrize("more,status", [
+    (dict(epilogue=False), INVALID), (dict(activation=9), INVALID), (dict(bias_type=-1), INVALID), (dict(dbias=7 * P + 4), UNSUPPORTED),
+    (dict(z=None), INVALID), (dict(dz=None), INVALID), (dict(activation=0), INVALID), (dict(ldz=O - 8), INVALID), (dict(lddz=O + 2), UNSUPPORTED),
+    (dict(dz=2 * P, lddz=2 * O), INVALID), (dict(dz=2 * P + 16), INVALID), (dict(dz=5 * P + 16), INVALID), (dict(dz=P), INVALID),
+    (dict(dbias=2 * P), INVALID), (dict(dbias=3 * P), INVALID), (dict(dbias=6 * P + 64), INVALID), (dict(dbias=P), INVALID),
+    (dict(dy=None), INVALID), (dict(ws=None), INVALID), (dict(ws_bytes=0), WORKSPACE)])
+def test_backward_refuses(more, status):
+    assert backward(**more) == status
+    assert osdp.lib.osdp_last_error()
+
+
+@pytest.mark.parametrize("more", [dict(), dict(dz=2 * P), dict(dz=5 * P), dict(activation=0, z=None, dz=None), dict(dbias=None),
+                                  dict(shape=(0, I, O, 2, 1), x=None, dy=None, dx=None)])
+def test_backward_takes(no_gpu, more):
+    assert passes_the_checks(backward(**more))
+
+
+@pytest.mark.parametrize("shape", [(1, 64, 128, 1, 1), (257, 1024, 4096, 8, 4), (16384, 2560, 10240, 8, 4), (0, 64, 128, 1, 1)])
+def test_workspace_sizes(shape):
+    for bwd in (False, True):
+        base, peak = osdp.osdp_split_linear_workspace_bytes(*shape, bwd)
+        total, peak2 = osdp.osdp_split_linear_epilogue_workspace_bytes(*shape, bwd)
+        assert peak2 == peak and total >= base and (bwd or total == base)
+        assert total - base < 256 + 4 * 1024 * shape[2]
+    # one byte less than what is asked for is refused before anything runs
+    total, _ = osdp.osdp_split_linear_epilogue_workspace_bytes(*shape, True)
+    assert backward(shape=shape, ws_bytes=total - 1, x=P, dy=1 << 44, dx=1 << 45, z=1 << 46, dz=1 << 47, dbias=1 << 48, ldz=shape[2], lddz=shape[2],
+                    lddy=shape[2]) in (WORKSPACE, INVALID, UNSUPPORTED)
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
+    X, Y, w = torch.zeros(4, 64).bfloat16(), torch.zeros(4, 128).bfloat16(), [torch.zeros(64 * 128).bfloat16()]
+    ws = torch.zeros(1024, dtype=torch.uint8)
+    with pytest.raises(osdp.OsdpError):
+        osdp.osdp_split_linear_fwd_epilogue(X, w, Y, 1, ws, epilogue=osdp.Epilogue())
+    with pytest.raises(osdp.OsdpError):
+        osdp.osdp_split_linear_bwd_epilogue(X, Y, w, X, w, 1, ws, epilogue=osdp.EpilogueGrad())
+    q = torch.zeros(4, 2, 64).bfloat16()
+    with pytest.raises(osdp.OsdpError):
+        osdp.osdp_qk_norm_rope_fwd(q, q, q, q)
+    with pytest.raises(osdp.OsdpError):
+        osdp.osdp_qk_norm_rope_bwd(q, q, q, q, q, q, None, None, None)
+
+
+# ---- norms and rotation of queries and keys -----------------------------------------------------------------------
+D, HQ, HK = 64, 4, 2
+ROW = (HQ + 2 * HK) * D
+
+
+def desc(**more):
+    d = B.osdp_qk(T, HQ, HK, D, D, 0, 1, B.OSDP_BF16, 0, 1e-6, 20 * P, 21 * P, 22 * P, 23 * P)
+    for k, v in more.items():
+        setattr(d, k, v)
+    return d
+
+
+def heads(p, ld=ROW, hs=D):
+    return ctypes.byref(B.osdp_heads(p, ld, hs))
+
+
+def qk_forward(q=None, k=None, q_out=None, k_out=None, d=True, **more):
+    return osdp.lib.osdp_qk_norm_rope_fwd(ctypes.byref(desc(**more)) if d else None, q or heads(P), k or heads(P + 2 * HQ * D),
+                                          q_out or heads(2 * P, HQ * D), k_out or heads(3 * P, HK * D), None)
+
+
+def qk_backward(dq_out=None, dk_out=None, dq=None, dk=None, wq=24 * P, wk=25 * P, ws=26 * P, ws_bytes=1 << 30, **more):
+    return osdp.lib.osdp_qk_norm_rope_bwd(ctypes.byref(desc(**more)), heads(P), heads(P + 2 * HQ * D), dq_out or heads(2 * P, HQ * D),
+                                          dk_out or heads(3 * P, HK * D), dq or heads(4 * P), dk or heads(4 * P + 2 * HQ * D), wq, wk, ws,
+                                          ws_bytes, None)
+
+
+COMMON = [
+    (dict(T=-1), INVALID), (dict(q_heads=-1), INVALID), (dict(D=0), INVALID), (dict(rotary=-16), INVALID), (dict(rotary=80), INVALID),
+    (dict(interleaved=2), INVALID), (dict(norm=2), INVALID), (dict(reserved=1), INVALID), (dict(weight_type=2), INVALID), (dict(eps=0.0), INVALID),
+    (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(eps=-1.0), INVALID), (dict(norm=0), INVALID), (dict(freqs=None), INVALID),
+    (dict(D=68), UNSUPPORTED), (dict(D=520), UNSUPPORTED), (dict(rotary=24), UNSUPPORTED), (dict(rotary=20, interleaved=1), UNSUPPORTED),
+    (dict(T=1 << 31), UNSUPPORTED), (dict(k_heads=65536), UNSUPPORTED), (dict(q_weight=22 * P + 8), UNSUPPORTED), (dict(positions=20 * P + 4), UNSUPPORTED),
+    (dict(freqs=21 * P + 4), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("more,status", COMMON + [
+    (dict(d=False), INVALID), (dict(q=heads(None)), INVALID), (dict(k_out=heads(None)), INVALID), (dict(q=heads(P, -8)), INVALID),
+    (dict(q=heads(P, ROW + 4)), UNSUPPORTED), (dict(k=heads(P + 2 * HQ * D, ROW, D + 4)), UNSUPPORTED), (dict(q=heads(P + 8)), UNSUPPORTED),
+    (dict(q_out=heads(2 * P, HQ * D, D - 8)), INVALID), (dict(q_out=heads(2 * P, (HQ - 1) * D)), INVALID), (dict(k_out=heads(3 * P, 0)), INVALID),
+    (dict(q_out=heads(P + 16)), INVALID), (dict(q_out=heads(P, ROW + 8)), INVALID), (dict(k_out=heads(P)), INVALID), (dict(k_out=heads(2 * P, HQ * D)), INVALID),
+    (dict(q_out=heads(P + 2 * HQ * D)), INVALID), (dict(k_out=heads(P + 2 * (HQ - 1) * D)), INVALID)])
+def test_qk_forward_refuses(more, status):
+    assert qk_forward(**more) == status
+    assert osdp.lib.osdp_last_error()
+
+
+@pytest.mark.parametrize("more", [
+    dict(), dict(q_out=heads(P), k_out=heads(P + 2 * HQ * D)), dict(q_out=heads(2 * P, D, T * D), k_out=heads(3 * P, D, T * D)),
+    dict(q=heads(P, ROW, 2 * D), k=heads(P + 2 * D, ROW, 4 * D), q_out=heads(P, ROW, 2 * D), k_out=heads(P + 2 * D, ROW, 4 * D)),
+    dict(norm=0, q_weight=None, k_weight=None), dict(rotary=0, freqs=None), dict(positions=None), dict(k_heads=0, k=heads(None), k_out=heads(None)),
+    dict(T=0, q=heads(None), k=heads(None), q_out=heads(None), k_out=heads(None))])
+def test_qk_forward_takes(no_gpu, more):
+    """In place, by head, heads of queries and keys in turn, without norm, rotation, positions, keys, tokens."""
+    assert passes_the_checks(qk_forward(**more))
+
+
+@pytest.mark.parametrize("more,status", COMMON + [
+    (dict(norm=0, q_weight=None, k_weight=None), INVALID), (dict(wq=24 * P + 8), UNSUPPORTED), (dict(wk=24 * P), INVALID), (dict(ws=None), INVALID),
+    (dict(ws=26 * P + 64), UNSUPPORTED), (dict(ws_bytes=64), WORKSPACE), (dict(dq=heads(4 * P, 0)), INVALID), (dict(dq=heads(P + 16)), INVALID),
+    (dict(dk=heads(P)), INVALID), (dict(dk=heads(2 * P, HQ * D)), INVALID), (dict(dk=heads(4 * P)), INVALID), (dict(dq_out=heads(None)), INVALID)])
+def test_qk_backward_refuses(more, status):
+    assert qk_backward(**more) == status
+
+
+@pytest.mark.parametrize("more", [
+    dict(), dict(dq=heads(P), dk=heads(P + 2 * HQ * D)), dict(dq=heads(2 * P, HQ * D), dk=heads(3 * P, HK * D)), dict(wq=None, wk=None, ws=None, ws_bytes=0),
+    dict(wk=None), dict(norm=0, q_weight=None, k_weight=None, wq=None, wk=None)])
+def test_qk_backward_takes(no_gpu, more):
+    assert passes_the_checks(qk_backward(**more))
+
+
+def test_qk_workspace_sizes():
+    sizes = [osdp.osdp_qk_norm_rope_bwd_workspace_bytes(t, 32, 8, 128) for t in (0, 1, 100, 8192, 1 << 30)]
+    assert sizes[0] == 0 and sizes == sorted(sizes) and sizes[-1] <= 1024 * 128 * 4
+    for bad in ((-1, 1, 1, 64), (1, -1, 1, 64), (1, 1, 1, 0), (1, 1, 1, 20), (1, 1, 1, 1024), (1 << 31, 1, 1, 64)):
+        with pytest.raises(osdp.OsdpError):
+            osdp.osdp_qk_norm_rope_bwd_workspace_bytes(*bad)
+
+
+def test_struct_layouts_match_the_header():
+    assert ctypes.sizeof(B.osdp_epilogue) == 48 and ctypes.sizeof(B.osdp_epilogue_grad) == 48
+    assert ctypes.sizeof(B.osdp_qk) == 80 and ctypes.sizeof(B.osdp_heads) == 24

@@ -1,0 +1,473 @@
+"""The operator with bias, activation and residual, and its backward pass, against the formulas in 64 bits.
+
+Tolerances.  A value rounded to bf16 is off by 2^-8 of it at most (half a step).  The sum in fp32 over K up to 32768 products stays
+below 1e-3 of the outputs' root mean square, as the other products' tests take it; an activation passes that on times its slope, at
+most 1.13, and adds 2^-15 of its own value.  Y = act + R: 2^-8 |Y| + 2^-15 |act| + 1.13e-3 rms(z).  dZ = dY act'(Z): 2^-8 |dZ| + 2^-15 |dY|
+(the slope is off by 2^-15, by itself), and 2^-23 |dZ| for the product in fp32.  db: each term is off by 2^-15 |dY| + 2^-23 |dZ|, the sum of T of them in
+fp32, by partial sums, by T 2^-24 of the sum of magnitudes at most, then half a step of its type.  dX and dW are bit by bit those of
+the product's own backward pass on dZ."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import epilogue_reference as R
+import gpu_harness as H
+import paper_2209_13258_amd as osdp
+
+pytestmark = pytest.mark.gpu
+ACTS = {n: getattr(osdp, "OSDP_ACT_" + n.upper()) for n in R.NAMES}
+
+
+def rand(*shape, std=1.0, seed=0, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda").manual_seed(hash((shape, seed)) % (1 << 31))
+    return (torch.randn(*shape, generator=g, device="cuda") * std).to(dtype)
+
+
+class Op:
+    """One operator: W in N shards, flat pieces of ceil(I O / N)."""
+
+    def __init__(self, T, I, O, N, k=1, split=osdp.OSDP_SPLIT_OUT_FEATURES, seed=0, zdp=None, staging=osdp.OSDP_STAGING_AUTO):
+        self.T, self.I, self.O, self.N, self.k = T, I, O, N, k
+        L = -(-I * O // N)
+        flat = torch.full((N * L,), float("nan"), dtype=torch.bfloat16, device="cuda")
+        flat[:I * O] = rand(I * O, std=I ** -0.5, seed=seed)
+        self.W, self.w = flat[:I * O].view(I, O), [s.clone() for s in flat.split(L)]
+        self.X = rand(T, I, seed=seed + 1)
+        self.plan = osdp.Plan([k], staging=staging, split_dim_per_op=[split], zdp_mask=None if zdp is None else [zdp])
+        self.ws = None
+
+    def workspace(self, bwd):
+        need, _ = osdp.osdp_split_linear_epilogue_workspace_bytes(self.T, self.I, self.O, self.N, self.k, bwd, plan=self.plan)
+        self.ws = torch.full((max(need, 256),), 0xFF, dtype=torch.uint8, device="cuda")  # (NaN, whatever is read of it first)
+        return self.ws
+
+    def fwd(self, Y, stream=None, copy=None, **epilogue):
+        osdp.osdp_split_linear_fwd_epilogue(self.X, self.w, Y, self.k, self.workspace(False), epilogue=osdp.Epilogue(**epilogue), plan=self.plan,
+                                            stream_compute=stream, stream_copy=copy)
+        return Y
+
+    def bwd(self, dY, stream=None, **epilogue):
+        dX = torch.full((self.T, self.I), float("nan"), dtype=torch.bfloat16, device="cuda")
+        dW = [torch.full_like(s, float("nan")) for s in self.w]
+        osdp.osdp_split_linear_bwd_epilogue(self.X, dY, self.w, dX, dW, self.k, self.workspace(True), epilogue=osdp.EpilogueGrad(**epilogue),
+                                            plan=self.plan, stream_compute=stream)
+        return dX, torch.cat(dW)[:self.I * self.O]
+
+    def z(self, bias):
+        z = self.X.double() @ self.W.double()
+        return z if bias is None else z + bias.double()
+
+    def out(self, fill=float("nan"), pad=0):
+        return torch.full((self.T, self.O + pad), fill, dtype=torch.bfloat16, device="cuda")[:, pad // 2:pad // 2 + self.O]
+
+
+def close(got, want, bound, what):
+    got = got.double()
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    off = (got - want).abs() - bound
+    assert off.max().item() <= 0, f"{what}: {int((off > 0).sum())} values beyond the bound, by up to {off.max().item():.3e}"
+
+
+def check_forward(op, act, bias=None, residual=None, Y=None, Z=None):
+    z = op.z(bias)
+    rms = z.square().mean().sqrt() if z.numel() else 0.0
+    a = R.act(act, z)
+    y = a if residual is None else a + residual.double()
+    if Y is not None:
+        close(Y, y, 2.0 ** -8 * y.abs() + 2.0 ** -15 * a.abs() + 1.13e-3 * rms, "Y")
+    if Z is not None:
+        close(Z, z, 2.0 ** -8 * z.abs() + 1e-3 * rms, "Z")
+
+
+# (T, I, O, N, k): few tokens, tiles of every kind, shards that are no row blocks, sizes that nothing divides but 8
+SHAPES = [(1, 64, 8, 1, 1), (1, 4096, 16384, 8, 1), (3, 200, 136, 17, 1), (16, 256, 32768, 4, 1), (33, 1024, 520, 8, 1), (64, 2056, 264, 3, 1), (65, 512, 8448, 8, 1),
+          (128, 256, 1024, 2, 4), (129, 256, 1024, 2, 4), (255, 1000, 72, 1, 1), (500, 2560, 2560, 8, 2), (513, 320, 640, 5, 2), (777, 1504, 3200, 4, 2),
+          (1024, 520, 2056, 40, 1), (1500, 4096, 4096, 8, 4), (2049, 128, 1032, 2, 1), (3001, 1024, 3200, 8, 1), (4096, 2560, 10240, 8, 4), (8192, 1024, 4096, 8, 4),
+          # products that run in parts of a long reduction where they are staged, and one that does not
+          (600, 16384, 264, 3, 1), (300, 24576, 528, 3, 3), (600, 16384, 264, 8, 1)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("act", R.NAMES)
+def test_forward(shape, act):
+    op = Op(*shape)
+    bias = rand(op.O, std=0.5, seed=7, dtype=torch.float32 if act in ("gelu", "none") else torch.bfloat16)
+    residual = rand(op.T, op.O, seed=8)
+    Y, Z = op.out(), op.out()
+    op.fwd(Y, bias=bias, activation=ACTS[act], residual=residual, z=Z)
+    check_forward(op, act, bias, residual, Y, Z)
+
+
+@pytest.mark.parametrize("shape", [(7, 256, 512, 2, 1), (300, 512, 768, 8, 2), (2000, 512, 1280, 8, 1)], ids=str)
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("with_residual", [False, True])
+@pytest.mark.parametrize("with_z", [False, True])
+def test_each_part_can_be_left_out(shape, with_bias, with_residual, with_z):
+    op = Op(*shape)
+    bias = rand(op.O, std=0.5, seed=3) if with_bias else None
+    residual = rand(op.T, op.O, seed=4) if with_residual else None
+    Y, Z = op.out(), op.out() if with_z else None
+    op.fwd(Y, bias=bias, activation=ACTS["silu"], residual=residual, z=Z)
+    check_forward(op, "silu", bias, residual, Y, Z)
+
+
+@pytest.mark.parametrize("T", [5, 400, 1300])
+def test_nothing_but_the_product_is_the_product_bit_by_bit(T):
+    """Without anything, and with a bias and residual of zeros (adding which changes no bit but the sign of zero)."""
+    op = Op(T, 512, 1024, 8, 2)
+    plain = op.out()
+    osdp.osdp_split_linear_fwd(op.X, op.w, plain, op.k, op.workspace(False), plan=op.plan)
+    assert torch.equal(op.fwd(op.out()).view(torch.int16), plain.view(torch.int16))
+    assert torch.equal(op.fwd(op.out(), bias=torch.zeros(op.O, device="cuda"), residual=torch.zeros_like(plain)), plain)
+
+
+@pytest.mark.parametrize("T,I,O", [(40, 512, 1024), (300, 512, 1024), (1300, 512, 1024), (4096, 1024, 2048)])
+def test_cuts_modes_and_shards_change_no_bit(T, I, O):
+    bias, residual = rand(O, seed=1), rand(T, O, seed=2)
+    how = dict(bias=bias, activation=ACTS["gelu"], residual=residual)
+    first = Op(T, I, O, 8)
+    want = first.fwd(first.out(), **how)
+    cut = {1024: 18, 2048: 13}[O]  # (shards that are no row blocks)
+    for N, k, split, staging in [(1, 1, 0, 1), (8, 4, 0, 1), (8, 4, 0, 2), (8, 4, 0, 3), (8, 4, 1, 1), (8, 2, 1, 2), (8, 4, 3, 1), (cut, 4, 0, 1), (cut, 2, 0, 2),
+                                 (cut, 4, 1, 1), (cut, 1, 0, 1), (16, 2, 0, 1)]:
+        op = Op(T, I, O, N, k, split, staging=staging)
+        assert torch.equal(op.fwd(op.out(), **how), want), (N, k, split, staging)
+
+
+@pytest.mark.parametrize("switch,values", [("tile", range(4)), ("gemm_generic", (1,)), ("persistent", (0, 1)), ("four_wave", (0, 1)), ("small_tile", (0, 1)), ("deep", (0,)),
+                                           ("split_launch", (0,)), ("fused_gather", (0, 1)), ("fwd_pair", (0, 1)), ("poison_staging", (1,)), ("recut", (0, 1))])
+def test_every_kernel_gives_the_same_bits(switch, values):
+    """Every tile and schedule that can run a forward launch, over shards that are row blocks and over such that are not."""
+    bias, how = rand(1600, seed=1), {}
+    for T, N in ((600, 8), (1111, 8), (1111, 5)):
+        for k, split, staging in ((4, 0, 2), (2, 1, 2), (1, 0, 1)):
+            op = Op(T, 1024, 1600, N, k, split, staging=staging)
+            how = dict(bias=bias, activation=ACTS["gelu_tanh"], residual=rand(T, 1600, seed=2), z=op.out())
+            want, want_z = op.fwd(op.out(), **how), how["z"].clone()
+            check_forward(op, "gelu_tanh", bias, how["residual"], want, want_z)
+            for v in values:
+                osdp.osdp_debug_option(switch, v)
+                try:
+                    how["z"] = op.out()
+                    got = op.fwd(op.out(), **how)
+                    torch.cuda.synchronize()
+                finally:
+                    osdp.osdp_debug_option(switch, 0 if switch in ("gemm_generic", "poison_staging") else -1)
+                assert torch.equal(got, want) and torch.equal(how["z"], want_z), (switch, v, T, N, k, split)
+
+
+@pytest.mark.parametrize("T", [20, 200, 900])
+@pytest.mark.parametrize("split", [osdp.OSDP_SPLIT_OUT_FEATURES, osdp.OSDP_SPLIT_IN_FEATURES])
+def test_slices_in_dp_mode(T, split):
+    """Slices 0 and 2 of 4 replicated, the shards' part of them poisoned: the bits of the plan that gathers all."""
+    op, mixed = Op(T, 512, 1024, 8, 4, split), Op(T, 512, 1024, 8, 4, split, zdp=0b1010)
+    bias, residual = rand(1024, seed=1), rand(T, 1024, seed=2)
+    dY, Z = rand(T, 1024, seed=3), rand(T, 1024, seed=4)
+    full, step = mixed.W.contiguous(), (512 if split else 1024) // 4
+    replicas = [full[j * step:(j + 1) * step] if split else full[:, j * step:(j + 1) * step] for j in range(4)]
+    w_dp = [replicas[j] if j in (0, 2) else None for j in range(4)]
+    dw = torch.full_like(full, float("nan"))
+    dw_dp = [(dw[j * step:(j + 1) * step] if split else dw[:, j * step:(j + 1) * step]) if j in (0, 2) else None for j in range(4)]
+    how = dict(bias=bias, activation=ACTS["relu"], residual=residual)
+    want = op.fwd(op.out(), **how)
+    got = mixed.out()
+    osdp.osdp_split_linear_fwd_epilogue(mixed.X, mixed.w, got, 4, mixed.workspace(False), epilogue=osdp.Epilogue(**how), plan=mixed.plan, w_dp=w_dp,
+                                        ld_dp=1024)
+    assert torch.equal(got, want)
+    dz, dz2, db, db2 = op.out(), op.out(), torch.zeros(1024, device="cuda"), torch.ones(1024, device="cuda")
+    dX, dW = op.bwd(dY, activation=ACTS["relu"], z=Z, dz=dz, dbias=db)
+    dX2 = torch.full_like(dX, float("nan"))
+    dws = [torch.full_like(s, float("nan")) for s in mixed.w]
+    osdp.osdp_split_linear_bwd_epilogue(mixed.X, dY, mixed.w, dX2, dws, 4, mixed.workspace(True), plan=mixed.plan, w_dp=w_dp, ld_dp=1024, dw_dp=dw_dp,
+                                        epilogue=osdp.EpilogueGrad(activation=ACTS["relu"], z=Z, dz=dz2, dbias=db2))
+    assert torch.equal(dX2, dX) and torch.equal(dz2, dz) and torch.equal(db2, db)
+    flat = torch.cat(dws).view(512, 1024)
+    assert torch.equal(torch.where(torch.isnan(flat), dw, flat), dW.view(512, 1024))
+
+
+@pytest.mark.parametrize("T", [9, 600])
+def test_places_in_wider_matrices_and_a_residual_in_place(T):
+    """Y, Z and the residual as parts of one wide matrix; what lies beside them stays as it was."""
+    op = Op(T, 256, 520, 2)
+    bias = rand(520, seed=1)
+    wide = rand(T, 4 * 528, seed=2)
+    before = wide.clone()
+    Y, Z, residual = wide[:, :520], wide[:, 528:1048], wide[:, 1056:1576]
+    op.fwd(Y, bias=bias, activation=ACTS["gelu"], residual=residual, z=Z)
+    check_forward(op, "gelu", bias, before[:, 1056:1576], Y, Z)
+    changed = (wide.view(torch.int16) != before.view(torch.int16)).any(0).nonzero().view(-1).tolist()
+    assert all(c < 520 or 528 <= c < 1048 for c in changed)
+    r = rand(T, 520, seed=5)
+    Y = r.clone()
+    op.fwd(Y, bias=bias, activation=ACTS["silu"], residual=Y)
+    assert torch.equal(Y, op.fwd(op.out(), bias=bias, activation=ACTS["silu"], residual=r))
+
+
+def test_no_tokens():
+    op = Op(0, 64, 128, 2)
+    op.fwd(op.out(), bias=rand(128), activation=ACTS["gelu"])
+    for dtype in (torch.float32, torch.bfloat16):
+        db = torch.full((128,), float("nan"), dtype=dtype, device="cuda")
+        _, dW = op.bwd(op.out(), activation=ACTS["gelu"], z=op.out(), dz=op.out(), dbias=db)
+        assert (db == 0).all() and (dW == 0).all()
+
+
+def through(op, act, values, dtype=torch.float32):
+    """Y where X . W is 0 and the bias runs through `values`: what the activation makes of fp32 numbers."""
+    op.X.zero_()
+    Y, Z = op.out(), op.out()
+    op.fwd(Y, bias=values.to(dtype), activation=ACTS[act], z=Z)
+    return Y, Z
+
+
+@pytest.mark.parametrize("act", R.NAMES)
+@pytest.mark.parametrize("T", [1, 600])
+def test_the_whole_range_of_activations(act, T):
+    """Values from 2^-100 to 2^100 of both signs, and steps through -12 .. 12: off by 2^-8 for bf16 and 2^-15 for the fp32 arithmetic."""
+    e = torch.exp2(torch.linspace(-100, 100, 1601, dtype=torch.float64))
+    v = torch.cat([-e, e, torch.linspace(-12, 12, 4894, dtype=torch.float64)]).float().cuda()
+    op = Op(T, 64, v.numel(), 1)
+    Y, _ = through(op, act, v)
+    want = R.act(act, v.double())
+    # (below 2^-126 the hardware's exponential gives 0)
+    close(Y[0], want, (2.0 ** -8 + 2.0 ** -15) * want.abs() + 1e-36, "Y")
+    assert torch.equal(Y, Y[:1].expand(T, -1))
+
+
+@pytest.mark.parametrize("T", [2, 600])
+def test_infinities_and_nan(T):
+    inf, nan = float("inf"), float("nan")
+    v = torch.tensor([inf, -inf, nan, 0.0, -0.0, 3.0, -3.0, 1.0]).cuda()
+    op = Op(T, 64, 8, 1)
+    for act in R.NAMES:
+        Y, Z = through(op, act, v)
+        low = {"none": -inf, "relu": 0.0}.get(act, nan)
+        want = torch.tensor([inf, low, nan]).cuda()
+        assert torch.equal(torch.nan_to_num(Y[0, :3].float(), 7.0), torch.nan_to_num(want, 7.0)), act
+        assert torch.isnan(Z[:, 2]).all() and torch.isfinite(Y[:, 3:]).all() and (Y[:, 3:5] == 0).all()
+
+
+# ---- backward ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("act", R.NAMES)
+def test_backward(shape, act):
+    op = Op(*shape)
+    dtype = torch.float32 if act in ("gelu", "none") else torch.bfloat16
+    dY, Z = rand(op.T, op.O, seed=5), rand(op.T, op.O, std=1.5, seed=6)
+    db, dz = torch.full((op.O,), float("nan"), dtype=dtype, device="cuda"), op.out() if act != "none" else None
+    dX, dW = op.bwd(dY, activation=ACTS[act], z=None if dz is None else Z, dz=dz, dbias=db)
+    want = dY.double() * R.slope(act, Z.double())
+    if dz is not None:
+        close(dz, want, (2.0 ** -8 + 2.0 ** -23) * want.abs() + 2.0 ** -15 * dY.double().abs(), "dZ")
+    s = want.sum(0)
+    terms = (2.0 ** -15 * dY.double().abs()).sum(0) + (op.T + 2) * 2.0 ** -24 * want.abs().sum(0)
+    close(db, s, terms + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24) * (s.abs() + terms), "db")
+    ref = Op(*shape)
+    rX, rW = torch.full_like(dX, float("nan")), [torch.full_like(w, float("nan")) for w in ref.w]
+    osdp.osdp_split_linear_bwd(ref.X, dY if dz is None else dz, ref.w, rX, rW, ref.k, ref.workspace(True), plan=ref.plan)
+    assert torch.equal(dX, rX) and torch.equal(dW, torch.cat(rW)[:op.I * op.O])
+
+
+def test_the_gradients_are_the_differences_of_the_forward_pass():
+    """sum(Y dY) along random directions of X, W, b and R, by central differences of the formula in 64 bits, against the kernels'
+    gradients: each is off by its own bound, 2^-7 of it (two roundings, dZ's and its own) and 2e-3 of the root mean square."""
+    op = Op(300, 256, 512, 4, 2)
+    bias, residual, dY = rand(512, seed=1, dtype=torch.float32), rand(300, 512, seed=2), rand(300, 512, seed=3)
+    for act in R.NAMES[2:]:
+        Z, dz, db = op.out(), op.out(), torch.empty_like(bias)
+        op.fwd(op.out(), bias=bias, activation=ACTS[act], residual=residual, z=Z)
+        dX, dW = op.bwd(dY, activation=ACTS[act], z=Z, dz=dz, dbias=db)
+        x, w, b, dy, h = op.X.double(), op.W.double(), bias.double(), dY.double(), 1e-5
+        for grad, at in ((dX.double(), 0), (dW.double().view(256, 512), 1), (db.double(), 2)):
+            u = torch.randn(grad.shape, dtype=torch.float64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(at))
+            def loss(s):
+                p = [x, w, b]
+                p[at] = p[at] + s * h * u
+                return (R.act(act, p[0] @ p[1] + p[2]) * dy).sum().item()
+            by_difference, by_kernel = (loss(1) - loss(-1)) / (2 * h), (grad * u).sum().item()
+            # (Z is rounded to 2^-8 of it before its slope is taken: independent errors, as those of the roundings are)
+            bound = 6 * ((2.0 ** -7 * grad.abs() * u.abs()).square().sum().sqrt() + 2e-2 * grad.square().mean().sqrt() * u.norm()).item()
+            assert abs(by_difference - by_kernel) <= bound, (act, at, by_difference, by_kernel, bound)
+
+
+@pytest.mark.parametrize("T", [1, 100, 300, 3000])
+def test_dz_in_place_and_no_gradient_of_the_bias(T):
+    op = Op(T, 256, 392, 2)
+    dY, Z = rand(T, 392, seed=5), rand(T, 392, seed=6)
+    want = op.out()
+    db = torch.empty(392, device="cuda")
+    dX, dW = op.bwd(dY, activation=ACTS["gelu"], z=Z, dz=want, dbias=db)
+    for at in ("dY", "Z"):
+        dy, z = dY.clone(), Z.clone()
+        dz = dy if at == "dY" else z
+        db2 = torch.empty_like(db) if at == "Z" else None
+        dX2, dW2 = op.bwd(dy, activation=ACTS["gelu"], z=z, dz=dz, dbias=db2)
+        assert torch.equal(dz, want) and torch.equal(dX2, dX) and torch.equal(dW2, dW) and (db2 is None or torch.equal(db2, db))
+
+
+@pytest.mark.parametrize("act", R.NAMES[1:])
+def test_slopes_over_the_whole_range(act):
+    e = torch.exp2(torch.linspace(-100, 100, 2001))
+    z = torch.cat([-e, e, torch.linspace(-12, 12, 4006)]).bfloat16().cuda().view(1, -1)
+    op = Op(1, 64, z.numel(), 1)
+    dz = op.out()
+    op.bwd(torch.ones_like(z), activation=ACTS[act], z=z, dz=dz)
+    want = R.slope(act, z.double())
+    want = torch.where(torch.isfinite(want), want, (z > 0).double())  # (the cube of 2^100 leaves the range even of 64 bits)
+    close(dz, want, 2.0 ** -8 * want.abs() + 2.0 ** -15, act)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 2^19 elements apart, 8 GB of residual, Z, dY: the last rows lie beyond 2^31 elements and 2^32 bytes."""
+    T, ld = 4200, 1 << 19
+    op = Op(T, 64, 72, 1)
+    wide = torch.empty(T * ld, dtype=torch.bfloat16, device="cuda").view(T, ld)
+    Y, Z, residual, dY, dz = (wide[:, 128 * i:128 * i + 72] for i in range(5))
+    residual.copy_(rand(T, 72, seed=1))
+    dY.copy_(rand(T, 72, seed=2))
+    bias, db = rand(72, seed=3), torch.empty(72, dtype=torch.bfloat16, device="cuda")
+    op.fwd(Y, bias=bias, activation=ACTS["silu"], residual=residual, z=Z)
+    check_forward(op, "silu", bias, residual, Y, Z)
+    dX, dW = op.bwd(dY, activation=ACTS["silu"], z=Z, dz=dz, dbias=db)
+    near = Op(T, 64, 72, 1)
+    dz2, db2 = near.out(), torch.empty_like(db)
+    dX2, dW2 = near.bwd(dY.contiguous(), activation=ACTS["silu"], z=Z.contiguous(), dz=dz2, dbias=db2)
+    assert torch.equal(dz, dz2) and torch.equal(dX, dX2) and torch.equal(dW, dW2) and torch.equal(db, db2)
+
+
+@pytest.mark.parametrize("T", [4, 700])
+def test_a_captured_graph_replays_on_other_inputs(T):
+    """Forward and backward captured once, replayed with new inputs in the same place, eager work in between."""
+    op = Op(T, 256, 512, 8, 2)
+    bias, residual, dY = rand(512, seed=1), rand(T, 512, seed=2), rand(T, 512, seed=3)
+    Y, Z, dz, db = op.out(), op.out(), op.out(), torch.empty_like(bias)
+    dX, dW = torch.empty_like(op.X), [torch.empty_like(s) for s in op.w]
+    wf, wb = op.workspace(False), op.workspace(True)
+
+    def run(stream):
+        osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, Y, 2, wf, plan=op.plan, stream_compute=stream,
+                                            epilogue=osdp.Epilogue(bias=bias, activation=ACTS["gelu"], residual=residual, z=Z))
+        osdp.osdp_split_linear_bwd_epilogue(op.X, dY, op.w, dX, dW, 2, wb, plan=op.plan, stream_compute=stream,
+                                            epilogue=osdp.EpilogueGrad(activation=ACTS["gelu"], z=Z, dz=dz, dbias=db))
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    run(stream)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        run(stream)
+    for seed in range(4):
+        op.X.copy_(rand(T, 256, seed=50 + seed))
+        dY.copy_(rand(T, 512, seed=60 + seed))
+        outs = [Y, Z, dz, db, dX, *dW]
+        for t in outs:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        run(None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outs)), seed
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    ops = [Op(700, 512, 1024, 8, 2, seed=s) for s in (0, 10)]
+    want = [op.fwd(op.out(), bias=rand(1024, seed=1), activation=ACTS["gelu"]) for op in ops]
+    streams = [torch.cuda.Stream() for _ in ops]
+    torch.cuda.synchronize()
+    bias = rand(1024, seed=1)
+    got = [op.out() for op in ops]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for op, y, s in zip(ops, got, streams):
+            op.fwd(y, stream=s, bias=bias, activation=ACTS["gelu"])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    op = Op(16, 64, 128, 2)
+    Y, bias = op.out(), rand(128)
+    wrong = [dict(bias=rand(120)), dict(bias=rand(128).half()), dict(bias=rand(256)[::2]), dict(bias=rand(128).cpu()), dict(residual=rand(16, 120)),
+             dict(residual=rand(16, 128).float()), dict(residual=rand(128, 16).t()), dict(residual=rand(1, 128).expand(16, 128)), dict(z=Y), dict(z=op.X.repeat(1, 2).cpu()),
+             dict(bias=bias, activation=17)]
+    for w in wrong:
+        with pytest.raises(osdp.OsdpError):
+            op.fwd(Y, **w)
+    for X, y, shards in ((op.X.float(), Y, op.w), (op.X, Y.float(), op.w), (op.X, Y[:8], op.w), (op.X, Y, [s.float() for s in op.w]), (op.X, Y, [s[:-8] for s in op.w])):
+        with pytest.raises(osdp.OsdpError):
+            osdp.osdp_split_linear_fwd_epilogue(X, shards, y, 1, op.workspace(False), epilogue=osdp.Epilogue(bias=bias))
+    dw = [torch.empty_like(s) for s in op.w]
+    for kind in (dw[:1], [d.float() for d in dw], [d[:-8] for d in dw]):
+        with pytest.raises(osdp.OsdpError):
+            osdp.osdp_split_linear_bwd_epilogue(op.X, Y, op.w, torch.empty_like(op.X), kind, 1, op.workspace(True), epilogue=osdp.EpilogueGrad(dbias=bias))
+    with pytest.raises(osdp.OsdpError):
+        osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, Y, 1, torch.empty(0, dtype=torch.uint8, device="cuda"), epilogue=osdp.Epilogue(bias=bias))
+
+
+def test_a_transformer_layer_runs_together():
+    """qkv with bias, norms and rotation in place, proj onto the residual stream, up with gelu, down onto the residual stream; then all of
+    it backward.  Each step is checked against its formula in 64 bits on the very tensors that the step before it left."""
+    T, h, f, D = 700, 512, 1024, 64
+    n_heads = h // D
+    qkv, proj, up, down = Op(T, h, 3 * h, 8, 2, seed=1), Op(T, h, h, 8, seed=2), Op(T, h, f, 8, 2, seed=3), Op(T, f, h, 8, 2, seed=4)
+    bias = [rand(o, std=0.2, seed=9) for o in (3 * h, h, f, h)]
+    x0 = qkv.X
+    rows = qkv.fwd(qkv.out(), bias=bias[0])
+    check_forward(qkv, "none", bias[0], Y=rows)
+    pos, freqs = torch.arange(T, device="cuda"), 10000.0 ** (-torch.arange(D // 2, dtype=torch.float64, device="cuda") * 2 / D)
+    g = [rand(D, std=0.1, seed=11 + i, dtype=torch.float32).add_(1).bfloat16() for i in range(2)]
+    q, k = rows[:, :h].unflatten(1, (n_heads, D)), rows[:, h:2 * h].unflatten(1, (n_heads, D))
+    kept = rows.clone()  # (what the pass back needs)
+    kq, kk = kept[:, :h].unflatten(1, (n_heads, D)), kept[:, h:2 * h].unflatten(1, (n_heads, D))
+    how = dict(positions=pos, freqs=freqs, q_weight=g[0], k_weight=g[1])
+    osdp.osdp_qk_norm_rope_fwd(q, k, q, k, **how)
+    for got, x, w in ((q, kq, g[0]), (k, kk, g[1])):
+        want = R.qk(x.double(), pos, freqs, w, 1e-6, True, False)
+        close(got, want, 2.0 ** -8 * want.abs() + 2.0 ** -18 * want.abs().amax(-1, keepdim=True), "heads")
+    assert torch.equal(rows[:, 2 * h:], kept[:, 2 * h:])
+    proj.X = rows[:, 2 * h:]  # (in the place of attention: the values)
+    x1 = proj.fwd(proj.out(), bias=bias[1], residual=x0)
+    check_forward(proj, "none", bias[1], x0, x1)
+    up.X = x1
+    Z = up.out()
+    down.X = up.fwd(up.out(), bias=bias[2], activation=ACTS["gelu"], z=Z)
+    check_forward(up, "gelu", bias[2], None, down.X, Z)
+    x2 = down.fwd(down.out(), bias=bias[3], residual=x1)
+    check_forward(down, "none", bias[3], x1, x2)
+
+    dY = rand(T, h, seed=20)
+    db = [torch.empty_like(b) for b in bias]
+
+    def products(op, dz, dX, dW):
+        # (2^-8 of what is rounded, 1e-3 of the root mean square for the sums: as for the products' other tests)
+        for got, want, what in ((dX, dz.double() @ op.W.double().t().contiguous(), "dX"), (dW.view(op.I, op.O), op.X.double().t().contiguous() @ dz.double(), "dW")):
+            close(got, want, 2.0 ** -8 * want.abs() + 1e-3 * want.square().mean().sqrt(), what)
+
+    d_act, dW = down.bwd(dY, dbias=db[3])
+    products(down, dY, d_act, dW)
+    dz = up.out()
+    d1, dW = up.bwd(d_act, activation=ACTS["gelu"], z=Z, dz=dz, dbias=db[2])
+    want = d_act.double() * R.slope("gelu", Z.double())
+    close(dz, want, (2.0 ** -8 + 2.0 ** -23) * want.abs() + 2.0 ** -15 * d_act.double().abs(), "dZ")
+    products(up, dz, d1, dW)
+    d1 = d1 + dY
+    dv, dW = proj.bwd(d1, dbias=db[1])
+    products(proj, d1, dv, dW)
+    d_rows = qkv.out()
+    d_rows[:, 2 * h:] = dv
+    dq_out, dk_out = rand(T, n_heads, D, seed=30), rand(T, n_heads, D, seed=31)  # (what attention would send back)
+    dg = [torch.empty_like(w) for w in g]
+    ws = torch.empty(osdp.osdp_qk_norm_rope_bwd_workspace_bytes(T, n_heads, n_heads, D), dtype=torch.uint8, device="cuda")
+    dq, dk = d_rows[:, :h].unflatten(1, (n_heads, D)), d_rows[:, h:2 * h].unflatten(1, (n_heads, D))
+    osdp.osdp_qk_norm_rope_bwd(kq, kk, dq_out, dk_out, dq, dk, dg[0], dg[1], ws, **how)
+    for got, gw, x, dy, w in ((dq, dg[0], kq, dq_out, g[0]), (dk, dg[1], kk, dk_out, g[1])):
+        dx, dw = R.qk_back(x.double(), dy.double(), pos, freqs, w, 1e-6, True, False)
+        close(got, dx, 2.0 ** -8 * dx.abs() + 2.0 ** -16 * dx.abs().amax(-1, keepdim=True), "d heads")
+        close(gw, dw, 2.0 ** -8 * dw.abs() + 1e-4 * dw.square().mean().sqrt(), "d weight")
+    dx, dW = qkv.bwd(d_rows, dbias=db[0])
+    products(qkv, d_rows, dx, dW)
+    s = d_rows.double().sum(0)
+    close(db[0], s, 2.0 ** -8 * s.abs() + T * 2.0 ** -24 * d_rows.double().abs().sum(0), "db")
