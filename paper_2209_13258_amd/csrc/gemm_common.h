@@ -64,7 +64,8 @@ struct GemmParams {
   // of an N-contiguous B (multiple of 64), or seg_n rows, which are columns of C, of a K-contiguous one.  0: not so.
   int32_t seg_k, seg_n;
   int32_t k_parts;     // > 1 (fp32 workspace epilogue with ldc = N, no second K segment): the grid is k_parts times the
-                       // tiles, part s takes k in [s K / k_parts, (s + 1) K / k_parts) and writes plane s of C ([M x N] fp32 each)
+                       // tiles, part s takes k in [s k_per, (s + 1) k_per), up to K, and writes plane s of C ([M x N] fp32 each)
+  int32_t k_per;       // length of a part, a multiple of 64
   void *C;
   int64_t ldc;
   const float *acc_in;

@@ -185,7 +185,7 @@ struct TileSource {
   int32_t n0, n_end, nb;        // the tile's columns (n_end: where those it may store end); its K blocks
   int32_t segment, segment_end; // B's K segment; the block where the next one begins
 
-  // Block 0 of the tile of rows m0 .. and tile column tn, reducing over k0 .. k0 + K (k0 > 0 only with one K segment).
+  // Block 0 of the tile of rows m0 .. and tile column tn, reducing over k0 .. k0 + K (k0 > 0 not with two staged K segments).
   __device__ __forceinline__ void begin(const GemmParams &p, int m0, int tn, int64_t k0, int K, int wave, int lane) {
     tile_columns<kBKc>(p, tn, BN, &n0, &n_end);
     nb = (K + kBK - 1) / kBK;
@@ -199,11 +199,21 @@ struct TileSource {
       base = static_cast<const uint16_t *>(p.shards.p[s]);
       nB = n0 - s * p.seg_n;
     }
-    if (!kBKc && p.seg_k) base = static_cast<const uint16_t *>(p.shards.p[0]);
+    segment = 0;
+    int64_t kB = k0;           // the first k inside the segment,
+    int to_end = p.seg_k;      // and how many there are from it on
+    if constexpr (kAK && !kBKc) {
+      if (p.seg_k) {
+        segment = __builtin_amdgcn_readfirstlane(static_cast<int>(k0) / p.seg_k);
+        base = static_cast<const uint16_t *>(p.shards.p[segment]);
+        kB = k0 - static_cast<int64_t>(segment) * p.seg_k;
+        to_end = __builtin_amdgcn_readfirstlane(p.seg_k - static_cast<int>(kB));
+      }
+    }
     a.begin(kAK ? p.A + static_cast<int64_t>(m0) * p.lda + k0 : p.A + m0 + k0 * p.lda, p.lda, p.M - m0, wave, lane);
-    b.begin(kBKc ? base + static_cast<int64_t>(nB) * ldb + k0 : base + nB + k0 * ldb, ldb, n_end - n0, wave, lane);
-    block = segment = 0;
-    segment_end = kAK && p.k_split ? p.k_split / kBK : (kAK && !kBKc && p.seg_k ? p.seg_k / kBK : 0x7fffffff);
+    b.begin(kBKc ? base + static_cast<int64_t>(nB) * ldb + k0 : base + nB + kB * ldb, ldb, n_end - n0, wave, lane);
+    block = 0;
+    segment_end = kAK && p.k_split ? p.k_split / kBK : (kAK && !kBKc && p.seg_k ? to_end / kBK : 0x7fffffff);
     due(p, K, wave, lane);
   }
   __device__ __forceinline__ void due(const GemmParams &p, int K, int wave, int lane) {
@@ -268,8 +278,9 @@ void gemm_dma_kernel(GemmParams p, int tiles_m, int tiles_n) {
   if (p.k_parts > 1) {
     const int tiles = tiles_m * tiles_n, part = __builtin_amdgcn_readfirstlane(pid / tiles);
     pid -= part * tiles;
-    K = __builtin_amdgcn_readfirstlane(p.K / p.k_parts);
-    k0 = static_cast<int64_t>(part) * K;
+    const int first = __builtin_amdgcn_readfirstlane(part * p.k_per);
+    K = __builtin_amdgcn_readfirstlane(p.k_per < p.K - first ? p.k_per : p.K - first);
+    k0 = first;
     plane_row = part * p.M;
   }
   tile_of_pid(pid, tiles_m, tiles_n, &tm, &tn);

@@ -82,8 +82,8 @@ __global__ __launch_bounds__(256) void gemm_generic_kernel(GemmParams p) {
   const int tiles = tiles_m * ((p.N + GBN - 1) / GBN);
   const int part = p.k_parts > 1 ? blockIdx.x / tiles : 0;
   const int bid = blockIdx.x - part * tiles;
-  const int k_len = p.k_parts > 1 ? p.K / p.k_parts : p.K;
-  const int k_begin = part * k_len, k_end = k_begin + k_len;
+  const int k_len = p.k_parts > 1 ? p.k_per : p.K;
+  const int k_begin = part * k_len, k_end = k_begin + k_len < p.K ? k_begin + k_len : p.K;
   const int plane_row = part * p.M;
   const int tm = bid % tiles_m, tn = bid / tiles_m;
   const int m0 = tm * GBM, n0 = tn * GBN;
@@ -450,7 +450,7 @@ hipError_t launch_four_wave(const GemmParams &p, hipStream_t stream, bool *carry
   // (3-12 % per launch).  It takes no gather along: *carry stays as it is and the caller launches the
   // gather by itself, which measured better on every workload than keeping the plain kernel for its sake.
   const int pst = debug_options().persistent.load(std::memory_order_relaxed);  // testing: 0 never, 1 for any number of tiles
-  if (pst != 0 && !(parts > 1 && (p.k_split || kAccIn)) && (pst == 1 || tile_count(p.M, p.N, 32 * MB, 32 * NB) * parts > kCUs))
+  if (pst != 0 && !(parts > 1 && (p.k_split || kAccIn || static_cast<int64_t>(parts) * p.k_per != p.K)) && (pst == 1 || tile_count(p.M, p.N, 32 * MB, 32 * NB) * parts > kCUs))
     return launch_w4p<MB, NB, kAK, kBK, kEpi, kAccIn>(p, stream);
   if constexpr (!(kAK && kBK)) {  // dX launches read every staged slice there is: they never carry a gather
     if (*carry) {
@@ -607,10 +607,11 @@ double plan_launches(int M, int N, int K, int kind, bool acc_in, int *axis, int 
 
 // The parts of a product split along K, each into its own plane.
 template <bool kAK, bool kBK>
-hipError_t launch_parts(const GemmParams &p, int parts, float *planes, size_t planes_bytes, hipStream_t stream, bool *carry) {
-  if (planes_bytes < static_cast<size_t>(parts) * p.M * p.N * 4) return hipErrorInvalidValue;
+hipError_t launch_parts(const GemmParams &p, int k_per, float *planes, size_t planes_bytes, hipStream_t stream, bool *carry) {
   GemmParams s = p;
-  s.k_parts = parts;
+  s.k_parts = (p.K + k_per - 1) / k_per;
+  s.k_per = k_per;
+  if (planes_bytes < static_cast<size_t>(s.k_parts) * p.M * p.N * 4) return hipErrorInvalidValue;
   s.C = planes;
   s.ldc = p.N;
   return launch_best<kAK, kBK, static_cast<int>(Epilogue::kF32Workspace), false>(s, stream, carry);
@@ -632,7 +633,7 @@ hipError_t launch_planned(const GemmParams &p, hipStream_t stream, bool *carry, 
     // continue one accumulator chain instead)
     const int parts = (p.k_split || !planes) ? 1 : forward_k_parts(p.M, p.K);
     if (parts > 1) {
-      const hipError_t e = launch_parts<kAK, kBK>(p, parts, planes, planes_bytes, stream, carry);
+      const hipError_t e = launch_parts<kAK, kBK>(p, p.K / parts, planes, planes_bytes, stream, carry);
       return e != hipSuccess ? e : launch_combine<kEpi>(p, parts, planes, stream);
     }
   }
@@ -694,17 +695,19 @@ bool skinny_by_lane(const WeightMap &w) {
   return w.dp_mask != 0 || w.lay.rows_per_shard == 0 || w.lay.rows_per_shard % (kBKc ? BN : BK) != 0;
 }
 
-template <int BM, int BN, int BK, int kStages, bool kBKc, bool kEpilogue = false>
+template <int BM, int BN, int BK, int kStages, bool kBKc, SkinnyResult kResult = SkinnyResult::kPlain>
 hipError_t launch_skinny_as(SkinnyParams p, hipStream_t stream) {
   constexpr size_t lds = static_cast<size_t>(kSkinnyWaves) * kStages * (BM + BN) * BK * sizeof(uint16_t);
   static_assert(lds + 2 * OSDP_MAX_SHARDS * 8 <= 160 * 1024, "the rings do not fit the 160 KB of LDS");
-  auto kernel = gemm_skinny_kernel<BM, BN, BK, kStages, kBKc, kEpilogue>;
+  auto kernel = gemm_skinny_kernel<BM, BN, BK, kStages, kBKc, kResult>;
   static bool configured[kMaxDevices] = {};
   const hipError_t e = allow_lds(kernel, lds, configured);
   if (e != hipSuccess) return e;
   p.tiles_m = (p.M + BM - 1) / BM;
   p.by_lane = skinny_by_lane<BN, BK, kBKc>(p.w);
-  hipLaunchKernelGGL(kernel, dim3(p.tiles_m * ((p.N + BN - 1) / BN)), dim3(kSkinnyWaves * 64), lds, stream, p);
+  p.tiles = p.tiles_m * ((p.N + BN - 1) / BN);
+  const int parts = kResult == SkinnyResult::kPlanes ? (p.K + p.k_per - 1) / p.k_per : 1;
+  hipLaunchKernelGGL(kernel, dim3(p.tiles * parts), dim3(kSkinnyWaves * 64), lds, stream, p);
   return hipGetLastError();
 }
 
@@ -738,20 +741,20 @@ SkinnyParams skinny_params(bool dx, const WeightMap &w, int64_t T, const void *a
 }
 
 // As many LDS stages as fit; 128 columns to a workgroup where that still gives every CU one, else 64.
-template <bool kEpilogue>
-hipError_t launch_skinny_forward(const SkinnyParams &p, hipStream_t stream) {
-  const int bm = skinny_rows(p.M, p.N);
-  if (p.N > 128 * (kCUs - 1) && p.M <= 64) {
-    if (p.M <= 16) return launch_skinny_as<16, 128, 32, 4, false, kEpilogue>(p, stream);
-    if (p.M <= 32) return launch_skinny_as<32, 128, 32, 3, false, kEpilogue>(p, stream);
-    if (p.M <= 48) return launch_skinny_as<48, 128, 32, 3, false, kEpilogue>(p, stream);
-    return launch_skinny_as<64, 128, 32, 3, false, kEpilogue>(p, stream);
-  }
-  if (bm == 16) return launch_skinny_as<16, 64, 32, 7, false, kEpilogue>(p, stream);
-  if (bm == 32) return launch_skinny_as<32, 64, 32, 6, false, kEpilogue>(p, stream);
-  if (bm == 48) return launch_skinny_as<48, 64, 32, 5, false, kEpilogue>(p, stream);
-  if (bm == 64) return launch_skinny_as<64, 64, 32, 4, false, kEpilogue>(p, stream);
-  return launch_skinny_as<128, 64, 32, 3, false, kEpilogue>(p, stream);
+template <SkinnyResult kResult>
+hipError_t launch_skinny_forward(const SkinnyParams &p, int bm, hipStream_t stream) {
+  if constexpr (kResult != SkinnyResult::kPlanes)
+    if (p.N > 128 * (kCUs - 1) && p.M <= 64) {
+      if (p.M <= 16) return launch_skinny_as<16, 128, 32, 4, false, kResult>(p, stream);
+      if (p.M <= 32) return launch_skinny_as<32, 128, 32, 3, false, kResult>(p, stream);
+      if (p.M <= 48) return launch_skinny_as<48, 128, 32, 3, false, kResult>(p, stream);
+      return launch_skinny_as<64, 128, 32, 3, false, kResult>(p, stream);
+    }
+  if (bm == 16) return launch_skinny_as<16, 64, 32, 7, false, kResult>(p, stream);
+  if (bm == 32) return launch_skinny_as<32, 64, 32, 6, false, kResult>(p, stream);
+  if (bm == 48) return launch_skinny_as<48, 64, 32, 5, false, kResult>(p, stream);
+  if (bm == 64) return launch_skinny_as<64, 64, 32, 4, false, kResult>(p, stream);
+  return launch_skinny_as<128, 64, 32, 3, false, kResult>(p, stream);
 }
 
 }  // namespace

@@ -24,6 +24,10 @@ namespace {
 
 constexpr int kSkinnyWaves = 4;
 
+// What becomes of a workgroup's sums: rounded; through the fused epilogue and rounded; or stored in fp32, those of a part of the
+// reduction each in a plane of their own.
+enum class SkinnyResult { kPlain, kFused, kPlanes };
+
 struct SkinnyParams {
   int32_t M, N, K;       // tokens, output columns, reduction length
   const uint16_t *A;     // X or dY
@@ -32,6 +36,8 @@ struct SkinnyParams {
   int64_t ldc;
   WeightMap w;
   FusedEpilogue fused;   // only read by kernels instantiated with it
+  float *planes;         // kernels that store partial sums: [parts][M][N]
+  int32_t k_per, tiles;  // and the length of a part, a multiple of 128, and the tiles of one
   int32_t tiles_m;       // row tiles; more than one only where that spreads a small product over more CUs
   int32_t by_lane;       // some K block may lie in more than one array: lanes need the tables
 };
@@ -174,7 +180,7 @@ struct SkinnyOperand {
 };
 
 // block(): which workgroup of the product this is (asked for where it is used: in front of everything else it costs 0.3 us).
-template <int BM, int BN, int BK, int kStages, bool kBKc, bool kEpilogue, class Block>
+template <int BM, int BN, int BK, int kStages, bool kBKc, SkinnyResult kResult, class Block>
 __device__ __forceinline__ void skinny_tile(const SkinnyParams &p, Block &&block) {
   constexpr int MB = BM / 16, NB = BN / 16, KS = BK / 32;
   using OpA = SkinnyOperand<true, BM, BK>;
@@ -196,15 +202,23 @@ __device__ __forceinline__ void skinny_tile(const SkinnyParams &p, Block &&block
     }
     __syncthreads();
   }
-  const int id = block(), tn = __builtin_amdgcn_readfirstlane(id / p.tiles_m);
+  int id = block();
+  int part = 0, k_first = 0, k_end = p.K;
+  if constexpr (kResult == SkinnyResult::kPlanes) {
+    part = __builtin_amdgcn_readfirstlane(id / p.tiles);
+    id -= part * p.tiles;
+    k_first = part * p.k_per;
+    k_end = k_first + p.k_per < p.K ? k_first + p.k_per : p.K;
+  }
+  const int tn = __builtin_amdgcn_readfirstlane(id / p.tiles_m);
   const int n0 = tn * BN, m0 = (id - tn * p.tiles_m) * BM;
   const int m_left = p.M - m0 < BM ? p.M - m0 : BM;
 
   // this wave's K blocks: a quarter of the reduction, in units of the largest K block of any tile
   constexpr int kUnit = kBKc ? 64 : 32;
   static_assert(kUnit % BK == 0, "the waves' ranges are whole K blocks");
-  const int blocks = (p.K + BK - 1) / BK, per = ((p.K + kUnit - 1) / kUnit + kSkinnyWaves - 1) / kSkinnyWaves * (kUnit / BK);
-  const int b0 = wave * per, b1 = b0 + per < blocks ? b0 + per : blocks;
+  const int blocks = (k_end + BK - 1) / BK, per = ((k_end - k_first + kUnit - 1) / kUnit + kSkinnyWaves - 1) / kSkinnyWaves * (kUnit / BK);
+  const int b0 = k_first / BK + wave * per, b1 = b0 + per < blocks ? b0 + per : blocks;
 
   // byte offset of this lane in load 0 of a block with rows of ld2 bytes; `h`: which of the two permutations
   auto lane_offset = [&](auto op, int h, uint32_t ld2) {
@@ -344,16 +358,20 @@ __device__ __forceinline__ void skinny_tile(const SkinnyParams &p, Block &&block
       for (int e = 0; e < 4; ++e) c[e] += d[e];
     }
     uint2 o;
-    if constexpr (kEpilogue) o = fused4(p.fused, c, m0 + m, n0 + n);
+    if constexpr (kResult == SkinnyResult::kPlanes) {
+      *reinterpret_cast<f32x4 *>(p.planes + (static_cast<int64_t>(part) * p.M + m0 + m) * p.N + n0 + n) = c;
+      continue;
+    }
+    if constexpr (kResult == SkinnyResult::kFused) o = fused4(p.fused, c, m0 + m, n0 + n);
     else o = uint2{pack_bf16x2(c[0], c[1]), pack_bf16x2(c[2], c[3])};
     store_global8(p.C + static_cast<int64_t>(m0 + m) * p.ldc + n0 + n, o);
   }
 }
 
-template <int BM, int BN, int BK, int kStages, bool kBKc, bool kEpilogue>
+template <int BM, int BN, int BK, int kStages, bool kBKc, SkinnyResult kResult>
 __global__ __launch_bounds__(kSkinnyWaves * 64, 1)
 void gemm_skinny_kernel(SkinnyParams p) {
-  skinny_tile<BM, BN, BK, kStages, kBKc, kEpilogue>(p, [] { return logical_block(); });
+  skinny_tile<BM, BN, BK, kStages, kBKc, kResult>(p, [] { return logical_block(); });
 }
 
 // The backward of few tokens as one launch: workgroups [0, n_dx) are those of dX, the others 128 x 128 tiles of dW into the
@@ -363,7 +381,7 @@ template <int BM, int BK, int kStages>
 __global__ __launch_bounds__(kSkinnyWaves * 64, 1)
 void few_token_backward_kernel(SkinnyParams dx, GemmParams dw, int n_dx, int tiles_m, int tiles_n) {
   const int id = blockIdx.x;
-  if (id < n_dx) skinny_tile<BM, 64, BK, kStages, true, false>(dx, [&] { return id; });
+  if (id < n_dx) skinny_tile<BM, 64, BK, kStages, true, SkinnyResult::kPlain>(dx, [&] { return id; });
   else gemm_w4_tile<4, 4, 4, false, false, static_cast<int>(Epilogue::kBf16ShardMajor), false, false>(dw, tiles_m, tiles_n, id - n_dx);
 }
 

@@ -200,8 +200,9 @@ __device__ __forceinline__ void gemm_w4_tile(const GemmParams &p, int tiles_m, i
   if (p.k_parts > 1) {
     const int tiles = tiles_m * tiles_n, part = __builtin_amdgcn_readfirstlane(pid / tiles);
     pid -= part * tiles;
-    K = __builtin_amdgcn_readfirstlane(p.K / p.k_parts);
-    k0 = static_cast<int64_t>(part) * K;
+    const int first = __builtin_amdgcn_readfirstlane(part * p.k_per);
+    K = __builtin_amdgcn_readfirstlane(p.k_per < p.K - first ? p.k_per : p.K - first);
+    k0 = first;
     plane_row = part * p.M;
   }
   tile_of_pid(pid, tiles_m, tiles_n, &tm, &tn);

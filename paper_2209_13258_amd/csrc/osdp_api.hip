@@ -714,13 +714,6 @@ GemmProblem weight_gemm(const Resolved &r, bool is_fwd, int j0, int j1, WeightVi
   return g;
 }
 
-// A forward launch that stores the result goes through the epilogue; col: the first of its columns in Y.
-void fuse(GemmProblem *g, const FusedEpilogue *ep, int64_t col) {
-  if (!ep || g->epilogue != Epilogue::kBf16RowMajor) return;
-  g->epilogue = Epilogue::kBf16Fused;
-  g->fused = fused_from(*ep, 0, col);
-}
-
 // dW over the sub-slices [j0, j1), written into the shard-major gradient: column slices give
 // dW[:, c0:c1] = X^T . dY[:, c0:c1], row slices dW[c0:c1, :] = X[:, c0:c1]^T . dY.
 // element offset of sub-slice j inside its slice's replica
@@ -1035,22 +1028,36 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
   if ((st = fill_table(w_shards, r.N, "w_shards", &tab)) != OSDP_OK) return st;
   if ((st = check_replicas(r, rep, false)) != OSDP_OK) return st;
   if ((st = check_workspace(r, workspace, workspace_bytes)) != OSDP_OK) return st;
+  // (with an epilogue: the planes of parts of the reduction lie behind everything else)
+  const size_t fused_bytes = ep ? fused_planes_bytes(r.T, r.I, r.O) : 0, fused_at = round_up(workspace_total(r), kSlotAlign);
+  if (fused_bytes > 0 && workspace_bytes < fused_at + fused_bytes)
+    return fail(OSDP_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace_bytes, fused_at + fused_bytes);
+  void *fused_planes = fused_bytes > 0 ? static_cast<char *>(workspace) + fused_at : nullptr;
   if ((st = device_ok()) != OSDP_OK) return st;
   if (no_tokens) return OSDP_OK;  // Y is empty: nothing is gathered, nothing is launched
   if (skinny_takes(false, r.T, ldx, r.layout, r.I)) {  // few tokens: one launch that reads the weights where they lie
     const double T = r.T, I = r.I, O = r.O;
     OSDP_HIP(timed(OSDP_KERNEL_GEMM_FWD, 2.0 * T * I * O, 2.0 * (T * I + I * O + T * O), sc,
                    [&] {
-                     return ep ? launch_skinny_fused(weight_map(r, tab, rep), r.T, X, ldx, Y, ldy, *ep, sc)
+                     return ep ? launch_skinny_fused(weight_map(r, tab, rep), r.T, X, ldx, Y, ldy, *ep, fused_planes, sc)
                                : launch_skinny(false, weight_map(r, tab, rep), r.T, X, ldx, Y, ldy, sc);
                    }));
     return OSDP_OK;
   }
   const bool in_place = ep ? !r.any_dp && gemm_reads_shards(r.T, ldx, r.layout, true) && switches_pay(r)
                            : one_chain(r, true) && gemm_reads_shards(r.T, ldx, r.layout) && switches_pay(r);
+  // A launch that stores columns of Y, whole sums, goes through the epilogue, in parts by the rule of the whole operator.
+  auto fuse = [&](GemmProblem *g, int64_t col, bool whole) {
+    if (!ep || g->epilogue != Epilogue::kBf16RowMajor) return;
+    g->epilogue = Epilogue::kBf16Fused;
+    g->fused = fused_from(*ep, 0, col);
+    g->parts = whole ? fused_planes : nullptr;
+    g->parts_bytes = fused_bytes;
+    g->k_per = static_cast<int32_t>(fused_k_per(r.T, r.I, r.O));
+  };
   if (in_place && !r.any_dp) {
     GemmProblem g = shard_gemm(r, true, tab, X, ldx, Y, ldy);
-    fuse(&g, ep, 0);
+    fuse(&g, 0, true);
     OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
     return OSDP_OK;
   }
@@ -1058,11 +1065,12 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
     const std::vector<Slice> runs = runs_in_place(r, true);
     for (const Slice &l : runs) {
       GemmProblem g = run_gemm(r, true, l, tab, rep, X, ldx, Y, ldy);
-      fuse(&g, ep, r.sub[l.c0].c0);
+      fuse(&g, r.sub[l.c0].c0, true);
       OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
     }
     if (!runs.empty()) return OSDP_OK;
   }
+  const bool whole = !r.rows || r.fwd.size() == 1;  // (row slices continue one chain, and so does their pass cut the other way)
   Resolved other;
   if (recut(shape, r, true, &other)) r = std::move(other);
 
@@ -1089,13 +1097,13 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
       if (j == 0 && !r.dp[0]) OSDP_HIP(do_gather(r, tab, r.sub[0], slot, sc));
       GemmProblem g = weight_gemm(r, /*is_fwd=*/true, j, j + 1, weights_of(r, rep, j, slot), WeightView{nullptr, 0}, X, ldx,
                                   Y, ldy, acc, static_cast<size_t>(j), static_cast<size_t>(n));
-      fuse(&g, ep, r.rows ? 0 : r.sub[j].c0);
       GatherRequest next;
       if (j + 1 < n && !r.dp[j + 1]) {
         next = gather_request(r, tab, r.sub[j + 1], ws + static_cast<size_t>((j + 1) % 2) * r.slot_bytes);
         g.carry = &next;
       }
       g.parts = planes; g.parts_bytes = planes_bytes;
+      fuse(&g, r.rows ? 0 : r.sub[j].c0, whole);
       OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
       if (poison && !r.dp[j]) OSDP_HIP(launch_fill16(slot, r.slot_bytes, kPoison, sc));
     }
@@ -1127,8 +1135,8 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
                             li, r.fwd.size())
               : weight_gemm(r, /*is_fwd=*/true, j0, j1, weights_of(r, rep, j0, slot_of[0]),
                             weights_of(r, rep, j1 - 1, slot_of[1]), X, ldx, Y, ldy, acc, li, r.fwd.size());
-    fuse(&g, ep, r.rows ? 0 : r.sub[j0].c0);
     g.parts = planes; g.parts_bytes = planes_bytes;
+    fuse(&g, r.rows ? 0 : r.sub[j0].c0, whole);
     OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
     if (poison && gathered) {  // the slices this launch read are dead: poison their slots before they are handed back
       if (joint) OSDP_HIP(launch_fill16(ws, r.slot_bytes * 2, kPoison, sc));
@@ -1246,7 +1254,8 @@ osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape *shape, 
   size_t base = 0;
   const osdp_status st = osdp_split_linear_workspace_bytes(shape, plan, op_index, is_bwd, &base, peak_weight_staging);
   if (st != OSDP_OK) return st;
-  if (total) *total = is_bwd ? round_up(base, kSlotAlign) + slope_workspace_bytes(shape->T, shape->O) : base;
+  if (total)
+    *total = round_up(base, kSlotAlign) + (is_bwd ? slope_workspace_bytes(shape->T, shape->O) : fused_planes_bytes(shape->T, shape->I, shape->O));
   return OSDP_OK;
 }
 

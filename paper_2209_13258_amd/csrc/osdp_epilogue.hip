@@ -6,6 +6,35 @@
 
 namespace osdp {
 
+namespace {
+// Few tokens: rows of a tile, and the length of a part of the reduction, a multiple of 128 (four waves' K blocks).
+// A workgroup streams 2 (rows + 64) bytes a unit of K at some 38 KB a us, where they come from a cache; the weights come from
+// memory once, at 5 TB/s; parts cost the planes' way out and back and a launch.
+struct SkinnyPlan {
+  int rows;
+  int64_t k_per;
+};
+SkinnyPlan skinny_plan(int64_t T, int64_t I, int64_t O) {
+  SkinnyPlan best{16, I};
+  double best_us = 0.0;
+  for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    const int64_t per = parts == 1 ? I : ((I + parts - 1) / parts + 127) / 128 * 128;
+    if (parts > 1 && per < 512) break;
+    for (int rows : {16, 32, 48, 64, 128}) {
+      const int64_t groups = ((T + rows - 1) / rows) * ((O + 63) / 64) * ((I + per - 1) / per);
+      const double stream = static_cast<double>((groups + kCUs - 1) / kCUs * (rows + 64) * 2 * per) / 38.0e3;
+      const double us = std::max(stream, 2.0 * static_cast<double>(I) * static_cast<double>(O) / 5.0e6) +
+                        (parts > 1 ? 3.5 + 8.0 * parts * static_cast<double>(T) * static_cast<double>(O) / 4.0e6 : 0.0);
+      if (best_us == 0.0 || us < best_us) {
+        best_us = us;
+        best = SkinnyPlan{rows, per};
+      }
+    }
+  }
+  return best;
+}
+}  // namespace
+
 hipError_t launch_gemm_fused(const GemmProblem &q, hipStream_t stream, bool *carry) {
   GemmParams p;
   const hipError_t e = launch_params(q, *carry, &p);
@@ -20,10 +49,37 @@ hipError_t launch_combine_fused(const GemmProblem &q, int parts, const float *pl
 }
 
 hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int64_t ldx, void *Y, int64_t ldy,
-                               const FusedEpilogue &fused, hipStream_t stream) {
+                               const FusedEpilogue &fused, void *planes, hipStream_t stream) {
   SkinnyParams p = skinny_params(false, w, T, X, ldx, Y, ldy);
   p.fused = fused;
-  return launch_skinny_forward<true>(p, stream);
+  const SkinnyPlan plan = skinny_plan(T, p.K, p.N);
+  if (plan.k_per >= p.K) return launch_skinny_forward<SkinnyResult::kFused>(p, skinny_rows(p.M, p.N), stream);
+  p.planes = static_cast<float *>(planes);
+  p.k_per = plan.k_per;
+  const hipError_t e = launch_skinny_forward<SkinnyResult::kPlanes>(p, plan.rows, stream);
+  if (e != hipSuccess) return e;
+  GemmParams c{};
+  c.M = p.M; c.N = p.N;
+  c.C = Y; c.ldc = ldy;
+  c.fused = fused;
+  return launch_combine<static_cast<int>(Epilogue::kBf16Fused)>(c, (p.K + plan.k_per - 1) / plan.k_per, p.planes, stream);
+}
+
+int64_t fused_k_per(int64_t T, int64_t I, int64_t O) {
+  // Of 128 x 128 tiles, one to a CU: 0.0105 us a unit of K.  The parts' planes and the launch that adds them up: some 11 us.
+  const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128);
+  const int64_t parts = std::min<int64_t>({kCUs / std::max<int64_t>(tiles, 1), I / 512, 32});
+  if (parts < 2 || I - I / parts < 1500) return I;
+  return ((I + parts - 1) / parts + 63) / 64 * 64;
+}
+
+size_t fused_planes_bytes(int64_t T, int64_t I, int64_t O) {
+  auto bytes = [&](int64_t k_per) {
+    const int64_t parts = (I + k_per - 1) / k_per;
+    return parts > 1 ? static_cast<size_t>(parts) * static_cast<size_t>(T) * static_cast<size_t>(O) * 4 : 0;
+  };
+  const size_t tiles = bytes(fused_k_per(T, I, O));
+  return T > 0 && T <= kSkinnyMaxTokens ? std::max(tiles, bytes(skinny_plan(T, I, O).k_per)) : tiles;
 }
 
 namespace {

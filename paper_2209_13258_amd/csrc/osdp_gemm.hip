@@ -111,10 +111,9 @@ hipError_t dispatch_gemm(const GemmProblem &q, hipStream_t stream, bool *carry) 
   const bool acc = q.acc_in != nullptr;
   if (q.epilogue == Epilogue::kBf16Fused) {
     if (!q.a_kcontig || q.b_kcontig) return hipErrorInvalidValue;
-    const int parts = (acc || p.k_split || !planes) ? 1 : forward_k_parts(p.M, p.K);
-    if (parts == 1) return launch_gemm_fused(q, stream, carry);
-    const hipError_t ep = launch_parts<true, false>(p, parts, planes, planes_bytes, stream, carry);
-    return ep != hipSuccess ? ep : launch_combine_fused(q, parts, planes, stream);
+    if (acc || p.k_split || !planes || q.k_per <= 0 || q.k_per >= p.K) return launch_gemm_fused(q, stream, carry);
+    const hipError_t ep = launch_parts<true, false>(p, q.k_per, planes, planes_bytes, stream, carry);
+    return ep != hipSuccess ? ep : launch_combine_fused(q, (p.K + q.k_per - 1) / q.k_per, planes, stream);
   }
   // The three GEMMs of the split linear layer, with the four accumulate forms for forward and dX, are the only combinations built.
   if (q.a_kcontig && !q.b_kcontig) {                                               // forward (accumulating when the reduction dimension is split)
@@ -153,7 +152,7 @@ hipError_t launch_skinny(bool dx, const WeightMap &w, int64_t T, const void *act
     if (bm <= 64) return launch_skinny_as<64, 64, 64, 2, true>(p, stream);
     return launch_skinny_as<128, 64, 32, 3, true>(p, stream);
   }
-  return launch_skinny_forward<false>(p, stream);
+  return launch_skinny_forward<SkinnyResult::kPlain>(p, skinny_rows(p.M, p.N), stream);
 }
 
 namespace {

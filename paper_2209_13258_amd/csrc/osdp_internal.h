@@ -136,6 +136,7 @@ struct GemmProblem {
   // product needs; with less the launch fails).  nullptr: the product is computed in one part whatever its shape.
   void *parts;
   size_t parts_bytes;
+  int32_t k_per;  // kBf16Fused, with `parts`: length of a part (fused_k_per); 0: one part
 };
 
 // Enqueue on `stream`.  Returns hipSuccess or the launch error.
@@ -155,7 +156,12 @@ hipError_t launch_skinny(bool dx, const WeightMap &w, int64_t T, const void *act
                          hipStream_t stream);
 // The forward product with an epilogue.
 hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int64_t ldx, void *Y, int64_t ldy,
-                               const FusedEpilogue &fused, hipStream_t stream);
+                               const FusedEpilogue &fused, void *planes, hipStream_t stream);
+
+// Products with an epilogue whose output has few tiles run in parts of the reduction: the length of a part (at least I: one
+// part), by T, I and O alone.  planes_bytes: what the parts' planes take, for few tokens or more.
+int64_t fused_k_per(int64_t T, int64_t I, int64_t O);
+size_t fused_planes_bytes(int64_t T, int64_t I, int64_t O);
 
 // dX of few tokens (skinny_takes) and dW of the whole matrix into the shards as one launch; takes: whether dW is the small
 // product that this is meant for (at most one 128 x 128 tile per CU) and the two fit beside each other.
