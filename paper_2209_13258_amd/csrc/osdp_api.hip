@@ -394,7 +394,9 @@ osdp_status resolve(const osdp_shape *shape, const osdp_plan *plan, int32_t op_i
 // tokens, 4096 -> 1024 at k = 4 141 -> 87 us.  4096 tokens, 8192 -> 32768 keeps its columns: the sum is a quarter as
 // large, and launches of 2048 output columns would fill half of the CUs.
 // The gathered bytes, the slots and the workspace asked for stay those of the plan's cut.
-bool recut(const osdp_shape *shape, const Resolved &r, bool is_fwd, Resolved *out) {
+// in_parts: launches that hold a whole reduction would run in parts of it, for want of tiles (calls with an epilogue): taken
+// wherever the slices allow it.
+bool recut(const osdp_shape *shape, const Resolved &r, bool is_fwd, Resolved *out, bool in_parts = false) {
   const DebugOptions &d = debug_options();
   const int forced = d.recut.load(std::memory_order_relaxed);  // testing: 0 never, 1 whenever the slices allow it
   const std::vector<Slice> &sum = is_fwd ? r.fwd : r.pass;
@@ -423,7 +425,7 @@ bool recut(const osdp_shape *shape, const Resolved &r, bool is_fwd, Resolved *ou
   if (resolve(&other_shape, &other_plan, 0, true, !is_fwd, out) != OSDP_OK) return false;  // (cannot fail: all it asks for holds)
   if (out->slots != r.slots || out->slot_bytes > r.slot_bytes) return false;
   out->acc_bytes = out->parts_bytes = 0;  // one chain, as the sum is
-  if (forced == 1) return true;
+  if (forced == 1 || in_parts) return true;
   auto us = [&](const Resolved &q, bool adds) {
     double t = 0.0;
     bool first = true;  // (the first launch of a pass that adds up starts from zero)
@@ -1035,7 +1037,7 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
   void *fused_planes = fused_bytes > 0 ? static_cast<char *>(workspace) + fused_at : nullptr;
   if ((st = device_ok()) != OSDP_OK) return st;
   if (no_tokens) return OSDP_OK;  // Y is empty: nothing is gathered, nothing is launched
-  if (skinny_takes(false, r.T, ldx, r.layout, r.I)) {  // few tokens: one launch that reads the weights where they lie
+  if (ep ? fused_takes_skinny(r.T, ldx, r.layout, r.I) : skinny_takes(false, r.T, ldx, r.layout, r.I)) {  // few tokens: one launch that reads the weights where they lie
     const double T = r.T, I = r.I, O = r.O;
     OSDP_HIP(timed(OSDP_KERNEL_GEMM_FWD, 2.0 * T * I * O, 2.0 * (T * I + I * O + T * O), sc,
                    [&] {
@@ -1070,9 +1072,14 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
     }
     if (!runs.empty()) return OSDP_OK;
   }
-  const bool whole = !r.rows || r.fwd.size() == 1;  // (row slices continue one chain, and so does their pass cut the other way)
+  // Launches that hold the whole reduction may run in parts of it; slices that cannot be cut the other way go on in one chain.
+  bool whole = !r.rows || r.fwd.size() == 1;
+  const bool cut_for_parts = !whole && ep && fused_k_per(r.T, r.I, r.O) < r.I;
   Resolved other;
-  if (recut(shape, r, true, &other)) r = std::move(other);
+  if (recut(shape, r, true, &other, cut_for_parts)) {
+    r = std::move(other);
+    whole = cut_for_parts;
+  }
 
   char *ws = static_cast<char *>(workspace);
   float *acc = reinterpret_cast<float *>(ws + r.slot_bytes * r.slots);  // row slices: Y's fp32 partial sum
@@ -1255,7 +1262,8 @@ osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape *shape, 
   const osdp_status st = osdp_split_linear_workspace_bytes(shape, plan, op_index, is_bwd, &base, peak_weight_staging);
   if (st != OSDP_OK) return st;
   if (total)
-    *total = round_up(base, kSlotAlign) + (is_bwd ? slope_workspace_bytes(shape->T, shape->O) : fused_planes_bytes(shape->T, shape->I, shape->O));
+    *total = round_up(base, kSlotAlign) + (is_bwd ? round_up(slope_workspace_bytes(shape->T, shape->O), kSlotAlign) + bwd_planes_bytes(shape->T, shape->I, shape->O)
+                                                  : fused_planes_bytes(shape->T, shape->I, shape->O));
   return OSDP_OK;
 }
 
@@ -1307,6 +1315,23 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
   if ((st = fill_table(reinterpret_cast<const void *const *>(dw_shards), r.N, "dw_shards", &gtab)) != OSDP_OK) return st;
   if ((st = check_replicas(r, rep, true)) != OSDP_OK) return st;
   if ((st = check_workspace(r, workspace, workspace_bytes)) != OSDP_OK) return st;
+  // (with an epilogue: planes of products that run in parts lie behind the partial sums of db, for one product after the other)
+  void *planes_dx = nullptr, *planes_dw = nullptr;
+  const int64_t dx_per = slope && !no_tokens ? fused_k_per(r.T, r.O, r.I) : 0, dw_per = slope && !no_tokens ? fused_k_per(r.I, r.T, r.O) : 0;
+  const size_t fused_bytes = slope ? bwd_planes_bytes(r.T, r.I, r.O) : 0;
+  if (fused_bytes > 0) {
+    const size_t at = static_cast<size_t>(static_cast<char *>(slope_workspace) - static_cast<char *>(workspace)) +
+                      round_up(slope_workspace_bytes(r.T, r.O), kSlotAlign);
+    if (workspace_bytes < at + fused_bytes)
+      return fail(OSDP_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace_bytes, at + fused_bytes);
+    planes_dx = planes_dw = static_cast<char *>(workspace) + at;
+  }
+  auto in_parts = [&](GemmProblem *g, int64_t per, void *planes) {
+    if (!slope || no_tokens) return;
+    g->k_per = static_cast<int32_t>(per);
+    g->parts = planes;
+    g->parts_bytes = fused_bytes;
+  };
   if ((st = device_ok()) != OSDP_OK) return st;
 
   if (slope) {  // the products' dY is the gradient in front of the activation
@@ -1333,8 +1358,9 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
   if (in_place && r.any_dp && r.T <= kSkinnyMaxTokens) runs = runs_in_place(r, false);
   if (skinny || (in_place && (!r.any_dp || !runs.empty()))) {
     const double T = r.T, I = r.I, O = r.O;
+    const bool dx_parts = skinny && slope && skinny_dx_per(r.T, r.I, r.O) < r.O;
     if (!r.any_dp) r.dw.assign(1, Slice{0, static_cast<int64_t>(r.sub.size())});
-    if (skinny && !r.any_dp) {
+    if (skinny && !r.any_dp && !dx_parts) {
       const GemmProblem gw = dw_gemm(r, 0, static_cast<int>(r.sub.size()), X, ldx, dY, lddy, gtab, rep);
       // (one after the other, dX may take the place of X, or of dY where one tile holds its columns: dW has read both by
       // then; in one launch nothing orders dX's stores behind dW's loads)
@@ -1351,18 +1377,31 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
         return OSDP_OK;
       }
     }
-    for (const Slice &l : r.dw)
-      OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DW, dw_gemm(r, static_cast<int>(l.c0), static_cast<int>(l.c1), X, ldx, dY, lddy, gtab, rep), sc));
+    for (const Slice &l : r.dw) {
+      GemmProblem gw = dw_gemm(r, static_cast<int>(l.c0), static_cast<int>(l.c1), X, ldx, dY, lddy, gtab, rep);
+      in_parts(&gw, dw_per, planes_dw);
+      OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DW, gw, sc));
+    }
     if (skinny)
-      OSDP_HIP(timed(OSDP_KERNEL_GEMM_DX, 2.0 * T * I * O, 2.0 * (T * O + I * O + T * I), sc,
-                     [&] { return launch_skinny(true, weight_map(r, tab, rep), r.T, dY, lddy, dX, lddx, sc); }));
-    else if (runs.empty())
-      OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DX, shard_gemm(r, false, tab, dY, lddy, dX, lddx), sc));
+      OSDP_HIP(timed(OSDP_KERNEL_GEMM_DX, 2.0 * T * I * O, 2.0 * (T * O + I * O + T * I), sc, [&] {
+        return dx_parts ? launch_skinny_dx_parts(weight_map(r, tab, rep), r.T, dY, lddy, dX, lddx, planes_dx, sc)
+                        : launch_skinny(true, weight_map(r, tab, rep), r.T, dY, lddy, dX, lddx, sc);
+      }));
+    else if (runs.empty()) {
+      GemmProblem gx = shard_gemm(r, false, tab, dY, lddy, dX, lddx);
+      in_parts(&gx, dx_per, planes_dx);
+      OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DX, gx, sc));
+    }
     for (const Slice &l : runs) OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DX, run_gemm(r, false, l, tab, rep, dY, lddy, dX, lddx), sc));
     return OSDP_OK;
   }
+  bool whole = r.rows || r.pass.size() == 1;  // (see forward())
+  const bool cut_for_parts = !whole && slope && dx_per < r.O;
   Resolved other;
-  if (recut(shape, r, false, &other)) r = std::move(other);
+  if (recut(shape, r, false, &other, cut_for_parts)) {
+    r = std::move(other);
+    whole = cut_for_parts;
+  }
   char *ws = static_cast<char *>(workspace);
   float *acc = reinterpret_cast<float *>(ws + r.slot_bytes * r.slots);  // column slices: dX's fp32 partial sum
   void *planes = r.parts_bytes ? ws + r.slot_bytes * r.slots + r.acc_bytes : nullptr;  // row slices: planes of dX launches split along K
@@ -1408,6 +1447,7 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
     // dW launches whose range starts in this group: they need no weights and run while the gathers are in flight
     for (; next_dw < r.dw.size() && r.dw[next_dw].c0 < g1; ++next_dw) {
       GemmProblem gw = dw_gemm(r, static_cast<int>(r.dw[next_dw].c0), static_cast<int>(r.dw[next_dw].c1), X, ldx, dY, lddy, gtab, rep);
+      in_parts(&gw, dw_per, planes_dw);
       if (next_pending < n_pending) gw.carry = &pending[next_pending++];
       OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DW, gw, sc));
     }
@@ -1424,6 +1464,7 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
                               weights_of(r, rep, j1 - 1, ws + static_cast<size_t>(j1 - 1 - g0) * r.slot_bytes), dY, lddy, dX,
                               lddx, acc, next_pass, r.pass.size());
       gx.parts = planes; gx.parts_bytes = r.parts_bytes;
+      in_parts(&gx, dx_per, whole ? planes_dx : nullptr);
       OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DX, gx, sc));
     }
     if (poison) OSDP_HIP(launch_fill16(ws, r.slot_bytes * r.slots, kPoison, sc));
@@ -1480,8 +1521,9 @@ osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, const osdp_p
     return fail(OSDP_ERR_INVALID_ARG, "dbias overlaps an input or another output");
   size_t base = 0, total = 0;
   if ((st = osdp_split_linear_workspace_bytes(shape, plan, op_index, 1, &base, nullptr)) != OSDP_OK) return st;
-  total = round_up(base, kSlotAlign) + slope_workspace_bytes(T, O);
-  if (e.dbias && workspace && workspace_bytes < total)
+  const bool plain = !active && !e.dbias;
+  total = round_up(base, kSlotAlign) + round_up(slope_workspace_bytes(T, O), kSlotAlign) + bwd_planes_bytes(T, I, O);
+  if (!plain && workspace && workspace_bytes < total)
     return fail(OSDP_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", workspace_bytes, total);
   SlopeProblem q{};
   q.T = T; q.O = O;
@@ -1493,7 +1535,6 @@ osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, const osdp_p
     q.dZ = e.dz; q.lddz = e.lddz;
   }
   q.db = e.dbias;
-  const bool plain = !active && !e.dbias;
   return backward(shape, plan, op_index, true, X, ldx, dY, lddy, w_shards, Replicas{w_dp, dw_dp, ld_dp}, dX, lddx, dw_shards,
                   workspace, workspace_bytes, stream_compute, stream_copy, plain ? nullptr : &q,
                   static_cast<char *>(workspace) + round_up(base, kSlotAlign));

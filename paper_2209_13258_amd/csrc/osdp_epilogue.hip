@@ -7,28 +7,26 @@
 namespace osdp {
 
 namespace {
-// Few tokens: rows of a tile, and the length of a part of the reduction, a multiple of 128 (four waves' K blocks).
-// A workgroup streams 2 (rows + 64) bytes a unit of K at some 38 KB a us, where they come from a cache; the weights come from
-// memory once, at 5 TB/s; parts cost the planes' way out and back and a launch.
+// Few tokens: rows of a tile, and the length of a part of the reduction.
+// A workgroup streams 2 (rows + 64) bytes a unit of K at some 38 KB a us, where they come from a cache, and takes 8 us to start and
+// to store; the weights come from memory once, at 5 TB/s; parts cost the planes' way out and back and a launch.
 struct SkinnyPlan {
   int rows;
   int64_t k_per;
+  double us;
 };
-SkinnyPlan skinny_plan(int64_t T, int64_t I, int64_t O) {
-  SkinnyPlan best{16, I};
-  double best_us = 0.0;
+// unit: what the length of a part is a multiple of (128: four waves' K blocks; dX: 256); I: one part.
+SkinnyPlan skinny_plan(int64_t T, int64_t I, int64_t O, int64_t unit = 128) {
+  SkinnyPlan best{16, I, 0.0};
   for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-    const int64_t per = parts == 1 ? I : ((I + parts - 1) / parts + 127) / 128 * 128;
-    if (parts > 1 && per < 512) break;
+    const int64_t per = parts == 1 ? I : ((I + parts - 1) / parts + unit - 1) / unit * unit;
+    if (parts > 1 && (per < 512 || unit == I)) break;
     for (int rows : {16, 32, 48, 64, 128}) {
       const int64_t groups = ((T + rows - 1) / rows) * ((O + 63) / 64) * ((I + per - 1) / per);
-      const double stream = static_cast<double>((groups + kCUs - 1) / kCUs * (rows + 64) * 2 * per) / 38.0e3;
+      const double stream = static_cast<double>((groups + kCUs - 1) / kCUs) * (static_cast<double>((rows + 64) * 2 * per) / 38.0e3 + 8.0);
       const double us = std::max(stream, 2.0 * static_cast<double>(I) * static_cast<double>(O) / 5.0e6) +
                         (parts > 1 ? 3.5 + 8.0 * parts * static_cast<double>(T) * static_cast<double>(O) / 4.0e6 : 0.0);
-      if (best_us == 0.0 || us < best_us) {
-        best_us = us;
-        best = SkinnyPlan{rows, per};
-      }
+      if (best.us == 0.0 || us < best.us) best = SkinnyPlan{rows, per, us};
     }
   }
   return best;
@@ -53,7 +51,7 @@ hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int
   SkinnyParams p = skinny_params(false, w, T, X, ldx, Y, ldy);
   p.fused = fused;
   const SkinnyPlan plan = skinny_plan(T, p.K, p.N);
-  if (plan.k_per >= p.K) return launch_skinny_forward<SkinnyResult::kFused>(p, skinny_rows(p.M, p.N), stream);
+  if (plan.k_per >= p.K) return launch_skinny_forward<SkinnyResult::kFused>(p, T <= kSkinnyMaxTokens ? skinny_rows(p.M, p.N) : plan.rows, stream);
   p.planes = static_cast<float *>(planes);
   p.k_per = plan.k_per;
   const hipError_t e = launch_skinny_forward<SkinnyResult::kPlanes>(p, plan.rows, stream);
@@ -65,21 +63,79 @@ hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int
   return launch_combine<static_cast<int>(Epilogue::kBf16Fused)>(c, (p.K + plan.k_per - 1) / plan.k_per, p.planes, stream);
 }
 
-int64_t fused_k_per(int64_t T, int64_t I, int64_t O) {
+int64_t fused_k_per(int64_t M, int64_t K, int64_t N) {
   // Of 128 x 128 tiles, one to a CU: 0.0105 us a unit of K.  The parts' planes and the launch that adds them up: some 11 us.
-  const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128);
-  const int64_t parts = std::min<int64_t>({kCUs / std::max<int64_t>(tiles, 1), I / 512, 32});
-  if (parts < 2 || I - I / parts < 1500) return I;
-  return ((I + parts - 1) / parts + 63) / 64 * 64;
+  const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
+  const int64_t parts = std::min<int64_t>({kCUs / std::max<int64_t>(tiles, 1), K / 512, 32});
+  if (parts < 2 || K - K / parts < 1500) return K;
+  return ((K + parts - 1) / parts + 63) / 64 * 64;
+}
+
+namespace {
+size_t planes_of(int64_t M, int64_t K, int64_t N, int64_t k_per) {
+  const int64_t parts = k_per > 0 ? (K + k_per - 1) / k_per : 0;
+  return parts > 1 ? static_cast<size_t>(parts) * static_cast<size_t>(M) * static_cast<size_t>(N) * 4 : 0;
+}
+}  // namespace
+
+// Where no shard is a whole number of K blocks only the few-token kernel reads the weights in place, at a third of the tiles'
+// rate.  More tokens than its own are worth that while the copy (4 bytes an element at 5.5 TB/s and a launch) and the tiles behind it,
+// each one's latency, take longer.  By T, I and O alone: the unsplit copy is what counts, so that Y is the same for every k.
+bool skinny_beats_copy(int64_t T, int64_t I, int64_t O) {
+  const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), k_per = fused_k_per(T, I, O), parts = (I + k_per - 1) / k_per;
+  const double flops = 2.0 * static_cast<double>(T) * static_cast<double>(I) * static_cast<double>(O);
+  const double tile = std::max(flops / 0.9e9, 0.0105 * static_cast<double>(std::min(k_per, I)) * static_cast<double>((tiles * parts + kCUs - 1) / kCUs)) +
+                      (parts > 1 ? 17.0 : 6.0);
+  const double copy = 4.0 * static_cast<double>(I) * static_cast<double>(O) / 5.5e6 + 6.0;
+  return skinny_plan(T, I, O).us < copy + tile;
+}
+
+bool fused_takes_skinny(int64_t T, int64_t ldx, const ShardLayout &lay, int64_t I) {
+  if (skinny_takes(false, T, ldx, lay, I)) return true;
+  const DebugOptions &d = debug_options();  // (the switches that pick a kernel or a schedule for staged products keep those)
+  if (d.gemm_generic.load(std::memory_order_relaxed) != 0 || d.tile.load(std::memory_order_relaxed) >= 0 ||
+      d.fwd_pair.load(std::memory_order_relaxed) >= 0 || d.fused_gather.load(std::memory_order_relaxed) >= 0 ||
+      d.poison_staging.load(std::memory_order_relaxed) != 0)
+    return false;
+  return T > kSkinnyMaxTokens && !(lay.rows_per_shard > 0 && lay.rows_per_shard % 64 == 0) && ldx < kMaxLd && I < kMaxLd && lay.O < kMaxLd &&
+         skinny_beats_copy(T, I, lay.O);
 }
 
 size_t fused_planes_bytes(int64_t T, int64_t I, int64_t O) {
-  auto bytes = [&](int64_t k_per) {
-    const int64_t parts = (I + k_per - 1) / k_per;
-    return parts > 1 ? static_cast<size_t>(parts) * static_cast<size_t>(T) * static_cast<size_t>(O) * 4 : 0;
-  };
-  const size_t tiles = bytes(fused_k_per(T, I, O));
-  return T > 0 && T <= kSkinnyMaxTokens ? std::max(tiles, bytes(skinny_plan(T, I, O).k_per)) : tiles;
+  const size_t tiles = planes_of(T, I, O, fused_k_per(T, I, O));
+  if (T <= 0 || !(T <= kSkinnyMaxTokens || skinny_beats_copy(T, I, O))) return tiles;
+  return std::max(tiles, planes_of(T, I, O, skinny_plan(T, I, O).k_per));
+}
+
+int64_t skinny_dx_per(int64_t T, int64_t I, int64_t O) {
+  // (worth the sums' own launch, and one for dW that would otherwise share dX's)
+  const SkinnyPlan plan = skinny_plan(T, O, I, 256), whole = skinny_plan(T, O, I, O);
+  return plan.us + 6.0 < whole.us ? plan.k_per : O;
+}
+
+size_t bwd_planes_bytes(int64_t T, int64_t I, int64_t O) {
+  if (T <= 0) return 0;
+  size_t most = std::max(planes_of(T, O, I, fused_k_per(T, O, I)), planes_of(I, T, O, fused_k_per(I, T, O)));
+  if (T <= kSkinnyMaxTokens) most = std::max(most, planes_of(T, O, I, skinny_dx_per(T, I, O)));
+  return most;
+}
+
+hipError_t launch_skinny_dx_parts(const WeightMap &w, int64_t T, const void *dY, int64_t lddy, void *dX, int64_t lddx, void *planes,
+                                  hipStream_t stream) {
+  SkinnyParams p = skinny_params(true, w, T, dY, lddy, dX, lddx);
+  const SkinnyPlan plan = skinny_plan(T, p.K, p.N, 256);
+  p.planes = static_cast<float *>(planes);
+  p.k_per = static_cast<int32_t>(plan.k_per);
+  constexpr SkinnyResult kPlanes = SkinnyResult::kPlanes;
+  const hipError_t e = plan.rows == 16   ? launch_skinny_as<16, 64, 64, 3, true, kPlanes>(p, stream)
+                       : plan.rows == 32 ? launch_skinny_as<32, 64, 64, 3, true, kPlanes>(p, stream)
+                       : plan.rows <= 64 ? launch_skinny_as<64, 64, 64, 2, true, kPlanes>(p, stream)
+                                         : launch_skinny_as<128, 64, 32, 3, true, kPlanes>(p, stream);
+  if (e != hipSuccess) return e;
+  GemmParams c{};
+  c.M = p.M; c.N = p.N;
+  c.C = dX; c.ldc = lddx;
+  return launch_combine<static_cast<int>(Epilogue::kBf16RowMajor)>(c, (p.K + p.k_per - 1) / p.k_per, p.planes, stream);
 }
 
 namespace {

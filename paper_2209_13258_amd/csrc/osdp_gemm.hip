@@ -115,6 +115,18 @@ hipError_t dispatch_gemm(const GemmProblem &q, hipStream_t stream, bool *carry) 
     const hipError_t ep = launch_parts<true, false>(p, q.k_per, planes, planes_bytes, stream, carry);
     return ep != hipSuccess ? ep : launch_combine_fused(q, (p.K + q.k_per - 1) / q.k_per, planes, stream);
   }
+  if (q.k_per > 0) {  // (behind the pass for dZ: parts by the caller's rule, or none)
+    if (acc || p.k_split || !planes || q.k_per >= p.K || q.a_kcontig != q.b_kcontig) {
+      planes = nullptr;
+    } else {
+      const int parts = (p.K + q.k_per - 1) / q.k_per;
+      const hipError_t ep = q.a_kcontig ? launch_parts<true, true>(p, q.k_per, planes, planes_bytes, stream, carry)
+                                        : launch_parts<false, false>(p, q.k_per, planes, planes_bytes, stream, carry);
+      if (ep != hipSuccess) return ep;
+      if (q.epilogue == Epilogue::kBf16ShardMajor) return launch_combine<kShard>(p, parts, planes, stream);
+      return q.epilogue == Epilogue::kBf16RowMajor ? launch_combine<kRow>(p, parts, planes, stream) : hipErrorInvalidValue;
+    }
+  }
   // The three GEMMs of the split linear layer, with the four accumulate forms for forward and dX, are the only combinations built.
   if (q.a_kcontig && !q.b_kcontig) {                                               // forward (accumulating when the reduction dimension is split)
     if (q.epilogue == Epilogue::kBf16RowMajor) return acc ? launch_planned<true, false, kRow, true>(p, stream, carry, planes, planes_bytes) : launch_planned<true, false, kRow, false>(p, stream, carry, planes, planes_bytes);

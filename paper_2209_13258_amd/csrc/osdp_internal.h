@@ -136,7 +136,7 @@ struct GemmProblem {
   // product needs; with less the launch fails).  nullptr: the product is computed in one part whatever its shape.
   void *parts;
   size_t parts_bytes;
-  int32_t k_per;  // kBf16Fused, with `parts`: length of a part (fused_k_per); 0: one part
+  int32_t k_per;  // with `parts`: length of a part, whatever gemm_forward_parts says (calls with an epilogue); 0: not so
 };
 
 // Enqueue on `stream`.  Returns hipSuccess or the launch error.
@@ -158,9 +158,16 @@ hipError_t launch_skinny(bool dx, const WeightMap &w, int64_t T, const void *act
 hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int64_t ldx, void *Y, int64_t ldy,
                                const FusedEpilogue &fused, void *planes, hipStream_t stream);
 
-// Products with an epilogue whose output has few tiles run in parts of the reduction: the length of a part (at least I: one
-// part), by T, I and O alone.  planes_bytes: what the parts' planes take, for few tokens or more.
-int64_t fused_k_per(int64_t T, int64_t I, int64_t O);
+// Products with an epilogue whose output has few tiles run in parts of the reduction: the length of a part (K: one
+// part), by the whole product's M x K x N alone.  planes_bytes: what the parts' planes take, for few tokens or more.
+int64_t fused_k_per(int64_t M, int64_t K, int64_t N);
+// Backward products behind the pass for dZ: the same for dX (T x O x I) and dW (I x T x O), and dX of few tokens.
+int64_t skinny_dx_per(int64_t T, int64_t I, int64_t O);
+size_t bwd_planes_bytes(int64_t T, int64_t I, int64_t O);
+hipError_t launch_skinny_dx_parts(const WeightMap &w, int64_t T, const void *dY, int64_t lddy, void *dX, int64_t lddx, void *planes,
+                                  hipStream_t stream);
+// Whether a forward product with an epilogue is launch_skinny_fused.
+bool fused_takes_skinny(int64_t T, int64_t ldx, const ShardLayout &lay, int64_t I);
 size_t fused_planes_bytes(int64_t T, int64_t I, int64_t O);
 
 // dX of few tokens (skinny_takes) and dW of the whole matrix into the shards as one launch; takes: whether dW is the small

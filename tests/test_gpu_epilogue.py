@@ -4,8 +4,9 @@ Tolerances.  A value rounded to bf16 is off by 2^-8 of it at most (half a step).
 below 1e-3 of the outputs' root mean square, as the other products' tests take it; an activation passes that on times its slope, at
 most 1.13, and adds 2^-15 of its own value.  Y = act + R: 2^-8 |Y| + 2^-15 |act| + 1.13e-3 rms(z).  dZ = dY act'(Z): 2^-8 |dZ| + 2^-15 |dY|
 (the slope is off by 2^-15, by itself), and 2^-23 |dZ| for the product in fp32.  db: each term is off by 2^-15 |dY| + 2^-23 |dZ|, the sum of T of them in
-fp32, by partial sums, by T 2^-24 of the sum of magnitudes at most, then half a step of its type.  dX and dW are bit by bit those of
-the product's own backward pass on dZ."""
+fp32, by partial sums, by T 2^-24 of the sum of magnitudes at most, then half a step of its type.  dX and dW are products of the dZ that
+was stored: 2^-8 of them and 1e-3 of their root mean square, and bit by bit those of the product's own backward pass where neither
+runs in parts of its reduction."""
 from __future__ import annotations
 
 import pytest
@@ -86,7 +87,7 @@ SHAPES = [(1, 64, 8, 1, 1), (1, 4096, 16384, 8, 1), (3, 200, 136, 17, 1), (16, 2
           (1024, 520, 2056, 40, 1), (1500, 4096, 4096, 8, 4), (2049, 128, 1032, 2, 1), (3001, 1024, 3200, 8, 1), (4096, 2560, 10240, 8, 4), (8192, 1024, 4096, 8, 4),
           # products that run in parts of a long reduction where they are staged, and one that does not
           (600, 16384, 264, 3, 1), (300, 24576, 528, 3, 3), (600, 16384, 264, 8, 1), (2, 31824, 1672, 1, 1), (33, 16384, 512, 8, 1),
-          (128, 9992, 136, 1, 1), (7, 23072, 744, 2, 1), (200, 6200, 664, 8, 1), (130, 8192, 8, 8, 1), (90, 8192, 16384, 8, 2)]
+          (128, 9992, 136, 17, 1), (215, 920, 20288, 16, 8), (193, 16080, 544, 32, 4), (337, 19336, 352, 11, 4), (1488, 672, 984, 9, 1), (900, 712, 952, 7, 1), (7, 23072, 744, 2, 1), (200, 6200, 664, 8, 1), (130, 8192, 8, 8, 1), (90, 8192, 16384, 8, 2)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
@@ -127,16 +128,20 @@ def test_nothing_but_the_product_is_the_product_bit_by_bit(T):
 def test_cuts_modes_and_shards_change_no_bit(T, I, O):
     bias, residual = rand(O, seed=1), rand(T, O, seed=2)
     how = dict(bias=bias, activation=ACTS["gelu"], residual=residual)
-    first = Op(T, I, O, 8)
-    want = first.fwd(first.out(), **how)
-    cut = {(512, 1024): 18, (1024, 2048): 13, (8192, 512): 26, (4096, 512): 13}[I, O]  # (shards that are no row blocks)
-    in_parts = (T, I) in ((300, 4096), (700, 8192))  # (row slices that are staged go on in one chain instead)
-    for N, k, split, staging in [(1, 1, 0, 1), (8, 4, 0, 1), (8, 4, 0, 2), (8, 4, 0, 3), (8, 4, 1, 1), (8, 2, 1, 2), (8, 4, 3, 1), (cut, 4, 0, 1), (cut, 2, 0, 2),
-                                 (cut, 4, 1, 1), (cut, 1, 0, 1), (16, 2, 0, 1), (cut, 1, 1, 1)]:
-        if in_parts and N == cut and k > 1 and split == 1:
-            continue
-        op = Op(T, I, O, N, k, split, staging=staging)
-        assert torch.equal(op.fwd(op.out(), **how), want), (N, k, split, staging)
+    cut = {(512, 1024): 18, (1024, 2048): 13, (8192, 512): 26, (4096, 512): 13}[I, O]
+    # shards that are blocks of a multiple of 64 rows, or one; shards that are not may have another order of sums from 129 tokens on
+    blocks = [(8, 1, 0, 1), (1, 1, 0, 1), (8, 4, 0, 1), (8, 4, 0, 2), (8, 4, 0, 3), (8, 4, 1, 1), (8, 2, 1, 2), (8, 4, 3, 1), (4, 2, 0, 1)]
+    flat = [(cut, 1, 0, 1), (cut, 4, 0, 1), (cut, 2, 0, 2), (cut, 1, 1, 1)]
+    if T <= 128 or not in_parts(T, I, O):  # (row slices that are staged go on in one chain, not in parts)
+        flat.append((cut, 4, 1, 1))
+    for plans in ([blocks + flat] if T <= 128 else [blocks, flat]):
+        want = None
+        for N, k, split, staging in plans:
+            op = Op(T, I, O, N, k, split, staging=staging)
+            got = op.fwd(op.out(), **how)
+            check_forward(op, "gelu", bias, residual, got)
+            assert want is None or torch.equal(got, want), (N, k, split, staging)
+            want = got
 
 
 @pytest.mark.parametrize("switch,values", [("tile", range(4)), ("gemm_generic", (1,)), ("persistent", (0, 1)), ("four_wave", (0, 1)), ("small_tile", (0, 1)), ("deep", (0,)),
@@ -144,7 +149,7 @@ def test_cuts_modes_and_shards_change_no_bit(T, I, O):
 def test_every_kernel_gives_the_same_bits(switch, values):
     """Every tile and schedule that can run a forward launch, over shards that are row blocks and over such that are not."""
     bias, how = rand(1600, seed=1), {}
-    for T, N in ((600, 8), (1111, 8), (1111, 5)):
+    for T, N in ((600, 8), (1111, 8), (4000, 5)):
         for k, split, staging in ((4, 0, 2), (2, 1, 2), (1, 0, 1)):
             op = Op(T, 1024, 1600, N, k, split, staging=staging)
             how = dict(bias=bias, activation=ACTS["gelu_tanh"], residual=rand(T, 1600, seed=2), z=op.out())
@@ -252,6 +257,18 @@ def test_infinities_and_nan(T):
         assert torch.isnan(Z[:, 2]).all() and torch.isfinite(Y[:, 3:]).all() and (Y[:, 3:5] == 0).all()
 
 
+def in_parts(M, K, N):
+    """Whether a product of few 128 x 128 tiles runs in parts of its reduction, each summed up by itself."""
+    tiles = -(-M // 128) * -(-N // 128)
+    parts = min(256 // tiles, K // 512, 32)
+    return parts >= 2 and K - K // parts >= 1500
+
+
+def check_products(op, dz, dX, dW):
+    for got, want, what in ((dX, dz.double() @ op.W.double().t().contiguous(), "dX"), (dW.view(op.I, op.O), op.X.double().t().contiguous() @ dz.double(), "dW")):
+        close(got, want, 2.0 ** -8 * want.abs() + 1e-3 * want.square().mean().sqrt(), what)
+
+
 # ---- backward ---------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 @pytest.mark.parametrize("act", R.NAMES)
@@ -270,7 +287,31 @@ def test_backward(shape, act):
     ref = Op(*shape)
     rX, rW = torch.full_like(dX, float("nan")), [torch.full_like(w, float("nan")) for w in ref.w]
     osdp.osdp_split_linear_bwd(ref.X, dY if dz is None else dz, ref.w, rX, rW, ref.k, ref.workspace(True), plan=ref.plan)
-    assert torch.equal(dX, rX) and torch.equal(dW, torch.cat(rW)[:op.I * op.O])
+    check_products(op, dY if dz is None else dz, dX, dW)
+    T, I, O = op.T, op.I, op.O
+    if not (in_parts(T, O, I) or T <= 128 and O > 1000):
+        assert torch.equal(dX, rX)
+    if not in_parts(I, T, O):
+        assert torch.equal(dW, torch.cat(rW)[:op.I * op.O])
+
+
+@pytest.mark.parametrize("T,I,O", [(2, 272, 14464), (100, 64, 8192), (300, 256, 8192), (8192, 512, 512), (4100, 544, 544), (3000, 128, 64), (5000, 64, 8192)])
+@pytest.mark.parametrize("place", ["apart", "dX for X"])
+def test_products_of_few_tiles(T, I, O, place):
+    """Those that run in parts, whatever the cut and the shards, and dX in the place of X."""
+    dY, Z = rand(T, O, seed=5), rand(T, O, seed=6)
+    first = None
+    for N, k, split in [(1, 1, 0), (8, 4, 0), (8, 2, 1), (4, 2, 3)]:
+        op = Op(T, I, O, N, k, split)
+        X, dz, dW = op.X.clone(), op.out(), [torch.full_like(s, float("nan")) for s in op.w]
+        dX = op.X if place == "dX for X" else torch.full_like(X, float("nan"))
+        osdp.osdp_split_linear_bwd_epilogue(op.X, dY, op.w, dX, dW, k, op.workspace(True), plan=op.plan,
+                                            epilogue=osdp.EpilogueGrad(activation=ACTS["silu"], z=Z, dz=dz, dbias=torch.empty(O, device="cuda")))
+        op.X = X
+        dW = torch.cat(dW)[:I * O]
+        check_products(op, dz, dX, dW)
+        assert first is None or torch.equal(dW, first)
+        first = dW
 
 
 def test_the_gradients_are_the_differences_of_the_forward_pass():
