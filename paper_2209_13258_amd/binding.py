@@ -15,6 +15,7 @@ from typing import Optional, Sequence
 from . import build as _build
 
 try:
+    from . import _pointers as _calls
     from ._pointers import pointers as _checked_pointers
 except ImportError as e:
     raise ImportError(f"{_build.POINTERS} is missing or of another Python: build it first (python paper_2209_13258_amd/build.py)") from e
@@ -231,6 +232,8 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+_calls.connect(*[ctypes.cast(f, ctypes.c_void_p).value for f in (lib.hipGetDevice, lib.osdp_qk_norm_rope_fwd, lib.osdp_qk_norm_rope_bwd,
+                                                                 lib.osdp_split_linear_fwd_epilogue, lib.osdp_split_linear_bwd_epilogue)])
 
 
 def _check(status: int) -> None:
@@ -767,6 +770,11 @@ def osdp_split_linear_epilogue_workspace_bytes(T, I, O, N, k, is_bwd: bool, plan
 def osdp_split_linear_fwd_epilogue(X, w_shards, Y, k, workspace, *, epilogue: Epilogue, plan: Optional[Plan] = None,
                                    op_index: int = 0, w_dp=None, ld_dp: int = 0, stream_compute=None, stream_copy=None):
     """Y[T x O] = activation(X[T x I] . W + bias) + residual; W as N shard tensors, and ``w_dp`` for slices in DP mode."""
+    if w_dp is None:
+        status = _calls.linear(X, w_shards, Y, k, workspace, plan, op_index, _stream(stream_compute), _stream(stream_copy),
+                               epilogue.activation, epilogue.z, epilogue.bias, epilogue.residual)
+        if status is not None:
+            return _check(status)
     T, I = X.shape
     O = Y.shape[1]
     device = _here(X, "X")
@@ -788,6 +796,11 @@ def osdp_split_linear_bwd_epilogue(X, dY, w_shards, dX, dw_shards, k, workspace,
                                    plan: Optional[Plan] = None, op_index: int = 0, w_dp=None, ld_dp: int = 0, dw_dp=None,
                                    stream_compute=None, stream_copy=None):
     """dz and dbias, then dX[T x I] and the shard-major dW from them; ``w_dp`` and ``dw_dp`` for slices in DP mode."""
+    if w_dp is None:
+        status = _calls.linear(X, w_shards, dY, k, workspace, plan, op_index, _stream(stream_compute), _stream(stream_copy),
+                               epilogue.activation, epilogue.z, epilogue.dbias, epilogue.dz, dX, dw_shards)
+        if status is not None:
+            return _check(status)
     T, I = X.shape
     O = dY.shape[1]
     device = _here(X, "X")
@@ -844,6 +857,9 @@ def osdp_qk_norm_rope_fwd(q, k, q_out, k_out, *, positions=None, freqs=None, q_w
     """Norms of queries and keys and their rotation: bf16 tensors [tokens, heads, D] of any strides (views of the qkv operator's
     output); ``positions`` int64 [tokens] (None: 0, 1, ..; negative: padding), ``freqs`` float64 [rotary / 2] (None: no rotation),
     weights bf16 or fp32 [D] (None: ones).  ``q_out`` may be q and ``k_out`` k."""
+    status = _calls.qk((q, k, q_out, k_out), positions, freqs, q_weight, k_weight, None, None, None, eps, norm, interleaved, _stream(stream))
+    if status is not None:
+        return _check(status)
     device = _here(q, "q")
     desc = _qk(q, k, device, positions, freqs, q_weight, k_weight, eps, norm, interleaved)
     _check(lib.osdp_qk_norm_rope_fwd(desc, _heads(q, "q", q.shape, device), _heads(k, "k", k.shape, device),
@@ -860,6 +876,10 @@ def osdp_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, wo
                           k_weight=None, eps: float = 1e-6, norm: bool = True, interleaved: bool = False, stream=None) -> None:
     """The pass back: ``q``, ``k`` and the rest as the forward call had them; ``dq`` (may be q or dq_out), ``dk``, and the weights'
     gradients (written, or None; of one type with the weights) from ``dq_out`` and ``dk_out``."""
+    status = _calls.qk((q, k, dq_out, dk_out, dq, dk), positions, freqs, q_weight, k_weight, dq_weight, dk_weight, workspace, eps, norm,
+                       interleaved, _stream(stream))
+    if status is not None:
+        return _check(status)
     device = _here(q, "q")
     desc = _qk(q, k, device, positions, freqs, q_weight, k_weight, eps, norm, interleaved)
     at = [None, None]

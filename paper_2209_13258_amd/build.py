@@ -44,7 +44,7 @@ def build_pointers() -> Path:
     """Compile csrc/pointers.c into paper_2209_13258_amd/_pointers.so, a module of the Python that runs."""
     tmp = POINTERS.with_suffix(f".so.tmp{os.getpid()}")
     subprocess.run(["gcc", "-O2", "-std=c11", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-Wextra", "-Wno-missing-field-initializers",
-                    f"-I{sysconfig.get_paths()['include']}", str(CSRC / "pointers.c"), "-o", str(tmp)], check=True)
+                    f"-I{sysconfig.get_paths()['include']}", f"-I{ROOT / 'include'}", str(CSRC / "pointers.c"), "-o", str(tmp)], check=True)
     os.replace(tmp, POINTERS)
     return POINTERS
 

@@ -232,3 +232,21 @@ def test_qk_workspace_sizes():
 def test_struct_layouts_match_the_header():
     assert ctypes.sizeof(B.osdp_epilogue) == 48 and ctypes.sizeof(B.osdp_epilogue_grad) == 48
     assert ctypes.sizeof(B.osdp_qk) == 80 and ctypes.sizeof(B.osdp_heads) == 24
+
+
+def test_the_short_way_into_the_library_answers_only_what_it_knows():
+    """Anything but the common call is left to Python: None, and nothing raised."""
+    calls, t = B._calls, torch.zeros(4, 2, 64).bfloat16()
+    assert calls.qk() is None and calls.qk(1, 2, 3) is None and calls.linear() is None and calls.linear(*range(13)) is None and calls.linear(*range(15)) is None
+    for heads_ in ((t,) * 4, (t,) * 5, (1, 2, 3, 4), ()):
+        assert calls.qk(heads_, None, None, None, None, None, None, None, 1e-6, True, False, None) is None
+    assert calls.qk((t,) * 4, None, None, None, None, None, None, None, 1, True, False, None) is None
+    X, w = torch.zeros(4, 64).bfloat16(), [torch.zeros(64 * 64).bfloat16()]
+    ws = torch.zeros(256, dtype=torch.uint8)
+    for plan in (None, osdp.Plan([1]), osdp.Plan([]), osdp.Plan([1.5]), osdp.Plan([1] * 100), "plan"):
+        assert calls.linear(X, w, X, 1, ws, plan, 0, None, None, 0, None, None, None) is None
+    assert calls.linear(X, [], X, 1, ws, None, 0, None, None, 0, None, None, None) is None
+    assert calls.linear(X, w * 65, X, 1, ws, None, 0, None, None, 0, None, None, None) is None
+    assert calls.linear(X, [None], X, 1 << 80, ws, None, 0, "s", None, 0, None, None, None) is None
+    with pytest.raises(TypeError):
+        calls.connect(1, 2)
