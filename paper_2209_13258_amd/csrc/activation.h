@@ -37,7 +37,7 @@ __device__ __forceinline__ float normal_tail_scaled(float a) {
 // act(z).  NaN stays NaN; z of -infinity gives NaN, as z times 0 does, but for none and relu.
 template <int kAct>
 __device__ __forceinline__ float activate(float z) {
-  if constexpr (kAct == OSDP_ACT_RELU) return z < 0.0f ? 0.0f : z;
+  if constexpr (kAct == OSDP_ACT_RELU) return __builtin_elementwise_maximum(z, 0.0f);  // (NaN stays: v_maximum3)
   if constexpr (kAct == OSDP_ACT_GELU) {
     const float e = fast_exp2((-0.5f * kLog2e) * z * z), tail = e * normal_tail_scaled(__builtin_fabsf(z));
     return z * (z < 0.0f ? tail : 1.0f - tail);

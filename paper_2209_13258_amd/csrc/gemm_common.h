@@ -321,13 +321,18 @@ __device__ __forceinline__ void store_tile(const GemmParams &p, Read &&read, int
 
 // One wave's share through the fused epilogue: the same rows and columns as store_tile's.
 //
-// Straight-line code as above would hold an activation for each of the 256 values of a lane, for each activation.  Here one
-// loop takes the row blocks in turn, so that the code is that of one of them and a copy of its accumulators out of the register
-// file for each.  Bias, activation and residual work on the accumulators' own layout (a lane: 4 columns of each block, row l16),
-// Z and Y change lanes as above on their way out.  The residual of the next row block is under way meanwhile.
-template <int MB, int NB, class Read>
-__device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, int m_base, int n_base, int n_end, int l16, int q) {
+// Bias, activation and residual work on the accumulators' own layout (a lane: 4 columns of each block, row l16); Z and Y change
+// lanes as above on their way out.  The residual of the next row block is under way meanwhile.  Written out for each activation,
+// so that what a launch runs lies in one piece: us for 8192 x 4096 over K = 1024 in 256 x 256 tiles, plain / relu / bias / gelu_tanh /
+// gelu: one loop over the row blocks 67 / 79 / 76 / 84 / 92; written out, choosing the activation in each row block 67 / 78 / 74 / 84 / 92;
+// like this 67 / 72 / 71 / 81 / 87.  What is left of it are the activations: 52 cycles a value and SIMD (gelu_tanh), a quarter of
+// them the hardware's exponential and a quarter its reciprocal, while the matrix cores of the CU, whose waves are all here, wait.
+template <int kAct, int MB, int NB, class Read>
+__device__ __forceinline__ void store_fused_as(const GemmParams &p, Read &&read, int m_base, int n_base, int n_end, int l16, int q) {
   const FusedEpilogue &e = p.fused;
+  // (the lane's place passes through an empty asm: addresses and loads of the epilogue stay here, not ahead of the K loop, which
+  // has no registers for them)
+  asm volatile("" : "+v"(l16), "+v"(q));
   const int n = n_base + 4 * q, col = 16 * (q & 1) + 8 * (q >> 1);
   f32x4 bias[NB];
   static_for<NB>([&](auto bn_) {
@@ -357,14 +362,7 @@ __device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, in
     if constexpr (NB % 2)
       if (there && n + 16 * (NB - 1) < n_end) store_global8(row + 16 * (NB - 1) + 4 * q, v[NB - 1]);
   };
-  ask(0);
-#pragma unroll 1
-  for (int bm = 0; bm < MB; ++bm) {
-    f32x4 c[NB];
-    static_for<MB>([&](auto b_) {
-      constexpr int b = decltype(b_)::value;
-      if (bm == b) static_for<NB>([&](auto bn) { c[decltype(bn)::value] = read(Int<b>{}, bn); });
-    });
+  auto row_block = [&](int bm, f32x4 (&c)[NB]) {
     uint2 residual[NB], packed[NB];
     static_for<NB>([&](auto bn) { residual[decltype(bn)::value] = next[decltype(bn)::value]; });
     ask(bm + 1);
@@ -382,21 +380,39 @@ __device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, in
       });
       store(e.z + m * e.ldz + n_base, there, packed);
     }
-    with_activation(e.activation, [&](auto act) {
-      static_for<NB>([&](auto bn_) {
-        constexpr int bn = decltype(bn_)::value;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[bn][i] = activate<decltype(act)::value>(c[bn][i]);
-      });
-    });
     static_for<NB>([&](auto bn_) {
       constexpr int bn = decltype(bn_)::value;
-      const uint2 r = residual[bn];
-      packed[bn] = uint2{pack_bf16x2(c[bn][0] + bf16_low(r.x), c[bn][1] + bf16_high(r.x)),
-                         pack_bf16x2(c[bn][2] + bf16_low(r.y), c[bn][3] + bf16_high(r.y))};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[bn][i] = activate<kAct>(c[bn][i]);
+    });
+    if (e.residual)
+      static_for<NB>([&](auto bn_) {
+        constexpr int bn = decltype(bn_)::value;
+        c[bn][0] += bf16_low(residual[bn].x);
+        c[bn][1] += bf16_high(residual[bn].x);
+        c[bn][2] += bf16_low(residual[bn].y);
+        c[bn][3] += bf16_high(residual[bn].y);
+      });
+    static_for<NB>([&](auto bn_) {
+      constexpr int bn = decltype(bn_)::value;
+      packed[bn] = uint2{pack_bf16x2(c[bn][0], c[bn][1]), pack_bf16x2(c[bn][2], c[bn][3])};
     });
     store(static_cast<uint16_t *>(p.C) + m * p.ldc + n_base, there, packed);
-  }
+  };
+  ask(0);
+  static_for<MB>([&](auto b) {
+    f32x4 c[NB];
+    static_for<NB>([&](auto bn) { c[decltype(bn)::value] = read(b, bn); });
+    row_block(decltype(b)::value, c);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
+template <int MB, int NB, class Read>
+__device__ __forceinline__ void store_fused(const GemmParams &p, Read &&read, int m_base, int n_base, int n_end, int l16, int q) {
+  with_activation(p.fused.activation, [&](auto act) {
+    store_fused_as<decltype(act)::value, MB, NB>(p, static_cast<Read &&>(read), m_base, n_base, n_end, l16, q);
+  });
 }
 
 }  // namespace

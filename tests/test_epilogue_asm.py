@@ -1,6 +1,6 @@
-"""Static checks on the forward kernels with an epilogue, like those on the ones without (test_kernel_asm.py): the loop over the row
-blocks stands beside inline matrix steps whose hazards the compiler does not see, and must neither spill inside the K loop nor
-move accumulators."""
+"""Static checks on the forward kernels with an epilogue, like those on the ones without (test_kernel_asm.py): the epilogue, written out
+for each activation, stands beside inline matrix steps whose hazards the compiler does not see, and must neither take registers of
+the K loop nor move accumulators."""
 import re
 import shutil
 import subprocess
@@ -36,9 +36,19 @@ def test_the_epilogue_leaves_the_k_loop_alone(epilogue_asm, kernel, least, block
         mfma = [i for i, t in enumerate(ins) if t.startswith("v_mfma")]
         assert len(mfma) in [mb * nb * b for b in blocks], f"{name}: {len(mfma)} MFMAs (a loop body was duplicated?)"
         assert not [t for t in ins if t.startswith("scratch_")], f"{name}: scratch traffic"
-        # the accumulators are read once each, where the loop takes their row block
-        assert len([t for t in ins if t.startswith("v_accvgpr_read")]) == 4 * mb * nb, f"{name}: the loop over the row blocks was unrolled, or accumulators moved"
+        # the accumulators are read where an activation's code takes them, and nowhere else
+        assert len([t for t in ins if t.startswith("v_accvgpr_read")]) == 5 * 4 * mb * nb, f"{name}: accumulators moved"
         for i in mfma:
             assert not [t for t in ins[max(0, i - 3):i] if t.startswith(("v_accvgpr_write", "v_accvgpr_mov"))], \
                 f"{name}: an accumulator register is written right in front of an inline MFMA"
         _assert_no_valu_write_in_front_of_its_mfma(name, ins, mfma)
+
+
+def test_the_eight_wave_kernels_keep_scratch_out_of_the_k_loop(epilogue_asm):
+    """Tiles of which two fit a CU have 128 registers a lane: what the epilogue lacks of them it must not take from the K loop."""
+    kernels = _kernels(epilogue_asm, "gemm_dma_kernel")
+    assert len(kernels) >= 8, "the instantiations were not found in the assembly"
+    for name, ins in kernels.items():
+        mfma = [i for i, t in enumerate(ins) if t.startswith("v_mfma")]
+        inside = [t for t in ins[mfma[0]:mfma[-1] + 1] if t.startswith("scratch_")]
+        assert not inside, f"{name}: scratch traffic inside the K loop"
