@@ -363,7 +363,10 @@ __global__ __launch_bounds__(1024) void qk_weight_kernel(QkParams p, int split, 
   else static_cast<__bf16 *>(out)[d] = static_cast<__bf16>(s_sum[threadIdx.x]);
 }
 
-constexpr int kMaxBackwardGroups = 1024;
+// Workgroups of the pass back: three to a CU, which is what its registers let run, so that all of them run from the start.  us for 8192
+// tokens, 32 + 8 heads of 128, with the sums' launch: 768 58, 1024 71; one head group at a time 79; held to 128 registers, which
+// spills, 1024 60.
+constexpr int kMaxBackwardGroups = 768;
 
 int log2_up(int64_t n) {
   int l = 0;
