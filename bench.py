@@ -67,6 +67,9 @@ def parse():
                          "all shards, with fp32 master copies and moments in 32 or 8 bits")
     ap.add_argument("--int8", action="store_true",
                     help="also time the workload's forward pass with its weights in 8-bit integers, and making them from the shards")
+    ap.add_argument("--epilogue", action="store_true",
+                    help="also time the step with what stands around its products in a transformer layer: biases, the inner operator's "
+                         "activation, residuals, and the norms and rotation of queries and keys, forward and backward")
     return ap.parse_args()
 
 
@@ -228,6 +231,53 @@ def int8_forward(st, iters, warmup):
     tq, t8, t16 = (median_ms(torch, call, iters, warmup, st.sc) for call in (make, forward, st.forward))
     return {"median_ms": round(t8, 4), "tops": round(ops / (t8 * 1e-3) / 1e12, 2), "bf16_median_ms": round(t16, 4),
             "bf16_tflops": round(ops / (t16 * 1e-3) / 1e12, 2), "quantize_ms": round(tq, 4)}
+
+
+def epilogue_step(st, iters, warmup):
+    """The step with a bias in every operator, gelu behind `up` (and an operator that stands alone), a residual onto `proj` and
+    `down`, and the norms and rotation of `qkv`'s queries and keys in heads of 128; and the step without any of it."""
+    torch, osdp, w = st.torch, st.osdp, st.w
+    new = lambda t: torch.empty_like(t)  # noqa: E731
+    need, extra = 256, {}
+    for d in st.ops:
+        op = d["op"]
+        for bwd in (False, True):
+            need = max(need, osdp.osdp_split_linear_epilogue_workspace_bytes(w.T, op.I, op.O, w.N, 0, bwd, st.plan, d["n"])[0])
+        x = extra[id(d)] = dict(bias=torch.zeros(op.O, device="cuda"), act=osdp.OSDP_ACT_NONE, residual=None, z=None, dz=None, dY=d["dY"])
+        x["db"] = new(x["bias"])
+        if op.name in ("up", "lin"):
+            x.update(act=osdp.OSDP_ACT_GELU_TANH, z=new(d["Y"]), dz=new(d["Y"]))
+        elif op.name != "qkv":
+            x["residual"] = d["dY"]
+        elif op.O % 384 == 0:
+            heads = lambda t, i, n=op.O // 384: t[:, 128 * n * i:128 * n * (i + 1)].unflatten(1, (n, 128))  # noqa: E731
+            out, x["dY"] = new(d["Y"]), d["dY"].clone()
+            x["heads"] = [[heads(t, i) for i in range(2)] for t in (d["Y"], out, d["dY"], x["dY"])]
+            x["g"] = [torch.ones(128, device="cuda") for _ in range(2)]
+            x["dg"] = [new(g) for g in x["g"]]
+            need = max(need, osdp.osdp_qk_norm_rope_bwd_workspace_bytes(w.T, op.O // 384, op.O // 384, 128))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    freqs = 10000.0 ** (-torch.arange(64, device="cuda", dtype=torch.float64) / 64)
+
+    def step():
+        streams = dict(plan=st.plan, stream_compute=st.sc, stream_copy=st.sp)
+        for d in st.ops:
+            x = extra[id(d)]
+            osdp.osdp_split_linear_fwd_epilogue(d["X"], d["W"], d["Y"], 0, ws, op_index=d["n"], **streams,
+                                                epilogue=osdp.Epilogue(bias=x["bias"], activation=x["act"], residual=x["residual"], z=x["z"]))
+            if "heads" in x:
+                h = x["heads"]
+                osdp.osdp_qk_norm_rope_fwd(*h[0], *h[1], freqs=freqs, q_weight=x["g"][0], k_weight=x["g"][1], stream=st.sc)
+        for d in reversed(st.ops):
+            x = extra[id(d)]
+            if "heads" in x:
+                h = x["heads"]
+                osdp.osdp_qk_norm_rope_bwd(*h[0], *h[2], *h[3], *x["dg"], ws, freqs=freqs, q_weight=x["g"][0], k_weight=x["g"][1], stream=st.sc)
+            osdp.osdp_split_linear_bwd_epilogue(d["X"], x["dY"], d["W"], d["dX"], d["dW"], 0, ws, op_index=d["n"], **streams,
+                                                epilogue=osdp.EpilogueGrad(activation=x["act"], z=x["z"], dz=x["dz"], dbias=x["db"]))
+    flops = w.layers * sum(6 * w.T * op.I * op.O for op in w.ops)
+    ms, plain = (median_ms(torch, call, iters, warmup, st.sc) for call in (step, st.step))
+    return {"median_ms_per_step": round(ms, 4), "tflops": round(flops / (ms * 1e-3) / 1e12, 2), "products_alone_ms_per_step": round(plain, 4)}
 
 
 def per_step_times(st, iters, warmup, serial):
@@ -685,6 +735,8 @@ def main():
         out["plan_search"] = plan_search(w, m["kernels"], staging, rows, torch, osdp, sub_steps, sub_warm)
     if a.int8:
         out["int8_forward"] = int8_forward(st, sub_steps, sub_warm)
+    if a.epilogue and a.zdp_slices is None:
+        out["epilogue_step"] = epilogue_step(st, sub_steps, sub_warm)
     if a.adamw:
         out["training_step"] = training_step(st, int(a.adamw), sub_steps, sub_warm)
     if not a.no_auto:
