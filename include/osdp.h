@@ -305,9 +305,11 @@ OSDP_API osdp_status osdp_split_linear_bwd_mixed(const osdp_shape *shape, const 
  *              gelu    z * Phi(z), Phi the normal distribution function
  *              gelu_tanh  z / 2 * (1 + tanh( sqrt(2 / pi) * (z + 0.044715 z^3) ))
  *              silu    z / (1 + exp(-z))
- * Activations and slopes are computed in fp32, off by less than 2^-15 relative (the slopes: of 1) before the rounding.  NaN in
+ * Activations and slopes are computed in fp32, off by less than 2^-15 relative (the slopes: of 1) before the rounding, but that
+ * gelu, gelu_tanh and silu may give 0 in the place of what is smaller than 2^-118.  NaN in
  * gives NaN out (relu's slope at NaN is 1); z of minus infinity gives NaN in gelu, gelu_tanh and silu, as minus infinity
- * times 0 does.  Without bias, activation, residual and Z the calls are osdp_split_linear_fwd_mixed and _bwd_mixed, bit for bit.
+ * times 0 does, and their slopes are NaN at either infinity.
+ * Without bias, activation, residual and Z the calls are osdp_split_linear_fwd_mixed and _bwd_mixed, bit for bit.
  * b and db are replicated vectors: fp32 or bf16, alike, 16-byte aligned, O elements. */
 
 typedef enum { OSDP_BF16 = 0, OSDP_F32 = 1 } osdp_dtype;
@@ -341,22 +343,28 @@ typedef struct {
   int32_t bias_type;    /* an osdp_dtype                                                             */
 } osdp_epilogue_grad;
 
-/* Bytes of workspace of the two calls below: those of osdp_split_linear_workspace_bytes, and, backward, the partial sums of
- * db behind them. */
+/* Bytes of workspace of the two calls below: those of osdp_split_linear_workspace_bytes; behind them, backward, the partial sums
+ * of db, and the fp32 planes of products that are summed in parts (see below; some MiB for few tokens and wide operators). */
 OSDP_API osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape *shape, const osdp_plan *plan,
                                                                 int32_t op_index, int32_t is_bwd, size_t *total,
                                                                 size_t *peak_weight_staging);
 
-/* Forward.  Plans, modes (w_dp: NULL when no slice is DP), few tokens and streams as osdp_split_linear_fwd_mixed.  Y and Z
- * overlap no input, each other or the workspace, but for a residual that is Y. */
+/* Forward.  Plans, modes (w_dp: NULL when no slice is DP) and streams as osdp_split_linear_fwd_mixed.  Y and Z
+ * overlap no input, each other or the workspace, but for a residual that is Y.
+ * Shards that are row blocks of a multiple of 64 rows are read where they lie for any T, unless slices are in DP mode; nothing is
+ * gathered then.  A long reduction with few outputs (less than half a 128 x 128 tile of Y for each CU, or T <= 128) is summed in
+ * parts of it, each accumulated on its own, added in ascending order in fp32.  The order of Y's additions is a matter of T, I, O and
+ * whether the shards are such row blocks: Y is bit-identical for every k, staging mode, stream choice and mode of the slices, as
+ * above, but for T > 128 with row slices that are staged or in DP mode and cannot be taken as column slices instead: these continue one chain. */
 OSDP_API osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
                                                     const osdp_epilogue *epilogue, const void *X, int64_t ldx,
                                                     const void *const *w_shards, const void *const *w_dp, int64_t ld_dp,
                                                     void *Y, int64_t ldy, void *workspace, size_t workspace_bytes,
                                                     void *stream_compute, void *stream_copy);
 
-/* Backward: one pass for dZ and db, then osdp_split_linear_bwd_mixed with dZ in the place of dY (which also says what dX may
- * take the place of: X, or with few tokens dZ).  db is the sum in fp32 in an order that T and O alone decide, rounded once if
+/* Backward: one pass for dZ and db, then the products of osdp_split_linear_bwd_mixed with dZ in the place of dY (which also says
+ * what dX may take the place of: X, or with few tokens dZ); shards are read in place and products summed in parts as above, dX's
+ * over O and dW's over T.  db is the sum in fp32 in an order that T and O alone decide, rounded once if
  * bias_type asks for it.  T = 0 stores db = 0 and dW = 0. */
 OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
                                                     const osdp_epilogue_grad *epilogue, const void *X, int64_t ldx,

@@ -853,8 +853,10 @@ bool switches_pay(const Resolved &r) {
 }
 
 // dX over the shards in place: its tiles do not reach over the end of a shard, which may cost more than the copies, and the trips
-// of a sum through memory (see recut), that it saves.  us in place / staged: 16384 tokens 2560 -> 10240 over 8 shards (320 rows,
-// two tiles of 160), k = 4 XX / 907; unsplit, staged in one piece, XX.
+// of a sum through memory (see recut), that it saves.  us of a backward pass with dX in place / staged: 16384 tokens 2560 -> 10240
+// over 8 shards (320 rows, two tiles of 160) 1648 / 1578, four slices 1600 / 1786; 8192 tokens 1024 -> 4096, four slices 148 / 207;
+// 2048 tokens 4096 -> 4096 over 64 shards (64 rows: narrow tiles) 179 / 138, four slices 185 / 197; 1000 tokens 4096 -> 16384 300 / 348.
+// What is estimated to be faster was so in each of these.
 bool shards_pay_dx(const Resolved &r) {
   double staged = 0.0;
   for (size_t j = 0; j < r.sub.size(); ++j) staged += gather_estimate_us(r.D * (r.sub[j].c1 - r.sub[j].c0));
@@ -1065,11 +1067,7 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
   }
   if (in_place && r.any_dp && r.T <= kSkinnyMaxTokens) {
     const std::vector<Slice> runs = runs_in_place(r, true);
-    for (const Slice &l : runs) {
-      GemmProblem g = run_gemm(r, true, l, tab, rep, X, ldx, Y, ldy);
-      fuse(&g, r.sub[l.c0].c0, true);
-      OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
-    }
+    for (const Slice &l : runs) OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, run_gemm(r, true, l, tab, rep, X, ldx, Y, ldy), sc));
     if (!runs.empty()) return OSDP_OK;
   }
   // Launches that hold the whole reduction may run in parts of it; slices that cannot be cut the other way go on in one chain.

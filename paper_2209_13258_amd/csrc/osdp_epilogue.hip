@@ -1,7 +1,9 @@
 // What stands around the products of the split operator:
 //   forward   Z = X . W + b,  Y = act(Z) + R      in the product's epilogue (store_fused in gemm_common.h)
 //   backward  dZ = dY * act'(Z),  db = sum over tokens of dZ      in one pass in front of the product's backward
-// The products are those of osdp_gemm.hip, in the same order of additions: without bias, activation and residual Y has the same bits.
+// The products are the kernels of osdp_gemm.hip.  Two things are done for them that the calls without an epilogue do not do, whose
+// order of additions is promised: shards are read in place for any number of tokens, and products of few output tiles run in parts
+// of the reduction, so that every CU has some, with a launch that adds the parts' planes up and goes through the epilogue.
 #include "gemm_launch.h"
 
 namespace osdp {
@@ -9,7 +11,8 @@ namespace osdp {
 namespace {
 // Few tokens: rows of a tile, and the length of a part of the reduction.
 // A workgroup streams 2 (rows + 64) bytes a unit of K at some 38 KB a us, where they come from a cache, and takes 8 us to start and
-// to store; the weights come from memory once, at 5 TB/s; parts cost the planes' way out and back and a launch.
+// to store; the weights come from memory once, at 5 TB/s; parts cost the planes' way out and back and a launch.  us in the parts
+// that this finds / in one: 1 token 4096 -> 4096 15.1 / 21.3, 33 tokens 8192 -> 1024 15.2 / 34.3, 128 tokens 16384 -> 2560 44.9 / 82.5.
 struct SkinnyPlan {
   int rows;
   int64_t k_per;
@@ -65,6 +68,8 @@ hipError_t launch_skinny_fused(const WeightMap &w, int64_t T, const void *X, int
 
 int64_t fused_k_per(int64_t M, int64_t K, int64_t N) {
   // Of 128 x 128 tiles, one to a CU: 0.0105 us a unit of K.  The parts' planes and the launch that adds them up: some 11 us.
+  // us in parts / in one: forward 300 tokens 8192 -> 1024 20.5 / 61.7, 500 tokens 4096 -> 1024 21.0 / 39.3; backward (the
+  // pass for db, dX and dW) 300 tokens 1024 -> 8192 35 / 75, 8192 tokens 512 -> 512 36 / 75, 16384 tokens 256 -> 1024 51 / 137.
   const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
   const int64_t parts = std::min<int64_t>({kCUs / std::max<int64_t>(tiles, 1), K / 512, 32});
   if (parts < 2 || K - K / parts < 1500) return K;
@@ -79,15 +84,16 @@ size_t planes_of(int64_t M, int64_t K, int64_t N, int64_t k_per) {
 }  // namespace
 
 // Where no shard is a whole number of K blocks only the few-token kernel reads the weights in place, at a third of the tiles'
-// rate.  More tokens than its own are worth that while the copy (4 bytes an element at 5.5 TB/s and a launch) and the tiles behind it,
-// each one's latency, take longer.  By T, I and O alone: the unsplit copy is what counts, so that Y is the same for every k.
+// rate.  More tokens than its own are worth that while the copy and the tiles behind it, each one's latency, take longer: three
+// quarters of what they would take one after the other, and the launches.  By T, I and O alone: the unsplit copy is what counts, so
+// that Y is the same for every k.  us in place / staged: 200 tokens 1024 -> 1024 10.3 / 15.0, 1000 tokens 13.4 / 16.3, 160 tokens
+// 8160 -> 1024 22.8 / 29.4, 300 tokens 2560 -> 2560 23.2 / 25.4; 400 tokens 4032 -> 4032 51 / 40.5.
 bool skinny_beats_copy(int64_t T, int64_t I, int64_t O) {
   const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), k_per = fused_k_per(T, I, O), parts = (I + k_per - 1) / k_per;
   const double flops = 2.0 * static_cast<double>(T) * static_cast<double>(I) * static_cast<double>(O);
-  const double tile = std::max(flops / 0.9e9, 0.0105 * static_cast<double>(std::min(k_per, I)) * static_cast<double>((tiles * parts + kCUs - 1) / kCUs)) +
-                      (parts > 1 ? 17.0 : 6.0);
+  const double tile = std::max(flops / 0.9e9, 0.0105 * static_cast<double>(std::min(k_per, I)) * static_cast<double>((tiles * parts + kCUs - 1) / kCUs));
   const double copy = 4.0 * static_cast<double>(I) * static_cast<double>(O) / 5.5e6 + 6.0;
-  return skinny_plan(T, I, O).us < copy + tile;
+  return skinny_plan(T, I, O).us < 0.75 * (copy + tile) + (parts > 1 ? 12.0 : 3.0);
 }
 
 bool fused_takes_skinny(int64_t T, int64_t ldx, const ShardLayout &lay, int64_t I) {
@@ -108,7 +114,8 @@ size_t fused_planes_bytes(int64_t T, int64_t I, int64_t O) {
 }
 
 int64_t skinny_dx_per(int64_t T, int64_t I, int64_t O) {
-  // (worth the sums' own launch, and one for dW that would otherwise share dX's)
+  // (worth the sums' own launch, and one for dW that would otherwise share dX's.  us of a backward pass in parts / in one: 33 tokens
+  // 1024 -> 8192 26.2 / 35.6, 100 tokens 2560 -> 16384 74 / 83)
   const SkinnyPlan plan = skinny_plan(T, O, I, 256), whole = skinny_plan(T, O, I, O);
   return plan.us + 6.0 < whole.us ? plan.k_per : O;
 }
@@ -147,7 +154,7 @@ namespace {
 // adds the planes in ascending order.  No atomics: the same inputs give the same bits.
 struct SlopeParams {
   int64_t T;
-  int32_t O, activation, lanes_log2, rows_per_group;
+  int32_t O, lanes_log2, rows_per_group;
   const uint16_t *dY;
   int64_t lddy;
   const uint16_t *Z;
@@ -297,7 +304,7 @@ hipError_t launch_slope(const SlopeProblem &q, void *workspace, hipStream_t stre
   const SlopeGrid g = slope_grid(q.T, q.O);
   SlopeParams p{};
   p.T = q.T; p.O = static_cast<int32_t>(q.O);
-  p.activation = q.activation; p.lanes_log2 = g.lanes_log2; p.rows_per_group = g.rows;
+  p.lanes_log2 = g.lanes_log2; p.rows_per_group = g.rows;
   p.dY = static_cast<const uint16_t *>(q.dY); p.lddy = q.lddy;
   p.Z = static_cast<const uint16_t *>(q.Z); p.ldz = q.ldz;
   p.dZ = static_cast<uint16_t *>(q.dZ); p.lddz = q.lddz;

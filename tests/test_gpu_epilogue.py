@@ -166,14 +166,15 @@ def test_every_kernel_gives_the_same_bits(switch, values):
                 assert torch.equal(got, want) and torch.equal(how["z"], want_z), (switch, v, T, N, k, split)
 
 
-@pytest.mark.parametrize("T", [20, 200, 900])
+@pytest.mark.parametrize("T,I,O", [(20, 512, 1024), (200, 512, 1024), (900, 512, 1024), (20, 4096, 512), (300, 4096, 512), (300, 512, 8192)])
 @pytest.mark.parametrize("split", [osdp.OSDP_SPLIT_OUT_FEATURES, osdp.OSDP_SPLIT_IN_FEATURES])
-def test_slices_in_dp_mode(T, split):
-    """Slices 0 and 2 of 4 replicated, the shards' part of them poisoned: the bits of the plan that gathers all."""
-    op, mixed = Op(T, 512, 1024, 8, 4, split), Op(T, 512, 1024, 8, 4, split, zdp=0b1010)
-    bias, residual = rand(1024, seed=1), rand(T, 1024, seed=2)
-    dY, Z = rand(T, 1024, seed=3), rand(T, 1024, seed=4)
-    full, step = mixed.W.contiguous(), (512 if split else 1024) // 4
+def test_slices_in_dp_mode(T, I, O, split):
+    """Slices 0 and 2 of 4 replicated, the shards' part of them poisoned: the bits of the plan that gathers all, but where slices that the
+    sum goes over are a chain and the whole runs in parts."""
+    op, mixed = Op(T, I, O, 8, 4, split), Op(T, I, O, 8, 4, split, zdp=0b1010)
+    bias, residual = rand(O, seed=1), rand(T, O, seed=2)
+    dY, Z = rand(T, O, seed=3), rand(T, O, seed=4)
+    full, step = mixed.W.contiguous(), (I if split else O) // 4
     replicas = [full[j * step:(j + 1) * step] if split else full[:, j * step:(j + 1) * step] for j in range(4)]
     w_dp = [replicas[j] if j in (0, 2) else None for j in range(4)]
     dw = torch.full_like(full, float("nan"))
@@ -182,17 +183,21 @@ def test_slices_in_dp_mode(T, split):
     want = op.fwd(op.out(), **how)
     got = mixed.out()
     osdp.osdp_split_linear_fwd_epilogue(mixed.X, mixed.w, got, 4, mixed.workspace(False), epilogue=osdp.Epilogue(**how), plan=mixed.plan, w_dp=w_dp,
-                                        ld_dp=1024)
-    assert torch.equal(got, want)
-    dz, dz2, db, db2 = op.out(), op.out(), torch.zeros(1024, device="cuda"), torch.ones(1024, device="cuda")
+                                        ld_dp=O)
+    check_forward(mixed, "relu", bias, residual, got)
+    assert T > 128 and split and in_parts(T, I, O) or torch.equal(got, want)
+    dz, dz2, db, db2 = op.out(), op.out(), torch.zeros(O, device="cuda"), torch.ones(O, device="cuda")
     dX, dW = op.bwd(dY, activation=ACTS["relu"], z=Z, dz=dz, dbias=db)
     dX2 = torch.full_like(dX, float("nan"))
     dws = [torch.full_like(s, float("nan")) for s in mixed.w]
-    osdp.osdp_split_linear_bwd_epilogue(mixed.X, dY, mixed.w, dX2, dws, 4, mixed.workspace(True), plan=mixed.plan, w_dp=w_dp, ld_dp=1024, dw_dp=dw_dp,
+    osdp.osdp_split_linear_bwd_epilogue(mixed.X, dY, mixed.w, dX2, dws, 4, mixed.workspace(True), plan=mixed.plan, w_dp=w_dp, ld_dp=O, dw_dp=dw_dp,
                                         epilogue=osdp.EpilogueGrad(activation=ACTS["relu"], z=Z, dz=dz2, dbias=db2))
-    assert torch.equal(dX2, dX) and torch.equal(dz2, dz) and torch.equal(db2, db)
-    flat = torch.cat(dws).view(512, 1024)
-    assert torch.equal(torch.where(torch.isnan(flat), dw, flat), dW.view(512, 1024))
+    assert torch.equal(dz2, dz) and torch.equal(db2, db)
+    flat = torch.cat(dws).view(I, O)
+    flat = torch.where(torch.isnan(flat), dw, flat)
+    check_products(mixed, dz, dX2, flat.flatten())
+    assert torch.equal(flat, dW.view(I, O))
+    assert T > 128 and not split and in_parts(T, O, I) or torch.equal(dX2, dX)
 
 
 @pytest.mark.parametrize("T", [9, 600])
@@ -381,11 +386,12 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(dz, dz2) and torch.equal(dX, dX2) and torch.equal(dW, dW2) and torch.equal(db, db2)
 
 
-@pytest.mark.parametrize("T", [4, 700])
-def test_a_captured_graph_replays_on_other_inputs(T):
+# (in one launch and staged; then what runs in parts: few tokens, tiles forward, tiles backward, few-token kernel for more of them)
+@pytest.mark.parametrize("T,I,O,N", [(4, 256, 512, 8), (700, 256, 512, 8), (33, 4096, 512, 8), (300, 4096, 512, 8), (4100, 512, 512, 8), (200, 1024, 1024, 32)])
+def test_a_captured_graph_replays_on_other_inputs(T, I, O, N):
     """Forward and backward captured once, replayed with new inputs in the same place, eager work in between."""
-    op = Op(T, 256, 512, 8, 2)
-    bias, residual, dY = rand(512, seed=1), rand(T, 512, seed=2), rand(T, 512, seed=3)
+    op = Op(T, I, O, N, 2)
+    bias, residual, dY = rand(O, seed=1), rand(T, O, seed=2), rand(T, O, seed=3)
     Y, Z, dz, db = op.out(), op.out(), op.out(), torch.empty_like(bias)
     dX, dW = torch.empty_like(op.X), [torch.empty_like(s) for s in op.w]
     wf, wb = op.workspace(False), op.workspace(True)
@@ -404,8 +410,8 @@ def test_a_captured_graph_replays_on_other_inputs(T):
     with torch.cuda.graph(graph, stream=stream):
         run(stream)
     for seed in range(4):
-        op.X.copy_(rand(T, 256, seed=50 + seed))
-        dY.copy_(rand(T, 512, seed=60 + seed))
+        op.X.copy_(rand(T, I, seed=50 + seed))
+        dY.copy_(rand(T, O, seed=60 + seed))
         outs = [Y, Z, dz, db, dX, *dW]
         for t in outs:
             t.fill_(float("nan"))
@@ -417,17 +423,17 @@ def test_a_captured_graph_replays_on_other_inputs(T):
         assert all(torch.equal(a, b) for a, b in zip(got, outs)), seed
 
 
-def test_two_streams_with_workspaces_of_their_own():
-    ops = [Op(700, 512, 1024, 8, 2, seed=s) for s in (0, 10)]
-    want = [op.fwd(op.out(), bias=rand(1024, seed=1), activation=ACTS["gelu"]) for op in ops]
-    streams = [torch.cuda.Stream() for _ in ops]
-    torch.cuda.synchronize()
+@pytest.mark.parametrize("T,I", [(700, 512), (40, 8192), (300, 8192)])
+def test_two_streams_with_workspaces_of_their_own(T, I):
+    ops = [Op(T, I, 1024, 8, 2, seed=s) for s in (0, 10)]
     bias = rand(1024, seed=1)
-    got = [op.out() for op in ops]
+    want = [op.fwd(op.out(), bias=bias, activation=ACTS["gelu"]) for op in ops]
+    streams, got, spaces = [torch.cuda.Stream() for _ in ops], [op.out() for op in ops], [op.workspace(False) for op in ops]
     torch.cuda.synchronize()
     for _ in range(5):
-        for op, y, s in zip(ops, got, streams):
-            op.fwd(y, stream=s, bias=bias, activation=ACTS["gelu"])
+        for op, y, s, ws in zip(ops, got, streams, spaces):
+            osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, y, op.k, ws, plan=op.plan, stream_compute=s,
+                                                epilogue=osdp.Epilogue(bias=bias, activation=ACTS["gelu"]))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
