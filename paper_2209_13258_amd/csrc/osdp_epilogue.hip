@@ -152,6 +152,8 @@ namespace {
 // lanes of them at a time; every lane keeps the sums of its 8 columns.  The sums of its row groups are added up through LDS in
 // ascending order, and, where more than one workgroup shares a column, written to a plane of the workspace; sum_planes_kernel
 // adds the planes in ascending order.  No atomics: the same inputs give the same bits.
+// HBM bound, 6 bytes an element: 8192 x 4096, gelu, 37 us (5.4 TB/s, its vector units busy all the while); 16384 x 10240, gelu_tanh,
+// 195 us (5.2 TB/s).  The sums cost 4 to 5 us beside that.
 struct SlopeParams {
   int64_t T;
   int32_t O, lanes_log2, rows_per_group;

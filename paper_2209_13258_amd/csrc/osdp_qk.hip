@@ -1,5 +1,6 @@
 // Norms of queries and keys for each head and their rotation by position, in one pass over the qkv operator's output, and the
-// pass back.  HBM bound: 4 bytes an element forward, 6 backward, against some 10 and 20 operations in fp32.
+// pass back.  HBM bound: 4 bytes an element forward, 6 backward, against some 10 and 20 operations in fp32.  8192 tokens, heads of
+// 128: forward 32 + 32 heads 57 us (4.7 TB/s), backward 32 + 8 heads 53 us (4.75 TB/s) and 5 us for the weights' sums.
 //
 // A head of D elements is held by a group of kG lanes (a power of two, 16 elements to a lane), so that its sum of squares takes
 // log2 kG steps between neighbouring lanes.  A lane's 16 elements are two pieces of 16 bytes, chosen so that both elements of every
