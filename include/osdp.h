@@ -351,10 +351,10 @@ OSDP_API osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape
 
 /* Forward.  Plans, modes (w_dp: NULL when no slice is DP) and streams as osdp_split_linear_fwd_mixed.  Y and Z
  * overlap no input, each other or the workspace, but for a residual that is Y.
- * Shards that are row blocks of a multiple of 64 rows are read where they lie for any T, unless slices are in DP mode; nothing is
- * gathered then.  A long reduction with few outputs (less than half a 128 x 128 tile of Y for each CU, or T <= 128) is summed in
+ * Shards that are row blocks of a multiple of 64 rows (backward: of 8), and a single shard, are read where they lie for any T,
+ * unless that is estimated to be slower or slices are in DP mode; nothing is gathered then.  A long reduction with few outputs (less than half a 128 x 128 tile of Y for each CU, or T <= 128) is summed in
  * parts of it, each accumulated on its own, added in ascending order in fp32.  The order of Y's additions is a matter of T, I, O and
- * whether the shards are such row blocks: Y is bit-identical for every k, staging mode, stream choice and mode of the slices, as
+ * whether the shards are row blocks of a multiple of 64 rows, or one: Y is bit-identical for every k, staging mode, stream choice and mode of the slices, as
  * above, but for T > 128 with row slices that are staged or in DP mode and cannot be taken as column slices instead: these continue one chain. */
 OSDP_API osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
                                                     const osdp_epilogue *epilogue, const void *X, int64_t ldx,

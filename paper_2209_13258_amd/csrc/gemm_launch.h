@@ -675,7 +675,7 @@ GemmParams gemm_params(const GemmProblem &q) {
 hipError_t launch_params(const GemmProblem &q, bool carry, GemmParams *out) {
   GemmParams &p = *out;
   p = gemm_params(q);
-  if (q.b_shard_rows && (!q.a_kcontig || q.acc_in || p.k_split || p.n_split || p.seg_k % 64)) return hipErrorInvalidValue;
+  if (q.b_shard_rows && (!q.a_kcontig || q.acc_in || p.k_split || p.n_split || p.seg_k % 64 || p.seg_n % 8)) return hipErrorInvalidValue;
   if (carry) {
     const GatherRequest &g = *q.carry;
     const uint64_t total = static_cast<uint64_t>(g.rows) * (static_cast<uint64_t>(g.w) / 8);

@@ -795,6 +795,16 @@ GemmProblem shard_gemm(const Resolved &r, bool is_fwd, const ShardTable &tab, co
   return g;
 }
 
+// The same for calls with an epilogue: one shard is a matrix like any other.
+GemmProblem shard_gemm_fused(const Resolved &r, bool is_fwd, const ShardTable &tab, const void *act, int64_t ld_act, void *out, int64_t ld_out) {
+  GemmProblem g = shard_gemm(r, is_fwd, tab, act, ld_act, out, ld_out);
+  if (r.N == 1) {
+    g.b_shard_rows = 0;
+    g.B = tab.p[0];
+  }
+  return g;
+}
+
 // A concatenating product of at most kSkinnyMaxTokens tokens whose gathered slices are neighbours, as are those in DP
 // mode, in one replica: one launch over the shards and one over the replica.  With one gathered slice a single launch over
 // both, the slice staged, is the faster one, and with more than two runs so are pairs of slices: each run is a launch of
@@ -858,6 +868,7 @@ bool switches_pay(const Resolved &r) {
 // 2048 tokens 4096 -> 4096 over 64 shards (64 rows: narrow tiles) 179 / 138, four slices 185 / 197; 1000 tokens 4096 -> 16384 300 / 348.
 // What is estimated to be faster was so in each of these.
 bool shards_pay_dx(const Resolved &r) {
+  if (r.N == 1) return true;
   double staged = 0.0;
   for (size_t j = 0; j < r.sub.size(); ++j) staged += gather_estimate_us(r.D * (r.sub[j].c1 - r.sub[j].c0));
   bool first = true;
@@ -1048,7 +1059,7 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
                    }));
     return OSDP_OK;
   }
-  const bool in_place = ep ? !r.any_dp && gemm_reads_shards(r.T, ldx, r.layout, true) && switches_pay(r)
+  const bool in_place = ep ? !r.any_dp && gemm_reads_shards(r.T, ldx, r.layout, true, r.N == 1) && switches_pay(r)
                            : one_chain(r, true) && gemm_reads_shards(r.T, ldx, r.layout) && switches_pay(r);
   // A launch that stores columns of Y, whole sums, goes through the epilogue, in parts by the rule of the whole operator.
   auto fuse = [&](GemmProblem *g, int64_t col, bool whole) {
@@ -1060,7 +1071,7 @@ static osdp_status forward(const osdp_shape *shape, const osdp_plan *plan, int32
     g->k_per = static_cast<int32_t>(fused_k_per(r.T, r.I, r.O));
   };
   if (in_place && !r.any_dp) {
-    GemmProblem g = shard_gemm(r, true, tab, X, ldx, Y, ldy);
+    GemmProblem g = ep ? shard_gemm_fused(r, true, tab, X, ldx, Y, ldy) : shard_gemm(r, true, tab, X, ldx, Y, ldy);
     fuse(&g, 0, true);
     OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_FWD, g, sc));
     return OSDP_OK;
@@ -1350,7 +1361,7 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
   }
   // Few tokens: nothing is staged (see forward()), and dW is one launch per destination.
   const bool skinny = skinny_takes(true, r.T, lddy, r.layout, r.I);
-  const bool in_place = !skinny && (slope ? !r.any_dp && gemm_reads_shards(r.T, lddy, r.layout, true) && shards_pay_dx(r)
+  const bool in_place = !skinny && (slope ? !r.any_dp && gemm_reads_shards(r.T, lddy, r.layout, true, true) && shards_pay_dx(r)
                                           : one_chain(r, false) && gemm_reads_shards(r.T, lddy, r.layout));
   std::vector<Slice> runs;
   if (in_place && r.any_dp && r.T <= kSkinnyMaxTokens) runs = runs_in_place(r, false);
@@ -1386,7 +1397,7 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
                         : launch_skinny(true, weight_map(r, tab, rep), r.T, dY, lddy, dX, lddx, sc);
       }));
     else if (runs.empty()) {
-      GemmProblem gx = shard_gemm(r, false, tab, dY, lddy, dX, lddx);
+      GemmProblem gx = slope ? shard_gemm_fused(r, false, tab, dY, lddy, dX, lddx) : shard_gemm(r, false, tab, dY, lddy, dX, lddx);
       in_parts(&gx, dx_per, planes_dx);
       OSDP_HIP(do_gemm(OSDP_KERNEL_GEMM_DX, gx, sc));
     }

@@ -88,11 +88,12 @@ size_t planes_of(int64_t M, int64_t K, int64_t N, int64_t k_per) {
 // quarters of what they would take one after the other, and the launches.  By T, I and O alone: the unsplit copy is what counts, so
 // that Y is the same for every k.  us in place / staged: 200 tokens 1024 -> 1024 10.3 / 15.0, 1000 tokens 13.4 / 16.3, 160 tokens
 // 8160 -> 1024 22.8 / 29.4, 300 tokens 2560 -> 2560 23.2 / 25.4; 400 tokens 4032 -> 4032 51 / 40.5.
-bool skinny_beats_copy(int64_t T, int64_t I, int64_t O) {
+// copied: not so where one shard holds the matrix, which tiles read as it lies (219 tokens 624 -> 512 8.6 / 12.0).
+bool skinny_beats_copy(int64_t T, int64_t I, int64_t O, bool copied = true) {
   const int64_t tiles = ((T + 127) / 128) * ((O + 127) / 128), k_per = fused_k_per(T, I, O), parts = (I + k_per - 1) / k_per;
   const double flops = 2.0 * static_cast<double>(T) * static_cast<double>(I) * static_cast<double>(O);
   const double tile = std::max(flops / 0.9e9, 0.0105 * static_cast<double>(std::min(k_per, I)) * static_cast<double>((tiles * parts + kCUs - 1) / kCUs));
-  const double copy = 4.0 * static_cast<double>(I) * static_cast<double>(O) / 5.5e6 + 6.0;
+  const double copy = (copied ? 4.0 * static_cast<double>(I) * static_cast<double>(O) / 5.5e6 : 0.0) + 6.0;
   return skinny_plan(T, I, O).us < 0.75 * (copy + tile) + (parts > 1 ? 12.0 : 3.0);
 }
 
@@ -104,11 +105,11 @@ bool fused_takes_skinny(int64_t T, int64_t ldx, const ShardLayout &lay, int64_t 
       d.poison_staging.load(std::memory_order_relaxed) != 0)
     return false;
   return T > kSkinnyMaxTokens && !(lay.rows_per_shard > 0 && lay.rows_per_shard % 64 == 0) && ldx < kMaxLd && I < kMaxLd && lay.O < kMaxLd &&
-         skinny_beats_copy(T, I, lay.O);
+         skinny_beats_copy(T, I, lay.O, lay.N > 1);
 }
 
 size_t fused_planes_bytes(int64_t T, int64_t I, int64_t O) {
-  const size_t tiles = planes_of(T, I, O, fused_k_per(T, I, O));
+  const size_t tiles = planes_of(T, I, O, fused_k_per(T, I, O));  // (for any N: with a copy the few-token kernel takes no fewer)
   if (T <= 0 || !(T <= kSkinnyMaxTokens || skinny_beats_copy(T, I, O))) return tiles;
   return std::max(tiles, planes_of(T, I, O, skinny_plan(T, I, O).k_per));
 }

@@ -18,12 +18,13 @@ namespace {
 bool shards_are_k_blocks(const ShardLayout &lay) { return lay.rows_per_shard > 0 && lay.rows_per_shard % 64 == 0; }
 }  // namespace
 
-bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay, bool any_tokens) {
+bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay, bool any_tokens, bool any_rows) {
   const DebugOptions &d = debug_options();
   const bool forced = d.gemm_generic.load(std::memory_order_relaxed) != 0 || d.tile.load(std::memory_order_relaxed) >= 0 ||
                       d.fwd_pair.load(std::memory_order_relaxed) >= 0 || d.fused_gather.load(std::memory_order_relaxed) >= 0 ||
                       d.poison_staging.load(std::memory_order_relaxed) != 0;  // (these ask for the staged schedule)
-  return !forced && (any_tokens || T <= kShardReadMaxTokens) && shards_are_k_blocks(lay) && ld_act < kMaxLd && lay.O < kMaxLd;
+  const bool fits = shards_are_k_blocks(lay) || (lay.rows_per_shard > 0 && any_rows && (lay.N == 1 || lay.rows_per_shard % 8 == 0));
+  return !forced && (any_tokens || T <= kShardReadMaxTokens) && fits && ld_act < kMaxLd && lay.O < kMaxLd;
 }
 
 int gemm_forward_parts(int64_t M, int64_t K) { return forward_k_parts(M, K); }

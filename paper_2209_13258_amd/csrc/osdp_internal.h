@@ -201,10 +201,11 @@ hipError_t launch_slope(const SlopeProblem &q, void *workspace, hipStream_t stre
 // (256 to 512 tokens, 1024 to 16384 features, 8 to 64 shards, k = 1 and 4: 1.05 to 2.5 times as fast as staged, but for
 // unsplit forwards over shards of 64 rows, see switches_pay; more than 512 tokens have not been timed in place.)
 constexpr int64_t kShardReadMaxTokens = 512;
+// any_rows: shards of a multiple of 8 rows will do (dX, whose tiles end with a shard), or one that holds the whole matrix.
 // any_tokens: the number of tokens does not count (calls with an epilogue, whose time counts where the plain call's kernel and
 // schedule are left as they are; us in place / staged, with a bias: 8192 tokens 1024 -> 4096 unsplit 74 / 76, four slices 73 / 106;
 // 4096 tokens 8192 -> 8192 388 / 433, four slices 393 / 498; 16384 tokens 2560 -> 10240, four slices 705 / 745).
-bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay, bool any_tokens = false);
+bool gemm_reads_shards(int64_t T, int64_t ld_act, const ShardLayout &lay, bool any_tokens = false, bool any_rows = false);
 
 // Number of parts of the reduction that a concatenating product of M x K is the sum of (1: one chain).
 int gemm_forward_parts(int64_t M, int64_t K);

@@ -85,6 +85,8 @@ def check_forward(op, act, bias=None, residual=None, Y=None, Z=None):
 SHAPES = [(1, 64, 8, 1, 1), (1, 4096, 16384, 8, 1), (3, 200, 136, 17, 1), (16, 256, 32768, 4, 1), (33, 1024, 520, 8, 1), (64, 2056, 264, 3, 1), (65, 512, 8448, 8, 1),
           (128, 256, 1024, 2, 4), (129, 256, 1024, 2, 4), (255, 1000, 72, 1, 1), (500, 2560, 2560, 8, 2), (513, 320, 640, 5, 2), (777, 1504, 3200, 4, 2),
           (1024, 520, 2056, 40, 1), (1500, 4096, 4096, 8, 4), (2049, 128, 1032, 2, 1), (3001, 1024, 3200, 8, 1), (4096, 2560, 10240, 8, 4), (8192, 1024, 4096, 8, 4),
+          # one shard, and shards of a multiple of 8 rows, which dX's tiles end with
+          (700, 1112, 1608, 1, 3), (200, 2616, 352, 1, 2), (130, 72, 136, 1, 1), (600, 1664, 512, 8, 4), (2000, 1088, 2048, 4, 2), (150, 128, 2048, 16, 1), (400, 640, 9000, 8, 3),
           # products that run in parts of a long reduction where they are staged, and one that does not
           (600, 16384, 264, 3, 1), (300, 24576, 528, 3, 3), (600, 16384, 264, 8, 1), (2, 31824, 1672, 1, 1), (33, 16384, 512, 8, 1),
           (128, 9992, 136, 17, 1), (215, 920, 20288, 16, 8), (193, 16080, 544, 32, 4), (337, 19336, 352, 11, 4), (1488, 672, 984, 9, 1), (900, 712, 952, 7, 1), (7, 23072, 744, 2, 1), (200, 6200, 664, 8, 1), (130, 8192, 8, 8, 1), (90, 8192, 16384, 8, 2)]
@@ -130,7 +132,7 @@ def test_cuts_modes_and_shards_change_no_bit(T, I, O):
     how = dict(bias=bias, activation=ACTS["gelu"], residual=residual)
     cut = {(512, 1024): 18, (1024, 2048): 13, (8192, 512): 26, (4096, 512): 13}[I, O]
     # shards that are blocks of a multiple of 64 rows, or one; shards that are not may have another order of sums from 129 tokens on
-    blocks = [(8, 1, 0, 1), (1, 1, 0, 1), (8, 4, 0, 1), (8, 4, 0, 2), (8, 4, 0, 3), (8, 4, 1, 1), (8, 2, 1, 2), (8, 4, 3, 1), (4, 2, 0, 1)]
+    blocks = [(8, 1, 0, 1), (1, 1, 0, 1), (8, 4, 0, 1), (8, 4, 0, 2), (8, 4, 0, 3), (8, 4, 1, 1), (8, 2, 1, 2), (8, 4, 3, 1), (4, 2, 0, 1), (1, 4, 0, 1), (1, 2, 1, 2)]
     flat = [(cut, 1, 0, 1), (cut, 4, 0, 1), (cut, 2, 0, 2), (cut, 1, 1, 1)]
     if T <= 128 or not in_parts(T, I, O):  # (row slices that are staged go on in one chain, not in parts)
         flat.append((cut, 4, 1, 1))
