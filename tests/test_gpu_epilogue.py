@@ -89,7 +89,7 @@ SHAPES = [(1, 64, 8, 1, 1), (1, 4096, 16384, 8, 1), (3, 200, 136, 17, 1), (16, 2
           (700, 1112, 1608, 1, 3), (200, 2616, 352, 1, 2), (130, 72, 136, 1, 1), (600, 1664, 512, 8, 4), (2000, 1088, 2048, 4, 2), (150, 128, 2048, 16, 1), (400, 640, 9000, 8, 3),
           # products that run in parts of a long reduction where they are staged, and one that does not
           (600, 16384, 264, 3, 1), (300, 24576, 528, 3, 3), (600, 16384, 264, 8, 1), (2, 31824, 1672, 1, 1), (33, 16384, 512, 8, 1),
-          (128, 9992, 136, 17, 1), (215, 920, 20288, 16, 8), (193, 16080, 544, 32, 4), (337, 19336, 352, 11, 4), (1488, 672, 984, 9, 1), (900, 712, 952, 7, 1), (7, 23072, 744, 2, 1), (200, 6200, 664, 8, 1), (130, 8192, 8, 8, 1), (90, 8192, 16384, 8, 2)]
+          (128, 9992, 136, 17, 1), (215, 920, 20288, 16, 8), (193, 16080, 544, 32, 4), (337, 19336, 352, 11, 4), (1488, 672, 984, 9, 1), (900, 712, 952, 7, 1), (7, 23080, 744, 2, 1), (200, 6200, 664, 8, 1), (130, 8192, 8, 8, 1), (90, 8192, 16384, 8, 2)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
