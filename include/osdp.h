@@ -382,7 +382,8 @@ OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, con
  * (dn: turned back), r = 1 / sqrt(..), xh = x r, t = dn * g:
  *     dx = r * (t - xh * mean_j(t_j xh_j))         dg_j = sum over tokens and heads of dn_j xh_j
  * Everything is computed in fp32 and rounded once, angles in 64 bits until less than a turn is left of them (then cos and sin to 2^-20).
- * Squares that leave the range of fp32 are taken of x / 2^70 instead.  dg is summed in an order that the sizes alone decide.
+ * Squares that would leave the range of fp32 are taken of x / 2^70 instead, beside eps / 2^140 (the gradients of such heads must be
+ * below 2^80).  dg is summed in an order that the sizes alone decide.
  *
  * A negative position marks a row of padding: its outputs are left as they are, and it adds nothing to dg, whatever it holds.
  *
@@ -407,7 +408,7 @@ typedef struct {
   int32_t norm;        /* 1 or 0; 0: the weights must be NULL                                        */
   int32_t weight_type; /* an osdp_dtype: of the weights and their gradients                          */
   int32_t reserved;    /* 0                                                                          */
-  double eps;          /* >= 1e-12                                                                   */
+  double eps;          /* 1e-12 to 1e30                                                              */
   const int64_t *positions; /* device [T], or NULL: row t has position t                             */
   const double *freqs;      /* device [rotary / 2], radians a position                               */
   const void *q_weight, *k_weight; /* device [D], 16-byte aligned, or NULL: ones                     */

@@ -152,7 +152,8 @@ struct Lane {
     return group_sum<kG>((has_first ? lo : 0.0f) + (has_second ? hi : 0.0f));
   }
   // 1 / sqrt(mean v^2 + eps) over the head.  Where squares leave the range in which the rest is safe, v is scaled by 2^-70 first,
-  // and so is *scale (eps is nothing beside such squares).
+  // and so is *scale; eps goes with the squares, by 2^-140 (in two steps: that number is none of fp32's normal ones.  An eps that
+  // ends below 2^-126 is nothing beside a mean of 2^-89 or more: the sum is above 2^60 and D at most 2^9).
   __device__ __forceinline__ float factor(const QkParams &p, float (&v)[16], float *scale) const {
     float s = dot(v, v), eps = p.eps;
     *scale = 1.0f;
@@ -161,7 +162,7 @@ struct Lane {
 #pragma unroll
       for (int e = 0; e < 16; ++e) v[e] *= 0x1p-70f;
       s = dot(v, v);
-      eps = 0.0f;
+      eps = eps * 0x1p-70f * 0x1p-70f;
     }
     return rsqrtf(__builtin_fmaf(s, 1.0f / static_cast<float>(p.D), eps));
   }

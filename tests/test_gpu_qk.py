@@ -339,3 +339,19 @@ def test_the_binding_refuses_what_does_not_fit():
         osdp.osdp_qk_norm_rope_bwd(q, k, q, k, torch.empty_like(q), torch.empty_like(k), w.clone(), w.float(), workspace(5, 4, 2, 64), q_weight=w, k_weight=w)
     with pytest.raises(osdp.OsdpError):
         osdp.osdp_qk_norm_rope_bwd(q, k, q, k, torch.empty_like(q), torch.empty_like(k), w.clone(), None, torch.empty(64, dtype=torch.uint8, device="cuda"), q_weight=w)
+
+
+@pytest.mark.parametrize("eps", [1e-12, 1e8, 1e18, 1e20, 1e30])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 20, 2.0 ** 28, 2.0 ** 31, 2.0 ** 50, 2.0 ** 66])
+def test_any_eps_beside_any_size_of_heads(size, eps):
+    """eps counts however large the squares beside it are.  Bounds as for other sizes of heads: 30 tokens of 3 heads, terms of dg off
+    by 2^-17 each, dx by (2^-15 + 64^1/2 2^-19) of the largest |r t|, some four times the root mean square."""
+    q, dy = rand(30, 3, 64, std=size), rand(30, 3, 64, seed=1)
+    w = rand(64, std=0.2, seed=2, dtype=torch.float32).add_(1)
+    how = dict(freqs=some_freqs(64), q_weight=w, k_weight=w, positions=torch.arange(30, device="cuda"), eps=eps)
+    out = forward(q, q, **how)[0]
+    check_forward(out, q, how["positions"], how["freqs"], w, eps=eps)
+    dx, _, dg, _ = backward(q, q, dy, dy, dtype=torch.float32, **how)
+    want, want_g = R.qk_back(q.double(), dy.double(), how["positions"], how["freqs"], w, eps, True, False)
+    assert ((dx.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * want.square().mean().sqrt()).all()
+    assert ((dg.double() - want_g).abs() <= 2.0 ** -10 * want_g.square().mean().sqrt()).all()
