@@ -1288,6 +1288,8 @@ osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, const osdp_p
   const int64_t T = shape->T, I = shape->I, O = shape->O;
   if ((st = check_vector(e.bias, e.activation, e.bias_type, "bias")) != OSDP_OK) return st;
   if (T > 0) {
+    // (before any look for overlaps, which divides by leading dimensions)
+    if ((st = check_matrix(X, ldx, I, "X")) != OSDP_OK || (st = check_matrix(Y, ldy, O, "Y")) != OSDP_OK) return st;
     if (e.residual && (st = check_matrix(e.residual, e.ld_residual, O, "residual")) != OSDP_OK) return st;
     if (e.z && (st = check_matrix(e.z, e.ldz, O, "z")) != OSDP_OK) return st;
     const bool in_place = e.residual == Y && e.ld_residual == ldy;

@@ -250,3 +250,17 @@ def test_the_short_way_into_the_library_answers_only_what_it_knows():
     assert calls.linear(X, [None], X, 1 << 80, ws, None, 0, "s", None, 0, None, None, None) is None
     with pytest.raises(TypeError):
         calls.connect(1, 2)
+
+
+@pytest.mark.parametrize("more", [dict(x=2 * P, ldx=0, ldy=0), dict(x=2 * P + 16, ldx=0, ldy=0), dict(ldx=0), dict(ldy=0), dict(x=2 * P, ldx=-O, ldy=-O),
+                                  dict(ldz=0), dict(ld_residual=0), dict(z=2 * P, ldz=0, ldy=0), dict(shape=(T, I, O, 2, 1), x=2 * P, ldx=0, ldy=0, z=None, residual=None)])
+def test_forward_refuses_rows_that_lie_on_each_other(more):
+    """Leading dimensions of 0 (an expanded tensor's) and below, alone and in two overlapping matrices."""
+    assert forward(**more) == INVALID
+    assert osdp.lib.osdp_last_error()
+
+
+@pytest.mark.parametrize("more", [dict(dy=6 * P, lddy=0, lddz=0), dict(lddy=0), dict(ldz=0, lddz=0, z=6 * P), dict(lddz=0), dict(dx=P, lddy=0), dict(lddy=-O)])
+def test_backward_refuses_rows_that_lie_on_each_other(more):
+    assert backward(**more) == INVALID
+    assert osdp.lib.osdp_last_error()
