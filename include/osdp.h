@@ -389,7 +389,8 @@ OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, con
  *
  * Heads lie anywhere: element d of head h of token t at p + t * ld + h * head_stride + d.  Outputs may be the inputs of the same
  * name (the same pointer and strides; backward: dq may be q or dq_out, dk alike), otherwise they overlap no input, nor each
- * other, nor themselves.  The parts of one wide row (queries, keys, values side by side) do not overlap.
+ * other, nor themselves.  The parts of one wide row (queries, keys, values side by side) do not overlap, nor do heads in turn in any
+ * order of heads and tokens; rows of two lengths in one stretch of memory are refused.
  * Shapes (else OSDP_ERR_UNSUPPORTED): D a multiple of 8 and at most 512; rotary a multiple of 16 (interleaved: 8), at most D;
  * strides multiples of 8, pointers 16-byte aligned; T < 2^31; heads at most 65535, either may be 0 (then its pointers are ignored). */
 

@@ -433,29 +433,41 @@ struct Extent {
 bool same(const osdp_heads &a, const osdp_heads &b, const Extent &e) {
   return a.p == b.p && (e.T == 1 || a.ld == b.ld) && (e.heads == 1 || a.head_stride == b.head_stride);
 }
-// Whether two sets of heads share memory: by their extents, and, rows of one length, by the places of their heads in them.
+// Whether two sets of heads share memory.  Head i of token t of the one and head j of token u of the other do where
+// |i hs_a - j hs_b - n ld - d| < D, with n = u - t and d the distance of the two pointers: exact for rows of one length, in any order of
+// heads and tokens.  Rows of two lengths are taken to share what their extents do, as are more than 2^20 pairs of heads of two strides.
+// (32-bit lengths and extents below 2^60: nothing here leaves 64 bits.)
 bool share(const Extent &a, const Extent &b) {
   if (a.empty() || b.empty() || a.end() <= b.begin() || b.end() <= a.begin()) return false;
-  const bool rows = (a.T == 1 && b.T == 1) || a.h->ld == b.h->ld;
-  if (!rows) return true;
-  const __int128 ld = a.T == 1 && b.T == 1 ? 0 : a.h->ld;
-  __int128 d = (b.begin() - a.begin()) / 2;
-  if (ld > 0) d %= ld;
-  for (int wrap = -1; wrap <= 1; ++wrap) {
-    const __int128 off = d + wrap * ld;  // where b's heads begin in a's rows
-    for (int64_t i = 0; i < a.heads; ++i) {
-      const __int128 at = static_cast<__int128>(i) * a.h->head_stride - off;  // a's head i, seen from b's first
-      const int64_t hs = b.h->head_stride;
-      if (hs <= 0 || b.heads == 1) {
-        if (at < b.D && -at < a.D) return true;
-        continue;
-      }
-      const __int128 j = at >= 0 ? at / hs : -1;
-      for (__int128 k = j; k <= j + 1; ++k)
-        if (k >= 0 && k < b.heads && at - k * hs < b.D && k * hs - at < a.D) return true;
-    }
-    if (ld == 0) break;
+  const int64_t D = a.D, last = a.T - 1, ld = last > 0 ? a.h->ld : 0;
+  if (last > 0 && (a.h->ld != b.h->ld || ld == 0)) return true;
+  const int64_t d = static_cast<int64_t>((b.begin() - a.begin()) / 2);
+  const int64_t hs_a = a.heads > 1 ? a.h->head_stride : 0, hs_b = b.heads > 1 ? b.h->head_stride : 0;
+  if (last > 0) {  // parts of one wide row, side by side
+    const int64_t row_a = (a.heads - 1) * hs_a + D, row_b = (b.heads - 1) * hs_b + D, place = (d % ld + ld) % ld;
+    if (place >= row_a && place + row_b <= ld) return false;
   }
+  auto meet = [&](int64_t off) {  // heads this far apart in tokens of one number
+    int64_t n = 0;
+    if (last > 0) {  // the largest n with off - n ld > -D, as far as there are tokens
+      const int64_t x = off + D - 1;
+      n = x >= 0 ? x / ld : -((ld - 1 - x) / ld);
+      n = std::max(-last, std::min(last, n));
+    }
+    const int64_t apart = off - n * ld;
+    return apart < D && -apart < D;
+  };
+  if (hs_a == hs_b || a.heads == 1 || b.heads == 1) {  // the difference of the heads' numbers is what counts
+    for (int64_t m = 0; m < a.heads; ++m)
+      if (meet(m * hs_a - d)) return true;
+    for (int64_t m = 1; m < b.heads; ++m)
+      if (meet(-m * hs_b - d)) return true;
+    return false;
+  }
+  if (a.heads * b.heads > (int64_t{1} << 20)) return true;
+  for (int64_t i = 0; i < a.heads; ++i)
+    for (int64_t j = 0; j < b.heads; ++j)
+      if (meet(i * hs_a - j * hs_b - d)) return true;
   return false;
 }
 
@@ -470,6 +482,8 @@ osdp_status check_heads(const osdp_heads *h, int64_t heads, const osdp_qk &q, co
   if (h->ld < 0 || h->head_stride < 0) return say(OSDP_ERR_INVALID_ARG, "a stride is negative");
   if ((q.T > 1 && h->ld % 8) || (heads > 1 && h->head_stride % 8)) return say(OSDP_ERR_UNSUPPORTED, "a stride is not a multiple of 8");
   if (!aligned(h->p)) return say(OSDP_ERR_UNSUPPORTED, "not 16-byte aligned");
+  if (static_cast<__int128>(q.T - 1) * h->ld + static_cast<__int128>(heads - 1) * h->head_stride >= (int64_t{1} << 60))
+    return say(OSDP_ERR_INVALID_ARG, "its strides leave the address space");
   if (written) {
     const __int128 D = q.D, row = static_cast<__int128>(heads - 1) * h->head_stride + D, column = static_cast<__int128>(q.T - 1) * h->ld + D;
     const bool heads_apart = heads == 1 || h->head_stride >= D, rows_apart = q.T == 1 || h->ld >= D;

@@ -2,6 +2,7 @@
 which need no GPU."""
 import ctypes
 import math
+import random
 
 import pytest
 import torch
@@ -264,3 +265,51 @@ def test_forward_refuses_rows_that_lie_on_each_other(more):
 def test_backward_refuses_rows_that_lie_on_each_other(more):
     assert backward(**more) == INVALID
     assert osdp.lib.osdp_last_error()
+
+
+def elements(p, ld, hs, tokens, n, D):
+    return {p // 2 + t * ld + h * hs + d for t in range(tokens) for h in range(n) for d in range(D)}
+
+
+def test_heads_that_share_memory_are_refused_and_others_are_not(no_gpu):
+    """Rows of one length, heads within a row or rows within a head, strides with and without a common divisor: every overlap that
+    there is, and no other, between the outputs and between an output and the other side's input."""
+    rng, seen = random.Random(5), {True: 0, False: 0}
+    for _ in range(6000):
+        t, n = rng.choice([1, 2, 3, 5]), [rng.choice([1, 1, 2, 3, 4]) for _ in range(2)]
+        d = rng.choice([8, 16, 24])
+        sides, row = [], 8 * rng.randint(d // 8, 14)
+        for i in range(2):
+            written = i == 0 or rng.random() < 0.5
+            hs = 8 * rng.randint(d // 8 if written else 0, 8) if rng.random() < 0.5 else rng.choice([row * t, row * t + 8, 2 * row * t, row * (t + 1) - 8])
+            sides.append((4 * P + 16 * rng.randint(0, 60) * i, row, hs, written))
+        (a, _, hs_a, _), (b, _, hs_b, b_written) = sides
+        itself = lambda hs, heads: not (heads == 1 or t == 1 or row >= (heads - 1) * hs + d or hs >= (t - 1) * row + d)  # noqa: E731
+        if itself(hs_a, n[0]) or b_written and itself(hs_b, n[1]) or n[0] > 1 and hs_a < d:
+            continue
+        want = bool(elements(a, row, hs_a, t, n[0], d) & elements(b, row, hs_b, t, n[1], d))
+        size = dict(T=t, q_heads=n[0], k_heads=n[1], D=d, rotary=0, freqs=None)
+        apart = dict(q=heads(P, 64 * d, d), q_out=heads(a, row, hs_a))
+        if b_written:
+            status = qk_forward(**size, **apart, k=heads(2 * P, 64 * d, d), k_out=heads(b, row, hs_b))
+        else:
+            status = qk_forward(**size, **apart, k=heads(b, row, hs_b), k_out=heads(2 * P, 64 * d, d))
+        assert passes_the_checks(status) != want, (size, sides, osdp.lib.osdp_last_error())
+        seen[want] += 1
+    assert min(seen.values()) > 500
+
+
+@pytest.mark.parametrize("more", [
+    # head 0 of the keys' token 50 is head 1 of the queries' token 0
+    dict(T=100, q_heads=2, k_heads=2, q_out=heads(4 * P, 256, 25728), k_out=heads(4 * P + 2 * 12928, 256, 25728)),
+    dict(q_out=heads(4 * P, 2 ** 59)), dict(q=heads(P, ROW, 2 ** 60))])
+def test_qk_forward_refuses_heads_in_each_other(more):
+    assert qk_forward(**more) == INVALID
+
+
+@pytest.mark.parametrize("more", [
+    dict(q_heads=2, k_heads=2, q_out=heads(4 * P, D, 2 * T * D), k_out=heads(4 * P + 2 * T * D, D, 2 * T * D)),   # [heads, 2, tokens, D]
+    dict(q_heads=4, k_heads=2, q_out=heads(4 * P, D, 2 * T * D), k_out=heads(4 * P + 2 * T * D, D, 4 * T * D)),
+    dict(q_heads=2, k_heads=2, q_out=heads(4 * P, 2 * D, 4 * T * D), k_out=heads(4 * P + 2 * D, 2 * D, 4 * T * D))])  # [heads, .., tokens, 2, D]
+def test_qk_forward_takes_heads_in_turn_by_head(no_gpu, more):
+    assert passes_the_checks(qk_forward(**more))
