@@ -352,10 +352,13 @@ OSDP_API osdp_status osdp_split_linear_epilogue_workspace_bytes(const osdp_shape
 /* Forward.  Plans, modes (w_dp: NULL when no slice is DP) and streams as osdp_split_linear_fwd_mixed.  Y and Z
  * overlap no input, each other or the workspace, but for a residual that is Y.
  * Shards that are row blocks of a multiple of 64 rows (backward: of 8), and a single shard, are read where they lie for any T,
- * unless that is estimated to be slower or slices are in DP mode; nothing is gathered then.  A long reduction with few outputs (less than half a 128 x 128 tile of Y for each CU, or T <= 128) is summed in
- * parts of it, each accumulated on its own, added in ascending order in fp32.  The order of Y's additions is a matter of T, I, O and
- * whether the shards are row blocks of a multiple of 64 rows, or one: Y is bit-identical for every k, staging mode, stream choice and mode of the slices, as
- * above, but for T > 128 with row slices that are staged or in DP mode and cannot be taken as column slices instead: these continue one chain. */
+ * unless that is estimated to be slower or slices are in DP mode; nothing is gathered then.  A long reduction with few outputs (less
+ * than half a 128 x 128 tile of Y for each CU, or T <= 128) is summed in parts of it, each accumulated on its own, added in ascending
+ * order in fp32.  The order of Y's additions is a matter of T, I, O and whether the shards are row blocks of a multiple of 64 rows, or
+ * one: Y is bit-identical for every k, staging mode, stream choice and mode of the slices, as above, but for row slices that are staged
+ * or in DP mode and cannot be taken as column slices instead (with slices in DP mode they never can): these continue one chain where
+ * the others run in parts.  Calls of the few-token kernel stage none and are not meant: T <= 128, but neither ldx >= 2^22 nor T > 64 with
+ * O > 8192 over shards of a multiple of 64 rows (see osdp_split_linear_fwd). */
 OSDP_API osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
                                                     const osdp_epilogue *epilogue, const void *X, int64_t ldx,
                                                     const void *const *w_shards, const void *const *w_dp, int64_t ld_dp,
@@ -364,8 +367,9 @@ OSDP_API osdp_status osdp_split_linear_fwd_epilogue(const osdp_shape *shape, con
 
 /* Backward: one pass for dZ and db, then the products of osdp_split_linear_bwd_mixed with dZ in the place of dY (which also says
  * what dX may take the place of: X, or with few tokens dZ); shards are read in place and products summed in parts as above, dX's
- * over O and dW's over T.  db is the sum in fp32 in an order that T and O alone decide, rounded once if
- * bias_type asks for it.  T = 0 stores db = 0 and dW = 0. */
+ * over O and dW's over T.  dW is bit-identical for every k, cut and mode of the slices; dX too, as above, but for column slices that are
+ * staged or in DP mode and cannot be taken as row slices instead, which continue one chain where the others run in parts.  db is the
+ * sum in fp32 in an order that T and O alone decide, rounded once if bias_type asks for it.  T = 0 stores db = 0 and dW = 0. */
 OSDP_API osdp_status osdp_split_linear_bwd_epilogue(const osdp_shape *shape, const osdp_plan *plan, int32_t op_index,
                                                     const osdp_epilogue_grad *epilogue, const void *X, int64_t ldx,
                                                     const void *dY, int64_t lddy, const void *const *w_shards,

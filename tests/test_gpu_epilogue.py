@@ -524,3 +524,53 @@ def test_a_transformer_layer_runs_together():
     products(qkv, d_rows, dx, dW)
     s = d_rows.double().sum(0)
     close(db[0], s, 2.0 ** -8 * s.abs() + T * 2.0 ** -24 * d_rows.double().abs().sum(0), "db")
+
+
+@pytest.mark.parametrize("T", [65, 100, 128])
+def test_wide_operators_of_a_hundred_tokens(T):
+    """More than 8192 output columns over shards of a multiple of 64 rows: from 65 tokens on the tiles' kernels, in parts of the
+    reduction.  All plans give the same bits but one with row slices in DP mode, which go on in one chain."""
+    I, O = 4096, 8448
+    assert in_parts(T, I, O)
+    bias, residual = rand(O, seed=1), rand(T, O, seed=2)
+    how = dict(bias=bias, activation=ACTS["gelu"], residual=residual)
+    want = None
+    for N, k, split, staging, zdp in [(8, 1, 0, 1, None), (1, 1, 0, 1, None), (8, 4, 0, 1, None), (8, 4, 0, 2, None), (8, 4, 1, 1, None), (8, 2, 1, 2, None), (64, 4, 1, 3, None),
+                                      (8, 4, 0, 1, 0b1010), (8, 4, 1, 1, 0b1010)]:
+        op = Op(T, I, O, N, k, split, staging=staging, zdp=zdp)
+        if zdp is None:
+            got = op.fwd(op.out(), **how)
+        else:
+            w, step, got = op.W.contiguous(), (I if split else O) // k, op.out()
+            w_dp = [w[j * step:(j + 1) * step] if split else w[:, j * step:(j + 1) * step] for j in range(k)]
+            osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, got, k, op.workspace(False), epilogue=osdp.Epilogue(**how), plan=op.plan, w_dp=w_dp, ld_dp=O)
+        if zdp is None or not split:
+            assert want is None or torch.equal(got, want), (N, k, split, staging, zdp)
+            want = got
+        check_forward(op, "gelu", bias, residual, got)
+
+
+@pytest.mark.parametrize("T,I,O,k", [(300, 520, 4168, 5), (300, 520, 4160, 5), (4168, 264, 520, 3), (100, 8448, 4096, 4), (40, 512, 4096, 4)])
+def test_gradients_of_products_in_parts_are_the_same_for_every_plan(T, I, O, k):
+    """Whatever the shards, cuts and modes of the slices, but that dX of column slices in DP mode goes on in one chain, and that of 65 to
+    128 tokens and more than 8192 in-features is the few-token kernel's, or the tiles' where shards are a multiple of 64 rows."""
+    dY, Z, want, want_dX = rand(T, O, seed=3), rand(T, O, seed=4), None, {}
+    for N, k_, split, staging, zdp in [(1, 1, 0, 1, None), (8, 1, 0, 1, None), (1, k, 1, 1, None), (8, k, 1, 1, None), (8, k, 1, 2, None), (8, k, 0, 1, None), (8, k, 0, 2, None), (8, k, 1, 1, 0b11010),
+                                      (8, k, 0, 1, 0b11010)]:
+        if split == 0 and O % (8 * k_):
+            continue
+        op = Op(T, I, O, N, k_, split, staging=staging, zdp=zdp)
+        full, step = op.W.contiguous(), (I if split else O) // k_
+        dw = torch.full_like(full, float("nan"))
+        cut = lambda m: [m[j * step:(j + 1) * step] if split else m[:, j * step:(j + 1) * step] for j in range(k_)]  # noqa: E731
+        dz, dX, dws = op.out(), torch.full_like(op.X, float("nan")), [torch.full_like(s, float("nan")) for s in op.w]
+        osdp.osdp_split_linear_bwd_epilogue(op.X, dY, op.w, dX, dws, k_, op.workspace(True), plan=op.plan, epilogue=osdp.EpilogueGrad(activation=ACTS["gelu"], z=Z, dz=dz),
+                                            **({} if zdp is None else dict(w_dp=cut(full), ld_dp=O, dw_dp=cut(dw))))
+        dW = torch.cat(dws)[:I * O].view(I, O)
+        dW = torch.where(torch.isnan(dW), dw, dW)
+        check_products(op, dz, dX, dW.flatten())
+        want = dW if want is None else want
+        assert torch.equal(dW, want), (N, k_, split, zdp)
+        if zdp is None or split:
+            kernel = 64 < T <= 128 and I > 8192 and I % (64 * N) == 0
+            assert torch.equal(dX, want_dX.setdefault(kernel, dX)), (N, k_, split, zdp)
