@@ -398,19 +398,23 @@ BackwardGrid backward_grid(int64_t T, int q_heads, int k_heads, int D) {
   const int tile = (64 / group) >> hl;
   const int64_t tiles = (T + tile - 1) / tile;
   const int cq = chunks_of(q_heads, hl, kBackwardUnroll), ck = chunks_of(k_heads, hl, kBackwardUnroll);
-  // (workgroups that the work could keep busy, and that of a side with no heads none)
-  const int64_t uq = cq ? (tiles + (4 >> waves_log2_of(cq)) - 1) / (4 >> waves_log2_of(cq)) * ((cq + 3) / 4) : 0;
-  const int64_t uk = ck ? (tiles + (4 >> waves_log2_of(ck)) - 1) / (4 >> waves_log2_of(ck)) * ((ck + 3) / 4) : 0;
+  // Workgroups that the token tiles can keep busy (of a side with no heads none).  Where both sides have more than run at once, they
+  // share those by their work, head groups beyond a workgroup's four waves included: a workgroup walks these itself.
+  const int64_t at_once[2] = {4 >> waves_log2_of(cq), 4 >> waves_log2_of(ck)};
+  const int64_t mq = cq ? (tiles + at_once[0] - 1) / at_once[0] : 0, mk = ck ? (tiles + at_once[1] - 1) / at_once[1] : 0;
   BackwardGrid g{};
-  if (uq + uk <= kMaxBackwardGroups) {
-    g.queries = static_cast<int>(uq);
-    g.all = static_cast<int>(uq + uk);
-  } else {
-    g.queries = static_cast<int>(kMaxBackwardGroups * static_cast<double>(uq) / static_cast<double>(uq + uk) + 0.5);
-    if (uq > 0) g.queries = std::max(g.queries, 1);
-    if (uk > 0) g.queries = std::min(g.queries, kMaxBackwardGroups - 1);
-    g.all = kMaxBackwardGroups;
+  if (mq + mk <= kMaxBackwardGroups) {
+    g.queries = static_cast<int>(mq);
+    g.all = static_cast<int>(mq + mk);
+    return g;
   }
+  const int64_t wq = mq * ((cq + 3) / 4), wk = mk * ((ck + 3) / 4);
+  int64_t queries = static_cast<int64_t>(kMaxBackwardGroups * static_cast<double>(wq) / static_cast<double>(wq + wk) + 0.5);
+  if (wq > 0) queries = std::max<int64_t>(queries, 1);
+  if (wk > 0) queries = std::min<int64_t>(queries, kMaxBackwardGroups - 1);
+  const int64_t keys = std::min(mk, kMaxBackwardGroups - std::min(queries, mq));
+  g.queries = static_cast<int>(std::min(mq, kMaxBackwardGroups - keys));
+  g.all = g.queries + static_cast<int>(keys);
   return g;
 }
 

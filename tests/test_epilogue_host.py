@@ -313,3 +313,17 @@ def test_qk_forward_refuses_heads_in_each_other(more):
     dict(q_heads=2, k_heads=2, q_out=heads(4 * P, 2 * D, 4 * T * D), k_out=heads(4 * P + 2 * D, 2 * D, 4 * T * D))])  # [heads, .., tokens, 2, D]
 def test_qk_forward_takes_heads_in_turn_by_head(no_gpu, more):
     assert passes_the_checks(qk_forward(**more))
+
+
+@pytest.mark.parametrize("tokens,q_heads,k_heads,D", [(100, 64, 64, 512), (64, 64, 8, 256), (3, 100, 100, 64), (300, 48, 1, 128), (1, 65535, 65535, 8), (1, 32, 8, 128), (767, 64, 1, 512)])
+def test_qk_backward_asks_for_no_plane_that_no_token_adds_to(tokens, q_heads, k_heads, D):
+    """A workgroup walks all heads of its tokens: each side has a plane of D sums for each token tile at most, which holds one token or more,
+    and both sides together have 768."""
+    planes = osdp.osdp_qk_norm_rope_bwd_workspace_bytes(tokens, q_heads, k_heads, D) // (4 * D)
+    assert 2 <= planes <= min(2 * tokens, 768)
+
+
+def test_qk_backward_gives_both_sides_workgroups():
+    """With more token tiles than workgroups that run at once: 768 in all, and for one side without heads too."""
+    for q_heads, k_heads in ((64, 1), (1, 64), (8, 8), (64, 0), (0, 1), (65535, 1)):
+        assert osdp.osdp_qk_norm_rope_bwd_workspace_bytes(1 << 20, q_heads, k_heads, 512) == 768 * 512 * 4
