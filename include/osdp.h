@@ -734,9 +734,10 @@ typedef struct {
   double bytes;     /* algorithmic bytes summed over launches: operands read once, output written once */
 } osdp_kernel_stats;
 
-/* Between begin and end every kernel launch of the calling thread is bracketed
- * by a pair of HIP events on its own stream (at most max_launches launches;
- * later ones are not timed).  osdp_profile_end synchronises the device and
+/* Between begin and end the calling thread's launches of gathers, of products (with what adds up a product's parts) and of the
+ * pass for dZ and db are bracketed by pairs of HIP events on their own streams (at most max_launches of them;
+ * later ones are not timed).  The pass for dZ and db is of no kind: it counts in osdp_profile_overlap alone.  The kernels of
+ * AdamW, of the operator in 8-bit integers and of the norms of queries and keys are not seen.  osdp_profile_end synchronises the device and
  * fills stats[OSDP_KERNEL_KINDS]. Not for use inside hot loops one wants
  * undisturbed: the event records sit between the kernels. */
 OSDP_API osdp_status osdp_profile_begin(int32_t max_launches);
@@ -744,8 +745,8 @@ OSDP_API osdp_status osdp_profile_end(osdp_kernel_stats *stats);
 
 /* After osdp_profile_end: how the launches of the profiled region lay in time (all streams on one clock).
  *   span_ms           : first launch start to last launch end
- *   idle_ms           : the part of the span in which no kernel of the library ran (launch gaps, event handling)
- *   gather_exposed_ms : the time in which a gather kernel ran and no GEMM did, i.e. gather time that no GEMM hid
+ *   idle_ms           : the part of the span in which none of these kernels ran (launch gaps, event handling)
+ *   gather_exposed_ms : the time in which a gather kernel ran and no other of these did, i.e. gather time that nothing hid
  *                       (gathers carried inside GEMM launches are not kernels of their own and do not appear here)
  * Any pointer may be NULL.  Host only. */
 OSDP_API osdp_status osdp_profile_overlap(double *span_ms, double *idle_ms, double *gather_exposed_ms);

@@ -560,6 +560,8 @@ hipError_t edge(hipStream_t from, hipStream_t to) {
 }
 
 // ---- per-kernel timing --------------------------------------------------------
+constexpr int kBesideKind = -1;  // launches beside gathers and products: only where they lie in time counts
+
 struct TimedLaunch {
   int kind;
   hipEvent_t start, stop;
@@ -575,7 +577,7 @@ struct Profile {
   int64_t persistent_launches = 0;  // GEMM launches that ran as the persistent kernel
   double carried_bytes = 0.0;
   // filled by osdp_profile_end for osdp_profile_overlap: [start, stop) of every timed launch in ms from the first event
-  std::vector<std::pair<double, double>> gemm_iv, gather_iv;
+  std::vector<std::pair<double, double>> gemm_iv, gather_iv, beside_iv;
 };
 
 // Total length of the union of intervals (sorts its argument).
@@ -1346,7 +1348,7 @@ static osdp_status backward(const osdp_shape *shape, const osdp_plan *plan, int3
   if ((st = device_ok()) != OSDP_OK) return st;
 
   if (slope) {  // the products' dY is the gradient in front of the activation
-    OSDP_HIP(launch_slope(*slope, slope_workspace, sc));
+    OSDP_HIP(timed(kBesideKind, 0.0, 0.0, sc, [&] { return launch_slope(*slope, slope_workspace, sc); }));
     if (slope->dZ) {
       dY = slope->dZ;
       lddy = slope->lddz;
@@ -1713,18 +1715,21 @@ osdp_status osdp_profile_end(osdp_kernel_stats *stats) {
   OSDP_HIP(hipDeviceSynchronize());
   pf.gemm_iv.clear();
   pf.gather_iv.clear();
+  pf.beside_iv.clear();
   for (TimedLaunch &t : pf.launches) {
     float ms = 0.f, from0 = 0.f;
     OSDP_HIP(hipEventElapsedTime(&ms, t.start, t.stop));
     OSDP_HIP(hipEventElapsedTime(&from0, pf.launches.front().start, t.start));
-    (t.kind == OSDP_KERNEL_GATHER ? pf.gather_iv : pf.gemm_iv).push_back({from0, static_cast<double>(from0) + ms});
+    (t.kind == OSDP_KERNEL_GATHER ? pf.gather_iv : t.kind == kBesideKind ? pf.beside_iv : pf.gemm_iv)
+        .push_back({from0, static_cast<double>(from0) + ms});
+    pf.spare.push_back(t.start);
+    pf.spare.push_back(t.stop);
+    if (t.kind == kBesideKind) continue;
     osdp_kernel_stats &s = stats[t.kind];
     s.launches += 1;
     s.ms += ms;
     s.flops += t.flops;
     s.bytes += t.bytes;
-    pf.spare.push_back(t.start);
-    pf.spare.push_back(t.stop);
   }
   pf.launches.clear();
   stats[OSDP_KERNEL_GATHER_CARRIED].launches = pf.carried_launches;
@@ -1736,17 +1741,19 @@ osdp_status osdp_profile_end(osdp_kernel_stats *stats) {
 osdp_status osdp_profile_overlap(double *span_ms, double *idle_ms, double *gather_exposed_ms) {
   Profile &pf = t_profile;
   if (pf.active) return fail(OSDP_ERR_INVALID_ARG, "osdp_profile_end has not been called");
-  std::vector<std::pair<double, double>> all = pf.gemm_iv, gemm = pf.gemm_iv, gather = pf.gather_iv;
-  all.insert(all.end(), gather.begin(), gather.end());
+  std::vector<std::pair<double, double>> others = pf.gemm_iv;
+  others.insert(others.end(), pf.beside_iv.begin(), pf.beside_iv.end());
+  std::vector<std::pair<double, double>> all = others;
+  all.insert(all.end(), pf.gather_iv.begin(), pf.gather_iv.end());
   double lo = 0.0, hi = 0.0;
   for (size_t i = 0; i < all.size(); ++i) {
     lo = i ? std::min(lo, all[i].first) : all[i].first;
     hi = i ? std::max(hi, all[i].second) : all[i].second;
   }
-  const double busy = union_length(all), busy_gemm = union_length(gemm);
+  const double busy = union_length(all), busy_others = union_length(others);
   if (span_ms) *span_ms = hi - lo;
   if (idle_ms) *idle_ms = (hi - lo) - busy;
-  if (gather_exposed_ms) *gather_exposed_ms = busy - busy_gemm;  // time covered by gathers and by no GEMM
+  if (gather_exposed_ms) *gather_exposed_ms = busy - busy_others;  // time covered by gathers alone
   return OSDP_OK;
 }
 

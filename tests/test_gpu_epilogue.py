@@ -574,3 +574,23 @@ def test_gradients_of_products_in_parts_are_the_same_for_every_plan(T, I, O, k):
         if zdp is None or split:
             kernel = 64 < T <= 128 and I > 8192 and I % (64 * N) == 0
             assert torch.equal(dX, want_dX.setdefault(kernel, dX)), (N, k_, split, zdp)
+
+
+def test_the_profile_sees_the_pass_for_dz():
+    """A backward pass whose dZ (2.1 GB read and written) takes longer than its products: in the span of the profile, and no idle time of it."""
+    T, I, O = 32768, 64, 10752
+    op, dY, Z = Op(T, I, O, 1), rand(T, O, seed=1), rand(T, O, seed=2)
+    dz, dX, dW, ws = torch.empty_like(dY), torch.empty_like(op.X), [torch.empty_like(s) for s in op.w], op.workspace(True)
+
+    def call():
+        osdp.osdp_split_linear_bwd_epilogue(op.X, dY, op.w, dX, dW, 1, ws, plan=op.plan, epilogue=osdp.EpilogueGrad(activation=ACTS["relu"], z=Z, dz=dz))
+
+    call()
+    torch.cuda.synchronize()
+    osdp.osdp_profile_begin(1000)
+    for _ in range(4):
+        call()
+    stats = osdp.osdp_profile_end()
+    lay = osdp.osdp_profile_overlap()
+    assert stats["gemm_dw"]["launches"] == 4 and stats["gemm_dx"]["launches"] == 4
+    assert lay["idle_ms"] < 0.25 * lay["span_ms"], (lay, stats)
