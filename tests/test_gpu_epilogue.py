@@ -594,3 +594,84 @@ def test_the_profile_sees_the_pass_for_dz():
     lay = osdp.osdp_profile_overlap()
     assert stats["gemm_dw"]["launches"] == 4 and stats["gemm_dx"]["launches"] == 4
     assert lay["idle_ms"] < 0.25 * lay["span_ms"], (lay, stats)
+
+
+# (reductions whose last part is shorter: a whole number of K blocks, the end of one, and parts alike; shards of 832 and 512 rows are
+# read in place, the others staged)
+@pytest.mark.parametrize("T,I,O,N", [(300, 4160, 520, 5), (300, 4160, 520, 8), (300, 8200, 520, 8), (300, 4096, 512, 8), (140, 24584, 264, 1)])
+def test_parts_of_a_reduction_give_the_same_bits_in_every_kernel(T, I, O, N):
+    assert in_parts(T, I, O)
+    op, bias, residual = Op(T, I, O, N), rand(O, seed=1), rand(T, O, seed=2)
+    want = want_z = None
+    for switches in [dict(tile=3), dict(tile=0), dict(tile=1), dict(tile=2), dict(tile=3, deep=0), dict(tile=1, deep=0), dict(tile=2, deep=0), dict(tile=0, persistent=1),
+                     dict(tile=0, persistent=0), dict(tile=0, four_wave=0), dict(tile=0, four_wave=1), dict(gemm_generic=1), dict(tile=3, recut=0)]:
+        Z = op.out()
+        got = switched(switches, lambda: op.fwd(op.out(), bias=bias, activation=ACTS["gelu"], residual=residual, z=Z))
+        if want is None:
+            want, want_z = got, Z
+            check_forward(op, "gelu", bias, residual, got, Z)
+        assert torch.equal(got, want) and torch.equal(Z, want_z), switches
+    if N == 5 or I == 4096:  # (no switch: over the shards where they lie)
+        assert torch.equal(op.fwd(op.out(), bias=bias, activation=ACTS["gelu"], residual=residual), want)
+
+
+@pytest.mark.parametrize("T,I,O,slices", [(300, 520, 4168, 5), (4168, 264, 520, 3), (3000, 520, 264, 5)])
+@pytest.mark.parametrize("N,sliced", [(1, False), (8, False), (8, True)])
+def test_parts_of_the_backward_reductions_give_the_same_bits_in_every_kernel(T, I, O, slices, N, sliced):
+    """dX over O and dW over T, with a shorter last part."""
+    assert in_parts(T, O, I) or in_parts(I, T, O)
+    k = slices if sliced else 1
+    op, dY, Z = Op(T, I, O, N, k, osdp.OSDP_SPLIT_IN_FEATURES), rand(T, O, seed=3), rand(T, O, seed=4)
+    want = None
+    for switches in [dict(tile=3), dict(tile=0), dict(tile=1), dict(tile=2), dict(tile=3, deep=0), dict(tile=1, deep=0), dict(tile=2, deep=0), dict(tile=0, persistent=1),
+                     dict(tile=0, four_wave=0), dict(tile=0, four_wave=1), dict(gemm_generic=1), dict(small_tile=0), dict(fused_gather=0), dict()]:
+        dz = op.out()
+        got = switched(switches, lambda: op.bwd(dY, activation=ACTS["silu"], z=Z, dz=dz, dbias=torch.empty(O, device="cuda")))
+        if want is None:
+            want = got
+            check_products(op, dz, *got)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), switches
+
+
+def switched(switches, call):
+    """What the call gives under these switches of the library."""
+    try:
+        for name, value in switches.items():
+            osdp.osdp_debug_option(name, value)
+        got = call()
+        torch.cuda.synchronize()
+        return got
+    finally:
+        for name in switches:
+            osdp.osdp_debug_option(name, 0 if name in ("gemm_generic", "poison_staging") else -1)
+
+
+# (slices staged in two slots, by launches of their own: the copy stream gathers one while the product of the other runs)
+@pytest.mark.parametrize("T,I,O,N", [(600, 1024, 4096, 32), (1111, 2080, 2048, 8), (300, 8224, 1024, 8), (300, 8224, 8192, 8), (4100, 544, 8192, 8)])
+@pytest.mark.parametrize("split", [osdp.OSDP_SPLIT_OUT_FEATURES, osdp.OSDP_SPLIT_IN_FEATURES])
+@pytest.mark.parametrize("poison", [0, 1])
+def test_two_streams_give_the_bits_of_one(T, I, O, N, split, poison):
+    k = 4
+    op = Op(T, I, O, N, k, split, staging=osdp.OSDP_STAGING_DOUBLE)
+    bias, residual, dY = rand(O, seed=1), rand(T, O, seed=2), rand(T, O, seed=3)
+    compute, copy = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step(streams):
+        Y, Z, dz, db = op.out(), op.out(), op.out(), torch.full_like(bias, float("nan"))
+        dX, dW = torch.full_like(op.X, float("nan")), [torch.full_like(s, float("nan")) for s in op.w]
+        ws, ws_back = op.workspace(False), op.workspace(True)
+        torch.cuda.synchronize()
+        osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, Y, k, ws, plan=op.plan, **streams,
+                                            epilogue=osdp.Epilogue(bias=bias, activation=ACTS["silu"], residual=residual, z=Z))
+        osdp.osdp_split_linear_bwd_epilogue(op.X, dY, op.w, dX, dW, k, ws_back, plan=op.plan, **streams,
+                                            epilogue=osdp.EpilogueGrad(activation=ACTS["silu"], z=Z, dz=dz, dbias=db))
+        torch.cuda.synchronize()
+        return [Y, Z, dz, db, dX, torch.cat(dW)[:I * O]]
+
+    switches = dict(fused_gather=0, fwd_pair=0, **(dict(poison_staging=1) if poison else {}))
+    want = switched(switches, lambda: step({}))
+    check_forward(op, "silu", bias, residual, want[0], want[1])
+    check_products(op, want[2], want[4], want[5])
+    for _ in range(3):
+        got = switched(switches, lambda: step(dict(stream_compute=compute.cuda_stream, stream_copy=copy.cuda_stream)))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

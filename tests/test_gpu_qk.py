@@ -355,3 +355,23 @@ def test_any_eps_beside_any_size_of_heads(size, eps):
     want, want_g = R.qk_back(q.double(), dy.double(), how["positions"], how["freqs"], w, eps, True, False)
     assert ((dx.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * want.square().mean().sqrt()).all()
     assert ((dg.double() - want_g).abs() <= 2.0 ** -10 * want_g.square().mean().sqrt()).all()
+
+
+# (T, query heads, key heads, D): one token tile to a workgroup and many, one head group and many
+@pytest.mark.parametrize("shape", [(100, 64, 64, 512), (700, 64, 3, 256), (2048, 32, 8, 128), (3000, 16, 4, 64), (5000, 8, 8, 128), (8192, 8, 2, 64), (20000, 3, 1, 80)], ids=str)
+def test_no_term_of_the_weights_gradients_is_lost_or_counted_twice(shape):
+    """Heads and gradients of +-1: the root mean square is 1, and without rotation dg is a sum of ones of both signs, up to 2^16 of them.
+    The factor (its root off by 2^-23, the mean over a D that is no power of two and eps of 1e-12 by 2^-24 each) and its product with a
+    gradient move the sum by less than 2^16 2^-21; fewer than 100 additions one after another (a lane's own terms, a workgroup's lane
+    groups, the workgroups) by 100 * 2^-24 * 2^16: less than 0.43 in all.  One term more or less moves every element by 1."""
+    T, HQ, HK, D = shape
+    g = torch.Generator(device="cuda").manual_seed(T)
+    sides = []
+    for heads in (HQ, HK):
+        x = torch.randint(0, 2, (T, heads, D), device="cuda", generator=g).mul_(2).sub_(1).bfloat16()
+        sides.append((x, torch.randint(0, 2, (T, heads, D), device="cuda", generator=g).mul_(2).sub_(1).bfloat16()))
+    (q, dq_out), (k, dk_out) = sides
+    out = backward(q, k, dq_out, dk_out, dtype=torch.float32, eps=1e-12)
+    for i, (x, dy) in enumerate(sides):
+        want = (x.double() * dy.double()).sum((0, 1))
+        assert (out[2 + i].double() - want).abs().max() < 0.43, i
