@@ -422,7 +422,8 @@ typedef struct {
 OSDP_API osdp_status osdp_qk_norm_rope_fwd(const osdp_qk *qk, const osdp_heads *q, const osdp_heads *k,
                                            const osdp_heads *q_out, const osdp_heads *k_out, void *stream);
 
-/* q and k are the forward call's inputs.  dq_weight, dk_weight: device [D] of weight_type, 16-byte aligned, written, or NULL.
+/* q and k are the forward call's inputs.  dq_weight, dk_weight: device [D] of weight_type, 16-byte aligned, written, or NULL;
+ * each apart from the other and from all else.
  *   workspace: device, 256-byte aligned, >= osdp_qk_norm_rope_bwd_workspace_bytes; may be NULL when that is not asked for (no
  *              weight gradients) */
 OSDP_API osdp_status osdp_qk_norm_rope_bwd(const osdp_qk *qk, const osdp_heads *q, const osdp_heads *k,

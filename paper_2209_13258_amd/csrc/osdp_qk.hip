@@ -644,7 +644,11 @@ osdp_status osdp_qk_norm_rope_bwd(const osdp_qk *qk, const osdp_heads *q, const 
   const bool sums = dq_weight || dk_weight;
   if (sums && !d.norm) return bad(OSDP_ERR_INVALID_ARG, "weight gradients are asked for without a norm");
   if (!aligned(dq_weight) || !aligned(dk_weight)) return bad(OSDP_ERR_UNSUPPORTED, "a weight gradient is not 16-byte aligned");
-  if (sums && dq_weight == dk_weight) return bad(OSDP_ERR_INVALID_ARG, "the two weight gradients are one");
+  if (dq_weight && dk_weight) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(dq_weight), b = reinterpret_cast<uintptr_t>(dk_weight);
+    if ((a < b ? b - a : a - b) < static_cast<uintptr_t>(d.D) * (d.weight_type == OSDP_F32 ? 4 : 2))
+      return bad(OSDP_ERR_INVALID_ARG, "the two weight gradients share memory");
+  }
   // (the inputs of the forward pass are read only for the norm)
   if ((d.norm && ((st = check_heads(q, d.q_heads, d, "q", false)) != OSDP_OK || (st = check_heads(k, d.k_heads, d, "k", false)) != OSDP_OK)) ||
       (st = check_heads(dq_out, d.q_heads, d, "dq_out", false)) != OSDP_OK || (st = check_heads(dk_out, d.k_heads, d, "dk_out", false)) != OSDP_OK ||

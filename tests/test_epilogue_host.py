@@ -327,3 +327,15 @@ def test_qk_backward_gives_both_sides_workgroups():
     """With more token tiles than workgroups that run at once: 768 in all, and for one side without heads too."""
     for q_heads, k_heads in ((64, 1), (1, 64), (8, 8), (64, 0), (0, 1), (65535, 1)):
         assert osdp.osdp_qk_norm_rope_bwd_workspace_bytes(1 << 20, q_heads, k_heads, 512) == 768 * 512 * 4
+
+
+@pytest.mark.parametrize("weight_type,size", [(B.OSDP_BF16, 2), (B.OSDP_F32, 4)])
+def test_qk_backward_refuses_weight_gradients_in_each_other(weight_type, size):
+    for off in (0, 16, D * size - 16):
+        assert qk_backward(weight_type=weight_type, wk=24 * P + off) == INVALID
+        assert qk_backward(weight_type=weight_type, wq=24 * P + off, wk=24 * P) == INVALID
+
+
+@pytest.mark.parametrize("weight_type,size", [(B.OSDP_BF16, 2), (B.OSDP_F32, 4)])
+def test_qk_backward_takes_weight_gradients_side_by_side(no_gpu, weight_type, size):
+    assert passes_the_checks(qk_backward(weight_type=weight_type, wk=24 * P + D * size))
