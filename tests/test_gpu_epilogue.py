@@ -9,6 +9,8 @@ was stored: 2^-8 of them and 1e-3 of their root mean square, and bit by bit thos
 runs in parts of its reduction."""
 from __future__ import annotations
 
+import threading
+
 import pytest
 import torch
 
@@ -675,3 +677,70 @@ def test_two_streams_give_the_bits_of_one(T, I, O, N, split, poison):
     for _ in range(3):
         got = switched(switches, lambda: step(dict(stream_compute=compute.cuda_stream, stream_copy=copy.cuda_stream)))
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("T,I,O,N", [(20, 520, 1032, 5), (100, 1024, 512, 32), (200, 1064, 520, 5), (700, 264, 2056, 3), (300, 8200, 520, 8)])
+@pytest.mark.parametrize("split", [osdp.OSDP_SPLIT_OUT_FEATURES, osdp.OSDP_SPLIT_IN_FEATURES])
+@pytest.mark.parametrize("zdp", [0b00000, 0b00011, 0b10001, 0b01110])
+def test_modes_of_slices_over_shards_that_are_no_row_blocks(T, I, O, N, split, zdp):
+    """All slices replicated, neighbours that lie together in the replica, the first and last alone: outputs and gradients."""
+    k = next(k for k in (5, 4, 3, 2, 1) if ((I if split else O) % (8 * k)) == 0)
+    op = Op(T, I, O, N, k, split, zdp=zdp & ((1 << k) - 1))
+    bias, residual, dY, Z = rand(O, seed=1), rand(T, O, seed=2), rand(T, O, seed=3), op.out()
+    full, step = op.W.contiguous(), (I if split else O) // k
+    dw = torch.full_like(full, float("nan"))
+    cut = lambda m: [(m[j * step:(j + 1) * step] if split else m[:, j * step:(j + 1) * step]) if not zdp >> j & 1 else None for j in range(k)]  # noqa: E731
+    Y, dz, dX, db = op.out(), op.out(), torch.full_like(op.X, float("nan")), torch.full((O,), float("nan"), device="cuda")
+    osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, Y, k, op.workspace(False), plan=op.plan, w_dp=cut(full), ld_dp=O,
+                                        epilogue=osdp.Epilogue(bias=bias, activation=ACTS["gelu"], residual=residual, z=Z))
+    check_forward(op, "gelu", bias, residual, Y, Z)
+    dws = [torch.full_like(s, float("nan")) for s in op.w]
+    osdp.osdp_split_linear_bwd_epilogue(op.X, dY, op.w, dX, dws, k, op.workspace(True), plan=op.plan, w_dp=cut(full), ld_dp=O, dw_dp=cut(dw),
+                                        epilogue=osdp.EpilogueGrad(activation=ACTS["gelu"], z=Z, dz=dz, dbias=db))
+    dW = torch.cat(dws)[:I * O].view(I, O)
+    check_products(op, dz, dX, torch.where(torch.isnan(dW), dw, dW).flatten())
+
+
+def test_calls_of_two_threads_at_once():
+    """Each with tensors, a workspace and a stream of its own: the results of calls one after another."""
+    shapes = [(33, 1024, 520, 8, 5), (300, 4096, 512, 8, 4)]
+    ops = [Op(*s, seed=10 * i) for i, s in enumerate(shapes)]
+    state = []
+    for op in ops:
+        s = dict(bias=rand(op.O, seed=1), residual=rand(op.T, op.O, seed=2), dY=rand(op.T, op.O, seed=3), stream=torch.cuda.Stream(), ws=op.workspace(False), wb=op.workspace(True))
+        s.update({n: op.out() for n in ("Y", "Z", "dz")}, dX=torch.empty_like(op.X), dW=[torch.empty_like(w) for w in op.w], db=torch.empty_like(s["bias"]))
+        state.append(s)
+
+    def step(op, s):
+        osdp.osdp_split_linear_fwd_epilogue(op.X, op.w, s["Y"], op.k, s["ws"], plan=op.plan, stream_compute=s["stream"],
+                                            epilogue=osdp.Epilogue(bias=s["bias"], activation=ACTS["gelu"], residual=s["residual"], z=s["Z"]))
+        osdp.osdp_split_linear_bwd_epilogue(op.X, s["dY"], op.w, s["dX"], s["dW"], op.k, s["wb"], plan=op.plan, stream_compute=s["stream"],
+                                            epilogue=osdp.EpilogueGrad(activation=ACTS["gelu"], z=s["Z"], dz=s["dz"], dbias=s["db"]))
+
+    def outputs(s):
+        return [t.clone() for t in (s["Y"], s["Z"], s["dz"], s["dX"], s["db"], *s["dW"])]
+
+    torch.cuda.synchronize()
+    want = []
+    for op, s in zip(ops, state):
+        step(op, s)
+        torch.cuda.synchronize()
+        want.append(outputs(s))
+    wrong = []
+
+    def work(i):
+        try:
+            for _ in range(50):
+                step(ops[i], state[i])
+        except Exception as e:  # noqa: BLE001 (whatever it is, the test's own thread says it)
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong, wrong
+    for s, w in zip(state, want):
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outputs(s), w))
