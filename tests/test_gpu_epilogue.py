@@ -744,3 +744,29 @@ def test_calls_of_two_threads_at_once():
     assert not wrong, wrong
     for s, w in zip(state, want):
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outputs(s), w))
+
+
+class OnlyPython:
+    """In the place of the binding's way through C: nothing is answered there."""
+    linear = qk = staticmethod(lambda *a: None)
+
+
+@pytest.mark.parametrize("T,ld", [(1, 0), (40, 0), (40, 24), (300, 8)])
+@pytest.mark.parametrize("parts", [(), ("bias", "residual", "z"), ("bias",), ("z",)])
+def test_both_ways_into_the_library_hand_over_the_same(monkeypatch, T, ld, parts):
+    """Tensors are looked at in C, or in Python where that gives no answer: the same bits, for rows of any length and parts left out."""
+    I, O, N, k = 264, 520, 3, 1
+    op, given = Op(T, I, O, N, k), []
+    wide = lambda cols, seed: rand(T, cols + ld, seed=seed)[:, :cols]  # noqa: E731
+    op.X, residual, dY = wide(I, 1), wide(O, 2), wide(O, 3)
+    for way in ("C", "Python"):
+        if way == "Python":
+            monkeypatch.setattr(osdp.binding, "_calls", OnlyPython)
+        bias = rand(O, seed=4, dtype=torch.float32) if "bias" in parts else None
+        act = ACTS["gelu"] if "z" in parts else ACTS["none"]
+        Y, Z, dz = (torch.full((T, O + ld), float("nan"), dtype=torch.bfloat16, device="cuda")[:, :O] for _ in range(3))
+        op.fwd(Y, bias=bias, activation=act, residual=residual if "residual" in parts else None, z=Z if "z" in parts else None)
+        db = None if bias is None else torch.full_like(bias, float("nan"))
+        dX, dW = op.bwd(dY, activation=act, z=Z if "z" in parts else None, dz=dz if "z" in parts else None, dbias=db)
+        given.append([t.clone() for t in (Y, Z, dz, dX, dW)] + ([] if db is None else [db]))
+    assert all(torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)) for a, b in zip(*given))

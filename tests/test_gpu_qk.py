@@ -375,3 +375,22 @@ def test_no_term_of_the_weights_gradients_is_lost_or_counted_twice(shape):
     for i, (x, dy) in enumerate(sides):
         want = (x.double() * dy.double()).sum((0, 1))
         assert (out[2 + i].double() - want).abs().max() < 0.43, i
+
+
+@pytest.mark.parametrize("T", [1, 70])
+@pytest.mark.parametrize("parts", ["all", "no positions", "no rotation", "no weights", "no norm", "no keys"])
+def test_both_ways_into_the_library_hand_over_the_same(monkeypatch, T, parts):
+    """Tensors are looked at in C, or in Python where that gives no answer: the same bits."""
+    HQ, HK, D = 6, 0 if parts == "no keys" else 2, 64
+    rows, given = rand(T, (HQ + 2 * HK) * D + 16), []
+    q, k = rows[:, :HQ * D].unflatten(1, (HQ, D)), rows[:, HQ * D:(HQ + HK) * D].unflatten(1, (HK, D))
+    w = rand(D, seed=1, dtype=torch.float32) if parts not in ("no weights", "no norm") else None
+    how = dict(positions=None if parts == "no positions" else torch.randint(0, 1000, (T,), device="cuda"), freqs=None if parts == "no rotation" else some_freqs(32),
+               q_weight=w, k_weight=w, eps=1e-5, norm=parts != "no norm", interleaved=parts == "all")
+    dy = rand(T, HQ, D, seed=2), rand(T, HK, D, seed=3)
+    for way in ("C", "Python"):
+        if way == "Python":
+            monkeypatch.setattr(osdp.binding, "_calls", type("OnlyPython", (), {"qk": staticmethod(lambda *a: None)}))
+        out = [*forward(q, k, **how), *backward(q, k, *dy, dtype=torch.float32, weights=parts != "no norm", **how)]
+        given.append([t for t in out if t is not None])
+    assert len(given[0]) == len(given[1]) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(*given))
